@@ -45,6 +45,10 @@ extern "C" {
 #define BSGA_BF16 0
 #define BSGA_FP32 1
 
+#define BSGA_NORM_NONE 0
+#define BSGA_NORM_RMS 1
+#define BSGA_NORM_LAYER 2
+
 /* ABI version of this header (bumped on incompatible change). */
 int bsga_version(void);
 
@@ -288,6 +292,45 @@ int bsga_linear(const void* x, int x_heads, const void* weight, const void* bias
                 void* out, void* stream);
 int bsga_layer_norm(const void* x, const void* weight, const void* bias, double eps, int64_t n_tokens, int features,
                     const int32_t* index, void* out, void* stream);
+
+/*
+ * Norms of queries and keys for each head and the rotation by position, in one pass, on the way from a projection's output to
+ * the attention's layout.  A row x is the 64 numbers of one head of one token:
+ *   norm       BSGA_NORM_NONE; BSGA_NORM_RMS: n = x / sqrt(mean x^2 + eps) * weight;
+ *              BSGA_NORM_LAYER: n = (x - mean) / sqrt(variance + eps) * weight + bias; statistics in fp32
+ *   axes       0 (positions NULL): no rotation.  1 or 2: the row is one segment of 64 or two of 32; in a segment of width W the numbers
+ *              j and j + W/2 turn by positions[token, segment] * base^(-2j/W).  Positions are any int32; angles do not lose precision
+ *              with their size.
+ *   q          [n_tokens, heads, 64], k and v [n_tokens, kv_heads, 64] with strides in elements (64 numbers of a row are contiguous; strides
+ *              are multiples of 16 bytes); each of q, k, v is NULL together with its output
+ *   weights, biases  nullable [64], dtype of the tensors
+ *   positions  [n_tokens, axes] int32
+ *   q_out      [heads, n_tokens, 64]
+ *   k_out, v_out  [kv_heads, n_tokens, 64], or with slots the caches [n_pages, kv_heads, page, 64]: token i goes to row slots[i] % page of
+ *              page slots[i] / page; tokens whose slot lies outside the cache are not written, slots are distinct.
+ *              v is moved as it is.  Outputs must not overlap inputs.
+ *   n_tokens may be 0.
+ */
+int bsga_qk_norm_rope(const void* q, const void* k, const void* v, int64_t q_token, int64_t q_head, int64_t k_token, int64_t k_head,
+                      int64_t v_token, int64_t v_head, int dtype, int64_t n_tokens, int heads, int kv_heads, int head_dim, int norm,
+                      double eps, const void* q_weight, const void* q_bias, const void* k_weight, const void* k_bias,
+                      const int32_t* positions, int axes, double base, const int32_t* slots, int64_t n_pages, int page, void* q_out,
+                      void* k_out, void* v_out, void* stream);
+
+/*
+ * Its gradient.  dq [heads, n_tokens, 64], dk and dv [kv_heads, n_tokens, 64]: gradients of q_out, k_out, v_out (without slots);
+ * q, k and the rest as they were given; dq_in, dk_in, dv_in: gradients of q, k, v, with strides of their own.
+ *   d_weights  nullable [2, 2, 64] float32: of q's weight and bias, then of k's (zeros for an absent tensor; the bias of a rms norm is
+ *              the sum that a bias would have); sums over tokens and heads in fp32 and fp64, always in the same order
+ *   workspace  with d_weights: bsga_qk_norm_rope_bwd_workspace_bytes(...) bytes, 16-byte aligned; overwritten
+ */
+size_t bsga_qk_norm_rope_bwd_workspace_bytes(int64_t n_tokens, int heads, int kv_heads);
+int bsga_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const void* q, const void* k, int64_t q_token,
+                          int64_t q_head, int64_t k_token, int64_t k_head, int dtype, int64_t n_tokens, int heads, int kv_heads, int head_dim,
+                          int norm, double eps, const void* q_weight, const void* k_weight, const int32_t* positions, int axes,
+                          double base, void* dq_in, void* dk_in, void* dv_in, int64_t dq_token, int64_t dq_head, int64_t dk_token,
+                          int64_t dk_head, int64_t dv_token, int64_t dv_head, float* d_weights, void* workspace, size_t workspace_bytes,
+                          void* stream);
 
 /*
  * Measurement aid, not part of the method: the rate the matrix pipes sustain on the MFMA instruction

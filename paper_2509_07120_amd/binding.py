@@ -48,6 +48,9 @@ EXPORTED_SYMBOLS = (
     "bsga_linear",
     "bsga_layer_norm",
     "bsga_probe_mfma",
+    "bsga_qk_norm_rope",
+    "bsga_qk_norm_rope_bwd",
+    "bsga_qk_norm_rope_bwd_workspace_bytes",
 )
 
 
@@ -119,6 +122,16 @@ def _load() -> ctypes.CDLL:
     lib.bsga_layer_norm.argtypes = [c_void_p, c_void_p, c_void_p, c_double, c_int64, c_int, c_void_p, c_void_p, c_void_p]
     lib.bsga_probe_mfma.restype = c_int
     lib.bsga_probe_mfma.argtypes = [c_int, c_int, c_int, c_void_p, c_size_t, ctypes.POINTER(c_double), c_void_p]
+    strides = [c_int64] * 6
+    norm = [c_int, c_double, c_void_p, c_void_p]
+    lib.bsga_qk_norm_rope.restype = c_int
+    lib.bsga_qk_norm_rope.argtypes = [c_void_p] * 3 + strides + [c_int, c_int64, c_int, c_int, c_int] + norm + [c_void_p] * 3 + [
+        c_int, c_double, c_void_p, c_int64, c_int] + [c_void_p] * 4
+    lib.bsga_qk_norm_rope_bwd.restype = c_int
+    lib.bsga_qk_norm_rope_bwd.argtypes = [c_void_p] * 5 + [c_int64] * 4 + [c_int, c_int64, c_int, c_int, c_int] + norm + [
+        c_void_p, c_int, c_double] + [c_void_p] * 3 + strides + [c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.bsga_qk_norm_rope_bwd_workspace_bytes.restype = c_size_t
+    lib.bsga_qk_norm_rope_bwd_workspace_bytes.argtypes = [c_int64, c_int, c_int]
     return lib
 
 
@@ -594,3 +607,132 @@ def bsga_probe_mfma(operands: int, softmax_mix: int, iters: int = 20000, repeats
         if r > 0:
             best = max(best, flops.value / (e0.elapsed_time(e1) * 1e-3) / 1e12)
     return best
+
+
+NORMS = {None: 0, "none": 0, "rms": 1, "layer": 2}
+
+
+def _rows(t: torch.Tensor, name: str, like: torch.Tensor, n_tokens: int, heads: Optional[int] = None) -> Tuple[int, int]:
+    """Strides of the tokens and the heads of t [n_tokens, heads, 64], whose rows are contiguous."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name} must be on the same device as the other tensors")
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != n_tokens or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{name} must be [n_tokens, heads, 64] with as many tokens and heads as the tensors beside it, got {tuple(shape)}")
+    if strides[2] != 1 and shape[2] > 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    return strides[0], strides[1]
+
+
+def _norm_args(q, k, positions, q_weight, k_weight, q_bias, k_bias, norm):
+    """What both directions of the norm with the rotation check; the number of axes."""
+    if norm not in NORMS:
+        raise ValueError(f"norm must be 'rms', 'layer' or None, got {norm!r}")
+    for name, t, x in (("q_weight", q_weight, q), ("k_weight", k_weight, k), ("q_bias", q_bias, q), ("k_bias", k_bias, k)):
+        if t is not None:
+            _require(t, name, x.dtype)
+            if t.numel() != x.shape[2] or t.get_device() != x.get_device():
+                raise ValueError(f"{name} must be [{x.shape[2]}] on the same device as the tensors")
+    if positions is None:
+        return 0
+    _require(positions, "positions", torch.int32)
+    if positions.dim() not in (1, 2) or positions.shape[0] != q.shape[0] or positions.get_device() != q.get_device():
+        raise ValueError("positions must be [n_tokens] or [n_tokens, axes] on the same device as the tensors")
+    return 1 if positions.dim() == 1 else positions.shape[1]
+
+
+def bsga_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                      q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                      q_bias: Optional[torch.Tensor] = None, k_bias: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+                      norm: Optional[str] = "rms", eps: float = 1e-6, base: float = 10000.0, k_cache: Optional[torch.Tensor] = None,
+                      v_cache: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None):
+    """q [N, H, 64], k and v [N, Hkv, 64] (views of a projection's output are fine) -> (q [H, N, 64], k [Hkv, N, 64], v or None): queries
+    and keys normed for each head ("rms", "layer" with weight and bias, or None) and turned by their position, v moved along.
+    positions: int32 [N] or [N, 1] turn the pairs (j, j + 32) of a row by position * base^(-j/32); [N, 2] the pairs (j, j + 16) of
+    its halves by the first and the second position.
+    With slots (int32 [N]) keys and values go to these tokens of the caches [pages, Hkv, page, 64] instead (those outside are not
+    written), and the caches are returned in their place."""
+    if not q.is_cuda:
+        raise ValueError("q must be a device tensor")
+    if q.dim() != 3:
+        raise ValueError("q must be [n_tokens, heads, 64]")
+    N, H, d = q.shape
+    code = _dtype_code(q)
+    qs = _rows(q, "q", q, N)
+    ks = _rows(k, "k", q, N)
+    K = k.shape[1]
+    vs = (0, 0) if v is None else _rows(v, "v", q, N, K)
+    if k.shape[2] != d or (v is not None and v.shape[2] != d):
+        raise ValueError("q, k and v must have the same head dimension")
+    axes = _norm_args(q, k, positions, q_weight, k_weight, q_bias, k_bias, norm)
+    q_out = torch.empty((H, N, d), dtype=q.dtype, device=q.device)
+    pages = page = 0
+    if slots is None:
+        if k_cache is not None or v_cache is not None:
+            raise ValueError("caches go with slots")
+        k_out = torch.empty((K, N, d), dtype=q.dtype, device=q.device)
+        v_out = None if v is None else torch.empty((K, N, d), dtype=q.dtype, device=q.device)
+    else:
+        _require(slots, "slots", torch.int32)
+        if slots.numel() != N or slots.get_device() != q.get_device():
+            raise ValueError("slots must have one entry per token, on the same device as the tensors")
+        if k_cache is None or (v is None) != (v_cache is None):
+            raise ValueError("slots need the cache of the keys, and of the values with v")
+        for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+            if t is not None:
+                _require(t, name, q.dtype)
+                if t.dim() != 4 or t.shape[1] != K or t.shape[3] != d or t.shape != k_cache.shape or t.get_device() != q.get_device():
+                    raise ValueError(f"{name} must be [pages, kv_heads, page, 64] on the same device as the tensors")
+        pages, page = k_cache.shape[0], k_cache.shape[2]
+        k_out, v_out = k_cache, v_cache
+    _check(lib.bsga_qk_norm_rope(_ptr(q), _ptr(k), _ptr(v), *qs, *ks, *vs, code, N, H, K, d, NORMS[norm], eps, _ptr(q_weight),
+                                 _ptr(q_bias), _ptr(k_weight), _ptr(k_bias), _ptr(positions), axes, base, _ptr(slots), pages, page,
+                                 _ptr(q_out), _ptr(k_out), _ptr(v_out), _stream(q)))
+    return q_out, k_out, v_out
+
+
+def bsga_qk_norm_rope_bwd(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
+                          positions: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                          k_weight: Optional[torch.Tensor] = None, q_bias: Optional[torch.Tensor] = None,
+                          k_bias: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None, norm: Optional[str] = "rms",
+                          eps: float = 1e-6, base: float = 10000.0):
+    """Gradient of bsga_qk_norm_rope (without slots): dq [H, N, 64], dk and dv [Hkv, N, 64] are the gradients of its outputs, the
+    rest is what it was given (the biases say only whether their gradients are wanted).  Returns the gradients of (q, k, v, q_weight, k_weight,
+    q_bias, k_bias), None for what was not given; those of q, k and v lie beside each other in one [N, H + 2 Hkv, 64] (without dv
+    [N, H + Hkv, 64]), as a projection's output does, those of weights and biases are float32."""
+    if not q.is_cuda:
+        raise ValueError("q must be a device tensor")
+    if q.dim() != 3:
+        raise ValueError("q must be [n_tokens, heads, 64]")
+    N, H, d = q.shape
+    code = _dtype_code(q)
+    qs = _rows(q, "q", q, N)
+    ks = _rows(k, "k", q, N)
+    K = k.shape[1]
+    if k.shape[2] != d:
+        raise ValueError("q and k must have the same head dimension")
+    for name, t, h in (("dq", dq, H), ("dk", dk, K), ("dv", dv, K)):
+        if t is not None:
+            _require(t, name, q.dtype)
+            if tuple(t.shape) != (h, N, d) or t.get_device() != q.get_device():
+                raise ValueError(f"{name} must be {(h, N, d)} on the same device as q")
+    axes = _norm_args(q, k, positions, q_weight, k_weight, q_bias, k_bias, norm)
+    dx = torch.empty((N, H + (K if dv is None else 2 * K), d), dtype=q.dtype, device=q.device)
+    dq_in, dk_in, dv_in = dx[:, :H], dx[:, H:H + K], None if dv is None else dx[:, H + K:]
+    row = dx.stride(0)
+    wanted = any(t is not None for t in (q_weight, k_weight, q_bias, k_bias))
+    dw = work = None
+    nbytes = 0
+    if wanted:
+        dw = torch.empty((2, 2, d), dtype=torch.float32, device=q.device)
+        nbytes = lib.bsga_qk_norm_rope_bwd_workspace_bytes(N, H, K)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    _check(lib.bsga_qk_norm_rope_bwd(_ptr(dq), _ptr(dk), _ptr(dv), _ptr(q), _ptr(k), *qs, *ks, code, N, H, K, d, NORMS[norm], eps,
+                                     _ptr(q_weight), _ptr(k_weight), _ptr(positions), axes, base, _ptr(dq_in), _ptr(dk_in), _ptr(dv_in),
+                                     row, d, row, d, row, d, _ptr(dw), _ptr(work), nbytes, _stream(q)))
+    of = [None if t is None else dw[x, y] for t, x, y in ((q_weight, 0, 0), (k_weight, 1, 0), (q_bias, 0, 1), (k_bias, 1, 1))]
+    return (dq_in, dk_in, dv_in, *of)
