@@ -333,6 +333,29 @@ int bsga_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const 
                           void* stream);
 
 /*
+ * Attention with a sliding window and a few first tokens that stay visible (sinks), for sequences that grow: frames that see the latest
+ * frames and the first one.  Query i stands at position p = q_start + i, key j at position j.  It sees key j if
+ *   j / frame <= p / frame   and   (p / frame - j / frame < window   or   j < sinks)        (whole quotients, rounded down)
+ * i.e. its own frame, the window - 1 frames before it and the first tokens; frame = 1 is the causal window of tokens, window = 0
+ * sets no limit.  Queries at negative positions see nothing.
+ *   o_i = sum_j softmax_j(softmax_scale * <q_i, k_j>) v_j;  a query that sees nothing yields zeros, lse = -inf
+ *   q          [heads, n_q, 64], k and v [kv_heads, n_k, 64], heads a multiple of kv_heads: query head h reads key head h / (heads / kv_heads);
+ *              strides of tokens and heads in elements, multiples of 16 bytes, a token's below 2^24 bytes; 64 numbers of a row are contiguous
+ *   q_start    position of the first query, in [-2^24, 2^25]; n_k - n_q where the queries are the last tokens
+ *   out        [heads, n_q, 64];  lse nullable [heads, n_q] float32, natural logarithms
+ *   workspace  nullable, bsga_window_attn_workspace_bytes(...) bytes, 16-byte aligned, overwritten: with it launches of few queries deal their keys
+ *              out to several workgroups; without it, or with less, results are the same up to the order of fp32 sums
+ * bf16: products on bf16 MFMA, logits, softmax and sums in fp32, the weights that multiply V rounded to bf16.  fp32: products on fp32 MFMA.
+ * A key that a query does not see has no part in its result, whatever its values.  The same bits every time.
+ */
+size_t bsga_window_attn_workspace_bytes(int dtype, int heads, int64_t n_q, int64_t n_k, int64_t q_start, int64_t frame, int64_t window,
+                                        int64_t sinks);
+int bsga_window_attn(const void* q, const void* k, const void* v, int64_t q_token, int64_t q_head, int64_t k_token, int64_t k_head,
+                     int64_t v_token, int64_t v_head, int dtype, int heads, int kv_heads, int64_t n_q, int64_t n_k, int head_dim,
+                     float softmax_scale, int64_t q_start, int64_t frame, int64_t window, int64_t sinks, void* out, float* lse,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Measurement aid, not part of the method: the rate the matrix pipes sustain on the MFMA instruction
  * the bf16 attention kernels use (32x32x16 bf16, the products of Eqs. (1)/(2)), with no memory traffic
  * at all, two workgroups of four waves per CU.  The part lowers its clock with the switching activity

@@ -51,6 +51,8 @@ EXPORTED_SYMBOLS = (
     "bsga_qk_norm_rope",
     "bsga_qk_norm_rope_bwd",
     "bsga_qk_norm_rope_bwd_workspace_bytes",
+    "bsga_window_attn",
+    "bsga_window_attn_workspace_bytes",
 )
 
 
@@ -132,6 +134,12 @@ def _load() -> ctypes.CDLL:
         c_void_p, c_int, c_double] + [c_void_p] * 3 + strides + [c_void_p, c_void_p, c_size_t, c_void_p]
     lib.bsga_qk_norm_rope_bwd_workspace_bytes.restype = c_size_t
     lib.bsga_qk_norm_rope_bwd_workspace_bytes.argtypes = [c_int64, c_int, c_int]
+    seen = [c_int64] * 4
+    lib.bsga_window_attn.restype = c_int
+    lib.bsga_window_attn.argtypes = [c_void_p] * 3 + strides + [c_int, c_int, c_int, c_int64, c_int64, c_int, c_float] + seen + [
+        c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.bsga_window_attn_workspace_bytes.restype = c_size_t
+    lib.bsga_window_attn_workspace_bytes.argtypes = [c_int, c_int, c_int64, c_int64] + seen
     return lib
 
 
@@ -736,3 +744,58 @@ def bsga_qk_norm_rope_bwd(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k
                                      row, d, row, d, row, d, _ptr(dw), _ptr(work), nbytes, _stream(q)))
     of = [None if t is None else dw[x, y] for t, x, y in ((q_weight, 0, 0), (k_weight, 1, 0), (q_bias, 0, 1), (k_bias, 1, 1))]
     return (dq_in, dk_in, dv_in, *of)
+
+
+def _head_rows(t: torch.Tensor, name: str, like: torch.Tensor) -> Tuple[int, int]:
+    """Strides of the tokens and the heads of t [heads, n_tokens, 64], whose rows are contiguous."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name} must be on the same device as q")
+    strides = t.stride()
+    if len(strides) != 3 or (strides[2] != 1 and t.shape[2] > 1):
+        raise ValueError(f"{name} must be [heads, n_tokens, 64] with contiguous rows")
+    return strides[1], strides[0]
+
+
+def _window_args(q, k, v, window, sinks, frame, q_start, softmax_scale):
+    """What both directions of the attention with a window check: strides, sizes and (q_start, frame, window, sinks)."""
+    qs, ks, vs = _head_rows(q, "q", q), _head_rows(k, "k", q), _head_rows(v, "v", q)
+    H, N, d = q.shape
+    K, M, _ = k.shape
+    if k.shape != v.shape or k.shape[2] != d:
+        raise ValueError("k and v must both be [kv_heads, n_k, head_dim]")
+    if window is not None and window < 1:
+        raise ValueError(f"window must be at least one frame, or None, got {window}")
+    seen = (M - N if q_start is None else q_start, frame, 0 if window is None else window, sinks)
+    scale = 1.0 / math.sqrt(d) if softmax_scale is None else float(softmax_scale)
+    return qs + ks + vs, H, K, N, M, d, seen, scale
+
+
+def bsga_window_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: Optional[int] = None, sinks: int = 0, frame: int = 1,
+                     q_start: Optional[int] = None, softmax_scale: Optional[float] = None, return_lse: bool = False,
+                     out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Attention of q [H, N, 64] over k, v [Hkv, M, 64] (views with contiguous rows are fine; H a multiple of Hkv) with a sliding window:
+    the query at position p sees the keys of its own frame of `frame` tokens and of the window - 1 frames before it, and the first
+    `sinks` tokens, never a later frame.  window = None: no limit.  q_start: position of the first query, by default M - N (the queries
+    are the last tokens).  A query that sees nothing yields zeros and lse -inf.  Returns O [H, N, 64] (and lse [H, N] float32)."""
+    code = _dtype_code(q)
+    strides, H, K, N, M, d, seen, scale = _window_args(q, k, v, window, sinks, frame, q_start, softmax_scale)
+    if out is None:
+        out = torch.empty((H, N, d), dtype=q.dtype, device=q.device)
+    else:
+        _require(out, "out", q.dtype)
+        if tuple(out.shape) != (H, N, d) or out.get_device() != q.get_device():
+            raise ValueError(f"out must be {(H, N, d)} on the same device as q")
+    lse = torch.empty((H, N), dtype=torch.float32, device=q.device) if return_lse else None
+    if workspace is None:
+        nbytes = lib.bsga_window_attn_workspace_bytes(code, H, N, M, *seen)
+        if nbytes > 0:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    _check(lib.bsga_window_attn(_ptr(q), _ptr(k), _ptr(v), *strides, code, H, K, N, M, d, scale, *seen, _ptr(out), _ptr(lse),
+                                _ptr(workspace), nbytes, _stream(q)))
+    return (out, lse) if return_lse else out

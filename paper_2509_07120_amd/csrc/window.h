@@ -1,0 +1,181 @@
+// What the kernels of attention with a window share, forward and backward: which keys a query sees, tiles of 64 rows in LDS, and operands of the
+// matrix products for both types.
+//
+// Query i stands at position p = q_start + i, in frame p / F.  It sees the keys [0, min(sinks, lo)) and [lo, hi) with hi the end of its
+// frame and lo the start of the frame window - 1 frames earlier; both cut to the keys that there are.  Both ends grow with p.
+#pragma once
+
+#include "bf16_tile.h"
+#include "bsga_internal.h"
+
+namespace bsga {
+namespace {
+
+constexpr int kTile = 64;            // rows of a tile
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct Seen {
+  int n_q, n_k, q_start, frame, window, sinks;
+  // [lo, hi) of query i; the keys in front of lo that it sees are those below `sinks`
+  __host__ __device__ void range(int i, int& lo, int& hi) const {
+    const int p = q_start + i;
+    if (p < 0) {
+      lo = hi = 0;
+      return;
+    }
+    const int f = p / frame;
+    hi = static_cast<int>(min(int64_t(f + 1) * frame, int64_t(n_k)));
+    lo = f < window ? 0 : static_cast<int>(min(int64_t(f + 1 - window) * frame, int64_t(hi)));
+  }
+  // The queries [first, last] that may see one of the keys [k0, k1) through the window; first > last: none
+  __host__ __device__ void queries_of(int k0, int k1, int& first, int& last) const {
+    const int64_t f0 = k0 / frame, f1 = (k1 - 1) / frame;
+    first = static_cast<int>(max(f0 * frame - q_start, int64_t(0)));
+    last = static_cast<int>(min((f1 + window) * frame - 1 - q_start, int64_t(n_q) - 1));
+  }
+};
+
+// A tensor [heads, tokens, 64] with strides in bytes.
+struct View {
+  const unsigned char* p;
+  int64_t token, head;
+};
+
+template <typename T>
+struct Ops;
+
+template <>
+struct Ops<__bf16> {
+  typedef bf16x8 A;                          // what a lane holds of an operand
+  static constexpr int kRow = 128;           // bytes of a row
+  static constexpr int kSteps = 4;           // products over the 64 numbers of a row
+  static constexpr int kCols = 2;            // products over 32 rows
+  static __device__ __forceinline__ f32x16 product(A a, A b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  // 16-byte chunk c of tile row r lies at c ^ swizzle(r)
+  static __device__ __forceinline__ int swizzle(int r) { return swz_k(r); }
+  // row r's numbers from memory: lane half g holds 8 of each 16
+  static __device__ __forceinline__ void row(const unsigned char* p, int g, A (&a)[kSteps]) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) a[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p + (2 * c + g) * 16));
+  }
+  static __device__ __forceinline__ void rows(const unsigned char* tile, int r, int g, A (&a)[kSteps]) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) a[c] = *LDS_PTR(bf16x8, tile + r * kRow + (((2 * c + g) ^ swizzle(r)) << 4));
+  }
+  // columns 32 db .. + 31 of the 32 tile rows from r0 on: lane (n, g) holds column n of the rows whose products' results lie in the lane
+  static __device__ __forceinline__ void columns(const unsigned char* tile, int r0, int db, int lane, A (&a)[kCols]) {
+    const int m = (lane & 15) >> 2, j = lane & 3, G = lane >> 4;
+    const int chunk = db * 4 + 2 * (G & 1) + (j >> 1);
+#pragma unroll
+    for (int cp = 0; cp < 2; ++cp) {
+      u32x2 x[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = r0 + 16 * cp + 8 * e + 4 * (lane >> 5) + m;
+        const unsigned char* p = tile + r * kRow + ((chunk ^ swizzle(r)) << 4) + (j & 1) * 8;
+        x[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(p)));
+      }
+      a[cp] = __builtin_bit_cast(bf16x8, u32x4{x[0][0], x[0][1], x[1][0], x[1][1]});
+    }
+  }
+  // a product's result, rounded to an operand
+  static __device__ __forceinline__ void round(const f32x16& x, A (&a)[kCols]) {
+#pragma unroll
+    for (int cp = 0; cp < 2; ++cp) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = pack_bf16(x[8 * cp + 2 * e], x[8 * cp + 2 * e + 1]);
+      a[cp] = __builtin_bit_cast(bf16x8, w);
+    }
+  }
+  static __device__ __forceinline__ float number(const unsigned char* p, int i) {
+    return __uint_as_float(static_cast<unsigned>(reinterpret_cast<const unsigned short*>(p)[i]) << 16);
+  }
+  static __device__ __forceinline__ void store4(unsigned char* p, int i, float a, float b, float c, float d) {
+    *reinterpret_cast<u32x2*>(p + i * 2) = u32x2{pack_bf16(a, b), pack_bf16(c, d)};
+  }
+  static __device__ __forceinline__ void store1(unsigned char* p, int i, float x) {
+    reinterpret_cast<unsigned short*>(p)[i] = static_cast<unsigned short>(pack_bf16(x, 0.f));
+  }
+};
+
+template <>
+struct Ops<float> {
+  typedef float A;
+  static constexpr int kRow = 256;
+  static constexpr int kSteps = 32;
+  static constexpr int kCols = 16;
+  static __device__ __forceinline__ f32x16 product(A a, A b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ int swizzle(int r) { return r & 15; }
+  // lane half g holds 4 of each 8 numbers
+  static __device__ __forceinline__ void row(const unsigned char* p, int g, A (&a)[kSteps]) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(p + (2 * c + g) * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[4 * c + e] = x[e];
+    }
+  }
+  static __device__ __forceinline__ void rows(const unsigned char* tile, int r, int g, A (&a)[kSteps]) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const f32x4 x = *LDS_PTR(f32x4, tile + r * kRow + (((2 * c + g) ^ swizzle(r)) << 4));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[4 * c + e] = x[e];
+    }
+  }
+  static __device__ __forceinline__ void columns(const unsigned char* tile, int r0, int db, int lane, A (&a)[kCols]) {
+    const int d = db * 32 + (lane & 31);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int r = r0 + 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3);
+      a[i] = *LDS_PTR(float, tile + r * kRow + (((d >> 2) ^ swizzle(r)) << 4) + (d & 3) * 4);
+    }
+  }
+  static __device__ __forceinline__ void round(const f32x16& x, A (&a)[kCols]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) a[i] = x[i];
+  }
+  static __device__ __forceinline__ float number(const unsigned char* p, int i) { return reinterpret_cast<const float*>(p)[i]; }
+  static __device__ __forceinline__ void store4(unsigned char* p, int i, float a, float b, float c, float d) {
+    *reinterpret_cast<f32x4*>(p + i * 4) = f32x4{a, b, c, d};
+  }
+  static __device__ __forceinline__ void store1(unsigned char* p, int i, float x) { reinterpret_cast<float*>(p)[i] = x; }
+};
+
+__device__ __forceinline__ void clear(f32x16& x) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = 0.f;
+}
+
+// Rows [r0, r0 + 64) of one head of a tensor straight into a tile (rows past the tensor's end become zeros), by `waves` waves.  The
+// descriptor starts at the tile, so that 32-bit offsets do whatever the tensor's size is.
+template <typename T, int WAVES>
+__device__ __forceinline__ void load_tile(const unsigned char* head, int64_t token, int n, int r0, unsigned lds, int wave, int lane) {
+  constexpr int kRow = Ops<T>::kRow, kChunks = kRow / 16, kRows = 64 / kChunks, kLoads = kTile / kRows;
+  const int64_t left = n - r0;
+  const i32x4 rsrc = make_rsrc(head + r0 * token, left > 0 ? static_cast<unsigned>((min(left, int64_t(kTile)) - 1) * token + kRow) : 0u);
+  const int r_in = lane / kChunks, pos = lane % kChunks;
+#pragma unroll
+  for (int i = 0; i < kLoads / WAVES; ++i) {
+    const int load = WAVES * i + wave;
+    const int r = load * kRows + r_in;
+    dma16<0>(rsrc, static_cast<unsigned>(r * token) + ((pos ^ Ops<T>::swizzle(r)) << 4), 0u, lds + load * 1024);
+  }
+}
+
+__device__ __forceinline__ unsigned lds_address(const unsigned char* p) {
+  return static_cast<unsigned>(reinterpret_cast<size_t>((const __attribute__((address_space(3))) unsigned char*)p));
+}
+
+// Workgroup w of a grid runs on XCD w % 8, and the chip holds `places` workgroups: inside each full group of them every XCD gets neighbours.
+__device__ __forceinline__ int64_t spread(int64_t w, int64_t all, int places) {
+  const int64_t base = w / places * places;
+  if (base + places > all) return w;
+  const int r = static_cast<int>(w - base);
+  return base + (r & 7) * (places >> 3) + (r >> 3);
+}
+
+}  // namespace
+}  // namespace bsga

@@ -1,0 +1,399 @@
+// Attention with a sliding window, counted in frames, and a few first tokens that stay visible.
+//
+// o_i = sum_j softmax_j(scale <q_i, k_j>) v_j over the keys that query i sees (window.h).  A workgroup takes 64 queries for each of its waves;
+// a wave holds its 64 queries as B operands and computes S^T = K Q^T, so that a lane has scores of one query, and their weights
+// are the B operand of O^T = V^T P^T as they are.  Tiles of 64 keys go straight into LDS, two ahead, one barrier a tile.  Every wave
+// sorts a tile for its own rows: seen by all (no masking), by none (skipped), by some.
+// Weights are exp2(scale log2(e) s - m) with the products' s in fp32: queries are not scaled beforehand, which would round them a second time.
+// The running maximum m follows when a tile exceeds it by 2^8.
+#include "window.h"
+
+#include <math.h>
+
+namespace bsga {
+namespace {
+
+constexpr float kRaise = 8.0f;
+constexpr int kPlaces = 512;   // workgroups of four waves that the chip holds
+
+struct WindowArgs {
+  View q, k, v;
+  unsigned char* out;     // [heads, n_q, 64]
+  float* lse;             // [heads, n_q] or null
+  float *part, *part_lse; // with splits: [splits][heads, n_q, 64] and [splits][heads, n_q]
+  Seen seen;
+  int heads, group, row_tiles, splits;
+  float scale_log2;
+};
+
+// The tiles of a workgroup's rows: `first` of them from key 0 on, then those from key tile `start` on.
+struct Tiles {
+  int first, start, count;
+  __host__ __device__ int key(int t) const { return (t < first ? t : start + t - first) * kTile; }
+};
+
+__host__ __device__ inline Tiles tiles_of(const Seen& s, int i0, int i1) {  // queries [i0, i1)
+  int lo, hi, lo1, hi1;
+  s.range(i0, lo, hi);
+  s.range(i1 - 1, lo1, hi1);
+  Tiles t;
+  t.first = (min(min(s.sinks, lo1), lo) + kTile - 1) / kTile;
+  t.start = max(lo / kTile, t.first);
+  t.count = t.first + max((hi1 + kTile - 1) / kTile - t.start, 0);
+  return t;
+}
+
+// One query again, by a wave on its own, over the keys that it sees and no others: rows whose result is not finite.  A key that a row does not
+// see is multiplied by a weight of zero in the products, which is not nothing if the value is infinite or not a number.
+template <typename T>
+__device__ void exact_row(const WindowArgs& a, const unsigned char* q, const unsigned char* k, const unsigned char* v, int i, int t0, int t1,
+                          const Tiles& tiles, unsigned char* out, float* part, float* lse, int lane) {
+  int lo, hi;
+  a.seen.range(i, lo, hi);
+  float m = -INFINITY, l = 0.f, o = 0.f;
+  for (int t = t0; t < t1; ++t) {
+    const int j = tiles.key(t) + lane;
+    const bool sees = j < hi && (j >= lo || j < a.seen.sinks);
+    float s = -INFINITY;
+    if (sees) {
+      s = 0.f;
+      for (int d = 0; d < 64; ++d) s += Ops<T>::number(q, d) * Ops<T>::number(k + j * a.k.token, d);
+      s *= a.scale_log2;
+    }
+    float top = s;
+    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    const float to = fmaxf(m, top);
+    const float keep = m == -INFINITY ? 0.f : exp2f(m - to);
+    const float w = sees ? exp2f(s - (to == -INFINITY ? 0.f : to)) : 0.f;  // (NaN stays)
+    float sum = w;
+    for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
+    l = l * keep + sum;
+    o *= keep;
+    m = to;
+    unsigned long long all = __ballot(sees);
+    while (all != 0) {
+      const int e = __builtin_ctzll(all);
+      all &= all - 1;
+      o += __shfl(w, e) * Ops<T>::number(v + (tiles.key(t) + int64_t(e)) * a.v.token, lane);
+    }
+  }
+  const float value = l == 0.f ? 0.f : o / l;
+  if (out != nullptr) Ops<T>::store1(out, lane, value);
+  else part[lane] = value;
+  if (lse != nullptr && lane == 0) *lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+template <typename T, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void window_kernel(const WindowArgs a) {
+  typedef Ops<T> P;
+  constexpr int kTileBytes = kTile * P::kRow;
+  extern __shared__ __align__(16) unsigned char smem[];  // K, V of buffer 0, K, V of buffer 1
+  const int lane = threadIdx.x & 63;
+  const int wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, g = lane >> 5;
+  // later rows see more where the window is long: they go first
+  const int64_t unit = spread(blockIdx.x, gridDim.x, kPlaces);
+  const int split = static_cast<int>(unit % a.splits);
+  const int h = static_cast<int>(unit / a.splits / a.row_tiles);
+  const int rt = a.row_tiles - 1 - static_cast<int>(unit / a.splits % a.row_tiles);
+  const int i0 = rt * kTile * WAVES, i1 = min(i0 + kTile * WAVES, a.seen.n_q);
+  const Tiles tiles = tiles_of(a.seen, i0, i1);
+  const int t0 = static_cast<int>(int64_t(tiles.count) * split / a.splits), t1 = static_cast<int>(int64_t(tiles.count) * (split + 1) / a.splits);
+  const unsigned char* const qh = a.q.p + h * a.q.head;
+  const unsigned char* const kh = a.k.p + h / a.group * a.k.head;
+  const unsigned char* const vh = a.v.p + h / a.group * a.v.head;
+  const unsigned lds = lds_address(smem);
+  auto issue = [&](int t, int buf) {
+    const int key = tiles.key(t);
+    load_tile<T, WAVES>(kh, a.k.token, a.seen.n_k, key, lds + buf * 2 * kTileBytes, wave, lane);
+    load_tile<T, WAVES>(vh, a.v.token, a.seen.n_k, key, lds + (buf * 2 + 1) * kTileBytes, wave, lane);
+  };
+  if (t0 < t1) issue(t0, 0);
+
+  // the wave's rows [w0, w1); rows past the end are computed as the last one and not stored
+  const int w0 = i0 + wave * kTile, w1 = min(w0 + kTile, a.seen.n_q);
+  const bool none = w0 >= a.seen.n_q;
+  typename P::A qf[2][P::kSteps];
+  int lo[2], hi[2], lo_min = 0, hi_min = 0, lo_max = 0, hi_max = 0;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int i = min(w0 + 32 * b + n, a.seen.n_q - 1);
+    P::row(qh + i * a.q.token, g, qf[b]);
+    a.seen.range(i, lo[b], hi[b]);
+  }
+  if (!none) {
+    a.seen.range(w0, lo_min, hi_min);
+    a.seen.range(w1 - 1, lo_max, hi_max);
+  }
+
+  f32x16 o[2][2];  // [dimensions][queries]
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+  for (int db = 0; db < 2; ++db)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) clear(o[db][b]);
+
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1;
+    if (t + 1 < t1) {
+      issue(t + 1, buf ^ 1);
+      constexpr int kInFlight = 2 * kTileBytes / 1024 / WAVES;
+      __builtin_amdgcn_s_waitcnt((kInFlight & 15) | (kInFlight >> 4 << 14) | 0x0f70);  // this tile's have landed
+    } else {
+      __builtin_amdgcn_s_waitcnt(0x0f70);
+    }
+    __syncthreads();
+    const int key = tiles.key(t);
+    const bool seen_by_none = none || key >= hi_max || (key + kTile <= lo_min && key >= a.seen.sinks);
+    const bool seen_by_all = key + kTile <= hi_min && (key >= lo_max || key + kTile <= a.seen.sinks || a.seen.sinks >= lo_max);
+    if (!seen_by_none) {
+      const unsigned char* const kt = smem + buf * 2 * kTileBytes;
+      const unsigned char* const vt = kt + kTileBytes;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        typename P::A ka[P::kSteps];
+        P::rows(kt, 32 * u + n, g, ka);
+        f32x16 s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          clear(s[b]);
+#pragma unroll
+          for (int c = 0; c < P::kSteps; ++c) s[b] = P::product(ka[c], qf[b][c], s[b]);
+          if (!seen_by_all) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int j = key + 32 * u + 8 * (i >> 2) + 4 * g + (i & 3);
+              s[b][i] = j < hi[b] && (j >= lo[b] || j < a.seen.sinks) ? s[b][i] : -INFINITY;
+            }
+          }
+        }
+        typename P::A w[2][P::kCols];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          float top = s[b][0];
+#pragma unroll
+          for (int i = 1; i < 16; ++i) top = fmaxf(top, s[b][i]);
+          top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+          const bool raise = m[b] == -INFINITY ? top > -INFINITY : top > m[b] + kRaise;
+          if (__any(raise)) {
+            const float to = raise ? top : m[b];
+            const float keep = m[b] == -INFINITY ? 1.f : exp2f(m[b] - to);  // (of nothing so far, what is kept is zero)
+            m[b] = to;
+            l[b] *= keep;
+#pragma unroll
+            for (int db = 0; db < 2; ++db)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[db][b][i] *= keep;
+          }
+          const float from = m[b] == -INFINITY ? 0.f : m[b];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], a.scale_log2, -from));
+            l[b] += s[b][i];
+          }
+          P::round(s[b], w[b]);
+        }
+#pragma unroll
+        for (int db = 0; db < 2; ++db) {
+          typename P::A va[P::kCols];
+          P::columns(vt, 32 * u, db, lane, va);
+#pragma unroll
+          for (int c = 0; c < P::kCols; ++c) {
+            o[db][0] = P::product(va[c], w[0][c], o[db][0]);
+            o[db][1] = P::product(va[c], w[1][c], o[db][1]);
+          }
+        }
+      }
+    }
+    __syncthreads();  // the buffer is read
+  }
+
+  if (none) return;  // (no barrier follows)
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const float sum = l[b] + __shfl_xor(l[b], 32);
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    bool bad = !(sum < INFINITY);
+#pragma unroll
+    for (int db = 0; db < 2; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        bad = bad || !(fabsf(o[db][b][i]) < INFINITY);
+        o[db][b][i] *= inv;
+      }
+    const int i = w0 + 32 * b + n;
+    const int64_t at = int64_t(h) * a.seen.n_q + i;
+    const int64_t in_part = int64_t(split) * a.heads * a.seen.n_q + at;
+    float* const lse = a.splits > 1 ? a.part_lse + in_part : a.lse != nullptr ? a.lse + at : nullptr;
+    if (i < a.seen.n_q) {
+#pragma unroll
+      for (int db = 0; db < 2; ++db)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const f32x16& x = o[db][b];
+          const int d = db * 32 + 8 * r + 4 * g;
+          if (a.splits > 1) *reinterpret_cast<f32x4*>(a.part + in_part * 64 + d) = f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
+          else P::store4(a.out + at * P::kRow, d, x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]);
+        }
+      if (lse != nullptr && g == 0) *lse = sum > 0.f ? (m[b] + log2f(sum)) * kLn2 : -INFINITY;
+    }
+    unsigned long long again = __ballot(bad && i < a.seen.n_q);
+    again = (again | again >> 32) & 0xffffffffull;
+    while (again != 0) {
+      const int row = w0 + 32 * b + __builtin_ctzll(again);
+      again &= again - 1;
+      const int64_t to = int64_t(h) * a.seen.n_q + row, to_part = int64_t(split) * a.heads * a.seen.n_q + to;
+      exact_row<T>(a, qh + row * a.q.token, kh, vh, row, t0, t1, tiles, a.splits > 1 ? nullptr : a.out + to * P::kRow,
+                   a.splits > 1 ? a.part + to_part * 64 : nullptr, a.splits > 1 ? a.part_lse + to_part : a.lse != nullptr ? a.lse + to : nullptr, lane);
+    }
+  }
+}
+
+// The splits of a row together: sixteen lanes to a row.
+template <typename T>
+__global__ __launch_bounds__(256) void window_join_kernel(const float* __restrict__ part, const float* __restrict__ part_lse, int64_t rows,
+                                                          int splits, unsigned char* __restrict__ out, float* __restrict__ lse) {
+  const int64_t row = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4);
+  const int d = (threadIdx.x & 15) * 4;
+  if (row >= rows) return;
+  float top = -INFINITY;
+  bool nan = false;
+  for (int s = 0; s < splits; ++s) {
+    const float x = part_lse[s * rows + row];
+    top = fmaxf(top, x);
+    nan = nan || x != x;
+  }
+  if (nan) top = NAN;
+  float sum = 0.f;
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < splits && top != -INFINITY; ++s) {
+    const float from = part_lse[s * rows + row];
+    if (from == -INFINITY) continue;  // saw nothing
+    const float w = exp2f((from - top) * kLog2e);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(part + (s * rows + row) * 64 + d);
+    sum += w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] += w * x[e];
+  }
+  const float inv = top == -INFINITY ? 0.f : 1.f / sum;
+  Ops<T>::store4(out + row * Ops<T>::kRow, d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+  if (lse != nullptr && d == 0) lse[row] = top == -INFINITY ? -INFINITY : top + log2f(sum) * kLn2;
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+int check_seen(const char* fn, int64_t n_q, int64_t n_k, int64_t q_start, int64_t frame, int64_t window, int64_t sinks, Seen& s) {
+  const int64_t most = int64_t(1) << 24;
+  if (n_q < 0 || n_q > most || n_k < 0 || n_k > most)
+    return fail(BSGA_ERR_INVALID_ARG, "%s: n_q and n_k must be in [0, 2^24], got %lld and %lld", fn, (long long)n_q, (long long)n_k);
+  if (q_start < -most || q_start > 2 * most)
+    return fail(BSGA_ERR_INVALID_ARG, "%s: q_start must be in [-2^24, 2^25], got %lld", fn, (long long)q_start);
+  if (frame < 1 || frame > most) return fail(BSGA_ERR_INVALID_ARG, "%s: frame must be in [1, 2^24] tokens, got %lld", fn, (long long)frame);
+  if (window < 0) return fail(BSGA_ERR_INVALID_ARG, "%s: window must be >= 0 frames (0: no limit), got %lld", fn, (long long)window);
+  if (sinks < 0) return fail(BSGA_ERR_INVALID_ARG, "%s: sinks must be >= 0, got %lld", fn, (long long)sinks);
+  s.n_q = static_cast<int>(n_q);
+  s.n_k = static_cast<int>(n_k);
+  s.q_start = static_cast<int>(q_start);
+  s.frame = static_cast<int>(frame);
+  s.window = window == 0 || window > 4 * most ? static_cast<int>(4 * most) : static_cast<int>(window);  // more frames than there are
+  s.sinks = static_cast<int>(sinks < n_k ? sinks : n_k);
+  return BSGA_OK;
+}
+
+int check_view(const char* fn, const char* name, const void* p, int64_t token, int64_t head, int size, View& v) {
+  if (!p || !aligned16(p) || token < 0 || head < 0 || token * size % 16 != 0 || head * size % 16 != 0 || token * size >= int64_t(1) << 24)
+    return fail(BSGA_ERR_INVALID_ARG, "%s: %s must be non-null, it and its strides multiples of 16 bytes, a token's stride in [0, 2^24) bytes", fn, name);
+  v = {static_cast<const unsigned char*>(p), token * size, head * size};
+  return BSGA_OK;
+}
+
+// Waves of a workgroup and splits of its keys.  Four waves share tiles; a launch of few rows takes one to a workgroup, and where that leaves
+// CUs without work the keys are dealt out too, at least four tiles to each.
+void shape_of(const Seen& s, int heads, int& waves, int& splits) {
+  const int64_t tiles4 = ceil_div(s.n_q, 4 * kTile) * heads;
+  waves = s.n_q > 2 * kTile ? 4 : 1;
+  splits = 1;
+  const int64_t units = waves == 4 ? tiles4 : ceil_div(s.n_q, kTile) * heads;
+  const int64_t places = waves == 4 ? kPlaces : 2 * kPlaces;
+  if (units * 2 > places) return;
+  int most = 0;  // the rows that see most are among the last ones, or, past the last key, the first
+  for (int64_t rt = 0, all = ceil_div(s.n_q, waves * kTile); rt < all; ++rt) {
+    const int i0 = static_cast<int>(rt * waves * kTile);
+    const int c = tiles_of(s, i0, static_cast<int>(min(int64_t(i0) + waves * kTile, int64_t(s.n_q)))).count;
+    most = c > most ? c : most;
+  }
+  splits = static_cast<int>(min(places / units, int64_t(most / 4)));
+  if (splits < 1) splits = 1;
+}
+
+size_t split_bytes(int heads, int64_t n_q, int splits) { return splits > 1 ? static_cast<size_t>(splits) * heads * n_q * 65 * sizeof(float) : 0; }
+
+template <typename T>
+int launch(const WindowArgs& a, int waves, hipStream_t s) {
+  const int64_t units = int64_t(a.heads) * a.row_tiles * a.splits;
+  if (units > 0x7fffffff) return fail(BSGA_ERR_UNSUPPORTED, "bsga_window_attn: too many rows");
+  const size_t lds = 4 * kTile * Ops<T>::kRow;
+  if (waves == 4) hipLaunchKernelGGL((window_kernel<T, 4>), dim3(static_cast<unsigned>(units)), dim3(256), lds, s, a);
+  else hipLaunchKernelGGL((window_kernel<T, 1>), dim3(static_cast<unsigned>(units)), dim3(64), lds, s, a);
+  if (int rc = check_hip(hipGetLastError(), "bsga_window_attn launch")) return rc;
+  if (a.splits == 1) return BSGA_OK;
+  const int64_t rows = int64_t(a.heads) * a.seen.n_q;
+  hipLaunchKernelGGL(window_join_kernel<T>, dim3(static_cast<unsigned>(ceil_div(rows, 16))), dim3(256), 0, s, a.part, a.part_lse, rows, a.splits,
+                     a.out, a.lse);
+  return check_hip(hipGetLastError(), "bsga_window_attn launch");
+}
+
+}  // namespace
+}  // namespace bsga
+
+using namespace bsga;
+
+extern "C" {
+
+size_t bsga_window_attn_workspace_bytes(int dtype, int heads, int64_t n_q, int64_t n_k, int64_t q_start, int64_t frame, int64_t window,
+                                        int64_t sinks) {
+  Seen s;
+  if ((dtype != BSGA_BF16 && dtype != BSGA_FP32) || heads < 1 || heads > 65535 || n_q < 1 || n_k < 1) return 0;
+  if (check_seen("", n_q, n_k, q_start, frame, window, sinks, s)) return 0;
+  int waves, splits;
+  shape_of(s, heads, waves, splits);
+  return split_bytes(heads, n_q, splits);
+}
+
+int bsga_window_attn(const void* q, const void* k, const void* v, int64_t q_token, int64_t q_head, int64_t k_token, int64_t k_head,
+                     int64_t v_token, int64_t v_head, int dtype, int heads, int kv_heads, int64_t n_q, int64_t n_k, int head_dim,
+                     float softmax_scale, int64_t q_start, int64_t frame, int64_t window, int64_t sinks, void* out, float* lse, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  const char* fn = "bsga_window_attn";
+  clear_error();
+  WindowArgs a = {};
+  if (dtype != BSGA_BF16 && dtype != BSGA_FP32) return fail(BSGA_ERR_INVALID_ARG, "%s: unknown dtype %d", fn, dtype);
+  if (head_dim != 64) return fail(BSGA_ERR_UNSUPPORTED, "%s: head_dim must be 64, got %d", fn, head_dim);
+  if (heads < 1 || heads > 65535 || kv_heads < 1 || heads % kv_heads != 0)
+    return fail(BSGA_ERR_INVALID_ARG, "%s: heads must be in [1, 65535] and a multiple of kv_heads, got %d and %d", fn, heads, kv_heads);
+  if (int rc = check_seen(fn, n_q, n_k, q_start, frame, window, sinks, a.seen)) return rc;
+  if (!(softmax_scale > 0.0f) || !isfinite(softmax_scale)) return fail(BSGA_ERR_INVALID_ARG, "%s: softmax_scale must be finite and > 0", fn);
+  if (n_q == 0) return BSGA_OK;
+  const int size = dtype == BSGA_BF16 ? 2 : 4;
+  if (int rc = check_view(fn, "q", q, q_token, q_head, size, a.q)) return rc;
+  if (n_k > 0) {
+    if (int rc = check_view(fn, "k", k, k_token, k_head, size, a.k)) return rc;
+    if (int rc = check_view(fn, "v", v, v_token, v_head, size, a.v)) return rc;
+  }
+  if (!out || !aligned16(out)) return fail(BSGA_ERR_INVALID_ARG, "%s: out must be non-null and 16-byte aligned", fn);
+  a.out = static_cast<unsigned char*>(out);
+  a.lse = lse;
+  a.heads = heads;
+  a.group = heads / kv_heads;
+  a.scale_log2 = softmax_scale * kLog2e;
+  int waves;
+  shape_of(a.seen, heads, waves, a.splits);
+  if (!workspace || !aligned16(workspace) || workspace_bytes < split_bytes(heads, n_q, a.splits)) a.splits = 1;  // one workgroup takes all keys of its rows
+  a.row_tiles = static_cast<int>(ceil_div(n_q, waves * kTile));
+  a.part = static_cast<float*>(workspace);
+  if (a.splits > 1) a.part_lse = a.part + int64_t(a.splits) * heads * n_q * 64;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return dtype == BSGA_BF16 ? launch<__bf16>(a, waves, s) : launch<float>(a, waves, s);
+}
+
+}  // extern "C"

@@ -1,0 +1,192 @@
+"""Attention with a sliding window and first tokens that stay visible, against the definition in float64 on an explicit mask.
+
+Bounds.  fp32 logits: a product of 64 terms is off by at most 64 roundings of 2^-24 of sum |q k| scale, and so is, relatively, a weight; with
+logits up to L = max sum |q k| scale that is 2^-18 L, and the sums add 2^-18 of sum p |v|.  bf16: the weights are rounded, 2^-9 of sum p |v|
+(they are rounded to nearest: half of 2^-8), and the result, 2^-9 |o|; the sum of weights is taken before the rounding."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+TYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def B():
+    import paper_2509_07120_amd as pkg
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return pkg
+
+
+def seen_by(N, M, window, sinks, frame, q_start, device="cuda"):
+    p = torch.arange(N, device=device)[:, None] + (M - N if q_start is None else q_start)
+    j = torch.arange(M, device=device)[None]
+    fp, fj = p.div(frame, rounding_mode="floor"), j // frame
+    near = (fp - fj < window) if window is not None else torch.ones_like(fp < fj)
+    return (fj <= fp) & (near | (j < sinks)) & (p >= 0)
+
+
+def attend(q, k, v, seen, scale):
+    """(o, lse, sum p |v|, largest sum |q k| scale of a query) in float64."""
+    G = q.shape[0] // k.shape[0]
+    q, k, v = q.double(), k.double().repeat_interleave(G, 0), v.double().repeat_interleave(G, 0)
+    x = torch.where(seen, q @ k.transpose(1, 2) * scale, -math.inf)
+    size = torch.where(seen, q.abs() @ k.abs().transpose(1, 2) * scale, 0).amax(-1)
+    top = x.amax(-1, keepdim=True)
+    p = torch.where(seen, (x - torch.where(top == -math.inf, 0, top)).exp(), 0)
+    s = p.sum(-1, keepdim=True)
+    w = torch.where(s > 0, p / s, 0)
+    return w @ v, torch.where(s > 0, s.log() + top, -math.inf)[..., 0], w @ v.abs(), size
+
+
+def draw(H, K, N, M, dtype, seed=0, gain=1.0, layout="heads"):
+    g = torch.Generator(device="cuda").manual_seed(seed + 7 * N + M + H)
+    out = []
+    for h, n in ((H, N), (K, M), (K, M)):
+        x = (gain * torch.randn((h, n, 64), generator=g, device="cuda")).to(dtype)
+        if layout == "tokens":  # [tokens, heads, 64], as a projection leaves it
+            x = x.transpose(0, 1).contiguous().transpose(0, 1)
+        if layout == "gaps":
+            wide = torch.full((h + 1, n + 5, 80), float("nan"), dtype=dtype, device="cuda")
+            wide[:h, :n, 8:72] = x
+            x = wide[:h, :n, 8:72]
+        out.append(x)
+    return out
+
+
+def check(o, lse, q, k, v, seen, scale=0.125):
+    want, wlse, pv, size = attend(q, k, v, seen, scale)
+    eps = torch.finfo(o.dtype).eps / 2
+    rounded = eps * pv if o.dtype == torch.bfloat16 else 0.0
+    slack = 2.0 ** -18 * (2 + size[..., None]) * pv + 1.05 * rounded
+    err = (o.double() - want).abs()
+    bound = slack + eps * (want.abs() + slack) + 1e-30
+    assert bool((err <= bound).all()), float((err - bound).max())
+    if lse is not None:
+        dark = wlse == -math.inf
+        assert bool((lse.double()[dark] == -math.inf).all())
+        off = (lse.double() - wlse)[~dark].abs()
+        assert bool((off <= (2.0 ** -18 * (2 + size) + 2.0 ** -23 * wlse.abs())[~dark]).all()), float(off.max())
+
+
+CASES = [  # heads, key heads, queries, keys, window, sinks, frame, q_start, type, layout
+    (1, 1, 1, 1, None, 0, 1, None, "bf16", "heads"),
+    (2, 1, 1, 700, 100, 3, 1, None, "bf16", "tokens"),
+    (3, 3, 64, 64, None, 0, 1, None, "bf16", "heads"),
+    (4, 2, 65, 65, 1, 0, 1, None, "bf16", "gaps"),
+    (2, 2, 128, 4000, 700, 64, 1, None, "bf16", "tokens"),
+    (4, 4, 257, 257, 64, 5, 1, None, "bf16", "heads"),
+    (6, 2, 300, 1000, 130, 130, 1, None, "bf16", "tokens"),
+    (2, 1, 1374, 3 * 1374, 2, 5, 1374, None, "bf16", "heads"),
+    (2, 2, 1000, 1000, 3, 111, 111, None, "bf16", "gaps"),
+    (3, 1, 999, 1500, 2, 0, 37, 100, "bf16", "heads"),         # later keys that no query sees
+    (2, 2, 700, 300, 100, 0, 1, -200, "bf16", "heads"),        # queries before the first key and past the last one
+    (2, 2, 700, 300, 100, 3, 1, -200, "bf16", "heads"),
+    (1, 1, 500, 10, 7, 0, 5, 0, "bf16", "heads"),
+    (5, 5, 3000, 3000, 1000, 4, 1, None, "bf16", "tokens"),
+    (2, 1, 5000, 5000, None, 0, 1, None, "bf16", "heads"),
+    (1, 1, 1, 1, 1, 0, 1, None, "fp32", "heads"),
+    (4, 1, 130, 130, 33, 2, 1, None, "fp32", "gaps"),
+    (2, 2, 300, 2000, 500, 70, 1, None, "fp32", "tokens"),
+    (2, 2, 700, 300, 100, 3, 1, -200, "fp32", "heads"),
+    (3, 3, 1374, 1374, 1, 0, 687, None, "fp32", "heads"),
+]
+
+
+@pytest.mark.parametrize("H,K,N,M,window,sinks,frame,q_start,dtype,layout", CASES)
+def test_forward(B, H, K, N, M, window, sinks, frame, q_start, dtype, layout):
+    q, k, v = draw(H, K, N, M, TYPES[dtype], layout=layout)
+    what = dict(window=window, sinks=sinks, frame=frame, q_start=q_start)
+    seen = seen_by(N, M, window, sinks, frame, q_start)
+    o, lse = B.bsga_window_attn(q, k, v, return_lse=True, **what)
+    check(o, lse, q, k, v, seen)
+    assert torch.equal(B.bsga_window_attn(q, k, v, **what), o)
+    # no room for splits: one workgroup takes all keys of its rows
+    o, lse = B.bsga_window_attn(q, k, v, return_lse=True, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"), **what)
+    check(o, lse, q, k, v, seen)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("gain", [0.0, 4.0, 12.0])
+def test_logits_of_any_size(B, dtype, gain):
+    """Logits of 0 and up to 150 and 1400: the running maximum has to follow."""
+    q, k, v = draw(2, 2, 600, 900, TYPES[dtype], gain=gain)
+    v = draw(2, 2, 600, 900, TYPES[dtype])[2]
+    q = q * 1.0
+    k[:, 400:] *= 2  # later keys outgrow what the first tiles have shown
+    seen = seen_by(600, 900, 500, 7, 1, None)
+    o, lse = B.bsga_window_attn(q, k, v, window=500, sinks=7, return_lse=True)
+    check(o, lse, q, k, v, seen)
+
+
+def test_scale(B):
+    q, k, v = draw(2, 2, 200, 200, torch.bfloat16)
+    for scale in (1.0, 0.01):
+        o = B.bsga_window_attn(q, k, v, window=60, softmax_scale=scale)
+        check(o, None, q, k, v, seen_by(200, 200, 60, 0, 1, None), scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf"), 3e38])
+@pytest.mark.parametrize("N", [90, 600])
+def test_values_in_masked_places(B, dtype, bad, N):
+    """Keys that a query does not see may hold anything; those that do see them get what the formula gives."""
+    M = N
+    q, k, v = draw(2, 1, N, M, TYPES[dtype])
+    seen = seen_by(N, M, 70, 3, 1, None)
+    clean = B.bsga_window_attn(q, k, v, window=70, sinks=3)
+    k2, v2 = k.clone(), v.clone()
+    k2[0, 40], v2[0, 41] = bad, bad
+    o = B.bsga_window_attn(q, k2, v2, window=70, sinks=3)
+    touched = seen[:, 40] | seen[:, 41]
+    assert not bool(touched.all())
+    check(o[:, ~touched], None, q[:, ~touched], k, v, seen[~touched])
+    if bad != 3e38:
+        alone = touched & ~seen[:, 40]
+        assert not bool(o[:, touched & seen[:, 41]].isfinite().any()) or bool(alone.any()) is False
+    assert clean.isfinite().all()
+
+
+def test_another_stream_and_a_graph(B):
+    q, k, v = draw(4, 2, 500, 3000, torch.bfloat16)
+
+    def step():
+        return B.bsga_window_attn(q, k, v, window=1000, sinks=4, return_lse=True)
+
+    want = step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for i in range(4):
+        q.mul_(1.0 + 0.25 * i)
+        v.neg_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, step()))
+
+
+def test_no_queries_and_no_keys(B):
+    q, k, v = draw(2, 2, 70, 70, torch.bfloat16)
+    assert B.bsga_window_attn(q[:, :0], k, v).shape == (2, 0, 64)
+    o, lse = B.bsga_window_attn(q, k[:, :0], v[:, :0], q_start=0, return_lse=True)
+    assert bool((o == 0).all()) and bool((lse == -math.inf).all())
+
+
+def test_offsets_past_32_bits(B):
+    """Rows of one head 8 KB apart over 2^19 + 100 tokens: the last ones lie past 2^32 bytes."""
+    M, N = (1 << 19) + 100, 70
+    big = torch.empty((M, 4096), dtype=torch.bfloat16, device="cuda")
+    q, _, _ = draw(1, 1, N, N, torch.bfloat16)
+    _, k, v = draw(1, 1, 1, 300, torch.bfloat16)
+    big[-300:, :64], big[-300:, 64:128] = k[0], v[0]
+    kb, vb = big[:, :64].unsqueeze(0), big[:, 64:128].unsqueeze(0)
+    o, lse = B.bsga_window_attn(q, kb, vb, window=200, return_lse=True)
+    check(o, lse, q, k, v, seen_by(N, 300, 200, 0, 1, None))
