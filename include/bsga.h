@@ -356,6 +356,20 @@ int bsga_window_attn(const void* q, const void* k, const void* v, int64_t q_toke
                      void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Its gradient.  dout [heads, n_q, 64] is the gradient of out; q, k, v and the rest as they were given, out and lse as bsga_window_attn
+ * returned them.  dq [heads, n_q, 64], dk and dv [kv_heads, n_k, 64] out (sums over the query heads that share a key head); keys
+ * that no query sees get zeros, queries that see nothing too.
+ *   workspace  bsga_window_attn_bwd_workspace_bytes(...) bytes, 16-byte aligned; overwritten
+ * bf16: products on bf16 MFMA, the weights and their gradients rounded to bf16 for the last product, sums in fp32.  No atomics: the same bits every time.
+ */
+size_t bsga_window_attn_bwd_workspace_bytes(int dtype, int heads, int kv_heads, int64_t n_q, int64_t n_k, int64_t q_start, int64_t frame,
+                                            int64_t window, int64_t sinks);
+int bsga_window_attn_bwd(const void* dout, const void* q, const void* k, const void* v, int64_t q_token, int64_t q_head, int64_t k_token,
+                         int64_t k_head, int64_t v_token, int64_t v_head, const void* out, const float* lse, int dtype, int heads,
+                         int kv_heads, int64_t n_q, int64_t n_k, int head_dim, float softmax_scale, int64_t q_start, int64_t frame,
+                         int64_t window, int64_t sinks, void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Measurement aid, not part of the method: the rate the matrix pipes sustain on the MFMA instruction
  * the bf16 attention kernels use (32x32x16 bf16, the products of Eqs. (1)/(2)), with no memory traffic
  * at all, two workgroups of four waves per CU.  The part lowers its clock with the switching activity

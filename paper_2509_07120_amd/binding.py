@@ -52,6 +52,8 @@ EXPORTED_SYMBOLS = (
     "bsga_qk_norm_rope_bwd",
     "bsga_qk_norm_rope_bwd_workspace_bytes",
     "bsga_window_attn",
+    "bsga_window_attn_bwd",
+    "bsga_window_attn_bwd_workspace_bytes",
     "bsga_window_attn_workspace_bytes",
 )
 
@@ -140,6 +142,11 @@ def _load() -> ctypes.CDLL:
         c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
     lib.bsga_window_attn_workspace_bytes.restype = c_size_t
     lib.bsga_window_attn_workspace_bytes.argtypes = [c_int, c_int, c_int64, c_int64] + seen
+    lib.bsga_window_attn_bwd.restype = c_int
+    lib.bsga_window_attn_bwd.argtypes = [c_void_p] * 4 + strides + [c_void_p, c_void_p, c_int, c_int, c_int, c_int64, c_int64, c_int,
+                                                                    c_float] + seen + [c_void_p] * 4 + [c_size_t, c_void_p]
+    lib.bsga_window_attn_bwd_workspace_bytes.restype = c_size_t
+    lib.bsga_window_attn_bwd_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int64, c_int64] + seen
     return lib
 
 
@@ -799,3 +806,27 @@ def bsga_window_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: 
     _check(lib.bsga_window_attn(_ptr(q), _ptr(k), _ptr(v), *strides, code, H, K, N, M, d, scale, *seen, _ptr(out), _ptr(lse),
                                 _ptr(workspace), nbytes, _stream(q)))
     return (out, lse) if return_lse else out
+
+
+def bsga_window_attn_bwd(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                         window: Optional[int] = None, sinks: int = 0, frame: int = 1, q_start: Optional[int] = None,
+                         softmax_scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradients (dq [H, N, 64], dk and dv [Hkv, M, 64]) of bsga_window_attn: dout is that of its output, out and lse are what it returned for
+    q, k, v and the same window."""
+    code = _dtype_code(q)
+    strides, H, K, N, M, d, seen, scale = _window_args(q, k, v, window, sinks, frame, q_start, softmax_scale)
+    for name, t, dtype, shape in (("dout", dout, q.dtype, (H, N, d)), ("out", out, q.dtype, (H, N, d)), ("lse", lse, torch.float32, (H, N))):
+        _require(t, name, dtype)
+        if tuple(t.shape) != shape or t.get_device() != q.get_device():
+            raise ValueError(f"{name} must be {shape} on the same device as q")
+    dq = torch.empty((H, N, d), dtype=q.dtype, device=q.device)
+    dk = torch.empty((K, M, d), dtype=q.dtype, device=q.device)
+    dv = torch.empty((K, M, d), dtype=q.dtype, device=q.device)
+    if workspace is None:
+        nbytes = lib.bsga_window_attn_bwd_workspace_bytes(code, H, K, N, M, *seen)
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes > 0 else None
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    _check(lib.bsga_window_attn_bwd(_ptr(dout), _ptr(q), _ptr(k), _ptr(v), *strides, _ptr(out), _ptr(lse), code, H, K, N, M, d, scale, *seen,
+                                    _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace), nbytes, _stream(q)))
+    return dq, dk, dv

@@ -28,19 +28,34 @@ struct Seen {
     hi = static_cast<int>(min(int64_t(f + 1) * frame, int64_t(n_k)));
     lo = f < window ? 0 : static_cast<int>(min(int64_t(f + 1 - window) * frame, int64_t(hi)));
   }
-  // The queries [first, last] that may see one of the keys [k0, k1) through the window; first > last: none
-  __host__ __device__ void queries_of(int k0, int k1, int& first, int& last) const {
-    const int64_t f0 = k0 / frame, f1 = (k1 - 1) / frame;
-    first = static_cast<int>(max(f0 * frame - q_start, int64_t(0)));
-    last = static_cast<int>(min((f1 + window) * frame - 1 - q_start, int64_t(n_q) - 1));
-  }
 };
+
+// The tiles of a workgroup's rows: `first` of them from key 0 on, then those from key tile `start` on.
+struct Tiles {
+  int first, start, count;
+  __host__ __device__ int key(int t) const { return (t < first ? t : start + t - first) * kTile; }
+};
+
+__host__ __device__ inline Tiles tiles_of(const Seen& s, int i0, int i1) {  // queries [i0, i1)
+  int lo, hi, lo1, hi1;
+  s.range(i0, lo, hi);
+  s.range(i1 - 1, lo1, hi1);
+  Tiles t;
+  t.first = (min(min(s.sinks, lo1), lo) + kTile - 1) / kTile;
+  t.start = max(lo / kTile, t.first);
+  t.count = t.first + max((hi1 + kTile - 1) / kTile - t.start, 0);
+  return t;
+}
 
 // A tensor [heads, tokens, 64] with strides in bytes.
 struct View {
   const unsigned char* p;
   int64_t token, head;
 };
+
+// 32-row parts of a wave's queries: more of them share the operands read from LDS, fp32 has no registers for two
+template <typename T>
+constexpr int kParts = sizeof(T) == 2 ? 2 : 1;
 
 template <typename T>
 struct Ops;
@@ -78,6 +93,14 @@ struct Ops<__bf16> {
       }
       a[cp] = __builtin_bit_cast(bf16x8, u32x4{x[0][0], x[0][1], x[1][0], x[1][1]});
     }
+  }
+  static __device__ __forceinline__ float dot(const A (&a)[kSteps], const A (&b)[kSteps]) {  // of the lane's halves of two rows
+    float s = 0.f;
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += static_cast<float>(a[c][e]) * static_cast<float>(b[c][e]);
+    return s;
   }
   // a product's result, rounded to an operand
   static __device__ __forceinline__ void round(const f32x16& x, A (&a)[kCols]) {
@@ -133,6 +156,12 @@ struct Ops<float> {
       a[i] = *LDS_PTR(float, tile + r * kRow + (((d >> 2) ^ swizzle(r)) << 4) + (d & 3) * 4);
     }
   }
+  static __device__ __forceinline__ float dot(const A (&a)[kSteps], const A (&b)[kSteps]) {
+    float s = 0.f;
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c) s += a[c] * b[c];
+    return s;
+  }
   static __device__ __forceinline__ void round(const f32x16& x, A (&a)[kCols]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) a[i] = x[i];
@@ -175,6 +204,33 @@ __device__ __forceinline__ int64_t spread(int64_t w, int64_t all, int places) {
   if (base + places > all) return w;
   const int r = static_cast<int>(w - base);
   return base + (r & 7) * (places >> 3) + (r >> 3);
+}
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+inline int check_seen(const char* fn, int64_t n_q, int64_t n_k, int64_t q_start, int64_t frame, int64_t window, int64_t sinks, Seen& s) {
+  const int64_t most = int64_t(1) << 24;
+  if (n_q < 0 || n_q > most || n_k < 0 || n_k > most)
+    return fail(BSGA_ERR_INVALID_ARG, "%s: n_q and n_k must be in [0, 2^24], got %lld and %lld", fn, (long long)n_q, (long long)n_k);
+  if (q_start < -most || q_start > 2 * most)
+    return fail(BSGA_ERR_INVALID_ARG, "%s: q_start must be in [-2^24, 2^25], got %lld", fn, (long long)q_start);
+  if (frame < 1 || frame > most) return fail(BSGA_ERR_INVALID_ARG, "%s: frame must be in [1, 2^24] tokens, got %lld", fn, (long long)frame);
+  if (window < 0) return fail(BSGA_ERR_INVALID_ARG, "%s: window must be >= 0 frames (0: no limit), got %lld", fn, (long long)window);
+  if (sinks < 0) return fail(BSGA_ERR_INVALID_ARG, "%s: sinks must be >= 0, got %lld", fn, (long long)sinks);
+  s.n_q = static_cast<int>(n_q);
+  s.n_k = static_cast<int>(n_k);
+  s.q_start = static_cast<int>(q_start);
+  s.frame = static_cast<int>(frame);
+  s.window = window == 0 || window > 4 * most ? static_cast<int>(4 * most) : static_cast<int>(window);  // more frames than there are
+  s.sinks = static_cast<int>(sinks < n_k ? sinks : n_k);
+  return BSGA_OK;
+}
+
+inline int check_view(const char* fn, const char* name, const void* p, int64_t token, int64_t head, int size, View& v) {
+  if (!p || !aligned16(p) || token < 0 || head < 0 || token * size % 16 != 0 || head * size % 16 != 0 || token * size >= int64_t(1) << 24)
+    return fail(BSGA_ERR_INVALID_ARG, "%s: %s must be non-null, it and its strides multiples of 16 bytes, a token's stride in [0, 2^24) bytes", fn, name);
+  v = {static_cast<const unsigned char*>(p), token * size, head * size};
+  return BSGA_OK;
 }
 
 }  // namespace

@@ -1,7 +1,7 @@
 // Attention with a sliding window, counted in frames, and a few first tokens that stay visible.
 //
-// o_i = sum_j softmax_j(scale <q_i, k_j>) v_j over the keys that query i sees (window.h).  A workgroup takes 64 queries for each of its waves;
-// a wave holds its 64 queries as B operands and computes S^T = K Q^T, so that a lane has scores of one query, and their weights
+// o_i = sum_j softmax_j(scale <q_i, k_j>) v_j over the keys that query i sees (window.h).  A workgroup takes 64 queries (fp32: 32) for each of its waves;
+// a wave holds its queries as B operands and computes S^T = K Q^T, so that a lane has scores of one query, and their weights
 // are the B operand of O^T = V^T P^T as they are.  Tiles of 64 keys go straight into LDS, two ahead, one barrier a tile.  Every wave
 // sorts a tile for its own rows: seen by all (no masking), by none (skipped), by some.
 // Weights are exp2(scale log2(e) s - m) with the products' s in fp32: queries are not scaled beforehand, which would round them a second time.
@@ -25,23 +25,6 @@ struct WindowArgs {
   int heads, group, row_tiles, splits;
   float scale_log2;
 };
-
-// The tiles of a workgroup's rows: `first` of them from key 0 on, then those from key tile `start` on.
-struct Tiles {
-  int first, start, count;
-  __host__ __device__ int key(int t) const { return (t < first ? t : start + t - first) * kTile; }
-};
-
-__host__ __device__ inline Tiles tiles_of(const Seen& s, int i0, int i1) {  // queries [i0, i1)
-  int lo, hi, lo1, hi1;
-  s.range(i0, lo, hi);
-  s.range(i1 - 1, lo1, hi1);
-  Tiles t;
-  t.first = (min(min(s.sinks, lo1), lo) + kTile - 1) / kTile;
-  t.start = max(lo / kTile, t.first);
-  t.count = t.first + max((hi1 + kTile - 1) / kTile - t.start, 0);
-  return t;
-}
 
 // One query again, by a wave on its own, over the keys that it sees and no others: rows whose result is not finite.  A key that a row does not
 // see is multiplied by a weight of zero in the products, which is not nothing if the value is infinite or not a number.
@@ -84,7 +67,7 @@ __device__ void exact_row(const WindowArgs& a, const unsigned char* q, const uns
 }
 
 template <typename T, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void window_kernel(const WindowArgs a) {
+__global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs a) {
   typedef Ops<T> P;
   constexpr int kTileBytes = kTile * P::kRow;
   extern __shared__ __align__(16) unsigned char smem[];  // K, V of buffer 0, K, V of buffer 1
@@ -96,7 +79,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void window_kernel(
   const int split = static_cast<int>(unit % a.splits);
   const int h = static_cast<int>(unit / a.splits / a.row_tiles);
   const int rt = a.row_tiles - 1 - static_cast<int>(unit / a.splits % a.row_tiles);
-  const int i0 = rt * kTile * WAVES, i1 = min(i0 + kTile * WAVES, a.seen.n_q);
+  constexpr int R = kParts<T>;
+  const int i0 = rt * 32 * R * WAVES, i1 = min(i0 + 32 * R * WAVES, a.seen.n_q);
   const Tiles tiles = tiles_of(a.seen, i0, i1);
   const int t0 = static_cast<int>(int64_t(tiles.count) * split / a.splits), t1 = static_cast<int>(int64_t(tiles.count) * (split + 1) / a.splits);
   const unsigned char* const qh = a.q.p + h * a.q.head;
@@ -111,12 +95,12 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void window_kernel(
   if (t0 < t1) issue(t0, 0);
 
   // the wave's rows [w0, w1); rows past the end are computed as the last one and not stored
-  const int w0 = i0 + wave * kTile, w1 = min(w0 + kTile, a.seen.n_q);
+  const int w0 = i0 + wave * 32 * R, w1 = min(w0 + 32 * R, a.seen.n_q);
   const bool none = w0 >= a.seen.n_q;
-  typename P::A qf[2][P::kSteps];
-  int lo[2], hi[2], lo_min = 0, hi_min = 0, lo_max = 0, hi_max = 0;
+  typename P::A qf[R][P::kSteps];
+  int lo[R], hi[R], lo_min = 0, hi_min = 0, lo_max = 0, hi_max = 0;
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+  for (int b = 0; b < R; ++b) {
     const int i = min(w0 + 32 * b + n, a.seen.n_q - 1);
     P::row(qh + i * a.q.token, g, qf[b]);
     a.seen.range(i, lo[b], hi[b]);
@@ -126,12 +110,15 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void window_kernel(
     a.seen.range(w1 - 1, lo_max, hi_max);
   }
 
-  f32x16 o[2][2];  // [dimensions][queries]
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  f32x16 o[2][R];  // [dimensions][queries]
+  float m[R], l[R];
 #pragma unroll
-  for (int db = 0; db < 2; ++db)
-#pragma unroll
-    for (int b = 0; b < 2; ++b) clear(o[db][b]);
+  for (int b = 0; b < R; ++b) {
+    clear(o[0][b]);
+    clear(o[1][b]);
+    m[b] = -INFINITY;
+    l[b] = 0.f;
+  }
 
   for (int t = t0; t < t1; ++t) {
     const int buf = (t - t0) & 1;
@@ -153,9 +140,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void window_kernel(
       for (int u = 0; u < 2; ++u) {
         typename P::A ka[P::kSteps];
         P::rows(kt, 32 * u + n, g, ka);
-        f32x16 s[2];
+        f32x16 s[R];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < R; ++b) {
           clear(s[b]);
 #pragma unroll
           for (int c = 0; c < P::kSteps; ++c) s[b] = P::product(ka[c], qf[b][c], s[b]);
@@ -167,9 +154,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void window_kernel(
             }
           }
         }
-        typename P::A w[2][P::kCols];
+        typename P::A w[R][P::kCols];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < R; ++b) {
           float top = s[b][0];
 #pragma unroll
           for (int i = 1; i < 16; ++i) top = fmaxf(top, s[b][i]);
@@ -198,10 +185,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void window_kernel(
           typename P::A va[P::kCols];
           P::columns(vt, 32 * u, db, lane, va);
 #pragma unroll
-          for (int c = 0; c < P::kCols; ++c) {
-            o[db][0] = P::product(va[c], w[0][c], o[db][0]);
-            o[db][1] = P::product(va[c], w[1][c], o[db][1]);
-          }
+          for (int c = 0; c < P::kCols; ++c)
+#pragma unroll
+            for (int b = 0; b < R; ++b) o[db][b] = P::product(va[c], w[b][c], o[db][b]);
         }
       }
     }
@@ -210,7 +196,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 2 : 1) void window_kernel(
 
   if (none) return;  // (no barrier follows)
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+  for (int b = 0; b < R; ++b) {
     const float sum = l[b] + __shfl_xor(l[b], 32);
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
     bool bad = !(sum < INFINITY);
@@ -280,46 +266,19 @@ __global__ __launch_bounds__(256) void window_join_kernel(const float* __restric
   if (lse != nullptr && d == 0) lse[row] = top == -INFINITY ? -INFINITY : top + log2f(sum) * kLn2;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-int check_seen(const char* fn, int64_t n_q, int64_t n_k, int64_t q_start, int64_t frame, int64_t window, int64_t sinks, Seen& s) {
-  const int64_t most = int64_t(1) << 24;
-  if (n_q < 0 || n_q > most || n_k < 0 || n_k > most)
-    return fail(BSGA_ERR_INVALID_ARG, "%s: n_q and n_k must be in [0, 2^24], got %lld and %lld", fn, (long long)n_q, (long long)n_k);
-  if (q_start < -most || q_start > 2 * most)
-    return fail(BSGA_ERR_INVALID_ARG, "%s: q_start must be in [-2^24, 2^25], got %lld", fn, (long long)q_start);
-  if (frame < 1 || frame > most) return fail(BSGA_ERR_INVALID_ARG, "%s: frame must be in [1, 2^24] tokens, got %lld", fn, (long long)frame);
-  if (window < 0) return fail(BSGA_ERR_INVALID_ARG, "%s: window must be >= 0 frames (0: no limit), got %lld", fn, (long long)window);
-  if (sinks < 0) return fail(BSGA_ERR_INVALID_ARG, "%s: sinks must be >= 0, got %lld", fn, (long long)sinks);
-  s.n_q = static_cast<int>(n_q);
-  s.n_k = static_cast<int>(n_k);
-  s.q_start = static_cast<int>(q_start);
-  s.frame = static_cast<int>(frame);
-  s.window = window == 0 || window > 4 * most ? static_cast<int>(4 * most) : static_cast<int>(window);  // more frames than there are
-  s.sinks = static_cast<int>(sinks < n_k ? sinks : n_k);
-  return BSGA_OK;
-}
-
-int check_view(const char* fn, const char* name, const void* p, int64_t token, int64_t head, int size, View& v) {
-  if (!p || !aligned16(p) || token < 0 || head < 0 || token * size % 16 != 0 || head * size % 16 != 0 || token * size >= int64_t(1) << 24)
-    return fail(BSGA_ERR_INVALID_ARG, "%s: %s must be non-null, it and its strides multiples of 16 bytes, a token's stride in [0, 2^24) bytes", fn, name);
-  v = {static_cast<const unsigned char*>(p), token * size, head * size};
-  return BSGA_OK;
-}
-
 // Waves of a workgroup and splits of its keys.  Four waves share tiles; a launch of few rows takes one to a workgroup, and where that leaves
 // CUs without work the keys are dealt out too, at least four tiles to each.
-void shape_of(const Seen& s, int heads, int& waves, int& splits) {
-  const int64_t tiles4 = ceil_div(s.n_q, 4 * kTile) * heads;
-  waves = s.n_q > 2 * kTile ? 4 : 1;
+void shape_of(const Seen& s, int rows, int heads, int& waves, int& splits) {  // rows of a wave
+  waves = s.n_q > 2 * rows ? 4 : 1;
+  rows *= waves;
   splits = 1;
-  const int64_t units = waves == 4 ? tiles4 : ceil_div(s.n_q, kTile) * heads;
+  const int64_t units = ceil_div(s.n_q, rows) * heads;
   const int64_t places = waves == 4 ? kPlaces : 2 * kPlaces;
   if (units * 2 > places) return;
   int most = 0;  // the rows that see most are among the last ones, or, past the last key, the first
-  for (int64_t rt = 0, all = ceil_div(s.n_q, waves * kTile); rt < all; ++rt) {
-    const int i0 = static_cast<int>(rt * waves * kTile);
-    const int c = tiles_of(s, i0, static_cast<int>(min(int64_t(i0) + waves * kTile, int64_t(s.n_q)))).count;
+  for (int64_t rt = 0, all = ceil_div(s.n_q, rows); rt < all; ++rt) {
+    const int i0 = static_cast<int>(rt * rows);
+    const int c = tiles_of(s, i0, min(i0 + rows, s.n_q)).count;
     most = c > most ? c : most;
   }
   splits = static_cast<int>(min(places / units, int64_t(most / 4)));
@@ -356,7 +315,7 @@ size_t bsga_window_attn_workspace_bytes(int dtype, int heads, int64_t n_q, int64
   if ((dtype != BSGA_BF16 && dtype != BSGA_FP32) || heads < 1 || heads > 65535 || n_q < 1 || n_k < 1) return 0;
   if (check_seen("", n_q, n_k, q_start, frame, window, sinks, s)) return 0;
   int waves, splits;
-  shape_of(s, heads, waves, splits);
+  shape_of(s, 32 * (dtype == BSGA_BF16 ? kParts<__bf16> : kParts<float>), heads, waves, splits);
   return split_bytes(heads, n_q, splits);
 }
 
@@ -386,10 +345,11 @@ int bsga_window_attn(const void* q, const void* k, const void* v, int64_t q_toke
   a.heads = heads;
   a.group = heads / kv_heads;
   a.scale_log2 = softmax_scale * kLog2e;
+  const int rows = 32 * (dtype == BSGA_BF16 ? kParts<__bf16> : kParts<float>);
   int waves;
-  shape_of(a.seen, heads, waves, a.splits);
+  shape_of(a.seen, rows, heads, waves, a.splits);
   if (!workspace || !aligned16(workspace) || workspace_bytes < split_bytes(heads, n_q, a.splits)) a.splits = 1;  // one workgroup takes all keys of its rows
-  a.row_tiles = static_cast<int>(ceil_div(n_q, waves * kTile));
+  a.row_tiles = static_cast<int>(ceil_div(n_q, waves * rows));
   a.part = static_cast<float*>(workspace);
   if (a.splits > 1) a.part_lse = a.part + int64_t(a.splits) * heads * n_q * 64;
   hipStream_t s = static_cast<hipStream_t>(stream);

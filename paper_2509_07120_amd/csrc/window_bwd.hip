@@ -1,0 +1,615 @@
+// The gradient of attention with a sliding window (window.hip).
+//
+// With P = exp(s - lse) for the keys j that query i sees and D_i = sum_d dO_id O_id:
+//   dV_j = sum_i P_ij dO_i,  dS_ij = P_ij (<dO_i, V_j> - D_i),  dQ_i = scale sum_j dS_ij K_j,  dK_j = scale sum_i dS_ij Q_i,
+// the sums of dV and dK over the query heads that share the key head as well.
+// Two kernels, so that every sum has one owner and one order (no atomics): one per query rows, which goes over the keys as the forward pass does and
+// leaves lse log2(e) and D for the other; one per key rows, which goes over the queries that see them.  Seven products in place of
+// the five that one kernel with shared sums of dQ would need.  Both recompute S and P from lse.
+// Key rows that are seen from far (the first tokens) have many more queries than others: their queries are dealt out to several workgroups, whose
+// sums in fp32 are added up at the end, always in the same order.
+#include "window.h"
+
+#include <math.h>
+
+namespace bsga {
+namespace {
+
+constexpr int kPlaces = 512;
+constexpr int kKeyRows = 128;     // keys of a workgroup, 32 for each wave
+constexpr int kStatBytes = 1024;  // lse and D of a tile's queries: 512 bytes, and as much that the load of a whole wave adds
+
+struct BwdArgs {
+  View q, k, v;
+  const unsigned char *out, *dout;  // [heads, n_q, 64]
+  const float* lse;
+  float* stats;                     // [heads, stat_rows][2]: lse log2(e), D; an even number of rows, so that tiles of them are aligned
+  unsigned char *dq, *dk, *dv;      // contiguous
+  float* part_q;                    // [q_splits][heads, n_q, 64]
+  float* part_kv[2];                // first tokens: [sink_splits][kv_heads, sink_rows, 128]; the others [splits][kv_heads, n_k - sink_rows, 128]
+  Seen seen;
+  int heads, kv_heads, group, stat_rows, row_tiles, q_splits;
+  int key_tiles, sink_tiles, sink_splits, splits;  // of kKeyRows keys
+  float scale, scale_log2;
+};
+
+// Queries that see key j: [first, last).
+struct Queries {
+  int first, last;
+};
+
+__host__ __device__ inline Queries queries_of(const Seen& s, int j) {
+  const int f = j / s.frame;
+  Queries r;
+  r.first = static_cast<int>(max(int64_t(f) * s.frame - s.q_start, int64_t(0)));
+  r.last = j < s.sinks ? s.n_q : static_cast<int>(max(min((int64_t(f) + s.window) * s.frame - s.q_start, int64_t(s.n_q)), int64_t(0)));
+  return r;
+}
+
+template <typename T>
+__device__ __forceinline__ float dot_rows(const unsigned char* x, const unsigned char* y) {
+  float s = 0.f;
+  for (int d = 0; d < 64; ++d) s += Ops<T>::number(x, d) * Ops<T>::number(y, d);
+  return s;
+}
+
+// The gradient of one query again, by a wave on its own, over the keys that it sees and no others, see exact_row in window.hip.
+template <typename T>
+__device__ float exact_query(const BwdArgs& a, const unsigned char* q, const unsigned char* dout, const unsigned char* k, const unsigned char* v,
+                             float lse2, float D, int i, int t0, int t1, const Tiles& tiles, int lane) {
+  int lo, hi;
+  a.seen.range(i, lo, hi);
+  float sum = 0.f;
+  for (int t = t0; t < t1; ++t) {
+    const int j = tiles.key(t) + lane;
+    const bool sees = j < hi && (j >= lo || j < a.seen.sinks);
+    float ds = 0.f;
+    if (sees) ds = exp2f(dot_rows<T>(q, k + j * a.k.token) * a.scale_log2 - lse2) * (dot_rows<T>(dout, v + j * a.v.token) - D);
+    unsigned long long all = __ballot(sees);
+    while (all != 0) {
+      const int e = __builtin_ctzll(all);
+      all &= all - 1;
+      sum += __shfl(ds, e) * Ops<T>::number(k + (tiles.key(t) + int64_t(e)) * a.k.token, lane);
+    }
+  }
+  return sum * a.scale;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256, 2) void window_dq_kernel(const BwdArgs a) {
+  typedef Ops<T> P;
+  constexpr int R = kParts<T>, WAVES = 4;
+  constexpr int kTileBytes = kTile * P::kRow;
+  extern __shared__ __align__(16) unsigned char smem[];  // K, V of buffer 0, K, V of buffer 1
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, g = lane >> 5;
+  const int64_t unit = spread(blockIdx.x, gridDim.x, kPlaces);
+  const int split = static_cast<int>(unit % a.q_splits);
+  const int h = static_cast<int>(unit / a.q_splits / a.row_tiles);
+  const int rt = a.row_tiles - 1 - static_cast<int>(unit / a.q_splits % a.row_tiles);
+  const int i0 = rt * 32 * R * WAVES, i1 = min(i0 + 32 * R * WAVES, a.seen.n_q);
+  const Tiles tiles = tiles_of(a.seen, i0, i1);
+  const int t0 = static_cast<int>(int64_t(tiles.count) * split / a.q_splits), t1 = static_cast<int>(int64_t(tiles.count) * (split + 1) / a.q_splits);
+  const unsigned char* const qh = a.q.p + h * a.q.head;
+  const unsigned char* const kh = a.k.p + h / a.group * a.k.head;
+  const unsigned char* const vh = a.v.p + h / a.group * a.v.head;
+  const int64_t row0 = int64_t(h) * a.seen.n_q;
+  const unsigned lds = lds_address(smem);
+  auto issue = [&](int t, int buf) {
+    const int key = tiles.key(t);
+    load_tile<T, WAVES>(kh, a.k.token, a.seen.n_k, key, lds + buf * 2 * kTileBytes, wave, lane);
+    load_tile<T, WAVES>(vh, a.v.token, a.seen.n_k, key, lds + (buf * 2 + 1) * kTileBytes, wave, lane);
+  };
+  if (t0 < t1) issue(t0, 0);
+
+  const int w0 = i0 + wave * 32 * R, w1 = min(w0 + 32 * R, a.seen.n_q);
+  const bool none = w0 >= a.seen.n_q;
+  typename P::A qf[R][P::kSteps], df[R][P::kSteps];
+  int lo[R], hi[R], lo_min = 0, hi_min = 0, lo_max = 0, hi_max = 0;
+  float lse2[R], D[R];
+#pragma unroll
+  for (int b = 0; b < R; ++b) {
+    const int i = min(w0 + 32 * b + n, a.seen.n_q - 1);
+    P::row(qh + i * a.q.token, g, qf[b]);
+    P::row(a.dout + (row0 + i) * P::kRow, g, df[b]);
+    a.seen.range(i, lo[b], hi[b]);
+    lse2[b] = a.lse[row0 + i] * kLog2e;
+    typename P::A of[P::kSteps];
+    P::row(a.out + (row0 + i) * P::kRow, g, of);
+    const float sum = P::dot(df[b], of);
+    D[b] = sum + __shfl_xor(sum, 32);
+    if (split == 0 && g == 0 && w0 + 32 * b + n < a.seen.n_q)
+      *reinterpret_cast<f32x2*>(a.stats + (int64_t(h) * a.stat_rows + i) * 2) = f32x2{lse2[b], D[b]};
+  }
+  if (!none) {
+    a.seen.range(w0, lo_min, hi_min);
+    a.seen.range(w1 - 1, lo_max, hi_max);
+  }
+
+  f32x16 dq[2][R];  // [dimensions][queries]
+#pragma unroll
+  for (int b = 0; b < R; ++b) {
+    clear(dq[0][b]);
+    clear(dq[1][b]);
+  }
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1;
+    if (t + 1 < t1) {
+      issue(t + 1, buf ^ 1);
+      constexpr int kInFlight = 2 * kTileBytes / 1024 / WAVES;
+      __builtin_amdgcn_s_waitcnt((kInFlight & 15) | (kInFlight >> 4 << 14) | 0x0f70);  // this tile's have landed
+    } else {
+      __builtin_amdgcn_s_waitcnt(0x0f70);
+    }
+    __syncthreads();
+    const int key = tiles.key(t);
+    const bool seen_by_none = none || key >= hi_max || (key + kTile <= lo_min && key >= a.seen.sinks);
+    const bool seen_by_all = key + kTile <= hi_min && (key >= lo_max || key + kTile <= a.seen.sinks || a.seen.sinks >= lo_max);
+    if (!seen_by_none) {
+      const unsigned char* const kt = smem + buf * 2 * kTileBytes;
+      const unsigned char* const vt = kt + kTileBytes;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        typename P::A w[R][P::kCols];
+        {
+          typename P::A ka[P::kSteps], va[P::kSteps];
+          P::rows(kt, 32 * u + n, g, ka);
+          P::rows(vt, 32 * u + n, g, va);
+#pragma unroll
+          for (int b = 0; b < R; ++b) {
+            f32x16 s, dp;
+            clear(s);
+            clear(dp);
+#pragma unroll
+            for (int c = 0; c < P::kSteps; ++c) {
+              s = P::product(ka[c], qf[b][c], s);
+              dp = P::product(va[c], df[b][c], dp);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, -lse2[b])) * (dp[i] - D[b]);
+            if (!seen_by_all) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const int j = key + 32 * u + 8 * (i >> 2) + 4 * g + (i & 3);
+                s[i] = j < hi[b] && (j >= lo[b] || j < a.seen.sinks) ? s[i] : 0.f;
+              }
+            }
+            P::round(s, w[b]);
+          }
+        }
+#pragma unroll
+        for (int db = 0; db < 2; ++db) {
+          typename P::A kc[P::kCols];
+          P::columns(kt, 32 * u, db, lane, kc);
+#pragma unroll
+          for (int c = 0; c < P::kCols; ++c)
+#pragma unroll
+            for (int b = 0; b < R; ++b) dq[db][b] = P::product(kc[c], w[b][c], dq[db][b]);
+        }
+      }
+    }
+    __syncthreads();
+  }
+
+  if (none) return;  // (no barrier follows)
+#pragma unroll
+  for (int b = 0; b < R; ++b) {
+    const int i = w0 + 32 * b + n;
+    const int64_t in_part = int64_t(split) * a.heads * a.seen.n_q + row0 + i;
+    bool bad = false;
+#pragma unroll
+    for (int db = 0; db < 2; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        dq[db][b][e] *= a.scale;
+        bad = bad || !(fabsf(dq[db][b][e]) < INFINITY);
+      }
+    if (i < a.seen.n_q) {
+#pragma unroll
+      for (int db = 0; db < 2; ++db)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const f32x16& x = dq[db][b];
+          const int d = db * 32 + 8 * r + 4 * g;
+          if (a.q_splits > 1) *reinterpret_cast<f32x4*>(a.part_q + in_part * 64 + d) = f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
+          else P::store4(a.dq + (row0 + i) * P::kRow, d, x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]);
+        }
+    }
+    unsigned long long again = __ballot(bad && i < a.seen.n_q);
+    again = (again | again >> 32) & 0xffffffffull;
+    while (again != 0) {
+      const int e = __builtin_ctzll(again);
+      again &= again - 1;
+      const int row = w0 + 32 * b + e;
+      const float x = exact_query<T>(a, qh + row * a.q.token, a.dout + (row0 + row) * P::kRow, kh, vh, __shfl(lse2[b], e), __shfl(D[b], e), row, t0,
+                                     t1, tiles, lane);
+      if (a.q_splits > 1) a.part_q[(int64_t(split) * a.heads * a.seen.n_q + row0 + row) * 64 + lane] = x;
+      else P::store1(a.dq + (row0 + row) * P::kRow, lane, x);
+    }
+  }
+}
+
+// A sequence of query tiles: those of each query head of the group in turn.
+struct Sequence {
+  int first, per_head, begin, end;  // first tile of a head, tiles of a head; this workgroup's part
+};
+
+// The gradients of one key again, by a wave on its own, over the queries that see it: as exact_query.  dk and dv of number `lane`.
+template <typename T>
+__device__ void exact_key(const BwdArgs& a, const unsigned char* k, const unsigned char* v, int j, int h0, const Sequence& seq, float& dk, float& dv,
+                          int lane) {
+  const Queries see = queries_of(a.seen, j);
+  dk = dv = 0.f;
+  for (int s = seq.begin; s < seq.end; ++s) {
+    const int h = h0 + s / seq.per_head, i0 = (seq.first + s % seq.per_head) * kTile;
+    const int64_t row0 = int64_t(h) * a.seen.n_q;
+    const unsigned char* const qh = a.q.p + h * a.q.head;
+    const int i = i0 + lane;
+    const bool sees = i >= see.first && i < see.last;
+    float p = 0.f, ds = 0.f;
+    if (sees) {
+      const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + (int64_t(h) * a.stat_rows + i) * 2);
+      p = exp2f(dot_rows<T>(qh + i * a.q.token, k) * a.scale_log2 - st[0]);
+      ds = p * (dot_rows<T>(a.dout + (row0 + i) * Ops<T>::kRow, v) - st[1]);
+    }
+    unsigned long long all = __ballot(sees);
+    while (all != 0) {
+      const int e = __builtin_ctzll(all);
+      all &= all - 1;
+      dv += __shfl(p, e) * Ops<T>::number(a.dout + (row0 + i0 + e) * Ops<T>::kRow, lane);
+      dk += __shfl(ds, e) * Ops<T>::number(qh + (i0 + e) * a.q.token, lane);
+    }
+  }
+  dk *= a.scale;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256, 2) void window_dkv_kernel(const BwdArgs a) {
+  typedef Ops<T> P;
+  constexpr int WAVES = 4;
+  constexpr int kTileBytes = kTile * P::kRow, kBuf = 2 * kTileBytes + kStatBytes;
+  extern __shared__ __align__(16) unsigned char smem[];  // Q, dO, lse and D of buffer 0, then of buffer 1
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, g = lane >> 5;
+  // the first tokens' units come first: they are the longest
+  const int64_t sink_units = int64_t(a.kv_heads) * a.sink_tiles * a.sink_splits;
+  const bool sink = blockIdx.x < sink_units;
+  const int64_t unit = sink ? blockIdx.x : spread(blockIdx.x - sink_units, gridDim.x - sink_units, kPlaces);
+  const int splits = sink ? a.sink_splits : a.splits, of_head = sink ? a.sink_tiles : a.key_tiles - a.sink_tiles;
+  const int split = static_cast<int>(unit % splits);
+  const int hk = static_cast<int>(unit / splits / of_head);
+  const int kt = static_cast<int>(unit / splits % of_head) + (sink ? 0 : a.sink_tiles);
+  const int j0 = kt * kKeyRows, j1 = min(j0 + kKeyRows, a.seen.n_k);
+  Sequence seq;
+  {
+    const Queries from = queries_of(a.seen, j0), to = queries_of(a.seen, j1 - 1);
+    const int last = j0 < a.seen.sinks ? a.seen.n_q : to.last;
+    seq.first = from.first / kTile;
+    seq.per_head = last > from.first ? (last + kTile - 1) / kTile - seq.first : 0;
+    const int64_t all = int64_t(seq.per_head) * a.group;
+    seq.begin = static_cast<int>(all * split / splits);
+    seq.end = static_cast<int>(all * (split + 1) / splits);
+  }
+  const int h0 = hk * a.group;
+  const unsigned lds = lds_address(smem);
+  auto issue = [&](int s, int buf) {
+    const int h = h0 + s / seq.per_head, i0 = (seq.first + s % seq.per_head) * kTile;
+    const unsigned at = lds + buf * kBuf;
+    load_tile<T, WAVES>(a.q.p + h * a.q.head, a.q.token, a.seen.n_q, i0, at, wave, lane);
+    load_tile<T, WAVES>(a.dout + int64_t(h) * a.seen.n_q * P::kRow, P::kRow, a.seen.n_q, i0, at + kTileBytes, wave, lane);
+    // every wave, so that all wait for the same number of loads: the same bytes to the same place
+    const int64_t row = int64_t(h) * a.stat_rows + i0;
+    dma16<0>(make_rsrc(a.stats + row * 2, static_cast<unsigned>(min(a.seen.n_q - i0, kTile)) * 8u), lane * 16, 0u, at + 2 * kTileBytes);
+  };
+  if (seq.begin < seq.end) issue(seq.begin, 0);
+
+  // the wave's keys [w0, w1): rows past the end are computed as the last one and not stored
+  const int w0 = j0 + wave * 32, w1 = min(w0 + 32, a.seen.n_k);
+  const bool none = w0 >= a.seen.n_k;
+  const int j = min(w0 + n, a.seen.n_k - 1);
+  const unsigned char* const kh = a.k.p + hk * a.k.head;
+  const unsigned char* const vh = a.v.p + hk * a.v.head;
+  typename P::A kf[P::kSteps], vf[P::kSteps];
+  P::row(kh + j * a.k.token, g, kf);
+  P::row(vh + j * a.v.token, g, vf);
+  const Queries see = queries_of(a.seen, j);
+  Queries head = {0, 0}, tail = {0, 0};
+  if (!none) {
+    head = queries_of(a.seen, w0);
+    tail = queries_of(a.seen, w1 - 1);
+  }
+  // queries of which all, and of which some, see all or some of the wave's keys
+  const int some_last = w0 < a.seen.sinks ? a.seen.n_q : tail.last;
+  const int all_last = none ? 0 : w1 <= a.seen.sinks ? a.seen.n_q : queries_of(a.seen, max(w0, a.seen.sinks)).last;
+
+  f32x16 dk[2], dv[2];  // [dimensions], keys in the columns
+#pragma unroll
+  for (int db = 0; db < 2; ++db) {
+    clear(dk[db]);
+    clear(dv[db]);
+  }
+  for (int s = seq.begin; s < seq.end; ++s) {
+    const int buf = (s - seq.begin) & 1;
+    if (s + 1 < seq.end) {
+      issue(s + 1, buf ^ 1);
+      constexpr int kInFlight = 2 * kTileBytes / 1024 / WAVES + 1;
+      __builtin_amdgcn_s_waitcnt((kInFlight & 15) | (kInFlight >> 4 << 14) | 0x0f70);  // this tile's have landed
+    } else {
+      __builtin_amdgcn_s_waitcnt(0x0f70);
+    }
+    __syncthreads();
+    const int i0 = (seq.first + s % seq.per_head) * kTile;
+    if (!none && i0 < some_last && i0 + kTile > head.first) {
+      const bool all = i0 >= tail.first && i0 + kTile <= all_last;
+      const unsigned char* const qt = smem + buf * kBuf;
+      const unsigned char* const dt = qt + kTileBytes;
+      const unsigned char* const st = dt + kTileBytes;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        f32x16 p, ds;
+        clear(p);
+        clear(ds);
+        {
+          typename P::A qa[P::kSteps], da[P::kSteps];
+          P::rows(qt, 32 * u + n, g, qa);
+          P::rows(dt, 32 * u + n, g, da);
+#pragma unroll
+          for (int c = 0; c < P::kSteps; ++c) {
+            p = P::product(qa[c], kf[c], p);
+            ds = P::product(da[c], vf[c], ds);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int r = 32 * u + 8 * (e >> 2) + 4 * g + (e & 3);
+          const f32x2 of_row = *LDS_PTR(f32x2, st + r * 8);
+          p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], a.scale_log2, -of_row[0]));
+          ds[e] = p[e] * (ds[e] - of_row[1]);
+        }
+        if (!all) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int i = i0 + 32 * u + 8 * (e >> 2) + 4 * g + (e & 3);
+            const bool sees = i >= see.first && i < see.last;
+            p[e] = sees ? p[e] : 0.f;
+            ds[e] = sees ? ds[e] : 0.f;
+          }
+        }
+        typename P::A pw[P::kCols], dw[P::kCols];
+        P::round(p, pw);
+        P::round(ds, dw);
+#pragma unroll
+        for (int db = 0; db < 2; ++db) {
+          typename P::A c0[P::kCols], c1[P::kCols];
+          P::columns(dt, 32 * u, db, lane, c0);
+          P::columns(qt, 32 * u, db, lane, c1);
+#pragma unroll
+          for (int c = 0; c < P::kCols; ++c) {
+            dv[db] = P::product(c0[c], pw[c], dv[db]);
+            dk[db] = P::product(c1[c], dw[c], dk[db]);
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+
+  if (none) return;  // (no barrier follows)
+  bool bad = false;
+#pragma unroll
+  for (int db = 0; db < 2; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      dk[db][e] *= a.scale;
+      bad = bad || !(fabsf(dk[db][e]) < INFINITY) || !(fabsf(dv[db][e]) < INFINITY);
+    }
+  const int sink_rows = min(a.sink_tiles * kKeyRows, a.seen.n_k);
+  const int64_t out0 = int64_t(hk) * a.seen.n_k;
+  // the place of key jj in the partial sums
+  auto part = [&](int jj) {
+    const int64_t rows = sink ? sink_rows : a.seen.n_k - sink_rows;
+    return a.part_kv[sink ? 0 : 1] + ((int64_t(split) * a.kv_heads + hk) * rows + jj - (sink ? 0 : sink_rows)) * 128;
+  };
+  if (w0 + n < a.seen.n_k) {
+#pragma unroll
+    for (int db = 0; db < 2; ++db)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int d = db * 32 + 8 * r + 4 * g;
+        const f32x16 &x = dk[db], &y = dv[db];
+        if (splits > 1) {
+          float* const to = part(j);
+          *reinterpret_cast<f32x4*>(to + d) = f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
+          *reinterpret_cast<f32x4*>(to + 64 + d) = f32x4{y[4 * r], y[4 * r + 1], y[4 * r + 2], y[4 * r + 3]};
+        } else {
+          P::store4(a.dk + (out0 + j) * P::kRow, d, x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]);
+          P::store4(a.dv + (out0 + j) * P::kRow, d, y[4 * r], y[4 * r + 1], y[4 * r + 2], y[4 * r + 3]);
+        }
+      }
+  }
+  unsigned long long again = __ballot(bad && w0 + n < a.seen.n_k);
+  again = (again | again >> 32) & 0xffffffffull;
+  while (again != 0) {
+    const int jj = w0 + __builtin_ctzll(again);
+    again &= again - 1;
+    float x, y;
+    exact_key<T>(a, kh + jj * a.k.token, vh + jj * a.v.token, jj, h0, seq, x, y, lane);
+    if (splits > 1) {
+      part(jj)[lane] = x;
+      part(jj)[64 + lane] = y;
+    } else {
+      P::store1(a.dk + (out0 + jj) * P::kRow, lane, x);
+      P::store1(a.dv + (out0 + jj) * P::kRow, lane, y);
+    }
+  }
+}
+
+// Sums of the splits: WIDTH numbers of each row, the second 64 to a tensor of their own.  Row r of head h goes to row first + r of it.
+template <typename T, int WIDTH>
+__global__ __launch_bounds__(256) void window_sum_kernel(const float* __restrict__ part, int64_t rows_of_head, int heads, int splits, int64_t first,
+                                                         int64_t out_rows, unsigned char* __restrict__ out0, unsigned char* __restrict__ out1) {
+  constexpr int kLanes = WIDTH / 4;
+  const int64_t rows = rows_of_head * heads;
+  const int64_t row = (int64_t(blockIdx.x) * 256 + threadIdx.x) / kLanes;
+  const int d = threadIdx.x % kLanes * 4;
+  if (row >= rows) return;
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < splits; ++s) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(part + (s * rows + row) * WIDTH + d);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] += x[e];
+  }
+  const int64_t to = row / rows_of_head * out_rows + first + row % rows_of_head;
+  Ops<T>::store4((d < 64 ? out0 : out1) + to * Ops<T>::kRow, d & 63, y[0], y[1], y[2], y[3]);
+}
+
+// How a launch is cut up.  Workgroups of query rows as in the forward pass; workgroups of keys get their queries in parts where there are
+// too few of them, and those of the first tokens, which all queries see, in parts as long as the others' queries.
+void shape_of(BwdArgs& a, int rows) {  // rows of a workgroup of queries
+  const Seen& s = a.seen;
+  a.stat_rows = (s.n_q + 1) & ~1;
+  a.row_tiles = static_cast<int>(ceil_div(s.n_q, rows));
+  a.q_splits = 1;
+  const int64_t units = int64_t(a.row_tiles) * a.heads;
+  if (units > 0 && units * 2 <= kPlaces) {
+    int most = 0;
+    for (int rt = 0; rt < a.row_tiles; ++rt) {
+      const int c = tiles_of(s, rt * rows, min((rt + 1) * rows, s.n_q)).count;
+      most = c > most ? c : most;
+    }
+    a.q_splits = static_cast<int>(max(min(kPlaces / units, int64_t(most / 4)), int64_t(1)));
+  }
+  a.key_tiles = static_cast<int>(ceil_div(s.n_k, kKeyRows));
+  const int64_t all = ceil_div(s.n_q, kTile) * a.group;  // query tiles of a key that all see
+  int64_t most = 0;                                      // and of one that is seen through the window
+  for (int kt = 0; kt < a.key_tiles; ++kt) {
+    const Queries from = queries_of(s, kt * kKeyRows), to = queries_of(s, min((kt + 1) * kKeyRows, s.n_k) - 1);
+    if (kt * kKeyRows < s.sinks || to.last <= from.first) continue;
+    const int64_t c = (ceil_div(to.last, kTile) - from.first / kTile) * a.group;
+    most = c > most ? c : most;
+  }
+  a.sink_tiles = static_cast<int>(ceil_div(s.sinks, kKeyRows));
+  const int64_t key_units = int64_t(a.key_tiles) * a.kv_heads;
+  a.splits = key_units > 0 && key_units * 2 <= kPlaces ? static_cast<int>(max(min(kPlaces / key_units, most / 4), int64_t(1))) : 1;
+  const int64_t part = max(most / a.splits, int64_t(16));
+  a.sink_splits = static_cast<int>(min(max(ceil_div(all, part), int64_t(1)), int64_t(64)));
+  if (key_units > 4 * kPlaces && a.sink_tiles == a.key_tiles) a.sink_splits = 1;  // everything is seen from everywhere
+}
+
+size_t stats_bytes(const BwdArgs& a) { return static_cast<size_t>(a.heads) * a.stat_rows * 8; }
+size_t part_q_bytes(const BwdArgs& a) { return a.q_splits > 1 ? static_cast<size_t>(a.q_splits) * a.heads * a.seen.n_q * 256 : 0; }
+size_t part_kv_bytes(const BwdArgs& a, bool sink) {
+  const int64_t sink_rows = min(int64_t(a.sink_tiles) * kKeyRows, int64_t(a.seen.n_k));
+  const int splits = sink ? a.sink_splits : a.splits;
+  return splits > 1 ? static_cast<size_t>(splits) * a.kv_heads * (sink ? sink_rows : a.seen.n_k - sink_rows) * 512 : 0;
+}
+
+template <typename T>
+int launch(const BwdArgs& a, hipStream_t s) {
+  const char* what = "bsga_window_attn_bwd launch";
+  const int64_t q_units = int64_t(a.heads) * a.row_tiles * a.q_splits;
+  const int64_t k_units = int64_t(a.kv_heads) * (int64_t(a.sink_tiles) * a.sink_splits + int64_t(a.key_tiles - a.sink_tiles) * a.splits);
+  if (q_units > 0x7fffffff || k_units > 0x7fffffff) return fail(BSGA_ERR_UNSUPPORTED, "bsga_window_attn_bwd: too many rows");
+  const int64_t q_rows = int64_t(a.heads) * a.seen.n_q;
+  if (q_units > 0) {
+    hipLaunchKernelGGL(window_dq_kernel<T>, dim3(static_cast<unsigned>(q_units)), dim3(256), 4 * kTile * Ops<T>::kRow, s, a);
+    if (int rc = check_hip(hipGetLastError(), what)) return rc;
+    if (a.q_splits > 1) {
+      hipLaunchKernelGGL((window_sum_kernel<T, 64>), dim3(static_cast<unsigned>(ceil_div(q_rows, 16))), dim3(256), 0, s, a.part_q, a.seen.n_q, a.heads,
+                         a.q_splits, 0, a.seen.n_q, a.dq, nullptr);
+      if (int rc = check_hip(hipGetLastError(), what)) return rc;
+    }
+  }
+  if (k_units == 0) return BSGA_OK;
+  hipLaunchKernelGGL(window_dkv_kernel<T>, dim3(static_cast<unsigned>(k_units)), dim3(256), 2 * (2 * kTile * Ops<T>::kRow + kStatBytes), s, a);
+  if (int rc = check_hip(hipGetLastError(), what)) return rc;
+  const int64_t sink_rows = min(int64_t(a.sink_tiles) * kKeyRows, int64_t(a.seen.n_k));
+  for (int x = 0; x < 2; ++x) {
+    const int splits = x == 0 ? a.sink_splits : a.splits;
+    const int64_t rows = x == 0 ? sink_rows : a.seen.n_k - sink_rows;
+    if (splits == 1 || rows == 0) continue;
+    hipLaunchKernelGGL((window_sum_kernel<T, 128>), dim3(static_cast<unsigned>(ceil_div(rows * a.kv_heads, 8))), dim3(256), 0, s, a.part_kv[x], rows,
+                       a.kv_heads, splits, x == 0 ? 0 : sink_rows, a.seen.n_k, a.dk, a.dv);
+    if (int rc = check_hip(hipGetLastError(), what)) return rc;
+  }
+  return BSGA_OK;
+}
+
+int rows_of(int dtype) { return 4 * 32 * (dtype == BSGA_BF16 ? kParts<__bf16> : kParts<float>); }
+
+}  // namespace
+}  // namespace bsga
+
+using namespace bsga;
+
+extern "C" {
+
+size_t bsga_window_attn_bwd_workspace_bytes(int dtype, int heads, int kv_heads, int64_t n_q, int64_t n_k, int64_t q_start, int64_t frame,
+                                            int64_t window, int64_t sinks) {
+  BwdArgs a = {};
+  if ((dtype != BSGA_BF16 && dtype != BSGA_FP32) || heads < 1 || heads > 65535 || kv_heads < 1 || heads % kv_heads != 0 || n_q < 0 || n_k < 0) return 0;
+  if (check_seen("", n_q, n_k, q_start, frame, window, sinks, a.seen)) return 0;
+  a.heads = heads;
+  a.kv_heads = kv_heads;
+  a.group = heads / kv_heads;
+  shape_of(a, rows_of(dtype));
+  return stats_bytes(a) + part_q_bytes(a) + part_kv_bytes(a, true) + part_kv_bytes(a, false);
+}
+
+int bsga_window_attn_bwd(const void* dout, const void* q, const void* k, const void* v, int64_t q_token, int64_t q_head, int64_t k_token,
+                         int64_t k_head, int64_t v_token, int64_t v_head, const void* out, const float* lse, int dtype, int heads, int kv_heads,
+                         int64_t n_q, int64_t n_k, int head_dim, float softmax_scale, int64_t q_start, int64_t frame, int64_t window, int64_t sinks,
+                         void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* fn = "bsga_window_attn_bwd";
+  clear_error();
+  BwdArgs a = {};
+  if (dtype != BSGA_BF16 && dtype != BSGA_FP32) return fail(BSGA_ERR_INVALID_ARG, "%s: unknown dtype %d", fn, dtype);
+  if (head_dim != 64) return fail(BSGA_ERR_UNSUPPORTED, "%s: head_dim must be 64, got %d", fn, head_dim);
+  if (heads < 1 || heads > 65535 || kv_heads < 1 || heads % kv_heads != 0)
+    return fail(BSGA_ERR_INVALID_ARG, "%s: heads must be in [1, 65535] and a multiple of kv_heads, got %d and %d", fn, heads, kv_heads);
+  if (int rc = check_seen(fn, n_q, n_k, q_start, frame, window, sinks, a.seen)) return rc;
+  if (!(softmax_scale > 0.0f) || !isfinite(softmax_scale)) return fail(BSGA_ERR_INVALID_ARG, "%s: softmax_scale must be finite and > 0", fn);
+  if (n_q == 0 && n_k == 0) return BSGA_OK;
+  const int size = dtype == BSGA_BF16 ? 2 : 4;
+  if (n_q > 0) {
+    if (int rc = check_view(fn, "q", q, q_token, q_head, size, a.q)) return rc;
+    if (!dout || !out || !lse || !dq || !aligned16(dout) || !aligned16(out) || !aligned16(dq))
+      return fail(BSGA_ERR_INVALID_ARG, "%s: dout, out, lse and dq must be non-null, tensors 16-byte aligned", fn);
+  }
+  if (n_k > 0) {
+    if (int rc = check_view(fn, "k", k, k_token, k_head, size, a.k)) return rc;
+    if (int rc = check_view(fn, "v", v, v_token, v_head, size, a.v)) return rc;
+    if (!dk || !dv || !aligned16(dk) || !aligned16(dv))
+      return fail(BSGA_ERR_INVALID_ARG, "%s: dk and dv must be non-null and 16-byte aligned", fn);
+  }
+  a.out = static_cast<const unsigned char*>(out);
+  a.dout = static_cast<const unsigned char*>(dout);
+  a.lse = lse;
+  a.dq = static_cast<unsigned char*>(dq);
+  a.dk = static_cast<unsigned char*>(dk);
+  a.dv = static_cast<unsigned char*>(dv);
+  a.heads = heads;
+  a.kv_heads = kv_heads;
+  a.group = heads / kv_heads;
+  a.scale = softmax_scale;
+  a.scale_log2 = softmax_scale * kLog2e;
+  shape_of(a, rows_of(dtype));
+  const size_t need = stats_bytes(a) + part_q_bytes(a) + part_kv_bytes(a, true) + part_kv_bytes(a, false);
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return fail(BSGA_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace ? workspace_bytes : 0, need);
+  if (!aligned16(workspace)) return fail(BSGA_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", fn);
+  unsigned char* at = static_cast<unsigned char*>(workspace);
+  a.stats = reinterpret_cast<float*>(at);
+  at += stats_bytes(a);
+  a.part_q = reinterpret_cast<float*>(at);
+  at += part_q_bytes(a);
+  a.part_kv[0] = reinterpret_cast<float*>(at);
+  at += part_kv_bytes(a, true);
+  a.part_kv[1] = reinterpret_cast<float*>(at);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return dtype == BSGA_BF16 ? launch<__bf16>(a, s) : launch<float>(a, s);
+}
+
+}  // extern "C"

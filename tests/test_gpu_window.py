@@ -1,8 +1,8 @@
 """Attention with a sliding window and first tokens that stay visible, against the definition in float64 on an explicit mask.
 
 Bounds.  fp32 logits: a product of 64 terms is off by at most 64 roundings of 2^-24 of sum |q k| scale, and so is, relatively, a weight; with
-logits up to L = max sum |q k| scale that is 2^-18 L, and the sums add 2^-18 of sum p |v|.  bf16: the weights are rounded, 2^-9 of sum p |v|
-(they are rounded to nearest: half of 2^-8), and the result, 2^-9 |o|; the sum of weights is taken before the rounding."""
+logits up to L = max sum |q k| scale that is 2^-18 L, and the sums add 2^-18 of sum p |v|.  bf16: the weights are rounded, 2^-8 of sum p |v|
+(half a step of eight significant bits), and the result, 2^-8 |o|; the sum of weights is taken before the rounding."""
 import math
 
 import pytest
