@@ -370,6 +370,26 @@ int bsga_window_attn_bwd(const void* dout, const void* q, const void* k, const v
                          int64_t window, int64_t sinks, void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Attention of one new token for each sequence over a cache of pages, for serving.  The query of sequence b stands at position
+ * lengths[b] - 1; its own key and value are in the cache already (bsga_qk_norm_rope with slots puts them there).  It sees the keys that
+ * bsga_window_attn's rule gives a query at that position (frame, window, sinks as there).
+ *   q           [batch, heads, 64] with strides in elements (multiples of 16 bytes; what bsga_qk_norm_rope returns, seen the other way round, is fine)
+ *   k_cache, v_cache  [n_pages, kv_heads, page, 64]
+ *   page_table  [batch, table_width] int32: key j of sequence b lies in row j % page of page page_table[b][j / page]; entries that no
+ *               visible key needs are not used, those outside [0, n_pages) are clamped into it
+ *   lengths     [batch] int32 device array, clamped into [0, table_width * page]; 0: zeros, lse = -inf
+ *   out         [batch, heads, 64];  lse nullable [batch, heads] float32
+ *   workspace   bsga_paged_attn_workspace_bytes(...) bytes, 16-byte aligned; overwritten: long sequences are shared out between workgroups
+ * Cache rows that the query does not see are not read.  bf16 and fp32, arithmetic as bsga_window_attn; the same bits every time.
+ */
+size_t bsga_paged_attn_workspace_bytes(int dtype, int64_t batch, int heads, int kv_heads, int64_t table_width, int64_t n_pages, int page,
+                                       int64_t frame, int64_t window, int64_t sinks);
+int bsga_paged_attn(const void* q, int64_t q_batch, int64_t q_head, const void* k_cache, const void* v_cache, int dtype, int64_t batch,
+                    int heads, int kv_heads, int head_dim, const int32_t* page_table, int64_t table_width, const int32_t* lengths,
+                    int64_t n_pages, int page, float softmax_scale, int64_t frame, int64_t window, int64_t sinks, void* out, float* lse,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Measurement aid, not part of the method: the rate the matrix pipes sustain on the MFMA instruction
  * the bf16 attention kernels use (32x32x16 bf16, the products of Eqs. (1)/(2)), with no memory traffic
  * at all, two workgroups of four waves per CU.  The part lowers its clock with the switching activity

@@ -48,6 +48,8 @@ EXPORTED_SYMBOLS = (
     "bsga_linear",
     "bsga_layer_norm",
     "bsga_probe_mfma",
+    "bsga_paged_attn",
+    "bsga_paged_attn_workspace_bytes",
     "bsga_qk_norm_rope",
     "bsga_qk_norm_rope_bwd",
     "bsga_qk_norm_rope_bwd_workspace_bytes",
@@ -147,6 +149,11 @@ def _load() -> ctypes.CDLL:
                                                                     c_float] + seen + [c_void_p] * 4 + [c_size_t, c_void_p]
     lib.bsga_window_attn_bwd_workspace_bytes.restype = c_size_t
     lib.bsga_window_attn_bwd_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int64, c_int64] + seen
+    lib.bsga_paged_attn.restype = c_int
+    lib.bsga_paged_attn.argtypes = [c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_int, c_int64, c_int, c_int, c_int, c_void_p, c_int64, c_void_p,
+                                    c_int64, c_int, c_float, c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.bsga_paged_attn_workspace_bytes.restype = c_size_t
+    lib.bsga_paged_attn_workspace_bytes.argtypes = [c_int, c_int64, c_int, c_int, c_int64, c_int64, c_int] + [c_int64] * 3
     return lib
 
 
@@ -830,3 +837,45 @@ def bsga_window_attn_bwd(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v
     _check(lib.bsga_window_attn_bwd(_ptr(dout), _ptr(q), _ptr(k), _ptr(v), *strides, _ptr(out), _ptr(lse), code, H, K, N, M, d, scale, *seen,
                                     _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace), nbytes, _stream(q)))
     return dq, dk, dv
+
+
+def bsga_paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+                    window: Optional[int] = None, sinks: int = 0, frame: int = 1, softmax_scale: Optional[float] = None,
+                    return_lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """Attention of one new token for each sequence, q [B, H, 64] (a view with contiguous rows is fine), over the caches [pages, Hkv, page, 64]:
+    key j of sequence b lies in row j % page of page page_table[b, j // page] (int32 [B, width]; entries are clamped to the pages there are).
+    The query of sequence b stands at position lengths[b] - 1 (int32 [B]), its own key is in the cache already; it sees what
+    bsga_window_attn's rule gives a query there.  Returns O [B, H, 64] (and lse [B, H] float32); a sequence of length 0 yields zeros and -inf."""
+    code = _dtype_code(q)
+    if not q.is_cuda:
+        raise ValueError("q must be a device tensor")
+    strides = q.stride()
+    if len(strides) != 3 or (strides[2] != 1 and q.shape[2] > 1):
+        raise ValueError("q must be [batch, heads, 64] with contiguous rows")
+    B, H, d = q.shape
+    at = q.get_device()
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        _require(t, name, q.dtype)
+        if t.dim() != 4 or t.shape[3] != d or t.shape != k_cache.shape or t.get_device() != at:
+            raise ValueError(f"{name} must be [pages, kv_heads, page, 64] on the same device as q")
+    for name, t, dims in (("page_table", page_table, 2), ("lengths", lengths, 1)):
+        _require(t, name, torch.int32)
+        if t.dim() != dims or t.shape[0] != B or t.get_device() != at:
+            raise ValueError(f"{name} must have a row for each sequence, on the same device as q")
+    if window is not None and window < 1:
+        raise ValueError(f"window must be at least one frame, or None, got {window}")
+    pages, K, page, _ = k_cache.shape
+    width = page_table.shape[1]
+    seen = (frame, 0 if window is None else window, sinks)
+    out = torch.empty((B, H, d), dtype=q.dtype, device=q.device)
+    lse = torch.empty((B, H), dtype=torch.float32, device=q.device) if return_lse else None
+    if workspace is None:
+        nbytes = lib.bsga_paged_attn_workspace_bytes(code, B, H, K, width, pages, page, *seen)
+        if nbytes > 0:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    _check(lib.bsga_paged_attn(_ptr(q), strides[0], strides[1], _ptr(k_cache), _ptr(v_cache), code, B, H, K, d, _ptr(page_table), width,
+                               _ptr(lengths), pages, page, 1.0 / math.sqrt(d) if softmax_scale is None else float(softmax_scale), *seen,
+                               _ptr(out), _ptr(lse), _ptr(workspace), nbytes, _stream(q)))
+    return (out, lse) if return_lse else out

@@ -233,5 +233,65 @@ inline int check_view(const char* fn, const char* name, const void* p, int64_t t
   return BSGA_OK;
 }
 
+// Parts of a row's keys together: out = sum_s exp(lse_s - lse) part_s.  A row takes GROUPS groups of sixteen lanes, each every GROUPS-th part.
+template <typename T, int GROUPS>
+__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, const float* __restrict__ part_lse, int64_t rows, int splits,
+                                                   unsigned char* __restrict__ out, float* __restrict__ lse) {
+  constexpr int kRows = 16 / GROUPS;  // of a workgroup
+  __shared__ f32x4 sums[16][16];
+  __shared__ float total[16];
+  const int which = threadIdx.x >> 4, group = which % GROUPS, d = (threadIdx.x & 15) * 4;
+  const int64_t row = int64_t(blockIdx.x) * kRows + which / GROUPS;
+  const bool live = row < rows;
+  float top = -INFINITY;
+  bool nan = false;
+  if (live)
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+      const float x = part_lse[s * rows + row];
+      top = fmaxf(top, x);
+      nan = nan || x != x;
+    }
+  if (nan) top = NAN;
+  float sum = 0.f;
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  if (live && top != -INFINITY)
+#pragma unroll 4
+    for (int s = group; s < splits; s += GROUPS) {
+      const float from = part_lse[s * rows + row];
+      const f32x4 x = *reinterpret_cast<const f32x4*>(part + (s * rows + row) * 64 + d);
+      const float w = from == -INFINITY ? 0.f : exp2f((from - top) * kLog2e);
+      sum += w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] += from == -INFINITY ? 0.f : w * x[e];  // (a part that saw nothing may hold anything)
+    }
+  if constexpr (GROUPS > 1) {
+    sums[which][threadIdx.x & 15] = y;
+    if (d == 0) total[which] = sum;
+    __syncthreads();
+    if (group != 0) return;
+    sum = 0.f;
+    y = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < GROUPS; ++s) {
+      sum += total[which + s];
+      y += sums[which + s][threadIdx.x & 15];
+    }
+  }
+  if (!live) return;
+  const float inv = top == -INFINITY ? 0.f : 1.f / sum;
+  Ops<T>::store4(out + row * Ops<T>::kRow, d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+  if (lse != nullptr && d == 0) lse[row] = top == -INFINITY ? -INFINITY : top + log2f(sum) * kLn2;
+}
+
+template <typename T>
+int launch_join(const float* part, const float* part_lse, int64_t rows, int splits, unsigned char* out, float* lse, hipStream_t s) {
+  if (splits > 8)
+    hipLaunchKernelGGL((join_kernel<T, 16>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, s, part, part_lse, rows, splits, out, lse);
+  else
+    hipLaunchKernelGGL((join_kernel<T, 1>), dim3(static_cast<unsigned>(ceil_div(rows, 16))), dim3(256), 0, s, part, part_lse, rows, splits, out, lse);
+  return check_hip(hipGetLastError(), "attention launch");
+}
+
 }  // namespace
 }  // namespace bsga

@@ -235,37 +235,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
   }
 }
 
-// The splits of a row together: sixteen lanes to a row.
-template <typename T>
-__global__ __launch_bounds__(256) void window_join_kernel(const float* __restrict__ part, const float* __restrict__ part_lse, int64_t rows,
-                                                          int splits, unsigned char* __restrict__ out, float* __restrict__ lse) {
-  const int64_t row = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4);
-  const int d = (threadIdx.x & 15) * 4;
-  if (row >= rows) return;
-  float top = -INFINITY;
-  bool nan = false;
-  for (int s = 0; s < splits; ++s) {
-    const float x = part_lse[s * rows + row];
-    top = fmaxf(top, x);
-    nan = nan || x != x;
-  }
-  if (nan) top = NAN;
-  float sum = 0.f;
-  f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits && top != -INFINITY; ++s) {
-    const float from = part_lse[s * rows + row];
-    if (from == -INFINITY) continue;  // saw nothing
-    const float w = exp2f((from - top) * kLog2e);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(part + (s * rows + row) * 64 + d);
-    sum += w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] += w * x[e];
-  }
-  const float inv = top == -INFINITY ? 0.f : 1.f / sum;
-  Ops<T>::store4(out + row * Ops<T>::kRow, d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-  if (lse != nullptr && d == 0) lse[row] = top == -INFINITY ? -INFINITY : top + log2f(sum) * kLn2;
-}
-
 // Waves of a workgroup and splits of its keys.  Four waves share tiles; a launch of few rows takes one to a workgroup, and where that leaves
 // CUs without work the keys are dealt out too, at least four tiles to each.
 void shape_of(const Seen& s, int rows, int heads, int& waves, int& splits) {  // rows of a wave
@@ -297,9 +266,7 @@ int launch(const WindowArgs& a, int waves, hipStream_t s) {
   if (int rc = check_hip(hipGetLastError(), "bsga_window_attn launch")) return rc;
   if (a.splits == 1) return BSGA_OK;
   const int64_t rows = int64_t(a.heads) * a.seen.n_q;
-  hipLaunchKernelGGL(window_join_kernel<T>, dim3(static_cast<unsigned>(ceil_div(rows, 16))), dim3(256), 0, s, a.part, a.part_lse, rows, a.splits,
-                     a.out, a.lse);
-  return check_hip(hipGetLastError(), "bsga_window_attn launch");
+  return launch_join<T>(a.part, a.part_lse, rows, a.splits, a.out, a.lse, s);
 }
 
 }  // namespace
