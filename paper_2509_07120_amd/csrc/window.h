@@ -67,8 +67,10 @@ struct Ops<__bf16> {
   static constexpr int kSteps = 4;           // products over the 64 numbers of a row
   static constexpr int kCols = 2;            // products over 32 rows
   static __device__ __forceinline__ f32x16 product(A a, A b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-  // 16-byte chunk c of tile row r lies at c ^ swizzle(r)
-  static __device__ __forceinline__ int swizzle(int r) { return swz_k(r); }
+  // 16-byte chunk c of tile row r lies at c ^ swizzle(r).  Rows are 128 bytes, two to the 64 banks: reading one chunk of 16 rows meets every
+  // bank once if the eight even rows (and the odd ones) have eight swizzles, and the transposing reads, of four chunks of four rows, if rows r and
+  // r + 2 differ in the bit of 4.  Bits 1, 2, 3 of r in reverse do both, and rows 16 apart have the same.
+  static __device__ __forceinline__ int swizzle(int r) { return ((r & 2) << 1) | ((r >> 1) & 2) | ((r >> 3) & 1); }
   // row r's numbers from memory: lane half g holds 8 of each 16
   static __device__ __forceinline__ void row(const unsigned char* p, int g, A (&a)[kSteps]) {
 #pragma unroll
@@ -130,7 +132,8 @@ struct Ops<float> {
   static constexpr int kSteps = 32;
   static constexpr int kCols = 16;
   static __device__ __forceinline__ f32x16 product(A a, A b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
-  static __device__ __forceinline__ int swizzle(int r) { return r & 15; }
+  // rows are 256 bytes, all 64 banks: 16 swizzles for 16 rows, and rows 4 apart, read by the two lane halves in columns(), differ in the bit of 8
+  static __device__ __forceinline__ int swizzle(int r) { return ((r & 4) << 1) | ((r >> 1) & 4) | (r & 3); }
   // lane half g holds 4 of each 8 numbers
   static __device__ __forceinline__ void row(const unsigned char* p, int g, A (&a)[kSteps]) {
 #pragma unroll
