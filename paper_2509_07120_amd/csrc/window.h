@@ -5,6 +5,8 @@
 // frame and lo the start of the frame window - 1 frames earlier; both cut to the keys that there are.  Both ends grow with p.
 #pragma once
 
+#include <type_traits>
+
 #include "bf16_tile.h"
 #include "bsga_internal.h"
 
@@ -181,21 +183,51 @@ __device__ __forceinline__ void clear(f32x16& x) {
   for (int i = 0; i < 16; ++i) x[i] = 0.f;
 }
 
-// Rows [r0, r0 + 64) of one head of a tensor straight into a tile (rows past the tensor's end become zeros), by `waves` waves.  The
+// Rows [r0, r0 + 64) of one head of a tensor straight into a tile (rows past the tensor's end become zeros), by `WAVES` waves.  The
 // descriptor starts at the tile, so that 32-bit offsets do whatever the tensor's size is.
 template <typename T, int WAVES>
-__device__ __forceinline__ void load_tile(const unsigned char* head, int64_t token, int n, int r0, unsigned lds, int wave, int lane) {
-  constexpr int kRow = Ops<T>::kRow, kChunks = kRow / 16, kRows = 64 / kChunks, kLoads = kTile / kRows;
-  const int64_t left = n - r0;
-  const i32x4 rsrc = make_rsrc(head + r0 * token, left > 0 ? static_cast<unsigned>((min(left, int64_t(kTile)) - 1) * token + kRow) : 0u);
-  const int r_in = lane / kChunks, pos = lane % kChunks;
+struct TileLoad {
+  static constexpr int kRow = Ops<T>::kRow, kChunks = kRow / 16, kRows = 64 / kChunks, kLoads = kTile / kRows / WAVES;
+  int64_t token;
+  unsigned offset[kLoads];  // of the lane's 16 bytes in each of the wave's loads
+  unsigned wave_lds;
+
+  __device__ __forceinline__ TileLoad(int64_t token, int wave, int lane) : token(token), wave_lds(wave * 1024u) {
+    const int pos = lane % kChunks;
 #pragma unroll
-  for (int i = 0; i < kLoads / WAVES; ++i) {
-    const int load = WAVES * i + wave;
-    const int r = load * kRows + r_in;
-    dma16<0>(rsrc, static_cast<unsigned>(r * token) + ((pos ^ Ops<T>::swizzle(r)) << 4), 0u, lds + load * 1024);
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = (WAVES * i + wave) * kRows + lane / kChunks;
+      offset[i] = static_cast<unsigned>(r * token) + ((pos ^ Ops<T>::swizzle(r)) << 4);
+    }
   }
-}
+  __device__ __forceinline__ i32x4 rsrc(const unsigned char* head, int n, int r0) const {
+    const int left = n - r0;
+    return make_rsrc(head + r0 * token, left > 0 ? static_cast<unsigned>((min(left, kTile) - 1) * token + kRow) : 0u);
+  }
+  template <int I>
+  __device__ __forceinline__ void one(i32x4 rsrc, std::integral_constant<int, I>, unsigned lds) const {
+    if constexpr (I < kLoads) dma16<WAVES * I * 1024>(rsrc, offset[I], 0u, __builtin_amdgcn_readfirstlane(lds + wave_lds));
+  }
+  // part I of four
+  template <int I>
+  __device__ __forceinline__ void quarter(i32x4 from, std::integral_constant<int, I>, unsigned lds) const {
+    if constexpr (kLoads < 4) {
+      one(from, std::integral_constant<int, I>{}, lds);
+    } else {
+      one(from, std::integral_constant<int, 2 * I>{}, lds);
+      one(from, std::integral_constant<int, 2 * I + 1>{}, lds);
+      static_assert(kLoads == 8, "two loads to a part");
+    }
+  }
+  template <int I = 0>
+  __device__ __forceinline__ void rest(i32x4 from, unsigned lds) const {
+    if constexpr (I < kLoads) {
+      one(from, std::integral_constant<int, I>{}, lds);
+      rest<I + 1>(from, lds);
+    }
+  }
+  __device__ __forceinline__ void all(const unsigned char* head, int n, int r0, unsigned lds) const { rest(rsrc(head, n, r0), lds); }
+};
 
 __device__ __forceinline__ unsigned lds_address(const unsigned char* p) {
   return static_cast<unsigned>(reinterpret_cast<size_t>((const __attribute__((address_space(3))) unsigned char*)p));

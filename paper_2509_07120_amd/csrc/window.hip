@@ -10,6 +10,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace bsga {
 namespace {
 
@@ -66,11 +68,17 @@ __device__ void exact_row(const WindowArgs& a, const unsigned char* q, const uns
   if (lse != nullptr && lane == 0) *lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
+template <int N>
+using Int = std::integral_constant<int, N>;
+
 template <typename T, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs a) {
   typedef Ops<T> P;
-  constexpr int kTileBytes = kTile * P::kRow;
+  constexpr int R = kParts<T>;
+  constexpr int kTileBytes = kTile * P::kRow, kBuf = 2 * kTileBytes;
+  constexpr bool kRuns = sizeof(T) == 2;  // tiles that all rows see go through run()
   extern __shared__ __align__(16) unsigned char smem[];  // K, V of buffer 0, K, V of buffer 1
+  __shared__ int flag;
   const int lane = threadIdx.x & 63;
   const int wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, g = lane >> 5;
@@ -79,7 +87,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
   const int split = static_cast<int>(unit % a.splits);
   const int h = static_cast<int>(unit / a.splits / a.row_tiles);
   const int rt = a.row_tiles - 1 - static_cast<int>(unit / a.splits % a.row_tiles);
-  constexpr int R = kParts<T>;
   const int i0 = rt * 32 * R * WAVES, i1 = min(i0 + 32 * R * WAVES, a.seen.n_q);
   const Tiles tiles = tiles_of(a.seen, i0, i1);
   const int t0 = static_cast<int>(int64_t(tiles.count) * split / a.splits), t1 = static_cast<int>(int64_t(tiles.count) * (split + 1) / a.splits);
@@ -87,12 +94,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
   const unsigned char* const kh = a.k.p + h / a.group * a.k.head;
   const unsigned char* const vh = a.v.p + h / a.group * a.v.head;
   const unsigned lds = lds_address(smem);
-  auto issue = [&](int t, int buf) {
-    const int key = tiles.key(t);
-    load_tile<T, WAVES>(kh, a.k.token, a.seen.n_k, key, lds + buf * 2 * kTileBytes, wave, lane);
-    load_tile<T, WAVES>(vh, a.v.token, a.seen.n_k, key, lds + (buf * 2 + 1) * kTileBytes, wave, lane);
+  const TileLoad<T, WAVES> k_load(a.k.token, wave, lane), v_load(a.v.token, wave, lane);
+  auto issue = [&](int t) {  // buffers by turns
+    const int key = tiles.key(t), buf = (t - t0) & 1;
+    k_load.all(kh, a.seen.n_k, key, lds + buf * kBuf);
+    v_load.all(vh, a.seen.n_k, key, lds + buf * kBuf + kTileBytes);
   };
-  if (t0 < t1) issue(t0, 0);
+  auto begin = [&]() {
+    if (t0 < t1) issue(t0);
+    if (t0 + 1 < t1) issue(t0 + 1);
+  };
+  begin();
 
   // the wave's rows [w0, w1); rows past the end are computed as the last one and not stored
   const int w0 = i0 + wave * 32 * R, w1 = min(w0 + 32 * R, a.seen.n_q);
@@ -109,89 +121,264 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
     a.seen.range(w0, lo_min, hi_min);
     a.seen.range(w1 - 1, lo_max, hi_max);
   }
+  auto seen_by_none = [&](int key) { return none || key >= hi_max || (key + kTile <= lo_min && key >= a.seen.sinks); };
+  auto seen_by_all = [&](int key) {
+    return !none && key + kTile <= hi_min && (key >= lo_max || key + kTile <= a.seen.sinks || a.seen.sinks >= lo_max);
+  };
 
   f32x16 o[2][R];  // [dimensions][queries]
   float m[R], l[R];
-#pragma unroll
-  for (int b = 0; b < R; ++b) {
-    clear(o[0][b]);
-    clear(o[1][b]);
-    m[b] = -INFINITY;
-    l[b] = 0.f;
-  }
 
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
-    if (t + 1 < t1) {
-      issue(t + 1, buf ^ 1);
-      constexpr int kInFlight = 2 * kTileBytes / 1024 / WAVES;
-      __builtin_amdgcn_s_waitcnt((kInFlight & 15) | (kInFlight >> 4 << 14) | 0x0f70);  // this tile's have landed
+  // A tile with masks and a maximum that follows.
+  auto plain = [&](int t) {
+    const int lane = fresh_lane(), n = lane & 31, g = lane >> 5;  // (addresses are not kept in registers between tiles)
+    const int key = tiles.key(t);
+    const bool all = seen_by_all(key);
+    const unsigned char* const kt = smem + ((t - t0) & 1) * kBuf;
+    const unsigned char* const vt = kt + kTileBytes;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      typename P::A ka[P::kSteps];
+      P::rows(kt, 32 * u + n, g, ka);
+      f32x16 s[R];
+#pragma unroll
+      for (int b = 0; b < R; ++b) {
+        clear(s[b]);
+#pragma unroll
+        for (int c = 0; c < P::kSteps; ++c) s[b] = P::product(ka[c], qf[b][c], s[b]);
+        if (!all) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int j = key + 32 * u + 8 * (i >> 2) + 4 * g + (i & 3);
+            s[b][i] = j < hi[b] && (j >= lo[b] || j < a.seen.sinks) ? s[b][i] : -INFINITY;
+          }
+        }
+      }
+      typename P::A w[R][P::kCols];
+#pragma unroll
+      for (int b = 0; b < R; ++b) {
+        float top = s[b][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[b][i]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+        const bool raise = m[b] == -INFINITY ? top > -INFINITY : top > m[b] + kRaise;
+        if (__any(raise)) {
+          const float to = raise ? top : m[b];
+          const float keep = m[b] == -INFINITY ? 1.f : exp2f(m[b] - to);  // (of nothing so far, what is kept is zero)
+          m[b] = to;
+          l[b] *= keep;
+#pragma unroll
+          for (int db = 0; db < 2; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[db][b][i] *= keep;
+        }
+        const float from = m[b] == -INFINITY ? 0.f : m[b];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], a.scale_log2, -from));
+          l[b] += s[b][i];
+        }
+        P::round(s[b], w[b]);
+      }
+#pragma unroll
+      for (int db = 0; db < 2; ++db) {
+        typename P::A va[P::kCols];
+        P::columns(vt, 32 * u, db, lane, va);
+#pragma unroll
+        for (int c = 0; c < P::kCols; ++c)
+#pragma unroll
+          for (int b = 0; b < R; ++b) o[db][b] = P::product(va[c], w[b][c], o[db][b]);
+      }
+    }
+  };
+
+  // Tiles from t on that all rows of the wave see; returns the first that is not one.  The vector instructions of one unit of 32 keys x 32
+  // queries stand between the products of its neighbours: unit N's weights beside the scores of unit N + 1 and the update of O by
+  // unit N - 1, one product and two weights to a slot.  Weights are taken from the maximum that the tiles before have left, without a look at the
+  // scores: there is room for 2^100 above it, and rows that need more are found at the end.
+  auto run = [&](int t) -> int {
+    if constexpr (!kRuns) {
+      return t;
+    } else {
+      const int lane = fresh_lane(), n = lane & 31, g = lane >> 5;
+      int kaddr[4], vaddr[2][2];  // of the first 32 rows: K chunks; [dimensions][rows + 8]
+#pragma unroll
+      for (int c = 0; c < 4; ++c) kaddr[c] = n * P::kRow + (((2 * c + g) ^ P::swizzle(n)) << 4);
+      {
+        const int mm = (lane & 15) >> 2, j = lane & 3, r = 4 * g + mm;
+#pragma unroll
+        for (int db = 0; db < 2; ++db)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            vaddr[db][e] = kTileBytes + (r + 8 * e) * P::kRow + (((db * 4 + 2 * ((lane >> 4) & 1) + (j >> 1)) ^ P::swizzle(r + 8 * e)) << 4) + (j & 1) * 8;
+      }
+      f32x16 sc[2];        // scores
+      u32x4 pw[2][2];      // weights: [queries][16 keys]
+      bf16x8 ka[4];        // K operands of the unit whose scores come next
+      bf16x8 va[2][2][2];  // V operands: [32 keys][dimensions][16 keys]
+      float ex[2][2];      // the two weights that are packed in the next slot
+      auto read_k = [&](int u) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) ka[c] = *LDS_PTR(bf16x8, smem + u * 32 * P::kRow + kaddr[c]);
+      };
+      auto read_v = [&](auto uc) {
+        constexpr int u = decltype(uc)::value;
+#pragma unroll
+        for (int db = 0; db < 2; ++db)
+#pragma unroll
+          for (int cp = 0; cp < 2; ++cp) {
+            u32x2 x[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              x[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(
+                                                   smem + (32 * u + 16 * cp) * P::kRow + vaddr[db][e])));
+            va[u][db][cp] = __builtin_bit_cast(bf16x8, u32x4{x[0][0], x[0][1], x[1][0], x[1][1]});
+          }
+      };
+      auto weight = [&](float s, float from) { return __builtin_amdgcn_exp2f(fmaf(s, a.scale_log2, -from)); };
+      auto slot = [&](auto nc, auto sc_, auto&& mid) {
+        constexpr int N = decltype(nc)::value, S = decltype(sc_)::value;
+        constexpr int BQ = N & 1, BN = (N + 1) & 1, BP = (N + 3) & 1, UP = ((N + 3) & 3) >> 1;  // queries of this unit, the next, the last; keys of the last
+        if constexpr (S < 4) {
+          if constexpr (S == 0) clear(sc[BN]);
+          sc[BN] = P::product(ka[S & 3], qf[BN][S & 3], sc[BN]);
+        } else {
+          o[S & 1][BP] = P::product(va[UP][S & 1][(S >> 1) & 1], __builtin_bit_cast(bf16x8, pw[BP][(S >> 1) & 1]), o[S & 1][BP]);
+        }
+        const unsigned pk = pack_bf16(ex[S & 1][0], ex[S & 1][1]);
+        l[BQ] += ex[S & 1][0] + ex[S & 1][1];
+        asm volatile("" : "+v"(l[BQ]));  // pinned: added up later, all of a unit's weights would stay alive
+        if constexpr (S < 7) {
+          ex[(S + 1) & 1][0] = weight(sc[BQ][2 * S + 2], m[BQ]);
+          ex[(S + 1) & 1][1] = weight(sc[BQ][2 * S + 3], m[BQ]);
+        } else {
+          ex[0][0] = weight(sc[BN][0], m[BN]);
+          ex[0][1] = weight(sc[BN][1], m[BN]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        pw[BQ][S >> 2][S & 3] = pk;
+        mid(sc_);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      auto four = [&](auto nc, auto&& mid) {
+        slot(nc, Int<0>{}, mid); slot(nc, Int<1>{}, mid); slot(nc, Int<2>{}, mid); slot(nc, Int<3>{}, mid);
+        slot(nc, Int<4>{}, mid); slot(nc, Int<5>{}, mid); slot(nc, Int<6>{}, mid); slot(nc, Int<7>{}, mid);
+      };
+      // On entry sc[0] holds the first scores, ka the K operands of the first 32 keys, pw[1] and va[1] the last unit before (zeros at the start).
+      unsigned to = lds + ((t - t0) & 1) * kBuf;  // the tile's buffer; the other one differs in one bit of the offset
+      auto turn = [&]() {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) kaddr[c] ^= kBuf;
+      };
+      if ((t - t0) & 1) {
+        turn();
+#pragma unroll
+        for (int db = 0; db < 2; ++db)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) vaddr[db][e] ^= kBuf;
+      }
+      auto tile = [&]() {
+        const int next = tiles.key(t + 2 < t1 ? t + 2 : t);  // past the end: a load that nobody reads, in place of a branch
+        const i32x4 krsrc = k_load.rsrc(kh, a.seen.n_k, next), vrsrc = v_load.rsrc(vh, a.seen.n_k, next);
+        four(Int<0>{}, [&](auto s) {
+          if constexpr (decltype(s)::value == 0) read_v(Int<0>{});
+          if constexpr (decltype(s)::value == 3) read_k(1);
+        });
+        four(Int<1>{}, [&](auto s) {
+          if constexpr (decltype(s)::value == 0) read_v(Int<1>{});
+          if constexpr (decltype(s)::value == 1) turn();
+          if constexpr (decltype(s)::value >= 4) vaddr[decltype(s)::value & 1][(decltype(s)::value >> 1) & 1] ^= kBuf;
+        });
+        four(Int<2>{}, [&](auto s) {
+          constexpr int S = decltype(s)::value;
+          if constexpr (S == 0) {  // the next tile has landed; this one is read, in every wave
+            __builtin_amdgcn_s_waitcnt(0x0f70);
+            __syncthreads();
+          }
+          if constexpr (S == 3) read_k(0);
+          if constexpr (S >= 4) k_load.quarter(krsrc, Int<S - 4>{}, to);
+        });
+        four(Int<3>{}, [&](auto s) {
+          constexpr int S = decltype(s)::value;
+          if constexpr (S < 4) v_load.quarter(vrsrc, Int<S>{}, to + kTileBytes);
+        });
+        to ^= lds ^ (lds + kBuf);
+      };
+      read_k(0);
+#pragma unroll
+      for (int cp = 0; cp < 2; ++cp) {
+        pw[1][cp] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int db = 0; db < 2; ++db) va[1][db][cp] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+      }
+      clear(sc[0]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) sc[0] = P::product(ka[c], qf[0][c], sc[0]);
+      ex[0][0] = weight(sc[0][0], m[0]);
+      ex[0][1] = weight(sc[0][1], m[0]);
+      __builtin_amdgcn_sched_barrier(0);
+      do {
+        tile();
+        ++t;
+      } while (t < t1 && seen_by_all(tiles.key(t)));
+#pragma unroll
+      for (int db = 0; db < 2; ++db)
+#pragma unroll
+        for (int cp = 0; cp < 2; ++cp) o[db][1] = P::product(va[1][db][cp], __builtin_bit_cast(bf16x8, pw[1][cp]), o[db][1]);
+      return t;
+    }
+  };
+
+  // All tiles.  At the top of the loop tile t has landed and the loads of the next are on their way; a tile is one barrier, after which its buffer is
+  // free and the loads of the tile after next are issued.  Returns whether (to the whole workgroup) rows left the range of run().
+  auto pass = [&](bool runs) -> bool {
+#pragma unroll
+    for (int b = 0; b < R; ++b) {
+      clear(o[0][b]);
+      clear(o[1][b]);
+      m[b] = -INFINITY;
+      l[b] = 0.f;
+    }
+    if (t0 + 1 < t1) {
+      constexpr int kInFlight = kBuf / 1024 / WAVES;
+      __builtin_amdgcn_s_waitcnt((kInFlight & 15) | (kInFlight >> 4 << 14) | 0x0f70);
     } else {
       __builtin_amdgcn_s_waitcnt(0x0f70);
     }
+    if (threadIdx.x == 0) flag = 0;
     __syncthreads();
-    const int key = tiles.key(t);
-    const bool seen_by_none = none || key >= hi_max || (key + kTile <= lo_min && key >= a.seen.sinks);
-    const bool seen_by_all = key + kTile <= hi_min && (key >= lo_max || key + kTile <= a.seen.sinks || a.seen.sinks >= lo_max);
-    if (!seen_by_none) {
-      const unsigned char* const kt = smem + buf * 2 * kTileBytes;
-      const unsigned char* const vt = kt + kTileBytes;
+    bool ready = false;  // whether all rows have a maximum
+    for (int t = t0; t < t1;) {
+      if (kRuns && runs && ready && seen_by_all(tiles.key(t))) t = run(t);
+      if (t >= t1) break;
+      if (!seen_by_none(tiles.key(t))) {
+        plain(t);
+        ready = true;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        typename P::A ka[P::kSteps];
-        P::rows(kt, 32 * u + n, g, ka);
-        f32x16 s[R];
-#pragma unroll
-        for (int b = 0; b < R; ++b) {
-          clear(s[b]);
-#pragma unroll
-          for (int c = 0; c < P::kSteps; ++c) s[b] = P::product(ka[c], qf[b][c], s[b]);
-          if (!seen_by_all) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int j = key + 32 * u + 8 * (i >> 2) + 4 * g + (i & 3);
-              s[b][i] = j < hi[b] && (j >= lo[b] || j < a.seen.sinks) ? s[b][i] : -INFINITY;
-            }
-          }
-        }
-        typename P::A w[R][P::kCols];
-#pragma unroll
-        for (int b = 0; b < R; ++b) {
-          float top = s[b][0];
-#pragma unroll
-          for (int i = 1; i < 16; ++i) top = fmaxf(top, s[b][i]);
-          top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
-          const bool raise = m[b] == -INFINITY ? top > -INFINITY : top > m[b] + kRaise;
-          if (__any(raise)) {
-            const float to = raise ? top : m[b];
-            const float keep = m[b] == -INFINITY ? 1.f : exp2f(m[b] - to);  // (of nothing so far, what is kept is zero)
-            m[b] = to;
-            l[b] *= keep;
-#pragma unroll
-            for (int db = 0; db < 2; ++db)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) o[db][b][i] *= keep;
-          }
-          const float from = m[b] == -INFINITY ? 0.f : m[b];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], a.scale_log2, -from));
-            l[b] += s[b][i];
-          }
-          P::round(s[b], w[b]);
-        }
-#pragma unroll
-        for (int db = 0; db < 2; ++db) {
-          typename P::A va[P::kCols];
-          P::columns(vt, 32 * u, db, lane, va);
-#pragma unroll
-          for (int c = 0; c < P::kCols; ++c)
-#pragma unroll
-            for (int b = 0; b < R; ++b) o[db][b] = P::product(va[c], w[b][c], o[db][b]);
-        }
+        for (int b = 0; b < R; ++b) ready = ready && __all(m[b] > -INFINITY);
       }
+      __builtin_amdgcn_s_waitcnt(0x0f70);
+      __syncthreads();
+      if (t + 2 < t1) issue(t + 2);
+      ++t;
     }
-    __syncthreads();  // the buffer is read
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // nothing is on its way into LDS any more
+    if (!kRuns || !runs) return false;
+    bool bad = false;
+#pragma unroll
+    for (int b = 0; b < R; ++b) {
+      bad = bad || !(l[b] < 0x1p100f);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) bad = bad || !(fabsf(o[0][b][i]) < INFINITY) || !(fabsf(o[1][b][i]) < INFINITY);
+    }
+    if (bad && !none) flag = 1;
+    __syncthreads();
+    return flag != 0;
+  };
+  if (pass(true)) {
+    __syncthreads();  // everybody has read the flag
+    begin();
+    pass(false);
   }
 
   if (none) return;  // (no barrier follows)

@@ -96,10 +96,11 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(const BwdArgs a) {
   const unsigned char* const vh = a.v.p + h / a.group * a.v.head;
   const int64_t row0 = int64_t(h) * a.seen.n_q;
   const unsigned lds = lds_address(smem);
+  const TileLoad<T, WAVES> k_load(a.k.token, wave, lane), v_load(a.v.token, wave, lane);
   auto issue = [&](int t, int buf) {
     const int key = tiles.key(t);
-    load_tile<T, WAVES>(kh, a.k.token, a.seen.n_k, key, lds + buf * 2 * kTileBytes, wave, lane);
-    load_tile<T, WAVES>(vh, a.v.token, a.seen.n_k, key, lds + (buf * 2 + 1) * kTileBytes, wave, lane);
+    k_load.all(kh, a.seen.n_k, key, lds + buf * 2 * kTileBytes);
+    v_load.all(vh, a.seen.n_k, key, lds + (buf * 2 + 1) * kTileBytes);
   };
   if (t0 < t1) issue(t0, 0);
 
@@ -294,11 +295,12 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(const BwdArgs a) {
   }
   const int h0 = hk * a.group;
   const unsigned lds = lds_address(smem);
+  const TileLoad<T, WAVES> q_load(a.q.token, wave, lane), d_load(P::kRow, wave, lane);
   auto issue = [&](int s, int buf) {
     const int h = h0 + s / seq.per_head, i0 = (seq.first + s % seq.per_head) * kTile;
     const unsigned at = lds + buf * kBuf;
-    load_tile<T, WAVES>(a.q.p + h * a.q.head, a.q.token, a.seen.n_q, i0, at, wave, lane);
-    load_tile<T, WAVES>(a.dout + int64_t(h) * a.seen.n_q * P::kRow, P::kRow, a.seen.n_q, i0, at + kTileBytes, wave, lane);
+    q_load.all(a.q.p + h * a.q.head, a.seen.n_q, i0, at);
+    d_load.all(a.dout + int64_t(h) * a.seen.n_q * P::kRow, a.seen.n_q, i0, at + kTileBytes);
     // every wave, so that all wait for the same number of loads: the same bytes to the same place
     const int64_t row = int64_t(h) * a.stat_rows + i0;
     dma16<0>(make_rsrc(a.stats + row * 2, static_cast<unsigned>(min(a.seen.n_q - i0, kTile)) * 8u), lane * 16, 0u, at + 2 * kTileBytes);
