@@ -3,9 +3,10 @@
 // With P = exp(s - lse) for the keys j that query i sees and D_i = sum_d dO_id O_id:
 //   dV_j = sum_i P_ij dO_i,  dS_ij = P_ij (<dO_i, V_j> - D_i),  dQ_i = scale sum_j dS_ij K_j,  dK_j = scale sum_i dS_ij Q_i,
 // the sums of dV and dK over the query heads that share the key head as well.
-// Two kernels, so that every sum has one owner and one order (no atomics): one per query rows, which goes over the keys as the forward pass does and
-// leaves lse log2(e) and D for the other; one per key rows, which goes over the queries that see them.  Seven products in place of
-// the five that one kernel with shared sums of dQ would need.  Both recompute S and P from lse.
+// Two kinds of workgroups, so that every sum has one owner and one order (no atomics): for query rows, which go over the keys as the forward pass
+// does, and for key rows, which go over the queries that see them.  Seven products in place of the five that one kind with shared
+// sums of dQ would need.  Both recompute S and P from lse.  They are one launch: the key rows' workgroups, which are longer, come first, and the
+// others fill up what they leave.
 // Key rows that are seen from far (the first tokens) have many more queries than others: their queries are dealt out to several workgroups, whose
 // sums in fp32 are added up at the end, always in the same order.
 #include "window.h"
@@ -17,13 +18,13 @@ namespace {
 
 constexpr int kPlaces = 512;
 constexpr int kKeyRows = 128;     // keys of a workgroup, 32 for each wave
-constexpr int kStatBytes = 1024;  // lse and D of a tile's queries: 512 bytes, and as much that the load of a whole wave adds
+constexpr int kStatBytes = 1024;  // of a tile's queries: 512 bytes, and as much that the load of a whole wave adds
 
 struct BwdArgs {
   View q, k, v;
   const unsigned char *out, *dout;  // [heads, n_q, 64]
   const float* lse;
-  float* stats;                     // [heads, stat_rows][2]: lse log2(e), D; an even number of rows, so that tiles of them are aligned
+  float* stats;                     // [heads][2][stat_rows]: -lse / scale and -D, what the products' sums of a query begin with; whole tiles of rows
   unsigned char *dq, *dk, *dv;      // contiguous
   float* part_q;                    // [q_splits][heads, n_q, 64]
   float* part_kv[2];                // first tokens: [sink_splits][kv_heads, sink_rows, 128]; the others [splits][kv_heads, n_k - sink_rows, 128]
@@ -56,7 +57,7 @@ __device__ __forceinline__ float dot_rows(const unsigned char* x, const unsigned
 // The gradient of one query again, by a wave on its own, over the keys that it sees and no others, see exact_row in window.hip.
 template <typename T>
 __device__ float exact_query(const BwdArgs& a, const unsigned char* q, const unsigned char* dout, const unsigned char* k, const unsigned char* v,
-                             float lse2, float D, int i, int t0, int t1, const Tiles& tiles, int lane) {
+                             float from, float D, int i, int t0, int t1, const Tiles& tiles, int lane) {
   int lo, hi;
   a.seen.range(i, lo, hi);
   float sum = 0.f;
@@ -64,7 +65,7 @@ __device__ float exact_query(const BwdArgs& a, const unsigned char* q, const uns
     const int j = tiles.key(t) + lane;
     const bool sees = j < hi && (j >= lo || j < a.seen.sinks);
     float ds = 0.f;
-    if (sees) ds = exp2f(dot_rows<T>(q, k + j * a.k.token) * a.scale_log2 - lse2) * (dot_rows<T>(dout, v + j * a.v.token) - D);
+    if (sees) ds = exp2f((dot_rows<T>(q, k + j * a.k.token) + from) * a.scale_log2) * (dot_rows<T>(dout, v + j * a.v.token) + D);
     unsigned long long all = __ballot(sees);
     while (all != 0) {
       const int e = __builtin_ctzll(all);
@@ -75,16 +76,16 @@ __device__ float exact_query(const BwdArgs& a, const unsigned char* q, const uns
   return sum * a.scale;
 }
 
+// dQ of 32 kParts queries for each of four waves.  smem: K, V of buffer 0, K, V of buffer 1.
 template <typename T>
-__global__ __launch_bounds__(256, 2) void window_dq_kernel(const BwdArgs a) {
+__device__ __forceinline__ void query_rows(const BwdArgs& a, int64_t block, int64_t blocks, unsigned char* smem) {
   typedef Ops<T> P;
   constexpr int R = kParts<T>, WAVES = 4;
   constexpr int kTileBytes = kTile * P::kRow;
-  extern __shared__ __align__(16) unsigned char smem[];  // K, V of buffer 0, K, V of buffer 1
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, g = lane >> 5;
-  const int64_t unit = spread(blockIdx.x, gridDim.x, kPlaces);
+  const int64_t unit = spread(block, blocks, kPlaces);
   const int split = static_cast<int>(unit % a.q_splits);
   const int h = static_cast<int>(unit / a.q_splits / a.row_tiles);
   const int rt = a.row_tiles - 1 - static_cast<int>(unit / a.q_splits % a.row_tiles);
@@ -108,20 +109,16 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(const BwdArgs a) {
   const bool none = w0 >= a.seen.n_q;
   typename P::A qf[R][P::kSteps], df[R][P::kSteps];
   int lo[R], hi[R], lo_min = 0, hi_min = 0, lo_max = 0, hi_max = 0;
-  float lse2[R], D[R];
+  float from[R], D[R];
 #pragma unroll
   for (int b = 0; b < R; ++b) {
     const int i = min(w0 + 32 * b + n, a.seen.n_q - 1);
     P::row(qh + i * a.q.token, g, qf[b]);
     P::row(a.dout + (row0 + i) * P::kRow, g, df[b]);
     a.seen.range(i, lo[b], hi[b]);
-    lse2[b] = a.lse[row0 + i] * kLog2e;
-    typename P::A of[P::kSteps];
-    P::row(a.out + (row0 + i) * P::kRow, g, of);
-    const float sum = P::dot(df[b], of);
-    D[b] = sum + __shfl_xor(sum, 32);
-    if (split == 0 && g == 0 && w0 + 32 * b + n < a.seen.n_q)
-      *reinterpret_cast<f32x2*>(a.stats + (int64_t(h) * a.stat_rows + i) * 2) = f32x2{lse2[b], D[b]};
+    const float* const st = a.stats + int64_t(h) * 2 * a.stat_rows + i;
+    from[b] = st[0] * a.scale_log2;
+    D[b] = st[a.stat_rows];
   }
   if (!none) {
     a.seen.range(w0, lo_min, hi_min);
@@ -168,7 +165,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(const BwdArgs a) {
               dp = P::product(va[c], df[b][c], dp);
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, -lse2[b])) * (dp[i] - D[b]);
+            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, from[b])) * (dp[i] + D[b]);
             if (!seen_by_all) {
 #pragma unroll
               for (int i = 0; i < 16; ++i) {
@@ -223,7 +220,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(const BwdArgs a) {
       const int e = __builtin_ctzll(again);
       again &= again - 1;
       const int row = w0 + 32 * b + e;
-      const float x = exact_query<T>(a, qh + row * a.q.token, a.dout + (row0 + row) * P::kRow, kh, vh, __shfl(lse2[b], e), __shfl(D[b], e), row, t0,
+      const float x = exact_query<T>(a, qh + row * a.q.token, a.dout + (row0 + row) * P::kRow, kh, vh, a.stats[int64_t(h) * 2 * a.stat_rows + row], __shfl(D[b], e), row, t0,
                                      t1, tiles, lane);
       if (a.q_splits > 1) a.part_q[(int64_t(split) * a.heads * a.seen.n_q + row0 + row) * 64 + lane] = x;
       else P::store1(a.dq + (row0 + row) * P::kRow, lane, x);
@@ -250,9 +247,9 @@ __device__ void exact_key(const BwdArgs& a, const unsigned char* k, const unsign
     const bool sees = i >= see.first && i < see.last;
     float p = 0.f, ds = 0.f;
     if (sees) {
-      const f32x2 st = *reinterpret_cast<const f32x2*>(a.stats + (int64_t(h) * a.stat_rows + i) * 2);
-      p = exp2f(dot_rows<T>(qh + i * a.q.token, k) * a.scale_log2 - st[0]);
-      ds = p * (dot_rows<T>(a.dout + (row0 + i) * Ops<T>::kRow, v) - st[1]);
+      const float* const st = a.stats + int64_t(h) * 2 * a.stat_rows + i;
+      p = exp2f((dot_rows<T>(qh + i * a.q.token, k) + st[0]) * a.scale_log2);
+      ds = p * (dot_rows<T>(a.dout + (row0 + i) * Ops<T>::kRow, v) + st[a.stat_rows]);
     }
     unsigned long long all = __ballot(sees);
     while (all != 0) {
@@ -265,19 +262,19 @@ __device__ void exact_key(const BwdArgs& a, const unsigned char* k, const unsign
   dk *= a.scale;
 }
 
+// dK and dV of 32 keys for each of four waves.  smem: Q, dO and what their sums begin with of buffer 0, then of buffer 1.
 template <typename T>
-__global__ __launch_bounds__(256, 2) void window_dkv_kernel(const BwdArgs a) {
+__device__ __forceinline__ void key_rows(const BwdArgs& a, int64_t block, int64_t blocks, unsigned char* smem) {
   typedef Ops<T> P;
   constexpr int WAVES = 4;
   constexpr int kTileBytes = kTile * P::kRow, kBuf = 2 * kTileBytes + kStatBytes;
-  extern __shared__ __align__(16) unsigned char smem[];  // Q, dO, lse and D of buffer 0, then of buffer 1
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, g = lane >> 5;
   // the first tokens' units come first: they are the longest
   const int64_t sink_units = int64_t(a.kv_heads) * a.sink_tiles * a.sink_splits;
-  const bool sink = blockIdx.x < sink_units;
-  const int64_t unit = sink ? blockIdx.x : spread(blockIdx.x - sink_units, gridDim.x - sink_units, kPlaces);
+  const bool sink = block < sink_units;
+  const int64_t unit = sink ? block : spread(block - sink_units, blocks - sink_units, kPlaces);
   const int splits = sink ? a.sink_splits : a.splits, of_head = sink ? a.sink_tiles : a.key_tiles - a.sink_tiles;
   const int split = static_cast<int>(unit % splits);
   const int hk = static_cast<int>(unit / splits / of_head);
@@ -301,9 +298,9 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(const BwdArgs a) {
     const unsigned at = lds + buf * kBuf;
     q_load.all(a.q.p + h * a.q.head, a.seen.n_q, i0, at);
     d_load.all(a.dout + int64_t(h) * a.seen.n_q * P::kRow, a.seen.n_q, i0, at + kTileBytes);
-    // every wave, so that all wait for the same number of loads: the same bytes to the same place
-    const int64_t row = int64_t(h) * a.stat_rows + i0;
-    dma16<0>(make_rsrc(a.stats + row * 2, static_cast<unsigned>(min(a.seen.n_q - i0, kTile)) * 8u), lane * 16, 0u, at + 2 * kTileBytes);
+    // every wave, so that all wait for the same number of loads: the same bytes to the same place, 256 of each kind
+    dma16<0>(make_rsrc(a.stats + int64_t(h) * 2 * a.stat_rows, a.stat_rows * 8u),
+             i0 * 4u + (lane < 16 ? lane * 16u : lane < 32 ? a.stat_rows * 4u + (lane - 16) * 16u : 1u << 30), 0u, at + 2 * kTileBytes);
   };
   if (seq.begin < seq.end) issue(seq.begin, 0);
 
@@ -351,8 +348,15 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(const BwdArgs a) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         f32x16 p, ds;
-        clear(p);
-        clear(ds);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const f32x4 x = *LDS_PTR(f32x4, st + (32 * u + 8 * r + 4 * g) * 4), y = *LDS_PTR(f32x4, st + 256 + (32 * u + 8 * r + 4 * g) * 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            p[4 * r + e] = x[e];
+            ds[4 * r + e] = y[e];
+          }
+        }
         {
           typename P::A qa[P::kSteps], da[P::kSteps];
           P::rows(qt, 32 * u + n, g, qa);
@@ -365,10 +369,8 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(const BwdArgs a) {
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int r = 32 * u + 8 * (e >> 2) + 4 * g + (e & 3);
-          const f32x2 of_row = *LDS_PTR(f32x2, st + r * 8);
-          p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], a.scale_log2, -of_row[0]));
-          ds[e] = p[e] * (ds[e] - of_row[1]);
+          p[e] = __builtin_amdgcn_exp2f(p[e] * a.scale_log2);
+          ds[e] *= p[e];
         }
         if (!all) {
 #pragma unroll
@@ -448,6 +450,30 @@ __global__ __launch_bounds__(256, 2) void window_dkv_kernel(const BwdArgs a) {
   }
 }
 
+// Eight lanes to a query: what its products' sums begin with.  A query that sees nothing has lse -inf, and -inf here: weights of zero.
+template <typename T>
+__global__ __launch_bounds__(256) void window_stats_kernel(const BwdArgs a) {
+  const int64_t row = int64_t(blockIdx.x) * 32 + (threadIdx.x >> 3);
+  if (row >= int64_t(a.heads) * a.seen.n_q) return;
+  const unsigned char *x = a.out + row * Ops<T>::kRow, *y = a.dout + row * Ops<T>::kRow;
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum += Ops<T>::number(x, (threadIdx.x & 7) * 8 + e) * Ops<T>::number(y, (threadIdx.x & 7) * 8 + e);
+  for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor(sum, o);
+  if ((threadIdx.x & 7) != 0) return;
+  const int64_t h = row / a.seen.n_q;
+  float* const st = a.stats + h * 2 * a.stat_rows + (row - h * a.seen.n_q);
+  st[0] = a.lse[row] == -INFINITY ? -INFINITY : -a.lse[row] / a.scale;
+  st[a.stat_rows] = -sum;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256, 2) void window_bwd_kernel(const BwdArgs a, int64_t key_blocks) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  if (blockIdx.x < key_blocks) key_rows<T>(a, blockIdx.x, key_blocks, smem);
+  else query_rows<T>(a, blockIdx.x - key_blocks, gridDim.x - key_blocks, smem);
+}
+
 // Sums of the splits: WIDTH numbers of each row, the second 64 to a tensor of their own.  Row r of head h goes to row first + r of it.
 template <typename T, int WIDTH>
 __global__ __launch_bounds__(256) void window_sum_kernel(const float* __restrict__ part, int64_t rows_of_head, int heads, int splits, int64_t first,
@@ -471,7 +497,7 @@ __global__ __launch_bounds__(256) void window_sum_kernel(const float* __restrict
 // too few of them, and those of the first tokens, which all queries see, in parts as long as the others' queries.
 void shape_of(BwdArgs& a, int rows) {  // rows of a workgroup of queries
   const Seen& s = a.seen;
-  a.stat_rows = (s.n_q + 1) & ~1;
+  a.stat_rows = static_cast<int>(ceil_div(s.n_q, kTile)) * kTile;
   a.row_tiles = static_cast<int>(ceil_div(s.n_q, rows));
   a.q_splits = 1;
   const int64_t units = int64_t(a.row_tiles) * a.heads;
@@ -513,20 +539,20 @@ int launch(const BwdArgs& a, hipStream_t s) {
   const char* what = "bsga_window_attn_bwd launch";
   const int64_t q_units = int64_t(a.heads) * a.row_tiles * a.q_splits;
   const int64_t k_units = int64_t(a.kv_heads) * (int64_t(a.sink_tiles) * a.sink_splits + int64_t(a.key_tiles - a.sink_tiles) * a.splits);
-  if (q_units > 0x7fffffff || k_units > 0x7fffffff) return fail(BSGA_ERR_UNSUPPORTED, "bsga_window_attn_bwd: too many rows");
+  if (q_units + k_units > 0x7fffffff) return fail(BSGA_ERR_UNSUPPORTED, "bsga_window_attn_bwd: too many rows");
   const int64_t q_rows = int64_t(a.heads) * a.seen.n_q;
-  if (q_units > 0) {
-    hipLaunchKernelGGL(window_dq_kernel<T>, dim3(static_cast<unsigned>(q_units)), dim3(256), 4 * kTile * Ops<T>::kRow, s, a);
+  if (q_rows > 0) {
+    hipLaunchKernelGGL(window_stats_kernel<T>, dim3(static_cast<unsigned>(ceil_div(q_rows, 32))), dim3(256), 0, s, a);
     if (int rc = check_hip(hipGetLastError(), what)) return rc;
-    if (a.q_splits > 1) {
-      hipLaunchKernelGGL((window_sum_kernel<T, 64>), dim3(static_cast<unsigned>(ceil_div(q_rows, 16))), dim3(256), 0, s, a.part_q, a.seen.n_q, a.heads,
-                         a.q_splits, 0, a.seen.n_q, a.dq, nullptr);
-      if (int rc = check_hip(hipGetLastError(), what)) return rc;
-    }
   }
-  if (k_units == 0) return BSGA_OK;
-  hipLaunchKernelGGL(window_dkv_kernel<T>, dim3(static_cast<unsigned>(k_units)), dim3(256), 2 * (2 * kTile * Ops<T>::kRow + kStatBytes), s, a);
+  hipLaunchKernelGGL(window_bwd_kernel<T>, dim3(static_cast<unsigned>(q_units + k_units)), dim3(256), 2 * (2 * kTile * Ops<T>::kRow + kStatBytes), s, a,
+                     k_units);
   if (int rc = check_hip(hipGetLastError(), what)) return rc;
+  if (a.q_splits > 1) {
+    hipLaunchKernelGGL((window_sum_kernel<T, 64>), dim3(static_cast<unsigned>(ceil_div(q_rows, 16))), dim3(256), 0, s, a.part_q, a.seen.n_q, a.heads,
+                       a.q_splits, 0, a.seen.n_q, a.dq, nullptr);
+    if (int rc = check_hip(hipGetLastError(), what)) return rc;
+  }
   const int64_t sink_rows = min(int64_t(a.sink_tiles) * kKeyRows, int64_t(a.seen.n_k));
   for (int x = 0; x < 2; ++x) {
     const int splits = x == 0 ? a.sink_splits : a.splits;
