@@ -13,11 +13,13 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace bsga {
 namespace {
 
 constexpr int kPlaces = 512;
-constexpr int kKeyRows = 128;     // keys of a workgroup, 32 for each wave
+constexpr int kOwnRows = 128;     // queries or keys of a workgroup, 32 for each wave
 constexpr int kStatBytes = 1024;  // of a tile's queries: 512 bytes, and as much that the load of a whole wave adds
 
 struct BwdArgs {
@@ -30,7 +32,7 @@ struct BwdArgs {
   float* part_kv[2];                // first tokens: [sink_splits][kv_heads, sink_rows, 128]; the others [splits][kv_heads, n_k - sink_rows, 128]
   Seen seen;
   int heads, kv_heads, group, stat_rows, row_tiles, q_splits;
-  int key_tiles, sink_tiles, sink_splits, splits;  // of kKeyRows keys
+  int key_tiles, sink_tiles, sink_splits, splits;  // of kOwnRows keys
   float scale, scale_log2;
 };
 
@@ -76,12 +78,182 @@ __device__ float exact_query(const BwdArgs& a, const unsigned char* q, const uns
   return sum * a.scale;
 }
 
-// dQ of 32 kParts queries for each of four waves.  smem: K, V of buffer 0, K, V of buffer 1.
+template <int N>
+using Int = std::integral_constant<int, N>;
+template <int A, int B, typename F>
+__device__ __forceinline__ void each(F&& f) {
+  if constexpr (A < B) {
+    f(Int<A>{});
+    each<A + 1, B>(f);
+  }
+}
+
+// Tiles of the streamed rows (X: those of the first product, Y: of the second) that see all of a wave's own rows, or are seen by them: from t on as
+// long as more(t).  A tile is two units of 32 streamed rows.  In unit N, while the vector instructions make P and dS of it, the
+// matrix pipe makes S and dP of unit N + 1 (eight products) and adds unit N - 1 to the sums (SUMS products: eight of key rows, four of query
+// rows): one product to a slot, with the operand that its register gets next asked for right behind it, half a unit ahead of its use.
+//   own0, own1  the wave's rows as operands of S and dP;  sums0 += columns of Y (key rows) or X (query rows) by P or dS, sums1 += columns of X by dS
+//   first0, first1  what S and dP of query rows begin with; those of key rows begin with the 64 + 64 numbers behind X and Y
+//   land(): all loads of the wave's next tile have landed and everybody has read the last one; load(I): load I of the tile after next
+template <int SUMS, typename More, typename Land, typename Load>
+__device__ __forceinline__ int run(int t, unsigned at, const unsigned char* smem, float scale_log2, const bf16x8 (&own0)[4], const bf16x8 (&own1)[4],
+                                   const f32x16& first0, const f32x16& first1, f32x16 (&sums0)[2], f32x16 (&sums1)[2], More&& more, Land&& land,
+                                   Load&& load) {
+  typedef Ops<__bf16> P;
+  constexpr bool KEYS = SUMS == 8;
+  constexpr int kTileBytes = kTile * P::kRow, kBuf = 2 * kTileBytes + (KEYS ? kStatBytes : 0), kSlots = SUMS + 8;
+  const int lane = fresh_lane(), n = lane & 31, g = lane >> 5;
+  int raddr[4], caddr[2][2];  // of the first 32 rows: chunks of a row; [dimensions][rows + 8] of the transposed operands
+#pragma unroll
+  for (int c = 0; c < 4; ++c) raddr[c] = n * P::kRow + (((2 * c + g) ^ P::swizzle(n)) << 4);
+  {
+    const int m = (lane & 15) >> 2, j = lane & 3, r = 4 * g + m;
+#pragma unroll
+    for (int db = 0; db < 2; ++db)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        caddr[db][e] = (r + 8 * e) * P::kRow + (((db * 4 + 2 * ((lane >> 4) & 1) + (j >> 1)) ^ P::swizzle(r + 8 * e)) << 4) + (j & 1) * 8;
+  }
+  unsigned next = at + kBuf == 3 * kBuf ? 0u : at + kBuf;  // the buffers' places: of this tile and of the next
+  f32x16 s[2], dp[2];                                       // [unit]; P and dS take their places
+  u32x4 pw[2], dw[2];                                       // packed: [16 streamed rows]
+  bf16x8 op[8];
+  auto row_operand = [&](auto ic, auto uc, unsigned from) {  // of S (0 to 3) and dP
+    constexpr int I = decltype(ic)::value, U = decltype(uc)::value;
+    op[I] = *LDS_PTR(bf16x8, smem + from + raddr[I & 3] + (I >> 2) * kTileBytes + U * 32 * P::kRow);
+  };
+  auto sum_operand = [&](auto ic, auto uc) {  // of the sums
+    constexpr int I = decltype(ic)::value, U = decltype(uc)::value;
+    constexpr int kind = KEYS ? I & 1 : 1, db = KEYS ? (I >> 1) & 1 : I & 1, cp = KEYS ? I >> 2 : I >> 1;
+    u32x2 x[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      x[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(
+                                           smem + at + caddr[db][e] + (kind == 0 ? kTileBytes : 0) + (32 * U + 16 * cp) * P::kRow)));
+    op[I] = __builtin_bit_cast(bf16x8, u32x4{x[0][0], x[0][1], x[1][0], x[1][1]});
+  };
+  auto begin_from = [&](auto ic, auto uc, unsigned from) {  // quarter I of what S and dP of key rows begin with
+    constexpr int I = decltype(ic)::value, U = decltype(uc)::value;
+    const unsigned char* const st = smem + from + 2 * kTileBytes + (32 * U + 8 * I) * 4 + g * 16;
+    const f32x4 x = *LDS_PTR(f32x4, st), y = *LDS_PTR(f32x4, st + 256);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      s[U][4 * I + e] = x[e];
+      dp[U][4 * I + e] = y[e];
+    }
+  };
+  auto product = [&](auto jc, auto uc) {  // number J of S and dP of unit U
+    constexpr int J = decltype(jc)::value, U = decltype(uc)::value;
+    if constexpr (J < 4) s[U] = P::product(op[J], own0[J & 3], !KEYS && J == 0 ? first0 : s[U]);
+    else dp[U] = P::product(op[J], own1[J & 3], !KEYS && J == 4 ? first1 : dp[U]);
+  };
+  auto add = [&](auto ic) {  // number I of the sums
+    constexpr int I = decltype(ic)::value;
+    if constexpr (KEYS) {
+      constexpr int db = (I >> 1) & 1, cp = I >> 2;
+      if constexpr ((I & 1) == 0) sums0[db] = P::product(op[I], __builtin_bit_cast(bf16x8, pw[cp]), sums0[db]);
+      else sums1[db] = P::product(op[I], __builtin_bit_cast(bf16x8, dw[cp]), sums1[db]);
+    } else {
+      sums0[I & 1] = P::product(op[I], __builtin_bit_cast(bf16x8, dw[I >> 1]), sums0[I & 1]);
+    }
+  };
+  auto slot = [&](auto uc, auto sc) {
+    constexpr int U = decltype(uc)::value, S = decltype(sc)::value, V = U ^ 1;
+    const unsigned from = U == 0 ? at : next;  // of unit N + 1
+    if constexpr (S < SUMS) {
+      add(Int<S>{});
+      row_operand(Int<S>{}, Int<V>{}, from);
+      if constexpr (SUMS == 4) row_operand(Int<4 + S>{}, Int<V>{}, from);
+      if constexpr (KEYS && S < 4) begin_from(Int<S>{}, Int<V>{}, from);
+    } else {
+      product(Int<S - SUMS>{}, Int<V>{});
+      if constexpr (S - SUMS < SUMS) sum_operand(Int<S - SUMS>{}, uc);
+    }
+    if constexpr (U == 1 && S >= 1 && S < 6) load(Int<S - 1>{});
+    // numbers of P done before slot x, of dS (two slots later: dP is the last that the matrix pipe makes), and words packed: the sums of the last
+    // unit read the first four until slot SUMS / 2 - 1, the others until SUMS - 1
+    constexpr auto ps = [](int x) { return x * 16 / kSlots; };
+    constexpr auto dss = [](int x) { return x >= kSlots ? 16 : x < 2 ? 0 : (x - 2) * 16 / kSlots; };
+    constexpr auto words = [](int done, int x) { return x < SUMS / 2 ? 0 : x < SUMS ? (done / 2 < 4 ? done / 2 : 4) : done / 2; };
+    each<ps(S), ps(S + 1)>([&](auto e) {
+      constexpr int E = decltype(e)::value;
+      s[U][E] = __builtin_amdgcn_exp2f(s[U][E] * scale_log2);
+    });
+    each<dss(S), dss(S + 1)>([&](auto e) {
+      constexpr int E = decltype(e)::value;
+      dp[U][E] *= s[U][E];
+    });
+    if constexpr (KEYS)
+      each<words(ps(S), S), words(ps(S + 1), S + 1)>([&](auto w) {
+        constexpr int W = decltype(w)::value;
+        pw[W >> 2][W & 3] = pack_bf16(s[U][2 * W], s[U][2 * W + 1]);
+      });
+    each<words(dss(S), S), words(dss(S + 1), S + 1)>([&](auto w) {
+      constexpr int W = decltype(w)::value;
+      dw[W >> 2][W & 3] = pack_bf16(dp[U][2 * W], dp[U][2 * W + 1]);
+    });
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  each<0, 8>([&](auto i) { row_operand(i, Int<0>{}, at); });
+  if constexpr (KEYS) each<0, 4>([&](auto i) { begin_from(i, Int<0>{}, at); });
+  each<0, 8>([&](auto j) { product(j, Int<0>{}); });
+#pragma unroll
+  for (int i = 0; i < 8; ++i) op[i] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+#pragma unroll
+  for (int i = 0; i < 2; ++i) pw[i] = dw[i] = u32x4{0u, 0u, 0u, 0u};
+  __builtin_amdgcn_sched_barrier(0);
+  do {
+    each<0, kSlots>([&](auto x) { slot(Int<0>{}, x); });
+    land();
+    each<0, kSlots>([&](auto x) { slot(Int<1>{}, x); });
+    at = next;
+    next = at + kBuf == 3 * kBuf ? 0u : at + kBuf;
+    ++t;
+  } while (more(t));
+  each<0, SUMS>([&](auto i) { add(i); });
+  return t;
+}
+
+// Buffers of a workgroup's tiles.  Three let a wave read the next tile while others are still at the last one, as run() does; fp32 has no
+// room for three and does not run.
+template <typename T>
+constexpr int Buffers = sizeof(T) == 2 ? 3 : 2;
+
+// The tiles [t0, t1) in turn, of which the first two are on their way (`loads` loads of each wave for a tile).  plain(t) takes one tile; ahead(t, land) takes
+// none or more and returns the first that is left.  A tile is one barrier, behind which its successor has landed in every wave.
+template <typename T, typename Issue, typename Plain, typename Ahead>
+__device__ __forceinline__ void stream(int t0, int t1, int loads, Issue&& issue, Plain&& plain, Ahead&& ahead) {
+  auto land = []() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    __syncthreads();
+  };
+  if (t0 + 1 < t1) {
+    if (loads == 4) __builtin_amdgcn_s_waitcnt(0x0f74);
+    else if (loads == 5) __builtin_amdgcn_s_waitcnt(0x0f75);
+    else if (loads == 8) __builtin_amdgcn_s_waitcnt(0x0f78);
+    else __builtin_amdgcn_s_waitcnt(0x0f70);
+  } else {
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+  }
+  __syncthreads();
+  for (int t = t0; t < t1; ++t) {
+    t = ahead(t, land);
+    if (t >= t1) break;
+    if constexpr (Buffers<T> == 2) plain(t);
+    land();
+    if (t + 2 < t1) issue(t + 2);
+    if constexpr (Buffers<T> == 3) plain(t);  // behind the barrier: the tile after next goes where the last one was
+  }
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // nothing is on its way into LDS any more
+}
+
+// dQ of 32 queries for each of four waves.  smem: K, V of each buffer.
 template <typename T>
 __device__ __forceinline__ void query_rows(const BwdArgs& a, int64_t block, int64_t blocks, unsigned char* smem) {
   typedef Ops<T> P;
-  constexpr int R = kParts<T>, WAVES = 4;
-  constexpr int kTileBytes = kTile * P::kRow;
+  constexpr int WAVES = 4, kBuffers = Buffers<T>;
+  constexpr int kTileBytes = kTile * P::kRow, kBuf = 2 * kTileBytes;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, g = lane >> 5;
@@ -89,7 +261,7 @@ __device__ __forceinline__ void query_rows(const BwdArgs& a, int64_t block, int6
   const int split = static_cast<int>(unit % a.q_splits);
   const int h = static_cast<int>(unit / a.q_splits / a.row_tiles);
   const int rt = a.row_tiles - 1 - static_cast<int>(unit / a.q_splits % a.row_tiles);
-  const int i0 = rt * 32 * R * WAVES, i1 = min(i0 + 32 * R * WAVES, a.seen.n_q);
+  const int i0 = rt * kOwnRows, i1 = min(i0 + kOwnRows, a.seen.n_q);
   const Tiles tiles = tiles_of(a.seen, i0, i1);
   const int t0 = static_cast<int>(int64_t(tiles.count) * split / a.q_splits), t1 = static_cast<int>(int64_t(tiles.count) * (split + 1) / a.q_splits);
   const unsigned char* const qh = a.q.p + h * a.q.head;
@@ -98,133 +270,140 @@ __device__ __forceinline__ void query_rows(const BwdArgs& a, int64_t block, int6
   const int64_t row0 = int64_t(h) * a.seen.n_q;
   const unsigned lds = lds_address(smem);
   const TileLoad<T, WAVES> k_load(a.k.token, wave, lane), v_load(a.v.token, wave, lane);
-  auto issue = [&](int t, int buf) {
+  auto place = [&](int t) { return static_cast<unsigned>((t - t0) % kBuffers) * kBuf; };
+  auto issue = [&](int t) {
     const int key = tiles.key(t);
-    k_load.all(kh, a.seen.n_k, key, lds + buf * 2 * kTileBytes);
-    v_load.all(vh, a.seen.n_k, key, lds + (buf * 2 + 1) * kTileBytes);
+    k_load.all(kh, a.seen.n_k, key, lds + place(t));
+    v_load.all(vh, a.seen.n_k, key, lds + place(t) + kTileBytes);
   };
-  if (t0 < t1) issue(t0, 0);
+  if (t0 < t1) issue(t0);
+  if (t0 + 1 < t1) issue(t0 + 1);
 
-  const int w0 = i0 + wave * 32 * R, w1 = min(w0 + 32 * R, a.seen.n_q);
+  const int w0 = i0 + wave * 32, w1 = min(w0 + 32, a.seen.n_q);
   const bool none = w0 >= a.seen.n_q;
-  typename P::A qf[R][P::kSteps], df[R][P::kSteps];
-  int lo[R], hi[R], lo_min = 0, hi_min = 0, lo_max = 0, hi_max = 0;
-  float from[R], D[R];
-#pragma unroll
-  for (int b = 0; b < R; ++b) {
-    const int i = min(w0 + 32 * b + n, a.seen.n_q - 1);
-    P::row(qh + i * a.q.token, g, qf[b]);
-    P::row(a.dout + (row0 + i) * P::kRow, g, df[b]);
-    a.seen.range(i, lo[b], hi[b]);
+  typename P::A qf[P::kSteps], df[P::kSteps];
+  int lo, hi, lo_min = 0, hi_min = 0, lo_max = 0, hi_max = 0;
+  f32x16 from, D;  // what S and dP begin with
+  {
+    const int i = min(w0 + n, a.seen.n_q - 1);
+    P::row(qh + i * a.q.token, g, qf);
+    P::row(a.dout + (row0 + i) * P::kRow, g, df);
+    a.seen.range(i, lo, hi);
     const float* const st = a.stats + int64_t(h) * 2 * a.stat_rows + i;
-    from[b] = st[0] * a.scale_log2;
-    D[b] = st[a.stat_rows];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      from[e] = st[0];
+      D[e] = st[a.stat_rows];
+    }
   }
   if (!none) {
     a.seen.range(w0, lo_min, hi_min);
     a.seen.range(w1 - 1, lo_max, hi_max);
   }
+  auto seen_by_none = [&](int key) { return none || key >= hi_max || (key + kTile <= lo_min && key >= a.seen.sinks); };
+  auto seen_by_all = [&](int key) {
+    return !none && key + kTile <= hi_min && (key >= lo_max || key + kTile <= a.seen.sinks || a.seen.sinks >= lo_max);
+  };
 
-  f32x16 dq[2][R];  // [dimensions][queries]
-#pragma unroll
-  for (int b = 0; b < R; ++b) {
-    clear(dq[0][b]);
-    clear(dq[1][b]);
-  }
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
-    if (t + 1 < t1) {
-      issue(t + 1, buf ^ 1);
-      constexpr int kInFlight = 2 * kTileBytes / 1024 / WAVES;
-      __builtin_amdgcn_s_waitcnt((kInFlight & 15) | (kInFlight >> 4 << 14) | 0x0f70);  // this tile's have landed
-    } else {
-      __builtin_amdgcn_s_waitcnt(0x0f70);
-    }
-    __syncthreads();
+  f32x16 dq[2];  // [dimensions], queries in the columns
+  clear(dq[0]);
+  clear(dq[1]);
+  auto plain = [&](int t) {
+    const int lane = fresh_lane(), n = lane & 31, g = lane >> 5;  // (addresses are not kept in registers between tiles)
     const int key = tiles.key(t);
-    const bool seen_by_none = none || key >= hi_max || (key + kTile <= lo_min && key >= a.seen.sinks);
-    const bool seen_by_all = key + kTile <= hi_min && (key >= lo_max || key + kTile <= a.seen.sinks || a.seen.sinks >= lo_max);
-    if (!seen_by_none) {
-      const unsigned char* const kt = smem + buf * 2 * kTileBytes;
-      const unsigned char* const vt = kt + kTileBytes;
+    const bool all = seen_by_all(key);
+    const unsigned char* const kt = smem + place(t);
+    const unsigned char* const vt = kt + kTileBytes;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        typename P::A w[R][P::kCols];
-        {
-          typename P::A ka[P::kSteps], va[P::kSteps];
-          P::rows(kt, 32 * u + n, g, ka);
-          P::rows(vt, 32 * u + n, g, va);
+    for (int u = 0; u < 2; ++u) {
+      typename P::A w[P::kCols];
+      {
+        typename P::A ka[P::kSteps], va[P::kSteps];
+        P::rows(kt, 32 * u + n, g, ka);
+        P::rows(vt, 32 * u + n, g, va);
+        f32x16 s = from, dp = D;
 #pragma unroll
-          for (int b = 0; b < R; ++b) {
-            f32x16 s, dp;
-            clear(s);
-            clear(dp);
+        for (int c = 0; c < P::kSteps; ++c) {
+          s = P::product(ka[c], qf[c], s);
+          dp = P::product(va[c], df[c], dp);
+        }
 #pragma unroll
-            for (int c = 0; c < P::kSteps; ++c) {
-              s = P::product(ka[c], qf[b][c], s);
-              dp = P::product(va[c], df[b][c], dp);
-            }
+        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * a.scale_log2) * dp[i];
+        if (!all) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.scale_log2, from[b])) * (dp[i] + D[b]);
-            if (!seen_by_all) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const int j = key + 32 * u + 8 * (i >> 2) + 4 * g + (i & 3);
-                s[i] = j < hi[b] && (j >= lo[b] || j < a.seen.sinks) ? s[i] : 0.f;
-              }
-            }
-            P::round(s, w[b]);
+          for (int i = 0; i < 16; ++i) {
+            const int j = key + 32 * u + 8 * (i >> 2) + 4 * g + (i & 3);
+            s[i] = j < hi && (j >= lo || j < a.seen.sinks) ? s[i] : 0.f;
           }
         }
+        P::round(s, w);
+      }
 #pragma unroll
-        for (int db = 0; db < 2; ++db) {
-          typename P::A kc[P::kCols];
-          P::columns(kt, 32 * u, db, lane, kc);
+      for (int db = 0; db < 2; ++db) {
+        typename P::A kc[P::kCols];
+        P::columns(kt, 32 * u, db, lane, kc);
 #pragma unroll
-          for (int c = 0; c < P::kCols; ++c)
-#pragma unroll
-            for (int b = 0; b < R; ++b) dq[db][b] = P::product(kc[c], w[b][c], dq[db][b]);
-        }
+        for (int c = 0; c < P::kCols; ++c) dq[db] = P::product(kc[c], w[c], dq[db]);
       }
     }
-    __syncthreads();
-  }
+  };
+  stream<T>(t0, t1, 2 * TileLoad<T, WAVES>::kLoads, issue, [&](int t) {
+    if (!seen_by_none(tiles.key(t))) plain(t);
+  }, [&](int t, auto&& land) {
+    if constexpr (sizeof(T) == 2) {
+      i32x4 krsrc, vrsrc;
+      unsigned to;
+      f32x16 unused[2];
+      if (seen_by_all(tiles.key(t)))
+        t = run<4>(t, place(t), smem, a.scale_log2, qf, df, from, D, dq, unused, [&](int x) { return x < t1 && seen_by_all(tiles.key(x)); },
+                   [&]() {
+                     land();
+                     const int x = min(t + 2, t1 - 1);  // past the end: a load that nobody reads, in place of a branch
+                     krsrc = k_load.rsrc(kh, a.seen.n_k, tiles.key(x));
+                     vrsrc = v_load.rsrc(vh, a.seen.n_k, tiles.key(x));
+                     to = lds + place(t + 2);
+                     ++t;
+                   },
+                   [&](auto i) {
+                     constexpr int I = decltype(i)::value;
+                     if constexpr (I < 2) k_load.one(krsrc, i, to);
+                     else v_load.one(vrsrc, Int<I - 2>{}, to + kTileBytes);
+                   });
+    }
+    return t;
+  });
 
   if (none) return;  // (no barrier follows)
+  const int i = w0 + n;
+  const int64_t in_part = int64_t(split) * a.heads * a.seen.n_q + row0 + i;
+  bool bad = false;
 #pragma unroll
-  for (int b = 0; b < R; ++b) {
-    const int i = w0 + 32 * b + n;
-    const int64_t in_part = int64_t(split) * a.heads * a.seen.n_q + row0 + i;
-    bool bad = false;
+  for (int db = 0; db < 2; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      dq[db][e] *= a.scale;
+      bad = bad || !(fabsf(dq[db][e]) < INFINITY);
+    }
+  if (i < a.seen.n_q) {
 #pragma unroll
     for (int db = 0; db < 2; ++db)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        dq[db][b][e] *= a.scale;
-        bad = bad || !(fabsf(dq[db][b][e]) < INFINITY);
+      for (int r = 0; r < 4; ++r) {
+        const f32x16& x = dq[db];
+        const int d = db * 32 + 8 * r + 4 * g;
+        if (a.q_splits > 1) *reinterpret_cast<f32x4*>(a.part_q + in_part * 64 + d) = f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
+        else P::store4(a.dq + (row0 + i) * P::kRow, d, x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]);
       }
-    if (i < a.seen.n_q) {
-#pragma unroll
-      for (int db = 0; db < 2; ++db)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const f32x16& x = dq[db][b];
-          const int d = db * 32 + 8 * r + 4 * g;
-          if (a.q_splits > 1) *reinterpret_cast<f32x4*>(a.part_q + in_part * 64 + d) = f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]};
-          else P::store4(a.dq + (row0 + i) * P::kRow, d, x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]);
-        }
-    }
-    unsigned long long again = __ballot(bad && i < a.seen.n_q);
-    again = (again | again >> 32) & 0xffffffffull;
-    while (again != 0) {
-      const int e = __builtin_ctzll(again);
-      again &= again - 1;
-      const int row = w0 + 32 * b + e;
-      const float x = exact_query<T>(a, qh + row * a.q.token, a.dout + (row0 + row) * P::kRow, kh, vh, a.stats[int64_t(h) * 2 * a.stat_rows + row], __shfl(D[b], e), row, t0,
-                                     t1, tiles, lane);
-      if (a.q_splits > 1) a.part_q[(int64_t(split) * a.heads * a.seen.n_q + row0 + row) * 64 + lane] = x;
-      else P::store1(a.dq + (row0 + row) * P::kRow, lane, x);
-    }
+  }
+  unsigned long long again = __ballot(bad && i < a.seen.n_q);
+  again = (again | again >> 32) & 0xffffffffull;
+  while (again != 0) {
+    const int row = w0 + __builtin_ctzll(again);
+    again &= again - 1;
+    const float* const st = a.stats + int64_t(h) * 2 * a.stat_rows + row;
+    const float x = exact_query<T>(a, qh + row * a.q.token, a.dout + (row0 + row) * P::kRow, kh, vh, st[0], st[a.stat_rows], row, t0, t1, tiles, lane);
+    if (a.q_splits > 1) a.part_q[(int64_t(split) * a.heads * a.seen.n_q + row0 + row) * 64 + lane] = x;
+    else P::store1(a.dq + (row0 + row) * P::kRow, lane, x);
   }
 }
 
@@ -262,11 +441,11 @@ __device__ void exact_key(const BwdArgs& a, const unsigned char* k, const unsign
   dk *= a.scale;
 }
 
-// dK and dV of 32 keys for each of four waves.  smem: Q, dO and what their sums begin with of buffer 0, then of buffer 1.
+// dK and dV of 32 keys for each of four waves.  smem: Q, dO and what S and dP begin with, of each buffer.
 template <typename T>
 __device__ __forceinline__ void key_rows(const BwdArgs& a, int64_t block, int64_t blocks, unsigned char* smem) {
   typedef Ops<T> P;
-  constexpr int WAVES = 4;
+  constexpr int WAVES = 4, kBuffers = Buffers<T>;
   constexpr int kTileBytes = kTile * P::kRow, kBuf = 2 * kTileBytes + kStatBytes;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -279,7 +458,7 @@ __device__ __forceinline__ void key_rows(const BwdArgs& a, int64_t block, int64_
   const int split = static_cast<int>(unit % splits);
   const int hk = static_cast<int>(unit / splits / of_head);
   const int kt = static_cast<int>(unit / splits % of_head) + (sink ? 0 : a.sink_tiles);
-  const int j0 = kt * kKeyRows, j1 = min(j0 + kKeyRows, a.seen.n_k);
+  const int j0 = kt * kOwnRows, j1 = min(j0 + kOwnRows, a.seen.n_k);
   Sequence seq;
   {
     const Queries from = queries_of(a.seen, j0), to = queries_of(a.seen, j1 - 1);
@@ -293,16 +472,21 @@ __device__ __forceinline__ void key_rows(const BwdArgs& a, int64_t block, int64_
   const int h0 = hk * a.group;
   const unsigned lds = lds_address(smem);
   const TileLoad<T, WAVES> q_load(a.q.token, wave, lane), d_load(P::kRow, wave, lane);
-  auto issue = [&](int s, int buf) {
-    const int h = h0 + s / seq.per_head, i0 = (seq.first + s % seq.per_head) * kTile;
-    const unsigned at = lds + buf * kBuf;
-    q_load.all(a.q.p + h * a.q.head, a.seen.n_q, i0, at);
-    d_load.all(a.dout + int64_t(h) * a.seen.n_q * P::kRow, a.seen.n_q, i0, at + kTileBytes);
-    // every wave, so that all wait for the same number of loads: the same bytes to the same place, 256 of each kind
-    dma16<0>(make_rsrc(a.stats + int64_t(h) * 2 * a.stat_rows, a.stat_rows * 8u),
-             i0 * 4u + (lane < 16 ? lane * 16u : lane < 32 ? a.stat_rows * 4u + (lane - 16) * 16u : 1u << 30), 0u, at + 2 * kTileBytes);
+  auto place = [&](int s) { return static_cast<unsigned>((s - seq.begin) % kBuffers) * kBuf; };
+  auto row_of = [&](int s) { return (seq.first + s % seq.per_head) * kTile; };
+  const unsigned stat_offset = lane < 16 ? lane * 16u : lane < 32 ? a.stat_rows * 4u + (lane - 16) * 16u : 1u << 30;
+  auto stat_rsrc = [&](int h) { return make_rsrc(a.stats + int64_t(h) * 2 * a.stat_rows, a.stat_rows * 8u); };
+  // (every wave, so that all wait for the same number of loads: the same bytes to the same place, 256 of each kind)
+  auto load_stats = [&](i32x4 rsrc, int i0, unsigned to) { dma16<0>(rsrc, stat_offset, i0 * 4u, __builtin_amdgcn_readfirstlane(to + 2 * kTileBytes)); };
+  auto issue = [&](int s) {
+    const int h = h0 + s / seq.per_head, i0 = row_of(s);
+    const unsigned to = lds + place(s);
+    q_load.all(a.q.p + h * a.q.head, a.seen.n_q, i0, to);
+    d_load.all(a.dout + int64_t(h) * a.seen.n_q * P::kRow, a.seen.n_q, i0, to + kTileBytes);
+    load_stats(stat_rsrc(h), i0, to);
   };
-  if (seq.begin < seq.end) issue(seq.begin, 0);
+  if (seq.begin < seq.end) issue(seq.begin);
+  if (seq.begin + 1 < seq.end) issue(seq.begin + 1);
 
   // the wave's keys [w0, w1): rows past the end are computed as the last one and not stored
   const int w0 = j0 + wave * 32, w1 = min(w0 + 32, a.seen.n_k);
@@ -329,76 +513,97 @@ __device__ __forceinline__ void key_rows(const BwdArgs& a, int64_t block, int64_
     clear(dk[db]);
     clear(dv[db]);
   }
-  for (int s = seq.begin; s < seq.end; ++s) {
-    const int buf = (s - seq.begin) & 1;
-    if (s + 1 < seq.end) {
-      issue(s + 1, buf ^ 1);
-      constexpr int kInFlight = 2 * kTileBytes / 1024 / WAVES + 1;
-      __builtin_amdgcn_s_waitcnt((kInFlight & 15) | (kInFlight >> 4 << 14) | 0x0f70);  // this tile's have landed
-    } else {
-      __builtin_amdgcn_s_waitcnt(0x0f70);
-    }
-    __syncthreads();
-    const int i0 = (seq.first + s % seq.per_head) * kTile;
-    if (!none && i0 < some_last && i0 + kTile > head.first) {
-      const bool all = i0 >= tail.first && i0 + kTile <= all_last;
-      const unsigned char* const qt = smem + buf * kBuf;
-      const unsigned char* const dt = qt + kTileBytes;
-      const unsigned char* const st = dt + kTileBytes;
+  auto seen_by_all = [&](int i0) { return i0 >= tail.first && i0 + kTile <= all_last; };
+  auto plain = [&](int s) {
+    const int lane = fresh_lane(), n = lane & 31, g = lane >> 5;  // (addresses are not kept in registers between tiles)
+    const int i0 = row_of(s);
+    const bool all = seen_by_all(i0);
+    const unsigned char* const qt = smem + place(s);
+    const unsigned char* const dt = qt + kTileBytes;
+    const unsigned char* const st = dt + kTileBytes;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f32x16 p, ds;
+    for (int u = 0; u < 2; ++u) {
+      f32x16 p, ds;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const f32x4 x = *LDS_PTR(f32x4, st + (32 * u + 8 * r + 4 * g) * 4), y = *LDS_PTR(f32x4, st + 256 + (32 * u + 8 * r + 4 * g) * 4);
+      for (int r = 0; r < 4; ++r) {
+        const f32x4 x = *LDS_PTR(f32x4, st + (32 * u + 8 * r + 4 * g) * 4), y = *LDS_PTR(f32x4, st + 256 + (32 * u + 8 * r + 4 * g) * 4);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            p[4 * r + e] = x[e];
-            ds[4 * r + e] = y[e];
-          }
+        for (int e = 0; e < 4; ++e) {
+          p[4 * r + e] = x[e];
+          ds[4 * r + e] = y[e];
         }
-        {
-          typename P::A qa[P::kSteps], da[P::kSteps];
-          P::rows(qt, 32 * u + n, g, qa);
-          P::rows(dt, 32 * u + n, g, da);
+      }
+      {
+        typename P::A qa[P::kSteps], da[P::kSteps];
+        P::rows(qt, 32 * u + n, g, qa);
+        P::rows(dt, 32 * u + n, g, da);
 #pragma unroll
-          for (int c = 0; c < P::kSteps; ++c) {
-            p = P::product(qa[c], kf[c], p);
-            ds = P::product(da[c], vf[c], ds);
-          }
+        for (int c = 0; c < P::kSteps; ++c) {
+          p = P::product(qa[c], kf[c], p);
+          ds = P::product(da[c], vf[c], ds);
         }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(p[e] * a.scale_log2);
+        ds[e] *= p[e];
+      }
+      if (!all) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(p[e] * a.scale_log2);
-          ds[e] *= p[e];
+          const int i = i0 + 32 * u + 8 * (e >> 2) + 4 * g + (e & 3);
+          const bool sees = i >= see.first && i < see.last;
+          p[e] = sees ? p[e] : 0.f;
+          ds[e] = sees ? ds[e] : 0.f;
         }
-        if (!all) {
+      }
+      typename P::A pw[P::kCols], dw[P::kCols];
+      P::round(p, pw);
+      P::round(ds, dw);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int i = i0 + 32 * u + 8 * (e >> 2) + 4 * g + (e & 3);
-            const bool sees = i >= see.first && i < see.last;
-            p[e] = sees ? p[e] : 0.f;
-            ds[e] = sees ? ds[e] : 0.f;
-          }
-        }
-        typename P::A pw[P::kCols], dw[P::kCols];
-        P::round(p, pw);
-        P::round(ds, dw);
+      for (int db = 0; db < 2; ++db) {
+        typename P::A c0[P::kCols], c1[P::kCols];
+        P::columns(dt, 32 * u, db, lane, c0);
+        P::columns(qt, 32 * u, db, lane, c1);
 #pragma unroll
-        for (int db = 0; db < 2; ++db) {
-          typename P::A c0[P::kCols], c1[P::kCols];
-          P::columns(dt, 32 * u, db, lane, c0);
-          P::columns(qt, 32 * u, db, lane, c1);
-#pragma unroll
-          for (int c = 0; c < P::kCols; ++c) {
-            dv[db] = P::product(c0[c], pw[c], dv[db]);
-            dk[db] = P::product(c1[c], dw[c], dk[db]);
-          }
+        for (int c = 0; c < P::kCols; ++c) {
+          dv[db] = P::product(c0[c], pw[c], dv[db]);
+          dk[db] = P::product(c1[c], dw[c], dk[db]);
         }
       }
     }
-    __syncthreads();
-  }
+  };
+  stream<T>(seq.begin, seq.end, 2 * TileLoad<T, WAVES>::kLoads + 1, issue, [&](int s) {
+    const int i0 = row_of(s);
+    if (!none && i0 < some_last && i0 + kTile > head.first) plain(s);
+  }, [&](int s, auto&& land) {
+    if constexpr (sizeof(T) == 2) {
+      i32x4 qrsrc, drsrc, srsrc;
+      int i0;
+      unsigned to;
+      const f32x16 unused = {};
+      if (!none && seen_by_all(row_of(s)))
+        s = run<8>(s, place(s), smem, a.scale_log2, kf, vf, unused, unused, dv, dk, [&](int x) { return x < seq.end && seen_by_all(row_of(x)); },
+                   [&]() {
+                     land();
+                     const int x = min(s + 2, seq.end - 1);  // past the end: a load that nobody reads, in place of a branch
+                     const int h = h0 + x / seq.per_head;
+                     i0 = row_of(x);
+                     qrsrc = q_load.rsrc(a.q.p + h * a.q.head, a.seen.n_q, i0);
+                     drsrc = d_load.rsrc(a.dout + int64_t(h) * a.seen.n_q * P::kRow, a.seen.n_q, i0);
+                     srsrc = stat_rsrc(h);
+                     to = lds + place(s + 2);
+                     ++s;
+                   },
+                   [&](auto i) {
+                     constexpr int I = decltype(i)::value;
+                     if constexpr (I < 2) q_load.one(qrsrc, i, to);
+                     else if constexpr (I < 4) d_load.one(drsrc, Int<I - 2>{}, to + kTileBytes);
+                     else load_stats(srsrc, i0, to);
+                   });
+    }
+    return s;
+  });
 
   if (none) return;  // (no barrier follows)
   bool bad = false;
@@ -409,7 +614,7 @@ __device__ __forceinline__ void key_rows(const BwdArgs& a, int64_t block, int64_
       dk[db][e] *= a.scale;
       bad = bad || !(fabsf(dk[db][e]) < INFINITY) || !(fabsf(dv[db][e]) < INFINITY);
     }
-  const int sink_rows = min(a.sink_tiles * kKeyRows, a.seen.n_k);
+  const int sink_rows = min(a.sink_tiles * kOwnRows, a.seen.n_k);
   const int64_t out0 = int64_t(hk) * a.seen.n_k;
   // the place of key jj in the partial sums
   auto part = [&](int jj) {
@@ -495,7 +700,8 @@ __global__ __launch_bounds__(256) void window_sum_kernel(const float* __restrict
 
 // How a launch is cut up.  Workgroups of query rows as in the forward pass; workgroups of keys get their queries in parts where there are
 // too few of them, and those of the first tokens, which all queries see, in parts as long as the others' queries.
-void shape_of(BwdArgs& a, int rows) {  // rows of a workgroup of queries
+void shape_of(BwdArgs& a) {
+  const int rows = kOwnRows;
   const Seen& s = a.seen;
   a.stat_rows = static_cast<int>(ceil_div(s.n_q, kTile)) * kTile;
   a.row_tiles = static_cast<int>(ceil_div(s.n_q, rows));
@@ -509,16 +715,16 @@ void shape_of(BwdArgs& a, int rows) {  // rows of a workgroup of queries
     }
     a.q_splits = static_cast<int>(max(min(kPlaces / units, int64_t(most / 4)), int64_t(1)));
   }
-  a.key_tiles = static_cast<int>(ceil_div(s.n_k, kKeyRows));
+  a.key_tiles = static_cast<int>(ceil_div(s.n_k, kOwnRows));
   const int64_t all = ceil_div(s.n_q, kTile) * a.group;  // query tiles of a key that all see
   int64_t most = 0;                                      // and of one that is seen through the window
   for (int kt = 0; kt < a.key_tiles; ++kt) {
-    const Queries from = queries_of(s, kt * kKeyRows), to = queries_of(s, min((kt + 1) * kKeyRows, s.n_k) - 1);
-    if (kt * kKeyRows < s.sinks || to.last <= from.first) continue;
+    const Queries from = queries_of(s, kt * kOwnRows), to = queries_of(s, min((kt + 1) * kOwnRows, s.n_k) - 1);
+    if (kt * kOwnRows < s.sinks || to.last <= from.first) continue;
     const int64_t c = (ceil_div(to.last, kTile) - from.first / kTile) * a.group;
     most = c > most ? c : most;
   }
-  a.sink_tiles = static_cast<int>(ceil_div(s.sinks, kKeyRows));
+  a.sink_tiles = static_cast<int>(ceil_div(s.sinks, kOwnRows));
   const int64_t key_units = int64_t(a.key_tiles) * a.kv_heads;
   a.splits = key_units > 0 && key_units * 2 <= kPlaces ? static_cast<int>(max(min(kPlaces / key_units, most / 4), int64_t(1))) : 1;
   const int64_t part = max(most / a.splits, int64_t(16));
@@ -529,7 +735,7 @@ void shape_of(BwdArgs& a, int rows) {  // rows of a workgroup of queries
 size_t stats_bytes(const BwdArgs& a) { return static_cast<size_t>(a.heads) * a.stat_rows * 8; }
 size_t part_q_bytes(const BwdArgs& a) { return a.q_splits > 1 ? static_cast<size_t>(a.q_splits) * a.heads * a.seen.n_q * 256 : 0; }
 size_t part_kv_bytes(const BwdArgs& a, bool sink) {
-  const int64_t sink_rows = min(int64_t(a.sink_tiles) * kKeyRows, int64_t(a.seen.n_k));
+  const int64_t sink_rows = min(int64_t(a.sink_tiles) * kOwnRows, int64_t(a.seen.n_k));
   const int splits = sink ? a.sink_splits : a.splits;
   return splits > 1 ? static_cast<size_t>(splits) * a.kv_heads * (sink ? sink_rows : a.seen.n_k - sink_rows) * 512 : 0;
 }
@@ -545,7 +751,7 @@ int launch(const BwdArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(window_stats_kernel<T>, dim3(static_cast<unsigned>(ceil_div(q_rows, 32))), dim3(256), 0, s, a);
     if (int rc = check_hip(hipGetLastError(), what)) return rc;
   }
-  hipLaunchKernelGGL(window_bwd_kernel<T>, dim3(static_cast<unsigned>(q_units + k_units)), dim3(256), 2 * (2 * kTile * Ops<T>::kRow + kStatBytes), s, a,
+  hipLaunchKernelGGL(window_bwd_kernel<T>, dim3(static_cast<unsigned>(q_units + k_units)), dim3(256), Buffers<T> * (2 * kTile * Ops<T>::kRow + kStatBytes), s, a,
                      k_units);
   if (int rc = check_hip(hipGetLastError(), what)) return rc;
   if (a.q_splits > 1) {
@@ -553,7 +759,7 @@ int launch(const BwdArgs& a, hipStream_t s) {
                        a.q_splits, 0, a.seen.n_q, a.dq, nullptr);
     if (int rc = check_hip(hipGetLastError(), what)) return rc;
   }
-  const int64_t sink_rows = min(int64_t(a.sink_tiles) * kKeyRows, int64_t(a.seen.n_k));
+  const int64_t sink_rows = min(int64_t(a.sink_tiles) * kOwnRows, int64_t(a.seen.n_k));
   for (int x = 0; x < 2; ++x) {
     const int splits = x == 0 ? a.sink_splits : a.splits;
     const int64_t rows = x == 0 ? sink_rows : a.seen.n_k - sink_rows;
@@ -564,8 +770,6 @@ int launch(const BwdArgs& a, hipStream_t s) {
   }
   return BSGA_OK;
 }
-
-int rows_of(int dtype) { return 4 * 32 * (dtype == BSGA_BF16 ? kParts<__bf16> : kParts<float>); }
 
 }  // namespace
 }  // namespace bsga
@@ -582,7 +786,7 @@ size_t bsga_window_attn_bwd_workspace_bytes(int dtype, int heads, int kv_heads, 
   a.heads = heads;
   a.kv_heads = kv_heads;
   a.group = heads / kv_heads;
-  shape_of(a, rows_of(dtype));
+  shape_of(a);
   return stats_bytes(a) + part_q_bytes(a) + part_kv_bytes(a, true) + part_kv_bytes(a, false);
 }
 
@@ -623,7 +827,7 @@ int bsga_window_attn_bwd(const void* dout, const void* q, const void* k, const v
   a.group = heads / kv_heads;
   a.scale = softmax_scale;
   a.scale_log2 = softmax_scale * kLog2e;
-  shape_of(a, rows_of(dtype));
+  shape_of(a);
   const size_t need = stats_bytes(a) + part_q_bytes(a) + part_kv_bytes(a, true) + part_kv_bytes(a, false);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(BSGA_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace ? workspace_bytes : 0, need);
