@@ -200,10 +200,11 @@ struct TileLoad {
       offset[i] = static_cast<unsigned>(r * token) + ((pos ^ Ops<T>::swizzle(r)) << 4);
     }
   }
-  __device__ __forceinline__ i32x4 rsrc(const unsigned char* head, int n, int r0) const {
-    const int left = n - r0;
-    return make_rsrc(head + r0 * token, left > 0 ? static_cast<unsigned>((min(left, kTile) - 1) * token + kRow) : 0u);
+  // descriptor of a tile that starts at p, with `left` rows from there to the tensor's end
+  __device__ __forceinline__ i32x4 rsrc_at(const unsigned char* p, int left) const {
+    return make_rsrc(p, left > 0 ? static_cast<unsigned>(min(left, kTile) - 1) * static_cast<unsigned>(token) + kRow : 0u);
   }
+  __device__ __forceinline__ i32x4 rsrc(const unsigned char* head, int n, int r0) const { return rsrc_at(head + r0 * token, n - r0); }
   template <int I>
   __device__ __forceinline__ void one(i32x4 rsrc, std::integral_constant<int, I>, unsigned lds) const {
     if constexpr (I < kLoads) dma16<WAVES * I * 1024>(rsrc, offset[I], 0u, __builtin_amdgcn_readfirstlane(lds + wave_lds));

@@ -186,11 +186,15 @@ __device__ __forceinline__ int run(int t, unsigned at, const unsigned char* smem
     if constexpr (KEYS)
       each<words(ps(S), S), words(ps(S + 1), S + 1)>([&](auto w) {
         constexpr int W = decltype(w)::value;
-        pw[W >> 2][W & 3] = pack_bf16(s[U][2 * W], s[U][2 * W + 1]);
+        unsigned x = pack_bf16(s[U][2 * W], s[U][2 * W + 1]);
+        asm volatile("" : "+v"(x));  // here, and not where it is used
+        pw[W >> 2][W & 3] = x;
       });
     each<words(dss(S), S), words(dss(S + 1), S + 1)>([&](auto w) {
       constexpr int W = decltype(w)::value;
-      dw[W >> 2][W & 3] = pack_bf16(dp[U][2 * W], dp[U][2 * W + 1]);
+      unsigned x = pack_bf16(dp[U][2 * W], dp[U][2 * W + 1]);
+      asm volatile("" : "+v"(x));
+      dw[W >> 2][W & 3] = x;
     });
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -351,24 +355,41 @@ __device__ __forceinline__ void query_rows(const BwdArgs& a, int64_t block, int6
     if (!seen_by_none(tiles.key(t))) plain(t);
   }, [&](int t, auto&& land) {
     if constexpr (sizeof(T) == 2) {
+      if (!seen_by_all(tiles.key(t))) return t;
+      // the keys of this tile, the next and the one after; and the places of the last in memory and in LDS.  Past the end: loads that nobody reads
+      int key = tiles.key(t), key1 = tiles.key(t + 1), key2 = tiles.key(t + 2);
+      const int jump = tiles.first > t + 2 ? tiles.first * kTile : -1, behind = tiles.start * kTile;  // where the window's tiles follow the first tokens'
+      const unsigned char *kp = kh + key2 * a.k.token, *vp = vh + key2 * a.v.token;
+      const int64_t k_step = kTile * a.k.token, v_step = kTile * a.v.token;
+      unsigned to = lds + place(t + 2);
       i32x4 krsrc, vrsrc;
-      unsigned to;
       f32x16 unused[2];
-      if (seen_by_all(tiles.key(t)))
-        t = run<4>(t, place(t), smem, a.scale_log2, qf, df, from, D, dq, unused, [&](int x) { return x < t1 && seen_by_all(tiles.key(x)); },
-                   [&]() {
-                     land();
-                     const int x = min(t + 2, t1 - 1);  // past the end: a load that nobody reads, in place of a branch
-                     krsrc = k_load.rsrc(kh, a.seen.n_k, tiles.key(x));
-                     vrsrc = v_load.rsrc(vh, a.seen.n_k, tiles.key(x));
-                     to = lds + place(t + 2);
-                     ++t;
-                   },
-                   [&](auto i) {
-                     constexpr int I = decltype(i)::value;
-                     if constexpr (I < 2) k_load.one(krsrc, i, to);
-                     else v_load.one(vrsrc, Int<I - 2>{}, to + kTileBytes);
-                   });
+      t = run<4>(t, place(t), smem, a.scale_log2, qf, df, from, D, dq, unused, [&](int x) { return x < t1 && seen_by_all(key); },
+                 [&]() {
+                   land();
+                   krsrc = k_load.rsrc_at(kp, a.seen.n_k - key2);
+                   vrsrc = v_load.rsrc_at(vp, a.seen.n_k - key2);
+                 },
+                 [&](auto i) {
+                   constexpr int I = decltype(i)::value;
+                   if constexpr (I < 2) {
+                     k_load.one(krsrc, i, to);
+                   } else if constexpr (I < 4) {
+                     v_load.one(vrsrc, Int<I - 2>{}, to + kTileBytes);
+                   } else {  // on to the next
+                     to = to + kBuf == lds + kBuffers * kBuf ? lds : to + kBuf;
+                     key = key1;
+                     key1 = key2;
+                     key2 += kTile;
+                     kp += k_step;
+                     vp += v_step;
+                     if (key2 == jump) {
+                       key2 = behind;
+                       kp = kh + key2 * a.k.token;
+                       vp = vh + key2 * a.v.token;
+                     }
+                   }
+                 });
     }
     return t;
   });
@@ -578,29 +599,51 @@ __device__ __forceinline__ void key_rows(const BwdArgs& a, int64_t block, int64_
     if (!none && i0 < some_last && i0 + kTile > head.first) plain(s);
   }, [&](int s, auto&& land) {
     if constexpr (sizeof(T) == 2) {
-      i32x4 qrsrc, drsrc, srsrc;
-      int i0;
-      unsigned to;
+      if (none || !seen_by_all(row_of(s))) return s;
+      // as above: the first queries of three tiles, and of the last of them its number in its head and its place
+      int i0 = row_of(s), i1 = row_of(s + 1), i2 = row_of(s + 2), of_head = (s + 2) % seq.per_head;
+      const int h = min(h0 + (s + 2) / seq.per_head, a.heads - 1);
+      const unsigned char* qp = a.q.p + h * a.q.head + i2 * a.q.token;
+      const unsigned char* dp = a.dout + (int64_t(h) * a.seen.n_q + i2) * P::kRow;
+      const float* sp = a.stats + int64_t(h) * 2 * a.stat_rows;
+      const int64_t q_step = kTile * a.q.token;
+      const int64_t q_turn = a.q.head - (seq.per_head - 1) * q_step;  // from the last tile of a head to the first of the next
+      const int64_t d_turn = (int64_t(a.seen.n_q) - (seq.per_head - 1) * kTile) * P::kRow;
+      int heads_left = a.heads - 1 - h;  // past the last one: the last one again, loads that nobody reads
+      unsigned to = lds + place(s + 2);
+      i32x4 qrsrc, drsrc;
       const f32x16 unused = {};
-      if (!none && seen_by_all(row_of(s)))
-        s = run<8>(s, place(s), smem, a.scale_log2, kf, vf, unused, unused, dv, dk, [&](int x) { return x < seq.end && seen_by_all(row_of(x)); },
-                   [&]() {
-                     land();
-                     const int x = min(s + 2, seq.end - 1);  // past the end: a load that nobody reads, in place of a branch
-                     const int h = h0 + x / seq.per_head;
-                     i0 = row_of(x);
-                     qrsrc = q_load.rsrc(a.q.p + h * a.q.head, a.seen.n_q, i0);
-                     drsrc = d_load.rsrc(a.dout + int64_t(h) * a.seen.n_q * P::kRow, a.seen.n_q, i0);
-                     srsrc = stat_rsrc(h);
-                     to = lds + place(s + 2);
-                     ++s;
-                   },
-                   [&](auto i) {
-                     constexpr int I = decltype(i)::value;
-                     if constexpr (I < 2) q_load.one(qrsrc, i, to);
-                     else if constexpr (I < 4) d_load.one(drsrc, Int<I - 2>{}, to + kTileBytes);
-                     else load_stats(srsrc, i0, to);
-                   });
+      s = run<8>(s, place(s), smem, a.scale_log2, kf, vf, unused, unused, dv, dk, [&](int x) { return x < seq.end && seen_by_all(i0); },
+                 [&]() {
+                   land();
+                   qrsrc = q_load.rsrc_at(qp, a.seen.n_q - i2);
+                   drsrc = d_load.rsrc_at(dp, a.seen.n_q - i2);
+                 },
+                 [&](auto i) {
+                   constexpr int I = decltype(i)::value;
+                   if constexpr (I < 2) {
+                     q_load.one(qrsrc, i, to);
+                   } else if constexpr (I < 4) {
+                     d_load.one(drsrc, Int<I - 2>{}, to + kTileBytes);
+                   } else {
+                     load_stats(make_rsrc(sp, a.stat_rows * 8u), i2, to);
+                     to = to + kBuf == lds + kBuffers * kBuf ? lds : to + kBuf;
+                     i0 = i1;
+                     i1 = i2;
+                     if (++of_head == seq.per_head) {
+                       of_head = 0;
+                       i2 = seq.first * kTile;
+                       qp += heads_left > 0 ? q_turn : q_turn - a.q.head;
+                       dp += heads_left > 0 ? d_turn : d_turn - int64_t(a.seen.n_q) * P::kRow;
+                       sp += heads_left > 0 ? 2 * a.stat_rows : 0;
+                       --heads_left;
+                     } else {
+                       i2 += kTile;
+                       qp += q_step;
+                       dp += kTile * P::kRow;
+                     }
+                   }
+                 });
     }
     return s;
   });
