@@ -283,18 +283,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(const PagedArgs a
   }
 }
 
-// Keys of a workgroup.  More workgroups than the chip holds at once (512) even out sequences of unequal length; each wave should have a few
-// pieces, and the stretch's page numbers have to fit.  The host knows the most that a sequence can see, not the lengths.
+// Keys of a workgroup.  The chip holds 512, and 300 with 64 KB on their way each draw what the memory gives; a sequence's stretches cost a second
+// kernel, and each wave should have a few pieces.  Measured, us, for at least 512 / 1024 / 2048 / 4096 workgroups: one sequence of 10,992 keys and 16
+// key heads 17.2 / 18.3 / 20.3 / 17.8; two of 412,200 and 312,300 509 / 485 / 493 / 498; 96 of up to 4,100 keys and 4 key heads 62 (no
+// stretches) / 75 / 68 / 71.  The host knows the most that a sequence can see, not its length: one long sequence among short ones must not be left to one
+// workgroup (4,608 keys take one about 30 us), and the workgroups that find nothing to do have to stay few.
 void shape_of(PagedArgs& a, int keys_of_piece) {
   int64_t most = int64_t(a.table_width) * a.page;
   if (a.window > 0) most = min(most, int64_t(a.window) * a.frame + a.sinks);
+  most = max(most, int64_t(1));
   const int64_t units = int64_t(a.batch) * a.kv_heads * a.head_blocks;
   const int64_t step = kWaves * keys_of_piece;
-  int64_t stretch = ceil_div(most, max(int64_t(2048) / units, int64_t(1)));
-  stretch = ceil_div(max(stretch, 2 * step), step) * step;
+  int64_t splits = max(int64_t(units > 256 || most * units < 512 * 1024 ? 512 : 1024) / units, int64_t(1));
+  if (units > 256) splits = max(splits, min(ceil_div(most, 4608), int64_t(4096) / units));
+  const int64_t stretch = ceil_div(max(ceil_div(most, splits), 2 * step), step) * step;
   const int64_t fits = int64_t(kTable - 4) * a.page / step * step;
-  a.stretch = static_cast<int>(min(min(stretch, fits), ceil_div(max(most, int64_t(1)), step) * step));
-  a.splits = static_cast<int>(max(ceil_div(most, a.stretch), int64_t(1)));
+  a.stretch = static_cast<int>(min(min(stretch, fits), ceil_div(most, step) * step));
+  a.splits = static_cast<int>(ceil_div(most, a.stretch));
 }
 
 size_t part_bytes(const PagedArgs& a) { return a.splits > 1 ? static_cast<size_t>(a.splits) * a.batch * a.heads * 65 * sizeof(float) : 0; }

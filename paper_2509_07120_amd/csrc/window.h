@@ -269,52 +269,56 @@ inline int check_view(const char* fn, const char* name, const void* p, int64_t t
   return BSGA_OK;
 }
 
-// Parts of a row's keys together: out = sum_s exp(lse_s - lse) part_s.  A row takes GROUPS groups of sixteen lanes, each every GROUPS-th part.
-template <typename T, int GROUPS>
+// Parts of a row's keys together: out = sum_s exp(lse_s - lse) part_s, a part that saw nothing (lse -inf) may hold anything.  Few parts: sixteen lanes to a
+// row.  Many (WIDE): a workgroup to a row, so that the loads of all parts are on their way together; 43 parts of 16 rows 6.7 -> FIGURE us.
+template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, const float* __restrict__ part_lse, int64_t rows, int splits,
                                                    unsigned char* __restrict__ out, float* __restrict__ lse) {
-  constexpr int kRows = 16 / GROUPS;  // of a workgroup
   __shared__ f32x4 sums[16][16];
-  __shared__ float total[16];
-  const int which = threadIdx.x >> 4, group = which % GROUPS, d = (threadIdx.x & 15) * 4;
-  const int64_t row = int64_t(blockIdx.x) * kRows + which / GROUPS;
-  const bool live = row < rows;
+  __shared__ float total[16], tops[4];
+  const int group = threadIdx.x >> 4, d = (threadIdx.x & 15) * 4;
+  const int64_t row = WIDE ? blockIdx.x : int64_t(blockIdx.x) * 16 + group;
+  if (!WIDE && row >= rows) return;
+  // the largest lse, NaN if one is
   float top = -INFINITY;
   bool nan = false;
-  if (live)
-#pragma unroll 4
-    for (int s = 0; s < splits; ++s) {
-      const float x = part_lse[s * rows + row];
-      top = fmaxf(top, x);
-      nan = nan || x != x;
-    }
+  for (int s = WIDE ? threadIdx.x : 0; s < splits; s += WIDE ? 256 : 1) {
+    const float x = part_lse[s * rows + row];
+    top = fmaxf(top, x);
+    nan = nan || x != x;
+  }
+  if constexpr (WIDE) {
+    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    nan = __syncthreads_or(nan);
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  }
   if (nan) top = NAN;
   float sum = 0.f;
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  if (live && top != -INFINITY)
+  if (top != -INFINITY)
 #pragma unroll 4
-    for (int s = group; s < splits; s += GROUPS) {
+    for (int s = WIDE ? group : 0; s < splits; s += WIDE ? 16 : 1) {
       const float from = part_lse[s * rows + row];
       const f32x4 x = *reinterpret_cast<const f32x4*>(part + (s * rows + row) * 64 + d);
       const float w = from == -INFINITY ? 0.f : exp2f((from - top) * kLog2e);
       sum += w;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] += from == -INFINITY ? 0.f : w * x[e];  // (a part that saw nothing may hold anything)
+      for (int e = 0; e < 4; ++e) y[e] += from == -INFINITY ? 0.f : w * x[e];
     }
-  if constexpr (GROUPS > 1) {
-    sums[which][threadIdx.x & 15] = y;
-    if (d == 0) total[which] = sum;
+  if constexpr (WIDE) {
+    sums[group][threadIdx.x & 15] = y;
+    if (d == 0) total[group] = sum;
     __syncthreads();
     if (group != 0) return;
     sum = 0.f;
     y = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int s = 0; s < GROUPS; ++s) {
-      sum += total[which + s];
-      y += sums[which + s][threadIdx.x & 15];
+    for (int s = 0; s < 16; ++s) {
+      sum += total[s];
+      y += sums[s][threadIdx.x & 15];
     }
   }
-  if (!live) return;
   const float inv = top == -INFINITY ? 0.f : 1.f / sum;
   Ops<T>::store4(out + row * Ops<T>::kRow, d, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
   if (lse != nullptr && d == 0) lse[row] = top == -INFINITY ? -INFINITY : top + log2f(sum) * kLn2;
@@ -323,9 +327,9 @@ __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ par
 template <typename T>
 int launch_join(const float* part, const float* part_lse, int64_t rows, int splits, unsigned char* out, float* lse, hipStream_t s) {
   if (splits > 8)
-    hipLaunchKernelGGL((join_kernel<T, 16>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, s, part, part_lse, rows, splits, out, lse);
+    hipLaunchKernelGGL((join_kernel<T, true>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, s, part, part_lse, rows, splits, out, lse);
   else
-    hipLaunchKernelGGL((join_kernel<T, 1>), dim3(static_cast<unsigned>(ceil_div(rows, 16))), dim3(256), 0, s, part, part_lse, rows, splits, out, lse);
+    hipLaunchKernelGGL((join_kernel<T, false>), dim3(static_cast<unsigned>(ceil_div(rows, 16))), dim3(256), 0, s, part, part_lse, rows, splits, out, lse);
   return check_hip(hipGetLastError(), "attention launch");
 }
 

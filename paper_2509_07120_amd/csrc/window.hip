@@ -422,23 +422,31 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
   }
 }
 
-// Waves of a workgroup and splits of its keys.  Four waves share tiles; a launch of few rows takes one to a workgroup, and where that leaves
-// CUs without work the keys are dealt out too, at least four tiles to each.
+// Waves of a workgroup and splits of its keys.  Four waves share tiles; a launch of few rows takes one to a workgroup.  The keys are dealt out
+// where that is worth a second kernel: the waves of a SIMD (1024 of them) share its pipes, so a launch takes as long as the SIMD with most waves, and one
+// that is alone on its SIMD is 1.4 times as slow as its share would be.  us a tile and wave as measured at 100 frames (fp32: 2 frames); parts cost
+// 528 bytes a row at 4 TB/s, and 5 us.  2,748 fp32 queries, 16 heads, window of 2,748: one part FIGURE1, two FIGURE2 us.
 void shape_of(const Seen& s, int rows, int heads, int& waves, int& splits) {  // rows of a wave
   waves = s.n_q > 2 * rows ? 4 : 1;
-  rows *= waves;
+  const double tile = rows == 64 ? 1.15 : 4.2;
+  const int64_t units = ceil_div(s.n_q, waves * rows) * heads;
   splits = 1;
-  const int64_t units = ceil_div(s.n_q, rows) * heads;
-  const int64_t places = waves == 4 ? kPlaces : 2 * kPlaces;
-  if (units * 2 > places) return;
+  if (units * waves > 8 * 1024) return;  // the last round is one of many
   int most = 0;  // the rows that see most are among the last ones, or, past the last key, the first
-  for (int64_t rt = 0, all = ceil_div(s.n_q, rows); rt < all; ++rt) {
-    const int i0 = static_cast<int>(rt * rows);
-    const int c = tiles_of(s, i0, min(i0 + rows, s.n_q)).count;
+  for (int64_t rt = 0, all = ceil_div(s.n_q, waves * rows); rt < all; ++rt) {
+    const int i0 = static_cast<int>(rt * waves * rows);
+    const int c = tiles_of(s, i0, min(i0 + waves * rows, s.n_q)).count;
     most = c > most ? c : most;
   }
-  splits = static_cast<int>(min(places / units, int64_t(most / 4)));
-  if (splits < 1) splits = 1;
+  double best = 0.0;
+  for (int n = 1; n == 1 || (n <= 64 && n <= most / 4); ++n) {
+    const int64_t on_simd = ceil_div(units * waves * n, 1024);
+    const double us = (on_simd == 1 ? 1.4 : static_cast<double>(on_simd)) * tile * static_cast<double>(ceil_div(most, n)) +
+                      (n > 1 ? 5.0 + static_cast<double>(heads) * s.n_q * n * 528 / 4e6 : 0.0);
+    if (n > 1 && us >= best) continue;
+    best = us;
+    splits = n;
+  }
 }
 
 size_t split_bytes(int heads, int64_t n_q, int splits) { return splits > 1 ? static_cast<size_t>(splits) * heads * n_q * 65 * sizeof(float) : 0; }
