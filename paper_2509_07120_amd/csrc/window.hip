@@ -422,26 +422,31 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
   }
 }
 
-// Waves of a workgroup and splits of its keys.  Four waves share tiles; a launch of few rows takes one to a workgroup.  The keys are dealt out
-// where that is worth a second kernel: the waves of a SIMD (1024 of them) share its pipes, so a launch takes as long as the SIMD with most waves, and one
-// that is alone on its SIMD is 1.4 times as slow as its share would be.  us a tile and wave as measured at 100 frames (fp32: 2 frames); parts cost
-// 528 bytes a row at 4 TB/s, and 5 us.  2,748 fp32 queries, 16 heads, window of 2,748: one part FIGURE1, two FIGURE2 us.
+// Waves of a workgroup and splits of its keys.  Four waves share tiles; a launch of few rows takes one to a workgroup.  The keys are dealt out where
+// that is worth a second kernel.  What a number of parts costs: the chip holds two workgroups of four waves to a CU (of one: four), a tile takes
+// such a pair twice 1.15 us (fp32 4.9) and one that is alone 1.4 times; whole rounds last as long as the mean workgroup, what is left over as the
+// longest; and parts cost 528 bytes a row at 4 TB/s and 5 us.  us for 1 / 3 / 5 / 8 parts with their join: one new frame (1,374 queries, 16 heads)
+// on 12 233 / 144 / 107 / 108, two frames in fp32 418 / 309 / 289 / 310.
 void shape_of(const Seen& s, int rows, int heads, int& waves, int& splits) {  // rows of a wave
+  const double tile = rows == 32 ? 4.9 : 1.15;
   waves = s.n_q > 2 * rows ? 4 : 1;
-  const double tile = rows == 64 ? 1.15 : 4.2;
-  const int64_t units = ceil_div(s.n_q, waves * rows) * heads;
+  rows *= waves;
   splits = 1;
-  if (units * waves > 8 * 1024) return;  // the last round is one of many
-  int most = 0;  // the rows that see most are among the last ones, or, past the last key, the first
-  for (int64_t rt = 0, all = ceil_div(s.n_q, waves * rows); rt < all; ++rt) {
-    const int i0 = static_cast<int>(rt * waves * rows);
-    const int c = tiles_of(s, i0, min(i0 + waves * rows, s.n_q)).count;
+  const int64_t units = ceil_div(s.n_q, rows) * heads, places = waves == 4 ? kPlaces : 2 * kPlaces;
+  if (units > 4 * places) return;  // the last round is one of many
+  int most = 0;
+  int64_t all = 0;
+  for (int i0 = 0; i0 < s.n_q; i0 += rows) {
+    const int c = tiles_of(s, i0, min(i0 + rows, s.n_q)).count;
     most = c > most ? c : most;
+    all += c;
   }
+  const double mean = static_cast<double>(all) / static_cast<double>(ceil_div(s.n_q, rows));
   double best = 0.0;
   for (int n = 1; n == 1 || (n <= 64 && n <= most / 4); ++n) {
-    const int64_t on_simd = ceil_div(units * waves * n, 1024);
-    const double us = (on_simd == 1 ? 1.4 : static_cast<double>(on_simd)) * tile * static_cast<double>(ceil_div(most, n)) +
+    const int64_t rounds = units * n / places, left = units * n - rounds * places;
+    const double full = waves == 4 ? 2.0 : 1.4;
+    const double us = tile * (static_cast<double>(rounds) * full * mean + (left == 0 ? 0.0 : left <= kPlaces / 2 ? 1.4 : full) * most) / n +
                       (n > 1 ? 5.0 + static_cast<double>(heads) * s.n_q * n * 528 / 4e6 : 0.0);
     if (n > 1 && us >= best) continue;
     best = us;
