@@ -634,37 +634,58 @@ def bsga_probe_mfma(operands: int, softmax_mix: int, iters: int = 20000, repeats
 NORMS = {None: 0, "none": 0, "rms": 1, "layer": 2}
 
 
-def _rows(t: torch.Tensor, name: str, like: torch.Tensor, n_tokens: int, heads: Optional[int] = None) -> Tuple[int, int]:
-    """Strides of the tokens and the heads of t [n_tokens, heads, 64], whose rows are contiguous."""
+def _wrong(t: torch.Tensor, name: str, dtype, at: int, beside: str) -> None:
+    """Says what is wrong with a tensor that is not a contiguous one of this type on this device."""
+    _require(t, name, dtype)
+    if t.get_device() != at:
+        raise ValueError(f"{name} must be on the same device as {beside}")
+
+
+# (calls on few rows are bound by the host: one condition for what is right, and the words for what is not elsewhere)
+def _rows(t: torch.Tensor, name: str, dtype, at: int, n_tokens: int, heads: Optional[int] = None) -> Tuple[int, int, int, int]:
+    """Strides of the tokens and the heads of t [n_tokens, heads, d], whose rows are contiguous, the heads and d."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if t.dtype != like.dtype:
-        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
-    if t.get_device() != like.get_device():
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.get_device() != at:
         raise ValueError(f"{name} must be on the same device as the other tensors")
-    shape, strides = t.shape, t.stride()
+    shape = t.shape
     if len(shape) != 3 or shape[0] != n_tokens or (heads is not None and shape[1] != heads):
         raise ValueError(f"{name} must be [n_tokens, heads, 64] with as many tokens and heads as the tensors beside it, got {tuple(shape)}")
-    if strides[2] != 1 and shape[2] > 1:
+    st, sh, one = t.stride()
+    if one != 1 and shape[2] > 1:
         raise ValueError(f"the rows of {name} must be contiguous")
-    return strides[0], strides[1]
+    return st, sh, shape[1], shape[2]
 
 
-def _norm_args(q, k, positions, q_weight, k_weight, q_bias, k_bias, norm):
-    """What both directions of the norm with the rotation check; the number of axes."""
-    if norm not in NORMS:
-        raise ValueError(f"norm must be 'rms', 'layer' or None, got {norm!r}")
-    for name, t, x in (("q_weight", q_weight, q), ("k_weight", k_weight, k), ("q_bias", q_bias, q), ("k_bias", k_bias, k)):
-        if t is not None:
-            _require(t, name, x.dtype)
-            if t.numel() != x.shape[2] or t.get_device() != x.get_device():
-                raise ValueError(f"{name} must be [{x.shape[2]}] on the same device as the tensors")
+def _norm_weight(t: Optional[torch.Tensor], name: str, dtype, at: int, d: int) -> Optional[int]:
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype or t.get_device() != at or not t.is_contiguous():
+        _wrong(t, name, dtype, at, "the tensors")
+    if t.numel() != d:
+        raise ValueError(f"{name} must be [{d}]")
+    return t.data_ptr()
+
+
+def _norm_positions(positions: Optional[torch.Tensor], at: int, n_tokens: int) -> Tuple[Optional[int], int]:
+    """Address and number of axes."""
     if positions is None:
-        return 0
-    _require(positions, "positions", torch.int32)
-    if positions.dim() not in (1, 2) or positions.shape[0] != q.shape[0] or positions.get_device() != q.get_device():
-        raise ValueError("positions must be [n_tokens] or [n_tokens, axes] on the same device as the tensors")
-    return 1 if positions.dim() == 1 else positions.shape[1]
+        return None, 0
+    if not positions.is_cuda or positions.dtype != torch.int32 or positions.get_device() != at or not positions.is_contiguous():
+        _wrong(positions, "positions", torch.int32, at, "the tensors")
+    shape = positions.shape
+    if len(shape) not in (1, 2) or shape[0] != n_tokens:
+        raise ValueError("positions must be [n_tokens] or [n_tokens, axes]")
+    return positions.data_ptr(), 1 if len(shape) == 1 else shape[1]
+
+
+def _norm_code(norm: Optional[str]) -> int:
+    code = NORMS.get(norm, -1)
+    if code < 0:
+        raise ValueError(f"norm must be 'rms', 'layer' or None, got {norm!r}")
+    return code
 
 
 def bsga_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: Optional[torch.Tensor] = None,
@@ -678,42 +699,43 @@ def bsga_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: Optional[torc
     its halves by the first and the second position.
     With slots (int32 [N]) keys and values go to these tokens of the caches [pages, Hkv, page, 64] instead (those outside are not
     written), and the caches are returned in their place."""
-    if not q.is_cuda:
-        raise ValueError("q must be a device tensor")
-    if q.dim() != 3:
-        raise ValueError("q must be [n_tokens, heads, 64]")
-    N, H, d = q.shape
+    dtype, at, N = q.dtype, q.get_device(), q.shape[0]
     code = _dtype_code(q)
-    qs = _rows(q, "q", q, N)
-    ks = _rows(k, "k", q, N)
-    K = k.shape[1]
-    vs = (0, 0) if v is None else _rows(v, "v", q, N, K)
-    if k.shape[2] != d or (v is not None and v.shape[2] != d):
+    qt, qh, H, d = _rows(q, "q", dtype, at, N)
+    kt, kh, K, kd = _rows(k, "k", dtype, at, N)
+    vt, vh, _, vd = (0, 0, K, d) if v is None else _rows(v, "v", dtype, at, N, K)
+    if kd != d or vd != d:
         raise ValueError("q, k and v must have the same head dimension")
-    axes = _norm_args(q, k, positions, q_weight, k_weight, q_bias, k_bias, norm)
-    q_out = torch.empty((H, N, d), dtype=q.dtype, device=q.device)
+    kind = _norm_code(norm)
+    qw, kw = _norm_weight(q_weight, "q_weight", dtype, at, d), _norm_weight(k_weight, "k_weight", dtype, at, d)
+    qb, kb = _norm_weight(q_bias, "q_bias", dtype, at, d), _norm_weight(k_bias, "k_bias", dtype, at, d)
+    where, axes = _norm_positions(positions, at, N)
+    q_out = q.new_empty((H, N, d))
     pages = page = 0
+    slot = None
     if slots is None:
         if k_cache is not None or v_cache is not None:
             raise ValueError("caches go with slots")
-        k_out = torch.empty((K, N, d), dtype=q.dtype, device=q.device)
-        v_out = None if v is None else torch.empty((K, N, d), dtype=q.dtype, device=q.device)
+        k_out = q.new_empty((K, N, d))
+        v_out = None if v is None else q.new_empty((K, N, d))
     else:
-        _require(slots, "slots", torch.int32)
-        if slots.numel() != N or slots.get_device() != q.get_device():
-            raise ValueError("slots must have one entry per token, on the same device as the tensors")
+        if not slots.is_cuda or slots.dtype != torch.int32 or slots.get_device() != at or not slots.is_contiguous():
+            _wrong(slots, "slots", torch.int32, at, "the tensors")
+        if slots.numel() != N:
+            raise ValueError("slots must have one entry per token")
         if k_cache is None or (v is None) != (v_cache is None):
             raise ValueError("slots need the cache of the keys, and of the values with v")
+        shape = k_cache.shape
         for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
             if t is not None:
-                _require(t, name, q.dtype)
-                if t.dim() != 4 or t.shape[1] != K or t.shape[3] != d or t.shape != k_cache.shape or t.get_device() != q.get_device():
-                    raise ValueError(f"{name} must be [pages, kv_heads, page, 64] on the same device as the tensors")
-        pages, page = k_cache.shape[0], k_cache.shape[2]
-        k_out, v_out = k_cache, v_cache
-    _check(lib.bsga_qk_norm_rope(_ptr(q), _ptr(k), _ptr(v), *qs, *ks, *vs, code, N, H, K, d, NORMS[norm], eps, _ptr(q_weight),
-                                 _ptr(q_bias), _ptr(k_weight), _ptr(k_bias), _ptr(positions), axes, base, _ptr(slots), pages, page,
-                                 _ptr(q_out), _ptr(k_out), _ptr(v_out), _stream(q)))
+                if not t.is_cuda or t.dtype != dtype or t.get_device() != at or not t.is_contiguous():
+                    _wrong(t, name, dtype, at, "the tensors")
+                if len(shape) != 4 or t.shape != shape or shape[1] != K or shape[3] != d:
+                    raise ValueError(f"{name} must be [pages, kv_heads, page, 64]")
+        pages, page = shape[0], shape[2]
+        k_out, v_out, slot = k_cache, v_cache, slots.data_ptr()
+    _check(lib.bsga_qk_norm_rope(q.data_ptr(), k.data_ptr(), _ptr(v), qt, qh, kt, kh, vt, vh, code, N, H, K, d, kind, eps, qw, qb, kw, kb, where, axes,
+                                 base, slot, pages, page, q_out.data_ptr(), k_out.data_ptr(), _ptr(v_out), _stream(q)))
     return q_out, k_out, v_out
 
 
@@ -726,38 +748,41 @@ def bsga_qk_norm_rope_bwd(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k
     rest is what it was given (the biases say only whether their gradients are wanted).  Returns the gradients of (q, k, v, q_weight, k_weight,
     q_bias, k_bias), None for what was not given; those of q, k and v lie beside each other in one [N, H + 2 Hkv, 64] (without dv
     [N, H + Hkv, 64]), as a projection's output does, those of weights and biases are float32."""
-    if not q.is_cuda:
-        raise ValueError("q must be a device tensor")
-    if q.dim() != 3:
-        raise ValueError("q must be [n_tokens, heads, 64]")
-    N, H, d = q.shape
+    dtype, at, N = q.dtype, q.get_device(), q.shape[0]
     code = _dtype_code(q)
-    qs = _rows(q, "q", q, N)
-    ks = _rows(k, "k", q, N)
-    K = k.shape[1]
-    if k.shape[2] != d:
+    qt, qh, H, d = _rows(q, "q", dtype, at, N)
+    kt, kh, K, kd = _rows(k, "k", dtype, at, N)
+    if kd != d:
         raise ValueError("q and k must have the same head dimension")
     for name, t, h in (("dq", dq, H), ("dk", dk, K), ("dv", dv, K)):
         if t is not None:
-            _require(t, name, q.dtype)
-            if tuple(t.shape) != (h, N, d) or t.get_device() != q.get_device():
-                raise ValueError(f"{name} must be {(h, N, d)} on the same device as q")
-    axes = _norm_args(q, k, positions, q_weight, k_weight, q_bias, k_bias, norm)
-    dx = torch.empty((N, H + (K if dv is None else 2 * K), d), dtype=q.dtype, device=q.device)
-    dq_in, dk_in, dv_in = dx[:, :H], dx[:, H:H + K], None if dv is None else dx[:, H + K:]
-    row = dx.stride(0)
-    wanted = any(t is not None for t in (q_weight, k_weight, q_bias, k_bias))
+            if not t.is_cuda or t.dtype != dtype or t.get_device() != at or not t.is_contiguous():
+                _wrong(t, name, dtype, at, "q")
+            if t.shape != (h, N, d):
+                raise ValueError(f"{name} must be {(h, N, d)}")
+    kind = _norm_code(norm)
+    qw, kw = _norm_weight(q_weight, "q_weight", dtype, at, d), _norm_weight(k_weight, "k_weight", dtype, at, d)
+    _norm_weight(q_bias, "q_bias", dtype, at, d), _norm_weight(k_bias, "k_bias", dtype, at, d)
+    where, axes = _norm_positions(positions, at, N)
+    parts = (H, K) if dv is None else (H, K, K)
+    dx = q.new_empty((N, sum(parts), d))
+    row, size = dx.stride(0), dx.element_size() * d
+    into = dx.data_ptr()  # (0 without tokens)
+    wanted = q_weight is not None or k_weight is not None or q_bias is not None or k_bias is not None
     dw = work = None
     nbytes = 0
     if wanted:
-        dw = torch.empty((2, 2, d), dtype=torch.float32, device=q.device)
         nbytes = lib.bsga_qk_norm_rope_bwd_workspace_bytes(N, H, K)
-        work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-    _check(lib.bsga_qk_norm_rope_bwd(_ptr(dq), _ptr(dk), _ptr(dv), _ptr(q), _ptr(k), *qs, *ks, code, N, H, K, d, NORMS[norm], eps,
-                                     _ptr(q_weight), _ptr(k_weight), _ptr(positions), axes, base, _ptr(dq_in), _ptr(dk_in), _ptr(dv_in),
-                                     row, d, row, d, row, d, _ptr(dw), _ptr(work), nbytes, _stream(q)))
-    of = [None if t is None else dw[x, y] for t, x, y in ((q_weight, 0, 0), (k_weight, 1, 0), (q_bias, 0, 1), (k_bias, 1, 1))]
-    return (dq_in, dk_in, dv_in, *of)
+        dw = q.new_empty((4, d), dtype=torch.float32)  # of q's weight and bias, then of k's
+        work = q.new_empty(nbytes, dtype=torch.uint8)
+    _check(lib.bsga_qk_norm_rope_bwd(dq.data_ptr(), dk.data_ptr(), _ptr(dv), q.data_ptr(), k.data_ptr(), qt, qh, kt, kh, code, N, H, K, d, kind, eps, qw,
+                                     kw, where, axes, base, into, into and into + H * size, None if dv is None else into and into + (H + K) * size, row, d, row,
+                                     d, row, d,
+                                     _ptr(dw), _ptr(work), nbytes, _stream(q)))
+    dq_in, dk_in, *rest = dx.split(parts, 1)
+    of = dw.unbind(0) if wanted else (None,) * 4
+    return (dq_in, dk_in, None if dv is None else rest[0], None if q_weight is None else of[0], None if k_weight is None else of[2],
+            None if q_bias is None else of[1], None if k_bias is None else of[3])
 
 
 def _head_rows(t: torch.Tensor, name: str, like: torch.Tensor) -> Tuple[int, int]:
@@ -778,8 +803,8 @@ def _window_args(q, k, v, window, sinks, frame, q_start, softmax_scale):
     """What both directions of the attention with a window check: strides, sizes and (q_start, frame, window, sinks)."""
     qs, ks, vs = _head_rows(q, "q", q), _head_rows(k, "k", q), _head_rows(v, "v", q)
     H, N, d = q.shape
-    K, M, _ = k.shape
-    if k.shape != v.shape or k.shape[2] != d:
+    K, M, kd = k.shape
+    if k.shape != v.shape or kd != d:
         raise ValueError("k and v must both be [kv_heads, n_k, head_dim]")
     if window is not None and window < 1:
         raise ValueError(f"window must be at least one frame, or None, got {window}")
@@ -798,16 +823,16 @@ def bsga_window_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: 
     code = _dtype_code(q)
     strides, H, K, N, M, d, seen, scale = _window_args(q, k, v, window, sinks, frame, q_start, softmax_scale)
     if out is None:
-        out = torch.empty((H, N, d), dtype=q.dtype, device=q.device)
+        out = q.new_empty((H, N, d))
     else:
         _require(out, "out", q.dtype)
         if tuple(out.shape) != (H, N, d) or out.get_device() != q.get_device():
             raise ValueError(f"out must be {(H, N, d)} on the same device as q")
-    lse = torch.empty((H, N), dtype=torch.float32, device=q.device) if return_lse else None
+    lse = q.new_empty((H, N), dtype=torch.float32) if return_lse else None
     if workspace is None:
         nbytes = lib.bsga_window_attn_workspace_bytes(code, H, N, M, *seen)
         if nbytes > 0:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+            workspace = q.new_empty(nbytes, dtype=torch.uint8)
     else:
         nbytes = workspace.numel() * workspace.element_size()
     _check(lib.bsga_window_attn(_ptr(q), _ptr(k), _ptr(v), *strides, code, H, K, N, M, d, scale, *seen, _ptr(out), _ptr(lse),
@@ -822,16 +847,16 @@ def bsga_window_attn_bwd(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v
     q, k, v and the same window."""
     code = _dtype_code(q)
     strides, H, K, N, M, d, seen, scale = _window_args(q, k, v, window, sinks, frame, q_start, softmax_scale)
+    at = q.get_device()
     for name, t, dtype, shape in (("dout", dout, q.dtype, (H, N, d)), ("out", out, q.dtype, (H, N, d)), ("lse", lse, torch.float32, (H, N))):
-        _require(t, name, dtype)
-        if tuple(t.shape) != shape or t.get_device() != q.get_device():
-            raise ValueError(f"{name} must be {shape} on the same device as q")
-    dq = torch.empty((H, N, d), dtype=q.dtype, device=q.device)
-    dk = torch.empty((K, M, d), dtype=q.dtype, device=q.device)
-    dv = torch.empty((K, M, d), dtype=q.dtype, device=q.device)
+        if not t.is_cuda or t.dtype != dtype or t.get_device() != at or not t.is_contiguous():
+            _wrong(t, name, dtype, at, "q")
+        if t.shape != shape:
+            raise ValueError(f"{name} must be {shape}")
+    dq, dk, dv = q.new_empty((H, N, d)), q.new_empty((K, M, d)), q.new_empty((K, M, d))
     if workspace is None:
         nbytes = lib.bsga_window_attn_bwd_workspace_bytes(code, H, K, N, M, *seen)
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes > 0 else None
+        workspace = q.new_empty(nbytes, dtype=torch.uint8) if nbytes > 0 else None
     else:
         nbytes = workspace.numel() * workspace.element_size()
     _check(lib.bsga_window_attn_bwd(_ptr(dout), _ptr(q), _ptr(k), _ptr(v), *strides, _ptr(out), _ptr(lse), code, H, K, N, M, d, scale, *seen,
@@ -854,25 +879,28 @@ def bsga_paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
         raise ValueError("q must be [batch, heads, 64] with contiguous rows")
     B, H, d = q.shape
     at = q.get_device()
+    dtype, shape = q.dtype, k_cache.shape
     for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        _require(t, name, q.dtype)
-        if t.dim() != 4 or t.shape[3] != d or t.shape != k_cache.shape or t.get_device() != at:
-            raise ValueError(f"{name} must be [pages, kv_heads, page, 64] on the same device as q")
+        if not t.is_cuda or t.dtype != dtype or t.get_device() != at or not t.is_contiguous():
+            _wrong(t, name, dtype, at, "q")
+        if len(shape) != 4 or t.shape != shape or shape[3] != d:
+            raise ValueError(f"{name} must be [pages, kv_heads, page, 64]")
     for name, t, dims in (("page_table", page_table, 2), ("lengths", lengths, 1)):
-        _require(t, name, torch.int32)
-        if t.dim() != dims or t.shape[0] != B or t.get_device() != at:
-            raise ValueError(f"{name} must have a row for each sequence, on the same device as q")
+        if not t.is_cuda or t.dtype != torch.int32 or t.get_device() != at or not t.is_contiguous():
+            _wrong(t, name, torch.int32, at, "q")
+        if len(t.shape) != dims or t.shape[0] != B:
+            raise ValueError(f"{name} must have a row for each sequence")
     if window is not None and window < 1:
         raise ValueError(f"window must be at least one frame, or None, got {window}")
-    pages, K, page, _ = k_cache.shape
+    pages, K, page, _ = shape
     width = page_table.shape[1]
     seen = (frame, 0 if window is None else window, sinks)
-    out = torch.empty((B, H, d), dtype=q.dtype, device=q.device)
-    lse = torch.empty((B, H), dtype=torch.float32, device=q.device) if return_lse else None
+    out = q.new_empty((B, H, d))
+    lse = q.new_empty((B, H), dtype=torch.float32) if return_lse else None
     if workspace is None:
         nbytes = lib.bsga_paged_attn_workspace_bytes(code, B, H, K, width, pages, page, *seen)
         if nbytes > 0:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+            workspace = q.new_empty(nbytes, dtype=torch.uint8)
     else:
         nbytes = workspace.numel() * workspace.element_size()
     _check(lib.bsga_paged_attn(_ptr(q), strides[0], strides[1], _ptr(k_cache), _ptr(v_cache), code, B, H, K, d, _ptr(page_table), width,

@@ -770,6 +770,8 @@ void shape_of(BwdArgs& a) {
   a.sink_tiles = static_cast<int>(ceil_div(s.sinks, kOwnRows));
   const int64_t key_units = int64_t(a.key_tiles) * a.kv_heads;
   a.splits = key_units > 0 && key_units * 2 <= kPlaces ? static_cast<int>(max(min(kPlaces / key_units, most / 4), int64_t(1))) : 1;
+  // launches of a few rounds end better with shorter workgroups: two frames in fp32 (704 workgroups) 943 us, queries' keys in two parts 854
+  if (a.q_splits == 1 && units + key_units < 3 * kPlaces && units + key_units >= kPlaces && tiles_of(s, max(s.n_q - rows, 0), s.n_q).count >= 16) a.q_splits = 2;
   const int64_t part = max(most / a.splits, int64_t(16));
   a.sink_splits = static_cast<int>(min(max(ceil_div(all, part), int64_t(1)), int64_t(64)));
   if (key_units > 4 * kPlaces && a.sink_tiles == a.key_tiles) a.sink_splits = 1;  // everything is seen from everywhere
