@@ -220,7 +220,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const NormRopeArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void norm_rope_bwd_kernel(const NormRopeArgs a) {
   __shared__ float sums[4][128];
   int h0, h1, group;
   const int kind = kind_of(a, blockIdx.y, h0, h1, group);

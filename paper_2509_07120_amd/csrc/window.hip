@@ -136,30 +136,36 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
     const bool all = seen_by_all(key);
     const unsigned char* const kt = smem + ((t - t0) & 1) * kBuf;
     const unsigned char* const vt = kt + kTileBytes;
+    constexpr int U = R == 1 ? 2 : 1;  // 32-key parts at a time: as many as registers allow, for fewer steps of the maximum
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      typename P::A ka[P::kSteps];
-      P::rows(kt, 32 * u + n, g, ka);
-      f32x16 s[R];
+    for (int u0 = 0; u0 < 2; u0 += U) {
+      f32x16 s[U][R];
 #pragma unroll
-      for (int b = 0; b < R; ++b) {
-        clear(s[b]);
+      for (int u = 0; u < U; ++u) {
+        typename P::A ka[P::kSteps];
+        P::rows(kt, 32 * (u0 + u) + n, g, ka);
 #pragma unroll
-        for (int c = 0; c < P::kSteps; ++c) s[b] = P::product(ka[c], qf[b][c], s[b]);
-        if (!all) {
+        for (int b = 0; b < R; ++b) {
+          clear(s[u][b]);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int j = key + 32 * u + 8 * (i >> 2) + 4 * g + (i & 3);
-            s[b][i] = j < hi[b] && (j >= lo[b] || j < a.seen.sinks) ? s[b][i] : -INFINITY;
+          for (int c = 0; c < P::kSteps; ++c) s[u][b] = P::product(ka[c], qf[b][c], s[u][b]);
+          if (!all) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int j = key + 32 * (u0 + u) + 8 * (i >> 2) + 4 * g + (i & 3);
+              s[u][b][i] = j < hi[b] && (j >= lo[b] || j < a.seen.sinks) ? s[u][b][i] : -INFINITY;
+            }
           }
         }
       }
-      typename P::A w[R][P::kCols];
+      typename P::A w[U][R][P::kCols];
 #pragma unroll
       for (int b = 0; b < R; ++b) {
-        float top = s[b][0];
+        float top = s[0][b][0];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[b][i]);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][b][i]);
         top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
         const bool raise = m[b] == -INFINITY ? top > -INFINITY : top > m[b] + kRaise;
         if (__any(raise)) {
@@ -174,21 +180,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
         }
         const float from = m[b] == -INFINITY ? 0.f : m[b];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], a.scale_log2, -from));
-          l[b] += s[b][i];
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            s[u][b][i] = __builtin_amdgcn_exp2f(fmaf(s[u][b][i], a.scale_log2, -from));
+            l[b] += s[u][b][i];
+          }
+          P::round(s[u][b], w[u][b]);
         }
-        P::round(s[b], w[b]);
       }
 #pragma unroll
-      for (int db = 0; db < 2; ++db) {
-        typename P::A va[P::kCols];
-        P::columns(vt, 32 * u, db, lane, va);
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int c = 0; c < P::kCols; ++c)
+        for (int db = 0; db < 2; ++db) {
+          typename P::A va[P::kCols];
+          P::columns(vt, 32 * (u0 + u), db, lane, va);
 #pragma unroll
-          for (int b = 0; b < R; ++b) o[db][b] = P::product(va[c], w[b][c], o[db][b]);
-      }
+          for (int c = 0; c < P::kCols; ++c)
+#pragma unroll
+            for (int b = 0; b < R; ++b) o[db][b] = P::product(va[c], w[u][b][c], o[db][b]);
+        }
     }
   };
 
