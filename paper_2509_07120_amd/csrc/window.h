@@ -55,10 +55,6 @@ struct View {
   int64_t token, head;
 };
 
-// 32-row parts of a wave's queries: more of them share the operands read from LDS, fp32 has no registers for two
-template <typename T>
-constexpr int kParts = sizeof(T) == 2 ? 2 : 1;
-
 template <typename T>
 struct Ops;
 

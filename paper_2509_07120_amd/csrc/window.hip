@@ -71,12 +71,11 @@ __device__ void exact_row(const WindowArgs& a, const unsigned char* q, const uns
 template <int N>
 using Int = std::integral_constant<int, N>;
 
-template <typename T, int WAVES>
+template <typename T, int WAVES, int R>  // R: 32-row parts of a wave's queries
 __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs a) {
   typedef Ops<T> P;
-  constexpr int R = kParts<T>;
   constexpr int kTileBytes = kTile * P::kRow, kBuf = 2 * kTileBytes;
-  constexpr bool kRuns = sizeof(T) == 2;  // tiles that all rows see go through run()
+  constexpr bool kRuns = sizeof(T) == 2 && R == 2;  // tiles that all rows see go through run()
   extern __shared__ __align__(16) unsigned char smem[];  // K, V of buffer 0, K, V of buffer 1
   __shared__ int flag;
   const int lane = threadIdx.x & 63;
@@ -433,18 +432,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
   }
 }
 
-// Waves of a workgroup and splits of its keys.  Four waves share tiles; a launch of few rows takes one to a workgroup.  The keys are dealt out where
-// that is worth a second kernel.  What a number of parts costs: the chip holds two workgroups of four waves to a CU (of one: four), a tile takes
-// such a pair twice 1.15 us (fp32 4.9) and one that is alone 1.4 times; whole rounds last as long as the mean workgroup, what is left over as the
-// longest; and parts cost 528 bytes a row at 4 TB/s and 5 us.  us for 1 / 3 / 5 / 8 parts with their join: one new frame (1,374 queries, 16 heads)
-// on 12 233 / 144 / 107 / 108, two frames in fp32 418 / 309 / 289 / 310.
-void shape_of(const Seen& s, int rows, int heads, int& waves, int& splits) {  // rows of a wave
-  const double tile = rows == 32 ? 4.9 : 1.15;
-  waves = s.n_q > 2 * rows ? 4 : 1;
-  rows *= waves;
-  splits = 1;
-  const int64_t units = ceil_div(s.n_q, rows) * heads, places = waves == 4 ? kPlaces : 2 * kPlaces;
-  if (units > 4 * places) return;  // the last round is one of many
+// How a launch is cut up: waves of a workgroup, 32-row parts of a wave's queries, splits of the keys.  Four waves share tiles; a launch of few rows
+// takes one to a workgroup, and one part where that holds them.  fp32 has no registers for two parts.
+struct Shape {
+  int waves, parts, splits;
+  int rows() const { return waves * parts * 32; }  // of a workgroup
+};
+
+// The keys are dealt out where that is worth a second kernel.  What a number of parts costs: the chip holds two workgroups of four waves to a CU (of one:
+// four), a tile takes such a pair twice 1.15 us (fp32 4.9) and one that is alone 1.4 times, a workgroup begins for 1.5 us; whole rounds last as
+// long as the mean workgroup, what is left over as the longest; and parts cost 528 bytes a row at 4 TB/s and 5 us.  us for 1 / 3 / 5 / 8 parts
+// with their join: one new frame (1,374 queries, 16 heads) on 12 233 / 144 / 107 / 108, two frames in fp32 418 / 309 / 289 / 310.
+Shape shape_of(const Seen& s, int heads, int dtype) {
+  const bool bf16 = dtype == BSGA_BF16;
+  const double tile = bf16 ? 1.15 : 4.9;
+  Shape best = {1, 1, 1};
+  if (bf16 && s.n_q > 32) best.parts = 2;
+  if (s.n_q > 2 * best.rows()) best.waves = 4;
+  const int rows = best.rows();
+  const int64_t units = ceil_div(s.n_q, rows) * heads, places = best.waves == 4 ? kPlaces : 2 * kPlaces;
+  if (units > 4 * places) return best;  // the last round is one of many
   int most = 0;
   int64_t all = 0;
   for (int i0 = 0; i0 < s.n_q; i0 += rows) {
@@ -453,31 +460,30 @@ void shape_of(const Seen& s, int rows, int heads, int& waves, int& splits) {  //
     all += c;
   }
   const double mean = static_cast<double>(all) / static_cast<double>(ceil_div(s.n_q, rows));
-  double best = 0.0;
-  for (int n = 1; n == 1 || (n <= 64 && n <= most / 4); ++n) {
+  const double full = best.waves == 4 ? 2.0 : 1.4;
+  double least = 0.0;
+  for (int n = 1; n == 1 || (n <= 64 && n <= most); ++n) {
     const int64_t rounds = units * n / places, left = units * n - rounds * places;
-    const double full = waves == 4 ? 2.0 : 1.4;
-    const double us = tile * (static_cast<double>(rounds) * full * mean + (left == 0 ? 0.0 : left <= kPlaces / 2 ? 1.4 : full) * most) / n +
+    const double us = static_cast<double>(rounds) * (full * tile * mean / n + 1.5) +
+                      (left == 0 ? 0.0 : (left <= kPlaces / 2 ? 1.4 : full) * tile * static_cast<double>(ceil_div(most, n)) + 1.5) +
                       (n > 1 ? 5.0 + static_cast<double>(heads) * s.n_q * n * 528 / 4e6 : 0.0);
-    if (n > 1 && us >= best) continue;
-    best = us;
-    splits = n;
+    if (n > 1 && us >= least) continue;
+    least = us;
+    best.splits = n;
   }
+  return best;
 }
 
 size_t split_bytes(int heads, int64_t n_q, int splits) { return splits > 1 ? static_cast<size_t>(splits) * heads * n_q * 65 * sizeof(float) : 0; }
 
-template <typename T>
-int launch(const WindowArgs& a, int waves, hipStream_t s) {
+template <typename T, int WAVES, int R>
+int launch(const WindowArgs& a, hipStream_t s) {
   const int64_t units = int64_t(a.heads) * a.row_tiles * a.splits;
   if (units > 0x7fffffff) return fail(BSGA_ERR_UNSUPPORTED, "bsga_window_attn: too many rows");
-  const size_t lds = 4 * kTile * Ops<T>::kRow;
-  if (waves == 4) hipLaunchKernelGGL((window_kernel<T, 4>), dim3(static_cast<unsigned>(units)), dim3(256), lds, s, a);
-  else hipLaunchKernelGGL((window_kernel<T, 1>), dim3(static_cast<unsigned>(units)), dim3(64), lds, s, a);
+  hipLaunchKernelGGL((window_kernel<T, WAVES, R>), dim3(static_cast<unsigned>(units)), dim3(64 * WAVES), 4 * kTile * Ops<T>::kRow, s, a);
   if (int rc = check_hip(hipGetLastError(), "bsga_window_attn launch")) return rc;
   if (a.splits == 1) return BSGA_OK;
-  const int64_t rows = int64_t(a.heads) * a.seen.n_q;
-  return launch_join<T>(a.part, a.part_lse, rows, a.splits, a.out, a.lse, s);
+  return launch_join<T>(a.part, a.part_lse, int64_t(a.heads) * a.seen.n_q, a.splits, a.out, a.lse, s);
 }
 
 }  // namespace
@@ -492,9 +498,7 @@ size_t bsga_window_attn_workspace_bytes(int dtype, int heads, int64_t n_q, int64
   Seen s;
   if ((dtype != BSGA_BF16 && dtype != BSGA_FP32) || heads < 1 || heads > 65535 || n_q < 1 || n_k < 1) return 0;
   if (check_seen("", n_q, n_k, q_start, frame, window, sinks, s)) return 0;
-  int waves, splits;
-  shape_of(s, 32 * (dtype == BSGA_BF16 ? kParts<__bf16> : kParts<float>), heads, waves, splits);
-  return split_bytes(heads, n_q, splits);
+  return split_bytes(heads, n_q, shape_of(s, heads, dtype).splits);
 }
 
 int bsga_window_attn(const void* q, const void* k, const void* v, int64_t q_token, int64_t q_head, int64_t k_token, int64_t k_head,
@@ -523,15 +527,16 @@ int bsga_window_attn(const void* q, const void* k, const void* v, int64_t q_toke
   a.heads = heads;
   a.group = heads / kv_heads;
   a.scale_log2 = softmax_scale * kLog2e;
-  const int rows = 32 * (dtype == BSGA_BF16 ? kParts<__bf16> : kParts<float>);
-  int waves;
-  shape_of(a.seen, rows, heads, waves, a.splits);
+  const Shape shape = shape_of(a.seen, heads, dtype);
+  a.splits = shape.splits;
   if (!workspace || !aligned16(workspace) || workspace_bytes < split_bytes(heads, n_q, a.splits)) a.splits = 1;  // one workgroup takes all keys of its rows
-  a.row_tiles = static_cast<int>(ceil_div(n_q, waves * rows));
+  a.row_tiles = static_cast<int>(ceil_div(n_q, shape.rows()));
   a.part = static_cast<float*>(workspace);
   if (a.splits > 1) a.part_lse = a.part + int64_t(a.splits) * heads * n_q * 64;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return dtype == BSGA_BF16 ? launch<__bf16>(a, waves, s) : launch<float>(a, waves, s);
+  if (dtype == BSGA_FP32) return shape.waves == 4 ? launch<float, 4, 1>(a, s) : launch<float, 1, 1>(a, s);
+  if (shape.waves == 4) return launch<__bf16, 4, 2>(a, s);
+  return shape.parts == 2 ? launch<__bf16, 1, 2>(a, s) : launch<__bf16, 1, 1>(a, s);
 }
 
 }  // extern "C"
