@@ -796,40 +796,61 @@ __global__ __launch_bounds__(256) void window_sum_kernel(const float* __restrict
   Ops<T>::store4((d < 64 ? out0 : out1) + to * Ops<T>::kRow, d & 63, y[0], y[1], y[2], y[3]);
 }
 
-// How a launch is cut up.  Workgroups of query rows as in the forward pass; workgroups of keys get their queries in parts where there are
-// too few of them, and those of the first tokens, which all queries see, in parts as long as the others' queries.
-void shape_of(BwdArgs& a) {
-  const int rows = kOwnRows;
+// How a launch is cut up.  A workgroup's rows go over at most so many tiles; longer ways are dealt out to several, whose sums are added up by one more
+// kernel for each kind (query rows, first tokens, other keys).  What that costs, as fitted to 20,011 tokens (bf16) and two frames (fp32): a CU takes 0.85
+// (9.5) us a tile of key rows and 0.63 (7) of query rows, a workgroup alone on its CU 1.4 times that; beside the whole work's share of a CU half of the
+// longest way of query rows counts, which end last, and a tenth of key rows'; parts are written and read at 4 TB/s, a sum is 3 us, a round of workgroups begins for 1.5.  Two frames in fp32, all
+// ways whole 943 us, queries in 2 parts 854, both in 3 835; forward and backward of 565 fp32 tokens of 16 heads, ways of 4 tiles 150, of 1 98.
+void shape_of(BwdArgs& a, bool bf16) {
   const Seen& s = a.seen;
   a.stat_rows = static_cast<int>(ceil_div(s.n_q, kTile)) * kTile;
-  a.row_tiles = static_cast<int>(ceil_div(s.n_q, rows));
-  a.q_splits = 1;
-  const int64_t units = int64_t(a.row_tiles) * a.heads;
-  if (units > 0 && units * 2 <= kPlaces) {
-    int most = 0;
-    for (int rt = 0; rt < a.row_tiles; ++rt) {
-      const int c = tiles_of(s, rt * rows, min((rt + 1) * rows, s.n_q)).count;
-      most = c > most ? c : most;
-    }
-    a.q_splits = static_cast<int>(max(min(kPlaces / units, int64_t(most / 4)), int64_t(1)));
-  }
+  a.row_tiles = static_cast<int>(ceil_div(s.n_q, kOwnRows));
   a.key_tiles = static_cast<int>(ceil_div(s.n_k, kOwnRows));
-  const int64_t all = ceil_div(s.n_q, kTile) * a.group;  // query tiles of a key that all see
-  int64_t most = 0;                                      // and of one that is seen through the window
-  for (int kt = 0; kt < a.key_tiles; ++kt) {
-    const Queries from = queries_of(s, kt * kOwnRows), to = queries_of(s, min((kt + 1) * kOwnRows, s.n_k) - 1);
-    if (kt * kOwnRows < s.sinks || to.last <= from.first) continue;
-    const int64_t c = (ceil_div(to.last, kTile) - from.first / kTile) * a.group;
-    most = c > most ? c : most;
-  }
   a.sink_tiles = static_cast<int>(ceil_div(s.sinks, kOwnRows));
-  const int64_t key_units = int64_t(a.key_tiles) * a.kv_heads;
-  a.splits = key_units > 0 && key_units * 2 <= kPlaces ? static_cast<int>(max(min(kPlaces / key_units, most / 4), int64_t(1))) : 1;
-  // launches of a few rounds end better with shorter workgroups: two frames in fp32 (704 workgroups) 943 us, queries' keys in two parts 854
-  if (a.q_splits == 1 && units + key_units < 3 * kPlaces && units + key_units >= kPlaces && tiles_of(s, max(s.n_q - rows, 0), s.n_q).count >= 16) a.q_splits = 2;
-  const int64_t part = max(most / a.splits, int64_t(16));
-  a.sink_splits = static_cast<int>(min(max(ceil_div(all, part), int64_t(1)), int64_t(64)));
-  if (key_units > 4 * kPlaces && a.sink_tiles == a.key_tiles) a.sink_splits = 1;  // everything is seen from everywhere
+  a.q_splits = a.splits = a.sink_splits = 1;
+  // tiles of the longest way of each kind, and of all
+  int64_t q_most = 0, q_all = 0, k_most = 0, k_all = 0;
+  for (int rt = 0; rt < a.row_tiles; ++rt) {
+    const int64_t c = tiles_of(s, rt * kOwnRows, min((rt + 1) * kOwnRows, s.n_q)).count;
+    q_most = max(q_most, c);
+    q_all += c;
+  }
+  for (int kt = a.sink_tiles; kt < a.key_tiles; ++kt) {
+    const Queries from = queries_of(s, kt * kOwnRows), to = queries_of(s, min((kt + 1) * kOwnRows, s.n_k) - 1);
+    if (to.last <= from.first) continue;
+    const int64_t c = (ceil_div(to.last, kTile) - from.first / kTile) * a.group;
+    k_most = max(k_most, c);
+    k_all += c;
+  }
+  const int64_t sink_most = a.sink_tiles > 0 ? ceil_div(s.n_q, kTile) * a.group : 0;
+  const double k_tile = bf16 ? 0.85 : 9.5, q_tile = bf16 ? 0.63 : 7.0;
+  const double share = (static_cast<double>(k_all + a.sink_tiles * sink_most) * a.kv_heads * k_tile + static_cast<double>(q_all) * a.heads * q_tile) / 256;
+  const double q_rows = static_cast<double>(a.heads) * s.n_q, sink_rows = static_cast<double>(a.kv_heads) * min(a.sink_tiles * kOwnRows, s.n_k),
+               k_rows = static_cast<double>(a.kv_heads) * s.n_k - sink_rows;
+  auto sum_us = [](int64_t splits, double rows, int bytes) { return splits > 1 ? 3.0 + rows * static_cast<double>(splits) * bytes * 2 / 4e6 : 0.0; };
+  const int64_t longest = max(max(q_most, k_most), sink_most);
+  double least = -1.0;
+  // ways of 1, 2, 3, 4, 6, 8, 12, ... tiles
+  for (int64_t kp = 1;; kp += kp > 1 && (kp & (kp - 1)) == 0 ? kp / 2 : kp > 2 ? kp / 3 : 1) {
+    const int64_t splits = max(ceil_div(k_most, kp), int64_t(1)), sink_splits = max(ceil_div(sink_most, kp), int64_t(1));
+    for (int64_t qp = 1; splits <= 64 && sink_splits <= 256; qp += qp > 1 && (qp & (qp - 1)) == 0 ? qp / 2 : qp > 2 ? qp / 3 : 1) {
+      const int64_t q_splits = max(ceil_div(q_most, qp), int64_t(1));
+      if (q_splits <= 64) {
+        const double k_way = max(ceil_div(k_most, splits), ceil_div(sink_most, sink_splits)) * k_tile, q_way = ceil_div(q_most, q_splits) * q_tile;
+        const int64_t groups = a.kv_heads * (a.sink_tiles * sink_splits + (a.key_tiles - a.sink_tiles) * splits) + int64_t(a.heads) * a.row_tiles * q_splits;
+        const double us = max(max(share, 1.4 * k_way), 1.4 * q_way) + 0.1 * k_way + 0.5 * q_way + 1.5 * static_cast<double>(ceil_div(groups, kPlaces)) + sum_us(splits, k_rows, 512) +
+                          sum_us(sink_splits, sink_rows, 512) + sum_us(q_splits, q_rows, 256);
+        if (least < 0.0 || us < least) {
+          least = us;
+          a.q_splits = static_cast<int>(q_splits);
+          a.splits = static_cast<int>(splits);
+          a.sink_splits = static_cast<int>(sink_splits);
+        }
+      }
+      if (qp >= q_most) break;
+    }
+    if (kp >= longest) break;
+  }
 }
 
 size_t stats_bytes(const BwdArgs& a) { return static_cast<size_t>(a.heads) * a.stat_rows * 8; }
@@ -890,7 +911,7 @@ size_t bsga_window_attn_bwd_workspace_bytes(int dtype, int heads, int kv_heads, 
   a.heads = heads;
   a.kv_heads = kv_heads;
   a.group = heads / kv_heads;
-  shape_of(a);
+  shape_of(a, dtype == BSGA_BF16);
   return stats_bytes(a) + part_q_bytes(a) + part_kv_bytes(a, true) + part_kv_bytes(a, false);
 }
 
@@ -931,7 +952,7 @@ int bsga_window_attn_bwd(const void* dout, const void* q, const void* k, const v
   a.group = heads / kv_heads;
   a.scale = softmax_scale;
   a.scale_log2 = softmax_scale * kLog2e;
-  shape_of(a);
+  shape_of(a, dtype == BSGA_BF16);
   const size_t need = stats_bytes(a) + part_q_bytes(a) + part_kv_bytes(a, true) + part_kv_bytes(a, false);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(BSGA_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace ? workspace_bytes : 0, need);
