@@ -82,7 +82,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
   const int wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, g = lane >> 5;
   // later rows see more where the window is long: they go first
-  const int64_t unit = spread(blockIdx.x, gridDim.x, kPlaces);
+  const int64_t unit = spread(blockIdx.x, gridDim.x, a.heads);
   const int split = static_cast<int>(unit % a.splits);
   const int h = static_cast<int>(unit / a.splits / a.row_tiles);
   const int rt = a.row_tiles - 1 - static_cast<int>(unit / a.splits % a.row_tiles);
@@ -211,39 +211,35 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
       return t;
     } else {
       const int lane = fresh_lane(), n = lane & 31, g = lane >> 5;
-      int kaddr[4], vaddr[2][2];  // of the first 32 rows: K chunks; [dimensions][rows + 8]
+      // In LDS, of the first 32 rows of the tile's buffer: K chunks; [dimensions][rows + 8].  (As offsets from smem each read would cost an addition.)
+      unsigned kaddr[4], vaddr[2][2];
+      unsigned to = lds + ((t - t0) & 1) * kBuf, other = ((t - t0) & 1) ? -kBuf : kBuf;  // the tile's buffer, and from it to the other one
 #pragma unroll
-      for (int c = 0; c < 4; ++c) kaddr[c] = n * P::kRow + (((2 * c + g) ^ P::swizzle(n)) << 4);
+      for (int c = 0; c < 4; ++c) kaddr[c] = to + n * P::kRow + (((2 * c + g) ^ P::swizzle(n)) << 4);
       {
         const int mm = (lane & 15) >> 2, j = lane & 3, r = 4 * g + mm;
 #pragma unroll
         for (int db = 0; db < 2; ++db)
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            vaddr[db][e] = kTileBytes + (r + 8 * e) * P::kRow + (((db * 4 + 2 * ((lane >> 4) & 1) + (j >> 1)) ^ P::swizzle(r + 8 * e)) << 4) + (j & 1) * 8;
+            vaddr[db][e] = to + kTileBytes + (r + 8 * e) * P::kRow + (((db * 4 + 2 * ((lane >> 4) & 1) + (j >> 1)) ^ P::swizzle(r + 8 * e)) << 4) + (j & 1) * 8;
       }
       f32x16 sc[2];        // scores
       u32x4 pw[2][2];      // weights: [queries][16 keys]
       bf16x8 ka[4];        // K operands of the unit whose scores come next
       bf16x8 va[2][2][2];  // V operands: [32 keys][dimensions][16 keys]
       float ex[2][2];      // the two weights that are packed in the next slot
-      auto read_k = [&](int u) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) ka[c] = *LDS_PTR(bf16x8, smem + u * 32 * P::kRow + kaddr[c]);
+      auto read_k = [&](int u, int c) {
+        ka[c] = *reinterpret_cast<const bf16x8 __attribute__((address_space(3)))*>(kaddr[c] + u * 32 * P::kRow);
       };
-      auto read_v = [&](auto uc) {
-        constexpr int u = decltype(uc)::value;
+      auto read_v = [&](auto uc, auto ic) {  // in the order of their use
+        constexpr int u = decltype(uc)::value, db = decltype(ic)::value & 1, cp = decltype(ic)::value >> 1;
+        u32x2 x[2];
 #pragma unroll
-        for (int db = 0; db < 2; ++db)
-#pragma unroll
-          for (int cp = 0; cp < 2; ++cp) {
-            u32x2 x[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-              x[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(
-                                                   smem + (32 * u + 16 * cp) * P::kRow + vaddr[db][e])));
-            va[u][db][cp] = __builtin_bit_cast(bf16x8, u32x4{x[0][0], x[0][1], x[1][0], x[1][1]});
-          }
+        for (int e = 0; e < 2; ++e)
+          x[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<s16x4 __attribute__((address_space(3)))*>(
+                                               vaddr[db][e] + (32 * u + 16 * cp) * P::kRow)));
+        va[u][db][cp] = __builtin_bit_cast(bf16x8, u32x4{x[0][0], x[0][1], x[1][0], x[1][1]});
       };
       auto weight = [&](float s, float from) { return __builtin_amdgcn_exp2f(fmaf(s, a.scale_log2, -from)); };
       auto slot = [&](auto nc, auto sc_, auto&& mid) {
@@ -275,29 +271,24 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
         slot(nc, Int<4>{}, mid); slot(nc, Int<5>{}, mid); slot(nc, Int<6>{}, mid); slot(nc, Int<7>{}, mid);
       };
       // On entry sc[0] holds the first scores, ka the K operands of the first 32 keys, pw[1] and va[1] the last unit before (zeros at the start).
-      unsigned to = lds + ((t - t0) & 1) * kBuf;  // the tile's buffer; the other one differs in one bit of the offset
       auto turn = [&]() {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) kaddr[c] ^= kBuf;
+        for (int c = 0; c < 4; ++c) kaddr[c] += other;
       };
-      if ((t - t0) & 1) {
-        turn();
-#pragma unroll
-        for (int db = 0; db < 2; ++db)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) vaddr[db][e] ^= kBuf;
-      }
       auto tile = [&]() {
         const int next = tiles.key(t + 2 < t1 ? t + 2 : t);  // past the end: a load that nobody reads, in place of a branch
         const i32x4 krsrc = k_load.rsrc(kh, a.seen.n_k, next), vrsrc = v_load.rsrc(vh, a.seen.n_k, next);
+        // One or two reads of LDS a slot, eight slots ahead of their use: the waves of a workgroup are in step, and reads in one go wait for each other.
         four(Int<0>{}, [&](auto s) {
-          if constexpr (decltype(s)::value == 0) read_v(Int<0>{});
-          if constexpr (decltype(s)::value == 3) read_k(1);
+          constexpr int S = decltype(s)::value;
+          if constexpr (S < 4) read_k(1, S);
+          else read_v(Int<0>{}, Int<S - 4>{});
         });
         four(Int<1>{}, [&](auto s) {
-          if constexpr (decltype(s)::value == 0) read_v(Int<1>{});
-          if constexpr (decltype(s)::value == 1) turn();
-          if constexpr (decltype(s)::value >= 4) vaddr[decltype(s)::value & 1][(decltype(s)::value >> 1) & 1] ^= kBuf;
+          constexpr int S = decltype(s)::value;
+          if constexpr (S < 4) read_v(Int<1>{}, s);
+          if constexpr (S == 4) turn();
+          if constexpr (S >= 4) vaddr[S & 1][(S >> 1) & 1] += other;
         });
         four(Int<2>{}, [&](auto s) {
           constexpr int S = decltype(s)::value;
@@ -305,16 +296,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
             __builtin_amdgcn_s_waitcnt(0x0f70);
             __syncthreads();
           }
-          if constexpr (S == 3) read_k(0);
-          if constexpr (S >= 4) k_load.quarter(krsrc, Int<S - 4>{}, to);
+          if constexpr (S < 4) read_k(0, S);
+          else k_load.quarter(krsrc, Int<S - 4>{}, to);
         });
         four(Int<3>{}, [&](auto s) {
           constexpr int S = decltype(s)::value;
           if constexpr (S < 4) v_load.quarter(vrsrc, Int<S>{}, to + kTileBytes);
         });
-        to ^= lds ^ (lds + kBuf);
+        to += other;
+        other = -other;
       };
-      read_k(0);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) read_k(0, c);
 #pragma unroll
       for (int cp = 0; cp < 2; ++cp) {
         pw[1][cp] = u32x4{0u, 0u, 0u, 0u};

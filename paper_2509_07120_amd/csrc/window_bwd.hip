@@ -267,7 +267,7 @@ __device__ __forceinline__ void query_rows(const BwdArgs& a, int64_t block, int6
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, g = lane >> 5;
-  const int64_t unit = spread(block, blocks, kPlaces);
+  const int64_t unit = spread(block, blocks, a.heads);
   const int split = static_cast<int>(unit % a.q_splits);
   const int h = static_cast<int>(unit / a.q_splits / a.row_tiles);
   const int rt = a.row_tiles - 1 - static_cast<int>(unit / a.q_splits % a.row_tiles);
@@ -491,7 +491,7 @@ __device__ __forceinline__ void key_rows(const BwdArgs& a, int64_t block, int64_
   // the first tokens' units come first: they are the longest
   const int64_t sink_units = int64_t(a.kv_heads) * a.sink_tiles * a.sink_splits;
   const bool sink = block < sink_units;
-  const int64_t unit = sink ? block : spread(block - sink_units, blocks - sink_units, kPlaces);
+  const int64_t unit = sink ? block : spread(block - sink_units, blocks - sink_units, a.kv_heads);
   const int splits = sink ? a.sink_splits : a.splits, of_head = sink ? a.sink_tiles : a.key_tiles - a.sink_tiles;
   const int split = static_cast<int>(unit % splits);
   const int hk = static_cast<int>(unit / splits / of_head);
