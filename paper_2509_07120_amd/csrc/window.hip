@@ -202,11 +202,32 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
     }
   };
 
-  // Tiles from t on that all rows of the wave see; returns the first that is not one.  The vector instructions of one unit of 32 keys x 32
+  // Whether the wave takes a tile through run(): every row sees all of it or nothing.  from: what is subtracted from a row's scores, its maximum or
+  // infinity.  (Rows of two frames share a wave, and tiles that one of them sees need no mask: through plain(), 32 frames take
+  // 1235 us instead of 1137.)
+  auto whole = [&](int key, bool ready, float (&from)[R]) -> bool {
+    if (ready && seen_by_all(key)) {
+#pragma unroll
+      for (int b = 0; b < R; ++b) from[b] = m[b];
+      return true;
+    }
+    if (seen_by_none(key)) return false;
+    bool ok = true;
+#pragma unroll
+    for (int b = 0; b < R; ++b) {
+      const bool in = key + kTile <= hi[b] && (key >= lo[b] || key + kTile <= a.seen.sinks);
+      const bool out = key >= hi[b] || (key + kTile <= lo[b] && key >= a.seen.sinks);
+      ok = ok && (out || (in && m[b] > -INFINITY));
+      from[b] = in ? m[b] : INFINITY;
+    }
+    return __all(ok);
+  };
+
+  // Tiles from t on that whole() lets through; returns the first that is not one.  The vector instructions of one unit of 32 keys x 32
   // queries stand between the products of its neighbours: unit N's weights beside the scores of unit N + 1 and the update of O by
   // unit N - 1, one product and two weights to a slot.  Weights are taken from the maximum that the tiles before have left, without a look at the
   // scores: there is room for 2^100 above it, and rows that need more are found at the end.
-  auto run = [&](int t) -> int {
+  auto run = [&](int t, bool ready, float (&from)[R]) -> int {
     if constexpr (!kRuns) {
       return t;
     } else {
@@ -229,6 +250,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
       bf16x8 ka[4];        // K operands of the unit whose scores come next
       bf16x8 va[2][2][2];  // V operands: [32 keys][dimensions][16 keys]
       float ex[2][2];      // the two weights that are packed in the next slot
+      float next_from[2] = {INFINITY, INFINITY};  // of the next tile, whose first weights are made in this one's last slot
       auto read_k = [&](int u, int c) {
         ka[c] = *reinterpret_cast<const bf16x8 __attribute__((address_space(3)))*>(kaddr[c] + u * 32 * P::kRow);
       };
@@ -255,11 +277,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
         l[BQ] += ex[S & 1][0] + ex[S & 1][1];
         asm volatile("" : "+v"(l[BQ]));  // pinned: added up later, all of a unit's weights would stay alive
         if constexpr (S < 7) {
-          ex[(S + 1) & 1][0] = weight(sc[BQ][2 * S + 2], m[BQ]);
-          ex[(S + 1) & 1][1] = weight(sc[BQ][2 * S + 3], m[BQ]);
+          ex[(S + 1) & 1][0] = weight(sc[BQ][2 * S + 2], from[BQ]);
+          ex[(S + 1) & 1][1] = weight(sc[BQ][2 * S + 3], from[BQ]);
         } else {
-          ex[0][0] = weight(sc[BN][0], m[BN]);
-          ex[0][1] = weight(sc[BN][1], m[BN]);
+          ex[0][0] = weight(sc[BN][0], N == 3 ? next_from[0] : from[BN]);
+          ex[0][1] = weight(sc[BN][1], N == 3 ? next_from[0] : from[BN]);
         }
         __builtin_amdgcn_sched_barrier(0);
         pw[BQ][S >> 2][S & 3] = pk;
@@ -317,13 +339,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
       clear(sc[0]);
 #pragma unroll
       for (int c = 0; c < 4; ++c) sc[0] = P::product(ka[c], qf[0][c], sc[0]);
-      ex[0][0] = weight(sc[0][0], m[0]);
-      ex[0][1] = weight(sc[0][1], m[0]);
+      ex[0][0] = weight(sc[0][0], from[0]);
+      ex[0][1] = weight(sc[0][1], from[0]);
       __builtin_amdgcn_sched_barrier(0);
-      do {
+      for (bool more = true; more; ++t) {
+        more = t + 1 < t1 && whole(tiles.key(t + 1), ready, next_from);
         tile();
-        ++t;
-      } while (t < t1 && seen_by_all(tiles.key(t)));
+        from[0] = next_from[0];
+        from[1] = next_from[1];
+      }
 #pragma unroll
       for (int db = 0; db < 2; ++db)
 #pragma unroll
@@ -352,7 +376,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
     __syncthreads();
     bool ready = false;  // whether all rows have a maximum
     for (int t = t0; t < t1;) {
-      if (kRuns && runs && ready && seen_by_all(tiles.key(t))) t = run(t);
+      if constexpr (kRuns) {
+        float from[R];
+        if (runs && whole(tiles.key(t), ready, from)) t = run(t, ready, from);
+      }
       if (t >= t1) break;
       if (!seen_by_none(tiles.key(t))) {
         plain(t);
