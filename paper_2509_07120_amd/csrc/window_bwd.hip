@@ -104,24 +104,27 @@ __device__ __forceinline__ int run(int t, unsigned at, const unsigned char* smem
   constexpr bool KEYS = SUMS == 8;
   constexpr int kTileBytes = kTile * P::kRow, kBuf = 2 * kTileBytes + (KEYS ? kStatBytes : 0), kSlots = SUMS + 8;
   const int lane = fresh_lane(), n = lane & 31, g = lane >> 5;
-  int raddr[4], caddr[2][2];  // of the first 32 rows: chunks of a row; [dimensions][rows + 8] of the transposed operands
+  // In LDS, of the first 32 rows: chunks of a row; [dimensions][rows + 8] of the transposed operands; where S and dP begin.  (As offsets each read
+  // would cost an addition.)
+  unsigned raddr[4], caddr[2][2], saddr = lds_address(smem) + at + 2 * kTileBytes + g * 16;
 #pragma unroll
-  for (int c = 0; c < 4; ++c) raddr[c] = n * P::kRow + (((2 * c + g) ^ P::swizzle(n)) << 4);
+  for (int c = 0; c < 4; ++c) raddr[c] = lds_address(smem) + at + n * P::kRow + (((2 * c + g) ^ P::swizzle(n)) << 4);
   {
     const int m = (lane & 15) >> 2, j = lane & 3, r = 4 * g + m;
 #pragma unroll
     for (int db = 0; db < 2; ++db)
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        caddr[db][e] = (r + 8 * e) * P::kRow + (((db * 4 + 2 * ((lane >> 4) & 1) + (j >> 1)) ^ P::swizzle(r + 8 * e)) << 4) + (j & 1) * 8;
+        caddr[db][e] = lds_address(smem) + at + (r + 8 * e) * P::kRow + (((db * 4 + 2 * ((lane >> 4) & 1) + (j >> 1)) ^ P::swizzle(r + 8 * e)) << 4) + (j & 1) * 8;
   }
-  unsigned next = at + kBuf == 3 * kBuf ? 0u : at + kBuf;  // the buffers' places: of this tile and of the next
+  auto step_from = [](unsigned at) { return at == 2 * kBuf ? static_cast<unsigned>(-2 * kBuf) : static_cast<unsigned>(kBuf); };
+  unsigned step = step_from(at), last_step = 0;  // from this tile's buffer to the next one, from the last one's to this
   f32x16 s[2], dp[2];                                       // [unit]; P and dS take their places
   u32x4 pw[2], dw[2];                                       // packed: [16 streamed rows]
   bf16x8 op[8];
-  auto row_operand = [&](auto ic, auto uc, unsigned from) {  // of S (0 to 3) and dP
+  auto row_operand = [&](auto ic, auto uc) {  // of S (0 to 3) and dP
     constexpr int I = decltype(ic)::value, U = decltype(uc)::value;
-    op[I] = *LDS_PTR(bf16x8, smem + from + raddr[I & 3] + (I >> 2) * kTileBytes + U * 32 * P::kRow);
+    op[I] = *reinterpret_cast<const bf16x8 __attribute__((address_space(3)))*>(raddr[I & 3] + (I >> 2) * kTileBytes + U * 32 * P::kRow);
   };
   auto sum_operand = [&](auto ic, auto uc) {  // of the sums
     constexpr int I = decltype(ic)::value, U = decltype(uc)::value;
@@ -129,14 +132,14 @@ __device__ __forceinline__ int run(int t, unsigned at, const unsigned char* smem
     u32x2 x[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e)
-      x[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(
-                                           smem + at + caddr[db][e] + (kind == 0 ? kTileBytes : 0) + (32 * U + 16 * cp) * P::kRow)));
+      x[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<s16x4 __attribute__((address_space(3)))*>(
+                                           caddr[db][e] + (kind == 0 ? kTileBytes : 0) + (32 * U + 16 * cp) * P::kRow)));
     op[I] = __builtin_bit_cast(bf16x8, u32x4{x[0][0], x[0][1], x[1][0], x[1][1]});
   };
-  auto begin_from = [&](auto ic, auto uc, unsigned from) {  // quarter I of what S and dP of key rows begin with
+  auto begin_from = [&](auto ic, auto uc) {  // quarter I of what S and dP of key rows begin with
     constexpr int I = decltype(ic)::value, U = decltype(uc)::value;
-    const unsigned char* const st = smem + from + 2 * kTileBytes + (32 * U + 8 * I) * 4 + g * 16;
-    const f32x4 x = *LDS_PTR(f32x4, st), y = *LDS_PTR(f32x4, st + 256);
+    typedef const f32x4 __attribute__((address_space(3)))* Quarter;
+    const f32x4 x = *reinterpret_cast<Quarter>(saddr + (32 * U + 8 * I) * 4), y = *reinterpret_cast<Quarter>(saddr + (32 * U + 8 * I) * 4 + 256);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       s[U][4 * I + e] = x[e];
@@ -160,16 +163,19 @@ __device__ __forceinline__ int run(int t, unsigned at, const unsigned char* smem
   };
   auto slot = [&](auto uc, auto sc) {
     constexpr int U = decltype(uc)::value, S = decltype(sc)::value, V = U ^ 1;
-    const unsigned from = U == 0 ? at : next;  // of unit N + 1
     if constexpr (S < SUMS) {
       add(Int<S>{});
-      row_operand(Int<S>{}, Int<V>{}, from);
-      if constexpr (SUMS == 4) row_operand(Int<4 + S>{}, Int<V>{}, from);
-      if constexpr (KEYS && S < 4) begin_from(Int<S>{}, Int<V>{}, from);
+      row_operand(Int<S>{}, Int<V>{});
+      if constexpr (SUMS == 4) row_operand(Int<4 + S>{}, Int<V>{});
+      if constexpr (KEYS && S < 4) begin_from(Int<S>{}, Int<V>{});
     } else {
       product(Int<S - SUMS>{}, Int<V>{});
       if constexpr (S - SUMS < SUMS) sum_operand(Int<S - SUMS>{}, uc);
     }
+    // on to the next buffer, whose rows are read from unit 1 on and whose columns from its own unit 0 on
+    if constexpr (U == 0 && S < 4) caddr[S & 1][S >> 1] += last_step;
+    if constexpr (U == 0 && S >= SUMS && S < SUMS + 4) raddr[S - SUMS] += step;
+    if constexpr (KEYS && U == 0 && S == SUMS + 4) saddr += step;
     if constexpr (U == 1 && S >= 1 && S < 6) load(Int<S - 1>{});
     // numbers of P done before slot x, of dS (two slots later: dP is the last that the matrix pipe makes), and words packed: the sums of the last
     // unit read the first four until slot SUMS / 2 - 1, the others until SUMS - 1
@@ -200,8 +206,8 @@ __device__ __forceinline__ int run(int t, unsigned at, const unsigned char* smem
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  each<0, 8>([&](auto i) { row_operand(i, Int<0>{}, at); });
-  if constexpr (KEYS) each<0, 4>([&](auto i) { begin_from(i, Int<0>{}, at); });
+  each<0, 8>([&](auto i) { row_operand(i, Int<0>{}); });
+  if constexpr (KEYS) each<0, 4>([&](auto i) { begin_from(i, Int<0>{}); });
   each<0, 8>([&](auto j) { product(j, Int<0>{}); });
 #pragma unroll
   for (int i = 0; i < 8; ++i) op[i] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
@@ -212,8 +218,9 @@ __device__ __forceinline__ int run(int t, unsigned at, const unsigned char* smem
     each<0, kSlots>([&](auto x) { slot(Int<0>{}, x); });
     land();
     each<0, kSlots>([&](auto x) { slot(Int<1>{}, x); });
-    at = next;
-    next = at + kBuf == 3 * kBuf ? 0u : at + kBuf;
+    at += step;
+    last_step = step;
+    step = step_from(at);
     ++t;
   } while (more(t));
   each<0, SUMS>([&](auto i) { add(i); });
