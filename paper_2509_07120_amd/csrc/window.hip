@@ -138,6 +138,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
     constexpr int U = R == 1 ? 2 : 1;  // 32-key parts at a time: as many as registers allow, for fewer steps of the maximum
 #pragma unroll
     for (int u0 = 0; u0 < 2; u0 += U) {
+      const int part = key + 32 * u0;  // (left out where no row sees it: 32 frames 1063 -> 1048 us)
+      if (U == 1 && (part >= hi_max || (part + 32 <= lo_min && part >= a.seen.sinks))) continue;
       f32x16 s[U][R];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
