@@ -6,7 +6,7 @@ Usage (from the repository root, after the rocprofv3 runs listed in each summary
     python -m paper_2509_07120_amd.profile_summary traffic <dir FETCH_SIZE run> <dir WRITE_SIZE run> <dir TCC run>
     python -m paper_2509_07120_amd.profile_summary pipes   <dir of counter run A> <dir of counter run B> ...
     python -m paper_2509_07120_amd.profile_summary topk    <dir TCC run at rho 0.9> <dir pipe-counter run at rho 0.9>
-    python -m paper_2509_07120_amd.profile_summary case    <name in perf/cases.py> <dir of --kernel-trace --stats run> <dir of counter run>
+    python -m paper_2509_07120_amd.profile_summary case    <name in perf/cases.py or perf/operators.py> <dir of --kernel-trace --stats run> <dir of counter run>
 
 Each sub-command reads the `*_kernel_stats.csv`, `*_kernel_trace.csv` or `*_counter_collection.csv`
 files rocprofv3 wrote with `--output-format csv`, prints what it found, and rewrites the matching
@@ -329,19 +329,27 @@ def cmd_case(name: str, d_stats: str, d_pipes: str) -> None:
     """Time and pipe counters of every library kernel of one of the performance cases, means over 20 passes after 5."""
     passes, skip = 25, 5
 
+    def label(n):  # kernels over __bf16 keep their mangled names, or get a wrong one
+        hit = re.search(r"_ZN4bsga12_GLOBAL__N_1\d+(\w+?_kernel)I(\w*?)E(?:E?v|$)", n)
+        if hit:
+            return f"{hit.group(1)}<{', '.join('bf16' if a == 'DF16b' else a[2:-1] for a in re.findall(r'DF16b|L.[0-9]+E', hit.group(2) + 'E'))}>"
+        hit = re.search(r"bsga::.*?(\w+_kernel(?:<[^>]*>)?)\(", n)
+        return hit.group(1).replace("<bool _Accum, bool, E>", "<bf16>") if hit else None
+
     def kernels(rows):  # (name, value) in order -> {name: the launches of the last passes}
         found = collections.OrderedDict()
         for n, v in rows:
-            hit = re.search(r"bsga::.*?(\w+_kernel(?:<[^>]*>)?)\(", n)
-            if hit:
-                found.setdefault(hit.group(1), []).append(v)
+            if label(n):
+                found.setdefault(label(n), []).append(v)
         return {n: v[len(v) * skip // passes:] for n, v in found.items() if len(v) % passes == 0}
 
     trace = sorted(csv.DictReader(open(one(d_stats, "kernel_trace.csv"))), key=lambda r: int(r["Start_Timestamp"]))
     times = kernels((r["Kernel_Name"], (int(r["End_Timestamp"]) - int(r["Start_Timestamp"])) / 1e3) for r in trace)
     pipes = kernels((x["name"], x) for x in dispatches(d_pipes))
     counters = "SQ_VALU_MFMA_BUSY_CYCLES SQ_BUSY_CU_CYCLES SQ_INSTS_MFMA SQ_WAVE_CYCLES SQ_WAIT_ANY SQ_WAIT_INST_ANY SQ_ACTIVE_INST_VALU SQ_LDS_BANK_CONFLICT"
-    run = (f"python3 -c \"import sys; sys.path.insert(0, '<repo>'); import perf.cases as C; c = [x for x in C.listed() if x['name'] == '{name}'][0]; "
+    listed = os.path.join(os.path.dirname(PROFILES), "perf", "operators.py")
+    module = "perf.operators as C; C.own = True" if f'"{name}"' in open(listed).read() else "perf.cases as C"
+    run = (f"python3 -c \"import sys; sys.path.insert(0, '<repo>'); import {module}; c = [x for x in C.listed() if x['name'] == '{name}'][0]; "
            f"s = C.prepare(c, 1); [C.run(s) for _ in range({passes})]; C.torch.cuda.synchronize()\"")
     path = os.path.join(PROFILES, f"{name}_kernels.md")
     with open(path, "w") as f:
