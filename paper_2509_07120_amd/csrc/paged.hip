@@ -201,7 +201,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(const PagedArgs a
   for (int p = wave; p < pieces; p += kWaves, buf ^= 1) {
     if (p + kWaves < pieces) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");  // the next piece's eight loads may be on their way
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    const unsigned char* const kt = mine + buf * kBuf;
+    unsigned char* const kt = mine + buf * kBuf;
+    const int left = x1 - x0 - p * P::kKeys;
+    if (left < P::kKeys) {  // the repeated values have weights of zero, which is not nothing if the last one is infinite
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = i * kRowsOfLoad + r_in;
+        if (r >= left) *reinterpret_cast<u32x4*>(kt + kPiece + r * kRow + pos * 16) = u32x4{0u, 0u, 0u, 0u};
+      }
+    }
     f32x4 w[P::kBlocks];
 #pragma unroll
     for (int blk = 0; blk < P::kBlocks; ++blk) {
@@ -211,7 +219,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(const PagedArgs a
 #pragma unroll
       for (int e = 0; e < P::kSteps; ++e) w[blk] = P::product(ka[e], qf[e], w[blk]);
     }
-    const int left = x1 - x0 - p * P::kKeys;
     float top = -INFINITY;
 #pragma unroll
     for (int blk = 0; blk < P::kBlocks; ++blk)

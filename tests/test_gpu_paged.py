@@ -102,6 +102,20 @@ def test_the_rows_it_sees_decide(B):
     assert torch.equal(o[0], clean[0]) and torch.equal(o[1, 2:], clean[1, 2:]) and bool(o[1, :2].isnan().all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n", [1, 37, 500])
+def test_an_infinite_last_value(B, dtype, n):
+    """It has a weight above zero: its number becomes infinite, by its sign, and the others stay as they were."""
+    q, kc, vc, table, lengths, _ = draw([n], 4, 2, 16, TYPES[dtype])
+    clean = B.bsga_paged_attn(q, kc, vc, table, lengths)
+    page, row = int(table[0, (n - 1) // 16]), (n - 1) % 16
+    vc[page, 0, row, 5], vc[page, 1, row, 40] = math.inf, -math.inf
+    o = B.bsga_paged_attn(q, kc, vc, table, lengths)
+    assert bool((o[0, :2, 5] == math.inf).all()) and bool((o[0, 2:, 40] == -math.inf).all())
+    o[0, :2, 5], o[0, 2:, 40] = clean[0, :2, 5], clean[0, 2:, 40]
+    assert torch.equal(o, clean)
+
+
 def test_lengths_and_pages_that_do_not_exist(B):
     """Lengths beyond the table and below zero are clamped, and so are page numbers: nothing outside the cache is read."""
     q, kc, vc, table, n, seqs = draw([64, 64, 64], 2, 1, 16, torch.bfloat16, spare=0)
