@@ -49,6 +49,11 @@ __host__ __device__ inline Tiles tiles_of(const Seen& s, int i0, int i1) {  // q
   return t;
 }
 
+// What all lanes agree on, in scalar registers: 64-bit minima are vector instructions, and whatever is computed from them each tile would be too
+// (descriptors, bounds: 45 of 250 instructions of a tile of the gradient's query rows).
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ Tiles scalar(const Tiles& t) { return {scalar(t.first), scalar(t.start), scalar(t.count)}; }
+
 // A tensor [heads, tokens, 64] with strides in bytes.
 struct View {
   const unsigned char* p;

@@ -275,19 +275,19 @@ __device__ __forceinline__ void query_rows(const BwdArgs& a, int64_t block, int6
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, g = lane >> 5;
   const int64_t unit = spread(block, blocks, a.heads);
-  const int split = static_cast<int>(unit % a.q_splits);
-  const int h = static_cast<int>(unit / a.q_splits / a.row_tiles);
-  const int rt = a.row_tiles - 1 - static_cast<int>(unit / a.q_splits % a.row_tiles);
+  const int split = scalar(static_cast<int>(unit % a.q_splits));
+  const int h = scalar(static_cast<int>(unit / a.q_splits / a.row_tiles));
+  const int rt = a.row_tiles - 1 - scalar(static_cast<int>(unit / a.q_splits % a.row_tiles));
   const int i0 = rt * kOwnRows, i1 = min(i0 + kOwnRows, a.seen.n_q);
-  const Tiles tiles = tiles_of(a.seen, i0, i1);
-  const int t0 = static_cast<int>(int64_t(tiles.count) * split / a.q_splits), t1 = static_cast<int>(int64_t(tiles.count) * (split + 1) / a.q_splits);
+  const Tiles tiles = scalar(tiles_of(a.seen, i0, i1));
+  const int t0 = scalar(static_cast<int>(int64_t(tiles.count) * split / a.q_splits)), t1 = scalar(static_cast<int>(int64_t(tiles.count) * (split + 1) / a.q_splits));
   const unsigned char* const qh = a.q.p + h * a.q.head;
   const unsigned char* const kh = a.k.p + h / a.group * a.k.head;
   const unsigned char* const vh = a.v.p + h / a.group * a.v.head;
   const int64_t row0 = int64_t(h) * a.seen.n_q;
   const unsigned lds = lds_address(smem);
   const TileLoad<T, WAVES> k_load(a.k.token, wave, lane), v_load(a.v.token, wave, lane);
-  auto place = [&](int t) { return static_cast<unsigned>((t - t0) % kBuffers) * kBuf; };
+  auto place = [&](int t) { return static_cast<unsigned>(scalar((t - t0) % kBuffers)) * kBuf; };
   auto issue = [&](int t) {
     const int key = tiles.key(t);
     k_load.all(kh, a.seen.n_k, key, lds + place(t));
@@ -317,6 +317,7 @@ __device__ __forceinline__ void query_rows(const BwdArgs& a, int64_t block, int6
     a.seen.range(w0, lo_min, hi_min);
     a.seen.range(w1 - 1, lo_max, hi_max);
   }
+  lo_min = scalar(lo_min), hi_min = scalar(hi_min), lo_max = scalar(lo_max), hi_max = scalar(hi_max);
   auto seen_by_none = [&](int key) { return none || key >= hi_max || (key + kTile <= lo_min && key >= a.seen.sinks); };
   auto seen_by_all = [&](int key) {
     return !none && key + kTile <= hi_min && (key >= lo_max || key + kTile <= a.seen.sinks || a.seen.sinks >= lo_max);
@@ -517,7 +518,7 @@ __device__ __forceinline__ void key_rows(const BwdArgs& a, int64_t block, int64_
   const int h0 = hk * a.group;
   const unsigned lds = lds_address(smem);
   const TileLoad<T, WAVES> q_load(a.q.token, wave, lane), d_load(P::kRow, wave, lane);
-  auto place = [&](int s) { return static_cast<unsigned>((s - seq.begin) % kBuffers) * kBuf; };
+  auto place = [&](int s) { return static_cast<unsigned>(scalar((s - seq.begin) % kBuffers)) * kBuf; };
   auto row_of = [&](int s) { return (seq.first + s % seq.per_head) * kTile; };
   const unsigned stat_offset = lane < 16 ? lane * 16u : lane < 32 ? a.stat_rows * 4u + (lane - 16) * 16u : 1u << 30;
   auto stat_rsrc = [&](int h) { return make_rsrc(a.stats + int64_t(h) * 2 * a.stat_rows, a.stat_rows * 8u); };
