@@ -455,11 +455,25 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
 }
 
 // How a launch is cut up: waves of a workgroup, 32-row parts of a wave's queries, splits of the keys.  Four waves share tiles; a launch of few rows
-// takes one to a workgroup, and one part where that holds them.  fp32 has no registers for two parts.
+// or short windows takes one to a workgroup, and one part where that holds them.  fp32 has no registers for two parts.
 struct Shape {
   int waves, parts, splits;
   int rows() const { return waves * parts * 32; }  // of a workgroup
 };
+
+// Whether a bf16 launch of more than 128 queries goes by waves of 64 queries on their own, not by four that share tiles: four go in step, and a tile
+// that one of them has to mask holds all of them up.  That counts where frames are no longer than a tile, so that every row sees other keys, and
+// the window is short (up to 8 tiles for 256 queries), or a CU has one such workgroup at most and few tiles to go through.  Measured, us, four / one:
+// 16 heads of 42,116 queries, windows of 1, 64, 256 and 1,024 tokens 123 / 99, 145 / 140, 207 / 196, 311 / 353; 8 heads of 1,100 queries, windows of 1, 64, 256 and
+// 1,024 19.7 / 10.0, 23.4 / 12.9, 22.1 / 17.6, 27.6 / 24.5; 16 heads, all keys before the query, 1,156 queries 33.9 / 27.7, 3,804 69 / 74; frames
+// of 500 tokens, window of two of them, 6,000 queries 60 / 78.
+bool goes_by_waves(const Seen& s, int heads) {
+  if (s.frame > kTile) return false;
+  const int rows = 256, row_tiles = static_cast<int>(ceil_div(s.n_q, rows)), step = row_tiles / 64 + 1;  // (64 of them or so)
+  int most = 0;
+  for (int rt = row_tiles - 1; rt >= 0; rt -= step) most = max(most, tiles_of(s, rt * rows, min((rt + 1) * rows, s.n_q)).count);
+  return most <= 8 || (int64_t(row_tiles) * heads <= kPlaces / 2 && most <= 32);
+}
 
 // The keys are dealt out where that is worth a second kernel.  What a number of parts costs: the chip holds two workgroups of four waves to a CU (of one:
 // four), a tile takes such a pair twice 1.15 us (fp32 4.9) and one that is alone 1.4 times, a workgroup begins for 1.5 us; whole rounds last as
@@ -470,7 +484,7 @@ Shape shape_of(const Seen& s, int heads, int dtype) {
   const double tile = bf16 ? 1.15 : 4.9;
   Shape best = {1, 1, 1};
   if (bf16 && s.n_q > 32) best.parts = 2;
-  if (s.n_q > 2 * best.rows()) best.waves = 4;
+  if (s.n_q > 2 * best.rows() && !(bf16 && goes_by_waves(s, heads))) best.waves = 4;
   const int rows = best.rows();
   const int64_t units = ceil_div(s.n_q, rows) * heads, places = best.waves == 4 ? kPlaces : 2 * kPlaces;
   if (units > 4 * places) return best;  // the last round is one of many
