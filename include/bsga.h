@@ -346,7 +346,8 @@ int bsga_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const 
  *   workspace  nullable, bsga_window_attn_workspace_bytes(...) bytes, 16-byte aligned, overwritten: with it launches of few queries deal their keys
  *              out to several workgroups; without it, or with less, results are the same up to the order of fp32 sums
  * bf16: products on bf16 MFMA, logits, softmax and sums in fp32, the weights that multiply V rounded to bf16.  fp32: products on fp32 MFMA.
- * A key that a query does not see has no part in its result, whatever its values.  The same bits every time.
+ * A key that a query does not see has no part in its result, whatever its values (an infinity or NaN among the unseen may change the order in which
+ * the seen ones are summed).  The same bits every time.
  */
 size_t bsga_window_attn_workspace_bytes(int dtype, int heads, int64_t n_q, int64_t n_k, int64_t q_start, int64_t frame, int64_t window,
                                         int64_t sinks);

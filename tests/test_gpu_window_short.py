@@ -26,13 +26,15 @@ def test_short_windows(B, H, K, N, M, window, sinks, frame):  # noqa: F811
 
 
 def test_rows_that_are_not_finite(B):  # noqa: F811
-    """A value that is not a number reaches the queries that see it, and no others."""
+    """A value that is not a number reaches the queries that see it, and no others (those of the same tile are computed again one by one, with sums in
+    another order)."""
     q, k, v = draw(2, 1, 1500, 1500, torch.bfloat16)
-    clean = B.bsga_window_attn(q, k, v, window=40)
+    clean = v.clone()
     v[0, 700, 3] = float("nan")
     o = B.bsga_window_attn(q, k, v, window=40)
-    assert bool(o[:, 700:740, 3].isnan().all())
-    o[:, 700:740, 3] = clean[:, 700:740, 3]
-    seen = torch.zeros(1500, dtype=torch.bool, device="cuda")
-    seen[700:740] = True
-    assert torch.equal(o[:, ~seen], clean[:, ~seen]) and bool(o.isfinite().all())
+    seen = seen_by(1500, 1500, 40, 0, 1, None)
+    touched = seen[:, 700]
+    assert int(touched.sum()) == 40 and bool(o[:, touched, 3].isnan().all())
+    check(o[:, ~touched], None, q[:, ~touched], k, clean, seen[~touched])
+    rest = torch.arange(64, device="cuda") != 3
+    check(o[:, touched][..., rest], None, q[:, touched], k, clean[..., rest], seen[touched])
