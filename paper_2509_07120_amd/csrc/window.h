@@ -184,6 +184,27 @@ __device__ __forceinline__ void clear(f32x16& x) {
   for (int i = 0; i < 16; ++i) x[i] = 0.f;
 }
 
+// Of a lane's numbers of one product, of tile rows `at` + 8 (i / 4) + i % 4, those outside [first, last) become `hidden`: three instructions for each.
+__device__ __forceinline__ void keep(f32x16& x, int at, int first, int last, float hidden) {
+  const int from = first - at;
+  const unsigned span = static_cast<unsigned>(max(last - first, 0));
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = static_cast<unsigned>(8 * (i >> 2) + (i & 3) - from) < span ? x[i] : hidden;
+}
+
+// Those that a query with the range [lo, hi) does not see; `sinks` for tile rows below that.
+__device__ __forceinline__ void keep_seen(f32x16& x, int at, int lo, int hi, int sinks, bool below_sinks, float hidden) {
+  if (!below_sinks) {
+    keep(x, at, lo, hi, hidden);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int j = at + 8 * (i >> 2) + (i & 3);
+    x[i] = j < hi && (j >= lo || j < sinks) ? x[i] : hidden;
+  }
+}
+
 // Rows [r0, r0 + 64) of one head of a tensor straight into a tile (rows past the tensor's end become zeros), by `WAVES` waves.  The
 // descriptor starts at the tile, so that 32-bit offsets do whatever the tensor's size is.
 template <typename T, int WAVES>

@@ -150,13 +150,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
           clear(s[u][b]);
 #pragma unroll
           for (int c = 0; c < P::kSteps; ++c) s[u][b] = P::product(ka[c], qf[b][c], s[u][b]);
-          if (!all) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int j = key + 32 * (u0 + u) + 8 * (i >> 2) + 4 * g + (i & 3);
-              s[u][b][i] = j < hi[b] && (j >= lo[b] || j < a.seen.sinks) ? s[u][b][i] : -INFINITY;
-            }
-          }
+          if (!all) keep_seen(s[u][b], key + 32 * (u0 + u) + 4 * g, lo[b], hi[b], a.seen.sinks, key + 32 * (u0 + u) < a.seen.sinks, -INFINITY);
         }
       }
       typename P::A w[U][R][P::kCols];

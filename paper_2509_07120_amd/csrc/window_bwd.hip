@@ -334,6 +334,7 @@ __device__ __forceinline__ void query_rows(const BwdArgs& a, int64_t block, int6
     const unsigned char* const vt = kt + kTileBytes;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
+      if (key + 32 * u >= hi_max || (key + 32 * u + 32 <= lo_min && key + 32 * u >= a.seen.sinks)) continue;  // no query of the wave sees these
       typename P::A w[P::kCols];
       {
         typename P::A ka[P::kSteps], va[P::kSteps];
@@ -358,13 +359,7 @@ __device__ __forceinline__ void query_rows(const BwdArgs& a, int64_t block, int6
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * a.scale_log2) * dp[i];
-        if (!all) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int j = key + 32 * u + 8 * (i >> 2) + 4 * g + (i & 3);
-            s[i] = j < hi && (j >= lo || j < a.seen.sinks) ? s[i] : 0.f;
-          }
-        }
+        if (!all) keep_seen(s, key + 32 * u + 4 * g, lo, hi, a.seen.sinks, key + 32 * u < a.seen.sinks, 0.f);
         P::round(s, w);
       }
 #pragma unroll
@@ -569,6 +564,7 @@ __device__ __forceinline__ void key_rows(const BwdArgs& a, int64_t block, int64_
     const unsigned char* const st = dt + kTileBytes;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
+      if (i0 + 32 * u >= some_last || i0 + 32 * u + 32 <= head.first) continue;  // no key of the wave is seen by these
       f32x16 p, ds;
       clear(p);
       clear(ds);
@@ -601,13 +597,8 @@ __device__ __forceinline__ void key_rows(const BwdArgs& a, int64_t block, int64_
         ds[e] *= p[e];
       }
       if (!all) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int i = i0 + 32 * u + 8 * (e >> 2) + 4 * g + (e & 3);
-          const bool sees = i >= see.first && i < see.last;
-          p[e] = sees ? p[e] : 0.f;
-          ds[e] = sees ? ds[e] : 0.f;
-        }
+        keep(p, i0 + 32 * u + 4 * g, see.first, see.last, 0.f);
+        keep(ds, i0 + 32 * u + 4 * g, see.first, see.last, 0.f);
       }
       typename P::A pw[P::kCols], dw[P::kCols];
       P::round(p, pw);
