@@ -68,6 +68,13 @@ __device__ void exact_row(const WindowArgs& a, const unsigned char* q, const uns
   if (lse != nullptr && lane == 0) *lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
+// The larger of what lanes n and n + 32 have, in both, without the way through LDS.
+__device__ __forceinline__ float top_of_halves(float x) {
+  const unsigned u = __float_as_uint(x);
+  const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+}
+
 template <int N>
 using Int = std::integral_constant<int, N>;
 
@@ -161,7 +168,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void window_kernel(const WindowArgs 
         for (int u = 0; u < U; ++u)
 #pragma unroll
           for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][b][i]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+        top = top_of_halves(top) * a.scale_log2;
         const bool raise = m[b] == -INFINITY ? top > -INFINITY : top > m[b] + kRaise;
         if (__any(raise)) {
           const float to = raise ? top : m[b];
