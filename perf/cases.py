@@ -7,7 +7,7 @@ dimension 64; 1 to 16 heads (16 for a whole layer, fewer for one rank of a head-
 thresholds tau from 0.8 to 0.95 and top-k sparsities rho from 0.5 to 0.9.  The values are the
 correspondence-structured activations of workload/synthetic.py, drawn on the GPU.
 
-The package is inference only: it has no backward pass.
+These paths are inference only: none of them has a backward pass.
 """
 import math
 
