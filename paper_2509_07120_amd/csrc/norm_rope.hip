@@ -433,7 +433,7 @@ int bsga_qk_norm_rope(const void* q, const void* k, const void* v, int64_t q_tok
                       {q_weight, k_weight}, {q_bias, k_bias}, positions, axes, base, a))
     return rc;
   for (int t = 0; t < 3; ++t) {
-    if (!x[t] != !y[t]) return fail(BSGA_ERR_INVALID_ARG, "%s: each input must come with its output", fn);
+    if (n_tokens > 0 && !x[t] != !y[t]) return fail(BSGA_ERR_INVALID_ARG, "%s: each input must come with its output", fn);
     if (!aligned16(y[t])) return fail(BSGA_ERR_INVALID_ARG, "%s: outputs must be 16-byte aligned", fn);
     a.y[t] = static_cast<unsigned char*>(y[t]);
   }
@@ -491,7 +491,7 @@ int bsga_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const 
     return rc;
   const int size = dtype == BSGA_BF16 ? 2 : 4;
   for (int t = 0; t < 3; ++t) {
-    if (!x[t] != !dy[t] || !x[t] != !dx[t])
+    if (n_tokens > 0 && (!x[t] != !dy[t] || !x[t] != !dx[t]))
       return fail(BSGA_ERR_INVALID_ARG, "%s: q and k come with the gradients of both sides, dv with dv_in", fn);
     if (!aligned16(dy[t]) || !aligned16(dx[t])) return fail(BSGA_ERR_INVALID_ARG, "%s: gradients must be 16-byte aligned", fn);
     const int64_t st = out_strides[2 * t], sh = out_strides[2 * t + 1];
