@@ -155,7 +155,7 @@ class StreamAttention(torch.nn.Module):
         positions = self._places(x.shape[0], x.device) if positions is None else positions
         q, k, v = qk_norm_rope(q, k, v, positions, self.q_weight, self.k_weight, self.q_bias, self.k_bias, norm=self.norm, base=self.base)
         o = window_attention(q, k, v, **self.seen)
-        return F.linear(o.transpose(0, 1).reshape(x.shape[0], -1), self.w_out, self.b_out)
+        return F.linear(o.transpose(0, 1).reshape(x.shape[0], self.heads * 64), self.w_out, self.b_out)
 
     def _linear(self, x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor) -> torch.Tensor:
         return B.bsga_linear(x, weight, bias) if x.dtype == torch.bfloat16 and x.shape[0] > 0 else F.linear(x, weight, bias)
@@ -174,7 +174,7 @@ class StreamAttention(torch.nn.Module):
         # (what the attention reads in one piece goes into the pages as well; it is normed and turned already)
         B.bsga_qk_norm_rope(k.transpose(0, 1), k.transpose(0, 1), v=v.transpose(0, 1), norm=None, k_cache=cache.k, v_cache=cache.v, slots=slots)
         o = B.bsga_window_attn(q, k, v, **self.seen)
-        return self._linear(B.bsga_merge_heads(o), self.w_out, self.b_out)
+        return self._linear(B.bsga_merge_heads(o) if N > 0 else o.view(0, self.heads * 64), self.w_out, self.b_out)
 
     @torch.no_grad()
     def step(self, x: torch.Tensor, cache: PagedCache, positions: Optional[torch.Tensor] = None) -> torch.Tensor:
