@@ -504,6 +504,9 @@ int bsga_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const 
   }
   if (d_weights && norm == BSGA_NORM_NONE) return fail(BSGA_ERR_INVALID_ARG, "%s: gradients of weights go with a norm", fn);
   if (d_weights && n_tokens > 0) {
+    // (the workspace's size goes by both, an absent tensor's as well, and would be 0 for what is no number of heads)
+    if (heads < 0 || heads > 65535 || kv_heads < 0 || kv_heads > 65535)
+      return fail(BSGA_ERR_INVALID_ARG, "%s: heads and kv_heads must be in [0, 65535], got %d and %d", fn, heads, kv_heads);
     const size_t need = bsga_qk_norm_rope_bwd_workspace_bytes(n_tokens, heads, kv_heads);
     if (!workspace || workspace_bytes < need)
       return fail(BSGA_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace ? workspace_bytes : 0, need);
