@@ -439,7 +439,7 @@ int bsga_qk_norm_rope(const void* q, const void* k, const void* v, int64_t q_tok
   }
   if (slots) {
     if (page < 1 || page > 65536) return fail(BSGA_ERR_INVALID_ARG, "%s: page must be in [1, 65536] tokens, got %d", fn, page);
-    if (n_pages < 1 || n_pages * page > (int64_t(1) << 31) - 1)
+    if (n_pages < 1 || n_pages > ((int64_t(1) << 31) - 1) / page)
       return fail(BSGA_ERR_INVALID_ARG, "%s: the cache must hold 1 to 2^31 - 1 tokens, got %lld pages of %d", fn, static_cast<long long>(n_pages), page);
     a.slots = slots;
     a.page = page;

@@ -328,7 +328,7 @@ int check_sizes(const char* fn, int dtype, int64_t batch, int heads, int kv_head
   if (page < 1 || page > 65536) return fail(BSGA_ERR_INVALID_ARG, "%s: page must be in [1, 65536] tokens, got %d", fn, page);
   const int64_t most = int64_t(1) << 30;
   if (n_pages < 0 || n_pages > most) return fail(BSGA_ERR_INVALID_ARG, "%s: n_pages must be in [0, 2^30], got %lld", fn, (long long)n_pages);
-  if (table_width < 0 || table_width * page > most)
+  if (table_width < 0 || table_width > most / page)
     return fail(BSGA_ERR_INVALID_ARG, "%s: a sequence's pages must hold up to 2^30 tokens, got %lld pages", fn, (long long)table_width);
   if (frame < 1 || frame > (1 << 24)) return fail(BSGA_ERR_INVALID_ARG, "%s: frame must be in [1, 2^24] tokens, got %lld", fn, (long long)frame);
   if (window < 0) return fail(BSGA_ERR_INVALID_ARG, "%s: window must be >= 0 frames (0: no limit), got %lld", fn, (long long)window);
