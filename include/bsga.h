@@ -360,6 +360,7 @@ int bsga_window_attn(const void* q, const void* k, const void* v, int64_t q_toke
  * Its gradient.  dout [heads, n_q, 64] is the gradient of out; q, k, v and the rest as they were given, out and lse as bsga_window_attn
  * returned them.  dq [heads, n_q, 64], dk and dv [kv_heads, n_k, 64] out (sums over the query heads that share a key head); keys
  * that no query sees get zeros, queries that see nothing too.
+ *   softmax_scale  at least 2^-120 (its reciprocal has to fit beside a logarithm)
  *   workspace  bsga_window_attn_bwd_workspace_bytes(...) bytes, 16-byte aligned; overwritten
  * bf16: products on bf16 MFMA, the weights and their gradients rounded to bf16 for the last product, sums in fp32.  No atomics: the same bits every time.
  */

@@ -942,7 +942,9 @@ int bsga_window_attn_bwd(const void* dout, const void* q, const void* k, const v
   if (heads < 1 || heads > 65535 || kv_heads < 1 || heads % kv_heads != 0)
     return fail(BSGA_ERR_INVALID_ARG, "%s: heads must be in [1, 65535] and a multiple of kv_heads, got %d and %d", fn, heads, kv_heads);
   if (int rc = check_seen(fn, n_q, n_k, q_start, frame, window, sinks, a.seen)) return rc;
-  if (!(softmax_scale > 0.0f) || !isfinite(softmax_scale)) return fail(BSGA_ERR_INVALID_ARG, "%s: softmax_scale must be finite and > 0", fn);
+  // (-lse / scale is what a query's sums begin with: below about 5e-38 that of a logarithm alone would be infinite, and every weight zero)
+  if (!(softmax_scale >= 0x1p-120f) || !isfinite(softmax_scale))
+    return fail(BSGA_ERR_INVALID_ARG, "%s: softmax_scale must be finite and at least 2^-120", fn);
   if (n_q == 0 && n_k == 0) return BSGA_OK;
   const int size = dtype == BSGA_BF16 ? 2 : 4;
   if (n_q > 0) {
