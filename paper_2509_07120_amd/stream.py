@@ -99,8 +99,12 @@ class PagedCache:
         self.lengths.copy_(self._send(self._length, self.lengths))
         return self._send(slots, self.lengths)
 
-    def trim(self, window: int, sinks: int = 0, frame: int = 1) -> int:
-        """Frees the pages that no later query sees; returns how many."""
+    def trim(self, window: Optional[int], sinks: int = 0, frame: int = 1) -> int:
+        """Frees the pages that no later query sees (window = None: none); returns how many."""
+        if (window is not None and window < 1) or sinks < 0 or frame < 1:
+            raise ValueError(f"window must be at least one frame, or None, sinks >= 0 and frame >= 1, got {window}, {sinks} and {frame}")
+        if window is None:
+            return 0
         freed = 0
         for b, n in enumerate(self._length):
             if n == 0:

@@ -1,0 +1,47 @@
+"""Bookkeeping of the paged cache, which is the host's: no GPU is needed."""
+import pytest
+import torch
+
+
+def _cache(*args, **kw):
+    import paper_2509_07120_amd as pkg
+    return pkg.PagedCache(*args, device="cpu", **kw)
+
+
+def _state(c):
+    return c.page_table.tolist(), c.lengths.tolist(), list(c._free), [list(p) for p in c._pages], list(c._length)
+
+
+def test_trim_without_a_window_frees_nothing():
+    c = _cache(2, 5, 1, page=4)
+    c.grow([6, 3])
+    before = _state(c)
+    assert c.trim(None) == 0 and c.trim(window=None, sinks=3, frame=2) == 0
+    assert _state(c) == before
+
+
+@pytest.mark.parametrize("window,sinks,frame", [(0, 0, 1), (-1, 0, 1), (2, -1, 1), (2, 0, 0), (2, 0, -3), (None, -1, 1), (None, 0, 0)])
+def test_trim_refuses_what_the_attention_refuses(window, sinks, frame):
+    """(0 is "no limit" at the C interface: taken as a window of nothing it would free tokens that are seen, the last ones among them)"""
+    c = _cache(1, 3, 1, page=4)
+    c.grow([6])
+    before = _state(c)
+    with pytest.raises(ValueError, match="window|sinks|frame"):
+        c.trim(window, sinks, frame)
+    assert _state(c) == before
+    assert c.grow([3]).tolist() == [6, 7, 8]
+
+
+@pytest.mark.parametrize("window", [1, 2, 3, 7])
+@pytest.mark.parametrize("sinks", [0, 1, 5, 9])
+@pytest.mark.parametrize("frame", [1, 3, 10])
+@pytest.mark.parametrize("page", [1, 4, 7])
+def test_trim_keeps_what_later_queries_see(window, sinks, frame, page):
+    for n in range(1, 60, 4):
+        c = _cache(1, 80, 1, page=page, dtype=torch.float32)
+        c.grow([n])
+        c.trim(window, sinks, frame)
+        seen = {j for p in range(n - 1, n + 40) for j in range(n) if j // frame <= p // frame and (p // frame - j // frame < window or j < sinks)}
+        assert all(c._pages[0][j // page] >= 0 for j in seen)
+        kept = {i for i, p in enumerate(c._pages[0]) if p >= 0}
+        assert kept == {j // page for j in seen} | {(n - 1) // page}  # and nothing else
