@@ -62,7 +62,8 @@ def window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: 
 
 class PagedCache:
     """Keys and values of several sequences in pages [pages, kv_heads, page, 64], and which page holds which tokens.  The bookkeeping is
-    the host's; grow() and trim() bring the device's table and lengths up to date on the current stream."""
+    the host's; grow() and trim() bring the device's table and lengths up to date on the current stream.  Places of the table without a page, of
+    freed ones too, hold -1, which bsga_paged_attn takes for page 0: check_seen() tells whether a window reaches them."""
 
     def __init__(self, sequences: int, pages: int, kv_heads: int, page: int = 64, width: Optional[int] = None, dtype=torch.bfloat16,
                  device="cuda"):
@@ -74,6 +75,7 @@ class PagedCache:
         self._free = list(range(pages - 1, -1, -1))
         self._pages: List[List[int]] = [[] for _ in range(sequences)]
         self._length = [0] * sequences
+        self._freed = [(0, 0)] * sequences  # (all of a sequence's freed pages lie in [first, end))
 
     def _send(self, values, like: torch.Tensor) -> torch.Tensor:
         return torch.tensor(values, dtype=torch.int32).to(like.device)
@@ -110,12 +112,28 @@ class PagedCache:
             if n == 0:
                 continue
             lo = max(0, ((n - 1) // frame + 1 - window) * frame)
-            for i in range(-(-min(sinks, lo) // self.page), lo // self.page):
-                if self._pages[b][i] >= 0:
-                    self._free.append(self._pages[b][i])
-                    self._pages[b][i] = -1
-                    freed += 1
+            gone = [i for i in range(-(-min(sinks, lo) // self.page), lo // self.page) if self._pages[b][i] >= 0]
+            if not gone:
+                continue
+            for i in gone:
+                self._free.append(self._pages[b][i])
+                self._pages[b][i] = -1
+            first, end = gone[0], gone[-1] + 1  # (what lies between them is freed)
+            self.page_table[b, first:end] = -1
+            before = self._freed[b]
+            self._freed[b] = (first, end) if before[0] == before[1] else (min(first, before[0]), max(end, before[1]))
+            freed += len(gone)
         return freed
+
+    def check_seen(self, window: Optional[int], sinks: int = 0, frame: int = 1) -> None:
+        """Raises if the next token of a sequence would see tokens whose pages trim() has freed."""
+        for b, (first, end) in enumerate(self._freed):
+            if first == end:
+                continue
+            lo = 0 if window is None else max(0, (self._length[b] // frame + 1 - window) * frame)
+            kept, near = -(-min(sinks, lo) // self.page), lo // self.page  # pages [0, kept) and from `near` on are seen
+            if any(self._pages[b][i] < 0 for part in (range(first, min(kept, end)), range(max(first, near), end)) for i in part):
+                raise ValueError(f"sequence {b} of the cache: tokens that a window of {window} with {sinks} first tokens sees have been freed")
 
 
 class StreamAttention(torch.nn.Module):
@@ -183,6 +201,7 @@ class StreamAttention(torch.nn.Module):
     @torch.no_grad()
     def step(self, x: torch.Tensor, cache: PagedCache, positions: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x [sequences, heads * 64], one token for each sequence."""
+        cache.check_seen(**self.seen)
         positions = cache.lengths.clone() if positions is None else positions
         slots = cache.grow([1] * x.shape[0])
         q, k, v = self._split(self._linear(x, self.w_qkv, self.b_qkv))

@@ -45,3 +45,48 @@ def test_trim_keeps_what_later_queries_see(window, sinks, frame, page):
         assert all(c._pages[0][j // page] >= 0 for j in seen)
         kept = {i for i, p in enumerate(c._pages[0]) if p >= 0}
         assert kept == {j // page for j in seen} | {(n - 1) // page}  # and nothing else
+
+
+def test_trim_takes_freed_pages_out_of_the_table():
+    c = _cache(2, 9, 1, page=4)
+    c.grow([23, 10])
+    assert c.trim(5, sinks=2) > 0
+    assert c.page_table[0].tolist() == [0, -1, -1, -1, 4, 5] + [-1] * 3  # tokens 18 to 22 and the first 2 stay
+    assert c.page_table[1].tolist() == [6, 7, 8] + [-1] * 6
+    assert sorted(c.grow([0, 12]).tolist()) == sorted([4 * 8 + 2, 4 * 8 + 3] + [4 * p + i for p in (3, 2) for i in range(4)] + [4, 5])
+    assert c.page_table[0].tolist() == [0, -1, -1, -1, 4, 5] + [-1] * 3
+
+
+@pytest.mark.parametrize("trimmed", [(5, 2, 1), (2, 0, 3), (1, 7, 4), (3, 9, 2)])
+@pytest.mark.parametrize("page", [1, 4])
+def test_windows_that_see_freed_tokens(trimmed, page):
+    """check_seen(), against the rule itself for the next token of every sequence."""
+    for window, sinks, frame in [(w, s, f) for w in (None, 1, 2, 3, 5, 6, 40) for s in (0, 2, 3, 7, 20) for f in (1, 2, 3, 4)]:
+        c = _cache(2, 200, 1, page=page)
+        c.check_seen(window, sinks, frame)  # nothing there, nothing freed
+        c.grow([23, 2])
+        c.check_seen(window, sinks, frame)
+        c.trim(*trimmed)
+        c.grow([6, 6])
+        c.trim(*trimmed)
+        bad = False
+        for b, p in ((0, 29), (1, 8)):
+            seen = [j for j in range(p) if j // frame <= p // frame and (window is None or p // frame - j // frame < window or j < sinks)]
+            bad |= any(c._pages[b][j // page] < 0 for j in seen)
+        if bad:
+            with pytest.raises(ValueError, match="sequence [01].*freed"):
+                c.check_seen(window, sinks, frame)
+        else:
+            c.check_seen(window, sinks, frame)
+
+
+def test_a_step_asks_before_it_grows():
+    import paper_2509_07120_amd as pkg
+    layer = pkg.StreamAttention(2, 1, window=9, dtype=torch.float32, device="cpu")
+    c = _cache(1, 9, 1, page=4, dtype=torch.float32)
+    c.grow([20])
+    c.trim(3)
+    before = _state(c)
+    with pytest.raises(ValueError, match="freed"):
+        layer.step(torch.zeros(1, 128), c)
+    assert _state(c) == before
