@@ -13,6 +13,7 @@ import torch.nn.functional as F
 from torch.autograd.function import once_differentiable
 
 from . import binding as B
+from .block import _calls_are_watched
 
 
 class _QkNormRope(torch.autograd.Function):
@@ -136,6 +137,22 @@ class PagedCache:
                 raise ValueError(f"sequence {b} of the cache: tokens that a window of {window} with {sinks} first tokens sees have been freed")
 
 
+def _takes(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor) -> bool:
+    """Whether a linear layer goes by bsga_linear: what that takes and gains by (GlobalAttentionBlock has the widths and what was measured), and
+    where torch's operation would be no more than its result."""
+    if type(x) is not torch.Tensor or x.dim() != 2 or not x.is_cuda or torch.is_autocast_enabled() or _calls_are_watched():
+        return False
+    N, D = x.shape
+    if any(type(t) is not torch.Tensor and type(t) is not torch.nn.Parameter for t in (weight, bias)):
+        return False
+    if any(t.dtype != torch.bfloat16 or t.device != x.device or not t.is_contiguous() or t.data_ptr() % 16 for t in (x, weight, bias)):
+        return False
+    if N < 1 or weight.shape[1] != D or (D > 1280 and (D > 2048 or N > 4096)):
+        return False
+    rows = weight.shape[0]
+    return max((N + 256) * D, (rows + 256) * D, N * rows) * 2 < 1 << 31
+
+
 class StreamAttention(torch.nn.Module):
     """One attention layer of such a model: x [N, heads * 64] -> [N, heads * 64], `kv_heads` key heads, norms of queries and keys for each
     head, rotation by positions ([N] or [N, axes] int32; by default a token's place in the sequence), window of `window` frames
@@ -180,7 +197,7 @@ class StreamAttention(torch.nn.Module):
         return F.linear(o.transpose(0, 1).reshape(x.shape[0], self.heads * 64), self.w_out, self.b_out)
 
     def _linear(self, x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor) -> torch.Tensor:
-        return B.bsga_linear(x, weight, bias) if x.dtype == torch.bfloat16 and x.shape[0] > 0 else F.linear(x, weight, bias)
+        return B.bsga_linear(x, weight, bias) if _takes(x, weight, bias) else F.linear(x, weight, bias)
 
     @torch.no_grad()
     def prefill(self, x: torch.Tensor, cache: PagedCache, b: int, positions: Optional[torch.Tensor] = None) -> torch.Tensor:

@@ -39,3 +39,73 @@ def test_empty_prompt(B, dtype):
     for i in range(5):
         o = layer.step(x[i:i + 1].repeat(2, 1), cache)
         assert float((o.double() - whole[i].double()).abs().max()) <= bar
+
+
+def _near(a, b, dtype=torch.bfloat16):
+    bar = 12 * 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -13  # outputs of O(1), a few roundings of values up to about 4
+    return float((a.double() - b.double()).abs().max()) <= bar
+
+
+class _Sees(torch.overrides.TorchFunctionMode):
+    def __init__(self):
+        super().__init__()
+        self.linear = 0
+
+    def __torch_function__(self, func, types, args=(), kwargs=None):
+        self.linear += func is torch.nn.functional.linear
+        return func(*args, **(kwargs or {}))
+
+
+class _Weight(torch.nn.Parameter):
+    pass
+
+
+def _unaligned(x):
+    return torch.cat([x.new_zeros(1), x.flatten()])[1:].view(x.shape)
+
+
+@pytest.mark.parametrize("what", ["nothing", "strided", "unaligned", "autocast", "function mode", "dispatch mode", "subclass", "width"])
+def test_prompts_and_steps_take_what_torch_s_linear_layer_takes(B, what, monkeypatch):
+    """By the library's linear layer where nothing asks for torch's, by torch's otherwise; the same outputs as forward() either way."""
+    from torch.utils.flop_counter import FlopCounterMode
+
+    import paper_2509_07120_amd.binding as binding
+    heads = 33 if what == "width" else 4
+    d = heads * 64
+    layer = B.StreamAttention(heads, 1, window=40, sinks=3)
+    cache = B.PagedCache(2, 40, 1, page=16)
+    x = _x(100, d, torch.bfloat16)
+    if what == "subclass":
+        layer.w_qkv, layer.b_out = _Weight(layer.w_qkv.data), _Weight(layer.b_out.data)
+    want = layer(x).detach()
+    calls, own = [], binding.bsga_linear
+    monkeypatch.setattr(binding, "bsga_linear", lambda *a, **k: calls.append(1) or own(*a, **k))
+    arrange = (lambda t: torch.stack([t, t], 2)[..., 0]) if what == "strided" else _unaligned if what == "unaligned" else lambda t: t
+    mode = {"autocast": lambda: torch.autocast("cuda", dtype=torch.bfloat16), "function mode": _Sees,
+            "dispatch mode": lambda: FlopCounterMode(display=False)}.get(what, torch.no_grad)()
+    with mode:
+        for b in range(2):
+            assert _near(layer.prefill(arrange(x[:98]), cache, b), want[:98])
+        for i in (98, 99):
+            step = layer.step(x[i:i + 1].expand(2, -1) if what == "strided" else arrange(x[i:i + 1].repeat(2, 1)), cache)
+            assert _near(step, want[i].expand(2, -1))
+    # (of two prompts and two steps; how x lies says nothing about the second layer)
+    assert len(calls) == {"nothing": 8, "strided": 4, "unaligned": 4}.get(what, 0)
+    if what == "function mode":
+        assert mode.linear == 8
+    if what == "dispatch mode":
+        assert mode.get_total_flops() >= 2 * (2 * 98 + 4) * d * (d + 2 * 64 + d)
+
+
+def test_long_prompt(B):
+    """More tokens than a linear layer of the library takes (outputs of 2 GiB): 255 frames of the headline's size."""
+    n = 255 * 1374
+    layer = B.StreamAttention(16, window=64)
+    cache = B.PagedCache(1, n // 256 + 1, 16, page=256)
+    x = torch.randn((n + 1, 1024), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
+    with torch.no_grad():
+        want = layer(x)
+    got = layer.prefill(x[:n], cache, 0)
+    assert _near(got[-3000:], want[n - 3000:n]) and _near(got[:3000], want[:3000])
+    del got
+    assert _near(layer.step(x[n:], cache), want[n:]) and cache.lengths.tolist() == [n + 1]
