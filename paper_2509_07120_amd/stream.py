@@ -6,6 +6,7 @@ Integration shape only, as GlobalAttentionBlock: random weights.
 """
 from __future__ import annotations
 
+from contextlib import contextmanager
 from typing import List, Optional, Sequence
 
 import torch
@@ -101,6 +102,26 @@ class PagedCache:
             self._length[b] += c
         self.lengths.copy_(self._send(self._length, self.lengths))
         return self._send(slots, self.lengths)
+
+    @contextmanager
+    def growing(self, counts: Sequence[int]):
+        """grow(), taken back if the body, which neither grows nor trims the cache itself, fails."""
+        slots = self.grow(counts)
+        try:
+            yield slots
+        except BaseException:
+            emptied = []
+            for b in range(len(counts) - 1, -1, -1):  # (pages go back in the order that hands them out again as before)
+                self._length[b] -= counts[b]
+                keep = -(-self._length[b] // self.page)
+                if keep < len(self._pages[b]):
+                    emptied.append((b, keep, len(self._pages[b])))
+                    self._free += reversed(self._pages[b][keep:])
+                    del self._pages[b][keep:]
+            for b, first, end in emptied:
+                self.page_table[b, first:end] = -1
+            self.lengths.copy_(self._send(self._length, self.lengths))
+            raise
 
     def trim(self, window: Optional[int], sinks: int = 0, frame: int = 1) -> int:
         """Frees the pages that no later query sees (window = None: none); returns how many."""
@@ -206,23 +227,23 @@ class StreamAttention(torch.nn.Module):
         N = x.shape[0]
         counts = [0] * len(cache._length)
         counts[b] = N
-        slots = cache.grow(counts)
-        q, k, v = self._split(self._linear(x, self.w_qkv, self.b_qkv))
-        positions = self._places(N, x.device) if positions is None else positions
-        q, k, v = B.bsga_qk_norm_rope(q, k, positions, self.q_weight, self.k_weight, self.q_bias, self.k_bias, v=v, norm=self.norm, base=self.base)
-        # (what the attention reads in one piece goes into the pages as well; it is normed and turned already)
-        B.bsga_qk_norm_rope(k.transpose(0, 1), k.transpose(0, 1), v=v.transpose(0, 1), norm=None, k_cache=cache.k, v_cache=cache.v, slots=slots)
-        o = B.bsga_window_attn(q, k, v, **self.seen)
-        return self._linear(B.bsga_merge_heads(o) if N > 0 else o.view(0, self.heads * 64), self.w_out, self.b_out)
+        with cache.growing(counts) as slots:
+            q, k, v = self._split(self._linear(x, self.w_qkv, self.b_qkv))
+            positions = self._places(N, x.device) if positions is None else positions
+            q, k, v = B.bsga_qk_norm_rope(q, k, positions, self.q_weight, self.k_weight, self.q_bias, self.k_bias, v=v, norm=self.norm, base=self.base)
+            # (what the attention reads in one piece goes into the pages as well; it is normed and turned already)
+            B.bsga_qk_norm_rope(k.transpose(0, 1), k.transpose(0, 1), v=v.transpose(0, 1), norm=None, k_cache=cache.k, v_cache=cache.v, slots=slots)
+            o = B.bsga_window_attn(q, k, v, **self.seen)
+            return self._linear(B.bsga_merge_heads(o) if N > 0 else o.view(0, self.heads * 64), self.w_out, self.b_out)
 
     @torch.no_grad()
     def step(self, x: torch.Tensor, cache: PagedCache, positions: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x [sequences, heads * 64], one token for each sequence."""
         cache.check_seen(**self.seen)
         positions = cache.lengths.clone() if positions is None else positions
-        slots = cache.grow([1] * x.shape[0])
-        q, k, v = self._split(self._linear(x, self.w_qkv, self.b_qkv))
-        q, _, _ = B.bsga_qk_norm_rope(q, k, positions, self.q_weight, self.k_weight, self.q_bias, self.k_bias, v=v, norm=self.norm, base=self.base,
-                                      k_cache=cache.k, v_cache=cache.v, slots=slots)
-        o = B.bsga_paged_attn(q.transpose(0, 1), cache.k, cache.v, cache.page_table, cache.lengths, **self.seen)
-        return self._linear(o.view(x.shape[0], -1), self.w_out, self.b_out)
+        with cache.growing([1] * x.shape[0]) as slots:
+            q, k, v = self._split(self._linear(x, self.w_qkv, self.b_qkv))
+            q, _, _ = B.bsga_qk_norm_rope(q, k, positions, self.q_weight, self.k_weight, self.q_bias, self.k_bias, v=v, norm=self.norm, base=self.base,
+                                          k_cache=cache.k, v_cache=cache.v, slots=slots)
+            o = B.bsga_paged_attn(q.transpose(0, 1), cache.k, cache.v, cache.page_table, cache.lengths, **self.seen)
+            return self._linear(o.view(x.shape[0], -1), self.w_out, self.b_out)

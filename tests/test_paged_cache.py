@@ -90,3 +90,33 @@ def test_a_step_asks_before_it_grows():
     with pytest.raises(ValueError, match="freed"):
         layer.step(torch.zeros(1, 128), c)
     assert _state(c) == before
+
+
+@pytest.mark.parametrize("counts", [[1, 1, 1], [0, 9, 0], [30, 0, 3], [3, 4, 5], [0, 0, 0]])
+def test_what_fails_behind_grow_is_taken_back(counts):
+    c = _cache(3, 30, 1, page=4)
+    c.grow([7, 0, 12])
+    c.trim(2)
+    before, slots = _state(c), []
+    with pytest.raises(KeyError):
+        with c.growing(counts) as got:
+            slots.append(got.tolist())
+            assert c._length == [a + b for a, b in zip([7, 0, 12], counts)]
+            raise KeyError
+    assert _state(c) == before
+    with c.growing(counts) as got:
+        assert got.tolist() == slots[0]  # the same places as the first time
+    assert c.lengths.tolist() == [a + b for a, b in zip([7, 0, 12], counts)]
+
+
+def test_a_prompt_and_a_step_that_fail_leave_the_cache_as_it_was():
+    """(on the CPU: the layer gets as far as the norm, which wants device tensors)"""
+    import paper_2509_07120_amd as pkg
+    layer = pkg.StreamAttention(2, 1, window=9, dtype=torch.float32, device="cpu")
+    c = _cache(2, 9, 1, page=4, dtype=torch.float32)
+    for call in (lambda: layer.prefill(torch.zeros(9, 128), c, 1), lambda: layer.prefill(torch.zeros(9, 64), c, 1),
+                 lambda: layer.step(torch.zeros(2, 128), c), lambda: layer.step(torch.zeros(2, 128), c, torch.zeros(3, dtype=torch.int32))):
+        before = _state(c)
+        with pytest.raises((ValueError, RuntimeError)):
+            call()
+        assert _state(c) == before
