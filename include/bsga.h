@@ -374,7 +374,7 @@ int bsga_window_attn_bwd(const void* dout, const void* q, const void* k, const v
 /*
  * Attention of one new token for each sequence over a cache of pages, for serving.  The query of sequence b stands at position
  * lengths[b] - 1; its own key and value are in the cache already (bsga_qk_norm_rope with slots puts them there).  It sees the keys that
- * bsga_window_attn's rule gives a query at that position (frame, window, sinks as there).
+ * bsga_window_attn's rule gives a query at that position (frame, window, sinks as there), of those that there are: its own frame up to itself.
  *   q           [batch, heads, 64] with strides in elements (multiples of 16 bytes; what bsga_qk_norm_rope returns, seen the other way round, is fine)
  *   k_cache, v_cache  [n_pages, kv_heads, page, 64]
  *   page_table  [batch, table_width] int32: key j of sequence b lies in row j % page of page page_table[b][j / page]; entries that no

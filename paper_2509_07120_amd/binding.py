@@ -870,7 +870,7 @@ def bsga_paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     """Attention of one new token for each sequence, q [B, H, 64] (a view with contiguous rows is fine), over the caches [pages, Hkv, page, 64]:
     key j of sequence b lies in row j % page of page page_table[b, j // page] (int32 [B, width]; entries are clamped to the pages there are).
     The query of sequence b stands at position lengths[b] - 1 (int32 [B]), its own key is in the cache already; it sees what
-    bsga_window_attn's rule gives a query there.  Returns O [B, H, 64] (and lse [B, H] float32); a sequence of length 0 yields zeros and -inf."""
+    bsga_window_attn's rule gives a query there (its own frame up to itself: later tokens are not there).  Returns O [B, H, 64] (and lse [B, H] float32); a sequence of length 0 yields zeros and -inf."""
     code = _dtype_code(q)
     if not q.is_cuda:
         raise ValueError("q must be a device tensor")

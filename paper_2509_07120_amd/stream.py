@@ -180,7 +180,9 @@ class StreamAttention(torch.nn.Module):
     of `frame` tokens and the first `sinks` tokens (see bsga_window_attn).
 
     forward(x) takes a whole sequence, with gradients; prefill(x, cache, b) the same for sequence b of an empty cache, and fills it;
-    step(x, cache) one more token for every sequence of the cache."""
+    step(x, cache) one more token for every sequence of the cache.  With frame > 1 that is another function than forward() and prefill(), whose tokens
+    see their whole frame: a token that comes alone sees its own frame up to itself, since the others are not there yet.  There is no way yet to
+    take a whole new frame on a cache."""
 
     def __init__(self, heads: int = 16, kv_heads: Optional[int] = None, window: Optional[int] = None, sinks: int = 0, frame: int = 1,
                  norm: str = "rms", base: float = 10000.0, dtype=torch.bfloat16, device="cuda", seed: int = 0):

@@ -109,3 +109,64 @@ def test_long_prompt(B):
     assert _near(got[-3000:], want[n - 3000:n]) and _near(got[:3000], want[:3000])
     del got
     assert _near(layer.step(x[n:], cache), want[n:]) and cache.lengths.tolist() == [n + 1]
+
+
+def test_single_tokens_of_a_frame(B):
+    """Steps of a layer whose tokens see their whole frame: against float64 over the keys that are there, which of the token's own frame are those up
+    to itself.  A whole sequence sees the later ones as well, and gives something else."""
+    frame, n, start = 10, 137, 90
+    layer = B.StreamAttention(4, 2, window=2, sinks=13, frame=frame, norm="layer")
+    cache = B.PagedCache(1, 20, 2, page=16)
+    x = _x(n, 256, torch.bfloat16)
+    params = {name: p.detach().double() for name, p in layer.named_parameters()}
+    at, key = torch.arange(n, device="cuda")[:, None], torch.arange(n, device="cuda")[None]
+    near = (at // frame - key // frame < 2) | (key < 13)
+    want = _definition(layer, x.double(), params, (key // frame <= at // frame) & near & ((key <= at) | (at < start)))
+    whole = layer(x).detach()
+    assert _near(layer.prefill(x[:start], cache, 0), want[:start]) and _near(whole[:start], want[:start])
+    differs = 0
+    for i in range(start, n):
+        assert _near(layer.step(x[i:i + 1], cache), want[i:i + 1])
+        differs += not _near(whole[i:i + 1], want[i:i + 1])
+    assert differs > 20  # (all but the last of each frame, and where too little is missing to tell)
+
+
+def _definition(layer, x, p, seen):
+    """The layer in float64, its parameters in p, under a mask."""
+    N, H, K = x.shape[0], layer.heads, layer.kv_heads
+    q, k, v = (x @ p["w_qkv"].T + p["b_qkv"]).view(N, H + 2 * K, 64).split([H, K, K], 1)
+    turn = torch.arange(N, device="cuda").double()[:, None, None] * layer.base ** (-torch.arange(32, device="cuda").double() / 32)
+
+    def rows(t, name):
+        if layer.norm == "layer":
+            t = t - t.mean(-1, keepdim=True)
+        t = t / (t.square().mean(-1, keepdim=True) + 1e-6).sqrt() * p[name + "_weight"] + p.get(name + "_bias", 0.0)
+        z = torch.complex(t[..., :32], t[..., 32:]) * torch.polar(torch.ones_like(turn), turn)
+        return torch.cat([z.real, z.imag], -1).transpose(0, 1)
+
+    q, k, v = rows(q, "q"), rows(k, "k").repeat_interleave(H // K, 0), v.transpose(0, 1).repeat_interleave(H // K, 0)
+    w = (q @ k.transpose(1, 2).contiguous() / 8).masked_fill(~seen, -torch.inf).softmax(-1)
+    return (w @ v).transpose(0, 1).reshape(N, -1) @ p["w_out"].T + p["b_out"]
+
+
+@pytest.mark.parametrize("window,sinks,page", [(40, 3, 16), (33, 0, 4), (16, 20, 8)])
+def test_steps_on_pages_that_were_freed_before(B, window, sinks, page):
+    """A cache with room for the windows only: every step gets what forward() gives, on pages that held other tokens before."""
+    layer = B.StreamAttention(4, 2, window=window, sinks=sinks)
+    need = -(-window // page) + 2 + -(-sinks // page) + 1
+    cache = B.PagedCache(2, 2 * need, 2, page=page, width=300 // page + 1)
+    xs = [_x(n, 256, torch.bfloat16, n) for n in (260, 270)]
+    whole = [layer(x).detach() for x in xs]
+    lens = (30, 40)
+    for b in range(2):
+        layer.prefill(xs[b][:lens[b]], cache, b)
+    held = {}
+    for i in range(230):
+        freed = cache.trim(window, sinks)
+        out = layer.step(torch.stack([x[n + i] for x, n in zip(xs, lens)]), cache)
+        for b in range(2):
+            for place, p in enumerate(cache._pages[b]):
+                if p >= 0:
+                    held.setdefault(p, set()).add((b, place))
+            assert _near(out[b], whole[b][lens[b] + i]), (b, i, freed)
+    assert max(len(places) for places in held.values()) >= 3
