@@ -176,8 +176,8 @@ def _takes(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor) -> bool:
 
 class StreamAttention(torch.nn.Module):
     """One attention layer of such a model: x [N, heads * 64] -> [N, heads * 64], `kv_heads` key heads, norms of queries and keys for each
-    head, rotation by positions ([N] or [N, axes] int32; by default a token's place in the sequence), window of `window` frames
-    of `frame` tokens and the first `sinks` tokens (see bsga_window_attn).
+    head (with `eps` beside the mean square or the variance), rotation by positions ([N] or [N, axes] int32; by default a token's place in the
+    sequence), window of `window` frames of `frame` tokens and the first `sinks` tokens (see bsga_window_attn).
 
     forward(x) takes a whole sequence, with gradients; prefill(x, cache, b) the same for sequence b of an empty cache, and fills it;
     step(x, cache) one more token for every sequence of the cache.  With frame > 1 that is another function than forward() and prefill(), whose tokens
@@ -185,11 +185,11 @@ class StreamAttention(torch.nn.Module):
     take a whole new frame on a cache."""
 
     def __init__(self, heads: int = 16, kv_heads: Optional[int] = None, window: Optional[int] = None, sinks: int = 0, frame: int = 1,
-                 norm: str = "rms", base: float = 10000.0, dtype=torch.bfloat16, device="cuda", seed: int = 0):
+                 norm: str = "rms", base: float = 10000.0, dtype=torch.bfloat16, device="cuda", seed: int = 0, eps: float = 1e-6):
         super().__init__()
         self.heads, self.kv_heads = heads, heads if kv_heads is None else kv_heads
         self.seen = dict(window=window, sinks=sinks, frame=frame)
-        self.norm, self.base = norm, base
+        self.norm, self.base, self.eps = norm, base, eps
         d, rows = heads * 64, (heads + 2 * self.kv_heads) * 64
         g = torch.Generator(device="cpu").manual_seed(seed)
 
@@ -215,7 +215,7 @@ class StreamAttention(torch.nn.Module):
     def forward(self, x: torch.Tensor, positions: Optional[torch.Tensor] = None) -> torch.Tensor:
         q, k, v = self._split(F.linear(x, self.w_qkv, self.b_qkv))
         positions = self._places(x.shape[0], x.device) if positions is None else positions
-        q, k, v = qk_norm_rope(q, k, v, positions, self.q_weight, self.k_weight, self.q_bias, self.k_bias, norm=self.norm, base=self.base)
+        q, k, v = qk_norm_rope(q, k, v, positions, self.q_weight, self.k_weight, self.q_bias, self.k_bias, norm=self.norm, eps=self.eps, base=self.base)
         o = window_attention(q, k, v, **self.seen)
         return F.linear(o.transpose(0, 1).reshape(x.shape[0], self.heads * 64), self.w_out, self.b_out)
 
@@ -232,7 +232,8 @@ class StreamAttention(torch.nn.Module):
         with cache.growing(counts) as slots:
             q, k, v = self._split(self._linear(x, self.w_qkv, self.b_qkv))
             positions = self._places(N, x.device) if positions is None else positions
-            q, k, v = B.bsga_qk_norm_rope(q, k, positions, self.q_weight, self.k_weight, self.q_bias, self.k_bias, v=v, norm=self.norm, base=self.base)
+            q, k, v = B.bsga_qk_norm_rope(q, k, positions, self.q_weight, self.k_weight, self.q_bias, self.k_bias, v=v, norm=self.norm, eps=self.eps,
+                                          base=self.base)
             # (what the attention reads in one piece goes into the pages as well; it is normed and turned already)
             B.bsga_qk_norm_rope(k.transpose(0, 1), k.transpose(0, 1), v=v.transpose(0, 1), norm=None, k_cache=cache.k, v_cache=cache.v, slots=slots)
             o = B.bsga_window_attn(q, k, v, **self.seen)
@@ -245,7 +246,7 @@ class StreamAttention(torch.nn.Module):
         positions = cache.lengths.clone() if positions is None else positions
         with cache.growing([1] * x.shape[0]) as slots:
             q, k, v = self._split(self._linear(x, self.w_qkv, self.b_qkv))
-            q, _, _ = B.bsga_qk_norm_rope(q, k, positions, self.q_weight, self.k_weight, self.q_bias, self.k_bias, v=v, norm=self.norm, base=self.base,
-                                          k_cache=cache.k, v_cache=cache.v, slots=slots)
+            q, _, _ = B.bsga_qk_norm_rope(q, k, positions, self.q_weight, self.k_weight, self.q_bias, self.k_bias, v=v, norm=self.norm, eps=self.eps,
+                                          base=self.base, k_cache=cache.k, v_cache=cache.v, slots=slots)
             o = B.bsga_paged_attn(q.transpose(0, 1), cache.k, cache.v, cache.page_table, cache.lengths, **self.seen)
             return self._linear(o.view(x.shape[0], -1), self.w_out, self.b_out)

@@ -140,7 +140,7 @@ def _definition(layer, x, p, seen):
     def rows(t, name):
         if layer.norm == "layer":
             t = t - t.mean(-1, keepdim=True)
-        t = t / (t.square().mean(-1, keepdim=True) + 1e-6).sqrt() * p[name + "_weight"] + p.get(name + "_bias", 0.0)
+        t = t / (t.square().mean(-1, keepdim=True) + layer.eps).sqrt() * p[name + "_weight"] + p.get(name + "_bias", 0.0)
         z = torch.complex(t[..., :32], t[..., 32:]) * torch.polar(torch.ones_like(turn), turn)
         return torch.cat([z.real, z.imag], -1).transpose(0, 1)
 
@@ -170,3 +170,17 @@ def test_steps_on_pages_that_were_freed_before(B, window, sinks, page):
                     held.setdefault(p, set()).add((b, place))
             assert _near(out[b], whole[b][lens[b] + i]), (b, i, freed)
     assert max(len(places) for places in held.values()) >= 3
+
+
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("eps", [1e-6, 0.5])
+def test_eps_of_the_norms(B, norm, eps):
+    """The whole sequence, a prompt and a step with it (0.5 is half of what it stands beside)."""
+    n = 60
+    layer = B.StreamAttention(4, 2, window=40, norm=norm, dtype=torch.float32, eps=eps)
+    x = _x(n, 256, torch.float32)
+    at, key = torch.arange(n, device="cuda")[:, None], torch.arange(n, device="cuda")[None]
+    want = _definition(layer, x.double(), {name: p.detach().double() for name, p in layer.named_parameters()}, (key <= at) & (at - key < 40))
+    cache = B.PagedCache(1, 8, 2, page=16, dtype=torch.float32)
+    assert _near(layer(x).detach(), want, torch.float32)
+    assert _near(layer.prefill(x[:-1], cache, 0), want[:-1], torch.float32) and _near(layer.step(x[-1:], cache), want[-1:], torch.float32)
