@@ -100,8 +100,10 @@ class PagedCache:
                 self.page_table[b, first:first + need[b]] = self._send(self._pages[b][first:], self.page_table)
             slots += [self._pages[b][i // self.page] * self.page + i % self.page for i in range(self._length[b], self._length[b] + c)]
             self._length[b] += c
-        self.lengths.copy_(self._send(self._length, self.lengths))
-        return self._send(slots, self.lengths)
+        both = self._send(self._length + slots, self.lengths)  # (one way to the device for the two)
+        lengths, slots = both.split((len(counts), len(slots)))
+        self.lengths.copy_(lengths)
+        return slots
 
     @contextmanager
     def growing(self, counts: Sequence[int]):
@@ -120,7 +122,7 @@ class PagedCache:
                     del self._pages[b][keep:]
             for b, first, end in emptied:
                 self.page_table[b, first:end] = -1
-            self.lengths.copy_(self._send(self._length, self.lengths))
+            self.lengths.copy_(torch.tensor(self._length, dtype=torch.int32))
             raise
 
     def trim(self, window: Optional[int], sinks: int = 0, frame: int = 1) -> int:
@@ -161,16 +163,17 @@ class PagedCache:
 def _takes(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor) -> bool:
     """Whether a linear layer goes by bsga_linear: what that takes and gains by (GlobalAttentionBlock has the widths and what was measured), and
     where torch's operation would be no more than its result."""
-    if type(x) is not torch.Tensor or x.dim() != 2 or not x.is_cuda or torch.is_autocast_enabled() or _calls_are_watched():
+    if type(x) is not torch.Tensor or torch.is_autocast_enabled() or _calls_are_watched():
         return False
-    N, D = x.shape
-    if any(type(t) is not torch.Tensor and type(t) is not torch.nn.Parameter for t in (weight, bias)):
+    at = x.get_device()
+    for t in (x, weight, bias):  # (a step of a few tokens is bound by the host: no more than is needed)
+        if (t.dtype is not torch.bfloat16 or t.get_device() != at or at < 0 or not t.is_contiguous() or t.data_ptr() % 16
+                or type(t) is not torch.nn.Parameter and type(t) is not torch.Tensor):
+            return False
+    shape, (rows, D) = x.shape, weight.shape
+    N = shape[0]
+    if len(shape) != 2 or N < 1 or shape[1] != D or (D > 1280 and (D > 2048 or N > 4096)):
         return False
-    if any(t.dtype != torch.bfloat16 or t.device != x.device or not t.is_contiguous() or t.data_ptr() % 16 for t in (x, weight, bias)):
-        return False
-    if N < 1 or weight.shape[1] != D or (D > 1280 and (D > 2048 or N > 4096)):
-        return False
-    rows = weight.shape[0]
     return max((N + 256) * D, (rows + 256) * D, N * rows) * 2 < 1 << 31
 
 
