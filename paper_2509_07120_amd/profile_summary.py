@@ -326,8 +326,9 @@ needed over a window of about +-50 tiles, many times what 4 MB of L2 hold.
 
 # ---------------------------------------------------------------------------------------------- case
 def cmd_case(name: str, d_stats: str, d_pipes: str) -> None:
-    """Time and pipe counters of every library kernel of one of the performance cases, means over 20 passes after 5."""
-    passes, skip = 25, 5
+    """Time and pipe counters of every library kernel of one of the performance cases, means over 25 passes after 100: the first ones are up to a tenth
+    slower than those of a card that has been at work for a while."""
+    passes, skip = 125, 100
 
     def label(n):  # kernels over __bf16 keep their mangled names, or get a wrong one
         hit = re.search(r"_ZN4bsga12_GLOBAL__N_1\d+(\w+?_kernel)I(\w*?)E(?:E?v|$)", n)
@@ -346,7 +347,7 @@ def cmd_case(name: str, d_stats: str, d_pipes: str) -> None:
     trace = sorted(csv.DictReader(open(one(d_stats, "kernel_trace.csv"))), key=lambda r: int(r["Start_Timestamp"]))
     times = kernels((r["Kernel_Name"], (int(r["End_Timestamp"]) - int(r["Start_Timestamp"])) / 1e3) for r in trace)
     pipes = kernels((x["name"], x) for x in dispatches(d_pipes))
-    counters = "SQ_VALU_MFMA_BUSY_CYCLES SQ_BUSY_CU_CYCLES SQ_INSTS_MFMA SQ_WAVE_CYCLES SQ_WAIT_ANY SQ_WAIT_INST_ANY SQ_ACTIVE_INST_VALU SQ_LDS_BANK_CONFLICT"
+    counters = "SQ_VALU_MFMA_BUSY_CYCLES SQ_BUSY_CU_CYCLES SQ_LDS_IDX_ACTIVE SQ_WAVE_CYCLES SQ_WAIT_ANY SQ_WAIT_INST_ANY SQ_ACTIVE_INST_VALU SQ_LDS_BANK_CONFLICT"
     listed = os.path.join(os.path.dirname(PROFILES), "perf", "operators.py")
     module = "perf.operators as C; C.own = True" if f'"{name}"' in open(listed).read() else "perf.cases as C"
     run = (f"python3 -c \"import sys; sys.path.insert(0, '<repo>'); import {module}; c = [x for x in C.listed() if x['name'] == '{name}'][0]; "
@@ -358,19 +359,22 @@ def cmd_case(name: str, d_stats: str, d_pipes: str) -> None:
                 f"    cd /tmp && export TMPDIR=/tmp && rocprofv3 --kernel-trace --stats -d <out>/stats -o stats --output-format csv -- {run}\n"
                 f"    cd /tmp && export TMPDIR=/tmp && rocprofv3 --pmc {counters} -d <out>/pipes -o pmc --output-format csv -- {run}\n\n"
                 f"Means over the last {passes - skip} of {passes} passes; times of the first command.  Columns as in attention_cfg4_mfma_utilisation.md; MFMA pipe "
-                "busy is of the time that CUs are busy, the wave time columns are shares of the time that waves are resident.\n\n"
-                "| kernel | launches a pass | us a launch | MFMA pipe busy | wave time waiting | ready but not issued | issuing VALU | LDS bank conflict cycles |\n"
-                "|---|---|---|---|---|---|---|---|\n")
+                "busy, LDS active and vector pipe (instructions issued, of the four SIMDs' time) are of the time that CUs are busy, the wave time columns are shares of the "
+                "time that waves are resident; busy cycles are a CU's for each us of the second command's launch: the clock, where all CUs are busy throughout.\n\n"
+                "| kernel | launches a pass | us a launch | MFMA pipe busy | vector pipe | LDS active | wave time waiting | ready but not issued | issuing VALU | "
+                "LDS bank conflict cycles | busy cycles a us |\n"
+                "|---|---|---|---|---|---|---|---|---|---|---|\n")
         for n, us in times.items():
             p = pipes.get(n, [])
 
             def mean(k):
                 return sum(x.get(k, 0.0) for x in p) / max(1, len(p))
 
-            wave = mean("SQ_WAVE_CYCLES") or float("nan")
+            wave, busy = mean("SQ_WAVE_CYCLES") or float("nan"), mean("SQ_BUSY_CU_CYCLES") or float("nan")
             f.write(f"| `{n}` | {len(us) / (passes - skip):g} | {sum(us) / len(us):.2f} | "
-                    f"{mean('SQ_VALU_MFMA_BUSY_CYCLES') / (4.0 * mean('SQ_BUSY_CU_CYCLES') or float('nan')):.3f} | {mean('SQ_WAIT_ANY') / wave:.3f} | "
-                    f"{mean('SQ_WAIT_INST_ANY') / wave:.3f} | {mean('SQ_ACTIVE_INST_VALU') / wave:.3f} | {mean('SQ_LDS_BANK_CONFLICT'):.4g} |\n")
+                    f"{mean('SQ_VALU_MFMA_BUSY_CYCLES') / (4.0 * busy):.3f} | {mean('SQ_ACTIVE_INST_VALU') / busy:.3f} | {mean('SQ_LDS_IDX_ACTIVE') / busy:.3f} | "
+                    f"{mean('SQ_WAIT_ANY') / wave:.3f} | {mean('SQ_WAIT_INST_ANY') / wave:.3f} | {mean('SQ_ACTIVE_INST_VALU') / wave:.3f} | "
+                    f"{mean('SQ_LDS_BANK_CONFLICT'):.4g} | {busy / 256 / (1e3 * mean('ms') or float('nan')):.0f} |\n")
     print(open(path).read())
 
 
