@@ -319,7 +319,8 @@ int bsga_qk_norm_rope(const void* q, const void* k, const void* v, int64_t q_tok
 
 /*
  * Its gradient.  dq [heads, n_tokens, 64], dk and dv [kv_heads, n_tokens, 64]: gradients of q_out, k_out, v_out (without slots);
- * q, k and the rest as they were given; dq_in, dk_in, dv_in: gradients of q, k, v, with strides of their own.
+ * q, k and the rest as they were given; dq_in, dk_in, dv_in: gradients of q, k, v, with strides of their own (rows must
+ * not overlap).
  *   d_weights  nullable [2, 2, 64] float32: of q's weight and bias, then of k's (zeros for an absent tensor; the bias of a rms norm is
  *              the sum that a bias would have); sums over tokens and heads in fp32 and fp64, always in the same order
  *   workspace  with d_weights: bsga_qk_norm_rope_bwd_workspace_bytes(...) bytes, 16-byte aligned; overwritten

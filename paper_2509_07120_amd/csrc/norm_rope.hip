@@ -5,7 +5,7 @@
 // position * base^(-2j/W).  Backwards, with g the gradient turned back and h the row before the weight: dw = sum g h, db = sum g,
 // dx = r (w g - [mean w g] - h mean(w g h)).
 //
-// HBM-bound: 100 frames of 48 heads (1.69 GB) 338 us, 5.0 TB/s, where a copy of 1 GiB reaches 5.2.  A row is read once and written once.  Four lanes hold a row, lane c eight of its pairs (so that the rotation stays in
+// HBM-bound: 100 frames of 48 heads (1.69 GB) 338 us, 5.0 TB/s, where a copy of 1 GiB reaches 5.1.  A row is read once and written once.  Four lanes hold a row, lane c eight of its pairs (so that the rotation stays in
 // the lane), and the sums over a row are two quad permutations.  A lane keeps its token over the heads that its workgroup takes: the angles are
 // computed once for them.  Angles are exact: base^(-2j/W) / 2 pi is a 64-bit fraction of a turn, and the product with the position
 // modulo 2^64 is the turn's fraction, whatever the position's size; fp32 would be off by 0.1 at position 10^6.

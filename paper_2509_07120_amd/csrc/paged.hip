@@ -1,8 +1,8 @@
 // Attention of one new token for each sequence over a cache of pages.
 //
 // The query of sequence b stands at position lengths[b] - 1, its own key is in the cache.  It sees the keys that window.h describes, in
-// the cache rows page_table[b][j / page], j % page.  HBM-bound: every visible key and value is read once for all the query heads that
-// share it, at 64 flop to the byte at most.  A workgroup takes a stretch of one sequence's visible keys and one key head; its four waves take
+// the cache rows page_table[b][j / page], j % page.  HBM-bound: every visible key and value is read once for up to 16 of the query heads
+// that share it (more of them: once for each 16), at 16 flop to the byte at most (fp32 8).  A workgroup takes a stretch of one sequence's visible keys and one key head; its four waves take
 // pieces of it in turn and wait for nobody: a wave moves its pieces straight into LDS of its own, two ahead (16 KB on their way for each
 // wave, 128 KB for each CU, where 8 TB/s at 2 us of latency ask for 64).  Up to 16 query heads are the columns of 16x16 products
 // S^T = K Q^T and O^T = V^T P^T, in which the weights are operands as they lie in the results.
@@ -293,11 +293,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(const PagedArgs a
 
 // Keys of a workgroup.  The chip holds 512, and 300 with 64 KB on their way each draw what the memory gives; a sequence's stretches cost a second
 // kernel, and each wave should have a few pieces.  Measured, us, for at least 512 / 1024 / 2048 / 4096 workgroups: one sequence of 10,992 keys and 16
-// key heads 17.2 / 18.3 / 20.3 / 17.8; two of 412,200 and 312,300 509 / 485 / 493 / 498; 96 of up to 4,100 keys and 4 key heads 62 (no
-// stretches) / 75 / 68 / 71.  The host knows the most that a sequence can see, not its length: one long sequence among short ones must not be left to one
+// key heads 14.6 / 15.2 / 15.3 / 15.2; two of 412,200 and 312,300 508 / 482 / 487 / 495; 96 of up to 4,100 keys and 4 key heads 60 (no
+// stretches) / 70 / 64 / 67.  The host knows the most that a sequence can see, not its length: one long sequence among short ones must not be left to one
 // workgroup (4,608 keys take one about 30 us), and the workgroups that find nothing to do have to stay few.
-// Up to 8 pieces for each wave are one workgroup's whatever the launch: 1,024 bf16 keys 10.2 us a call and 18.7 alone, in stretches of 256 with
-// their second kernel 14.5 and 18.1; 512 fp32 keys 10.4 and 18.5, 14.7 and 19.5.
+// Up to 8 pieces for each wave are one workgroup's whatever the launch: 1,024 bf16 keys 9.9 us a call and 27.2 alone, in stretches of 256 with
+// their second kernel 13.8 and 26.7; 512 fp32 keys 13.0 and 30.3, 14.2 and 29.7.
 void shape_of(PagedArgs& a, int keys_of_piece) {
   int64_t most = int64_t(a.table_width) * a.page;
   if (a.window > 0) most = min(most, int64_t(a.window) * a.frame + a.sinks);

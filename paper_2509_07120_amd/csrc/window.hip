@@ -8,7 +8,7 @@
 // The running maximum m follows when a tile exceeds it by 2^8.
 //
 // Bound by vector issue: 32 keys x 32 queries are 8 products (256 cycles of the matrix pipe) and 448 cycles of exponentials, scaling, sums and packing for
-// a wave, two waves to a SIMD.  100 frames of 16 heads, window of 4 and the first: 3.79 TFLOP in 3.8 ms, 1.0 PFLOP/s, matrix pipe 53 % busy at 1.75 GHz.
+// a wave, two waves to a SIMD.  100 frames of 16 heads, window of 4 and the first: 3.79 TFLOP in 3.8 ms, 1.0 PFLOP/s, matrix pipe 53 % and vector pipe 75 % busy at 1.82 GHz.
 #include "window.h"
 
 #include <math.h>

@@ -65,7 +65,9 @@ def window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: 
 class PagedCache:
     """Keys and values of several sequences in pages [pages, kv_heads, page, 64], and which page holds which tokens.  The bookkeeping is
     the host's; grow() and trim() bring the device's table and lengths up to date on the current stream.  Places of the table without a page, of
-    freed ones too, hold -1, which bsga_paged_attn takes for page 0: check_seen() tells whether a window reaches them."""
+    freed ones too, hold -1, which bsga_paged_attn takes for page 0: check_seen() tells whether a window reaches them.
+    width: pages of the longest sequence, by default all.  The attention is dealt out by it, so a table much wider than its sequences is slow: 16
+    sequences of 12,000 tokens on 4 key heads, page 64, take 38 us with a width of 188 and 225 with 3,008."""
 
     def __init__(self, sequences: int, pages: int, kv_heads: int, page: int = 64, width: Optional[int] = None, dtype=torch.bfloat16,
                  device="cuda"):
