@@ -18,6 +18,9 @@ int check_hip(hipError_t e, const char* what);
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Whether a stride of so many numbers of `size` bytes is a multiple of 16 bytes, not negative, and small enough to be computed with.
+inline bool whole_stride(int64_t stride, int size) { return stride >= 0 && stride <= (int64_t(1) << 40) && stride * size % 16 == 0; }
+
 // Number of blocks when tokens [0, n_first) and [n_first, n_tokens) are cut into blocks separately
 // (no block crosses n_first).  n_first = n_tokens or 0 gives ceil(n_tokens / block).
 inline int64_t split_blocks(int64_t n_tokens, int64_t n_first, int64_t block) {

@@ -367,7 +367,7 @@ int common(const char* fn, const void* const (&x)[3], const int64_t (&strides)[6
     if (x[t] == nullptr) continue;
     if (h < 1 || h > 65535)
       return fail(BSGA_ERR_INVALID_ARG, "%s: heads of %s must be in [1, 65535], got %d", fn, names[t], h);
-    if (!aligned16(x[t]) || strides[2 * t] < 0 || strides[2 * t + 1] < 0 || strides[2 * t] * size % 16 != 0 || strides[2 * t + 1] * size % 16 != 0)
+    if (!aligned16(x[t]) || !whole_stride(strides[2 * t], size) || !whole_stride(strides[2 * t + 1], size))
       return fail(BSGA_ERR_INVALID_ARG, "%s: %s and its strides must be multiples of 16 bytes, the strides not negative", fn, names[t]);
     if (t < 2) {
       if (!aligned16(weight[t]) || !aligned16(bias[t]))
@@ -495,7 +495,7 @@ int bsga_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const 
       return fail(BSGA_ERR_INVALID_ARG, "%s: q and k come with the gradients of both sides, dv with dv_in", fn);
     if (!aligned16(dy[t]) || !aligned16(dx[t])) return fail(BSGA_ERR_INVALID_ARG, "%s: gradients must be 16-byte aligned", fn);
     const int64_t st = out_strides[2 * t], sh = out_strides[2 * t + 1];
-    if (x[t] && (st < 0 || sh < 0 || st * size % 16 != 0 || sh * size % 16 != 0))
+    if (x[t] && (!whole_stride(st, size) || !whole_stride(sh, size)))
       return fail(BSGA_ERR_INVALID_ARG, "%s: the gradients' strides must be multiples of 16 bytes and not negative", fn);
     a.dy[t] = static_cast<const unsigned char*>(dy[t]);
     a.dx[t] = static_cast<unsigned char*>(dx[t]);

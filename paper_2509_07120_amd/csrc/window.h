@@ -287,7 +287,7 @@ inline int check_seen(const char* fn, int64_t n_q, int64_t n_k, int64_t q_start,
 }
 
 inline int check_view(const char* fn, const char* name, const void* p, int64_t token, int64_t head, int size, View& v) {
-  if (!p || !aligned16(p) || token < 0 || head < 0 || token * size % 16 != 0 || head * size % 16 != 0 || token * size >= int64_t(1) << 24)
+  if (!p || !aligned16(p) || !whole_stride(token, size) || !whole_stride(head, size) || token >= (int64_t(1) << 24) / size)
     return fail(BSGA_ERR_INVALID_ARG, "%s: %s must be non-null, it and its strides multiples of 16 bytes, a token's stride in [0, 2^24) bytes", fn, name);
   v = {static_cast<const unsigned char*>(p), token * size, head * size};
   return BSGA_OK;
