@@ -18,6 +18,12 @@ int check_hip(hipError_t e, const char* what);
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// HIP's min and max are on the host those of int alone, and cut int64_t and double down to it: host code that has more than ints takes these.
+template <typename T>
+__host__ __device__ constexpr T smaller(T a, T b) { return a < b ? a : b; }
+template <typename T>
+__host__ __device__ constexpr T larger(T a, T b) { return a > b ? a : b; }
+
 // Whether a stride of so many numbers of `size` bytes is a multiple of 16 bytes, not negative, and small enough to be computed with.
 inline bool whole_stride(int64_t stride, int size) { return stride >= 0 && stride <= (int64_t(1) << 40) && stride * size % 16 == 0; }
 

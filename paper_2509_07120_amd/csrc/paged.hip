@@ -300,8 +300,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(const PagedArgs a
 // their second kernel 13.8 and 26.7; 512 fp32 keys 13.0 and 30.3, 14.2 and 29.7.
 void shape_of(PagedArgs& a, int keys_of_piece) {
   int64_t most = int64_t(a.table_width) * a.page;
-  if (a.window > 0) most = min(most, int64_t(a.window) * a.frame + a.sinks);
-  most = max(most, int64_t(1));
+  if (a.window > 0) most = smaller(most, int64_t(a.window) * a.frame + a.sinks);
+  most = larger(most, int64_t(1));
   const int64_t units = int64_t(a.batch) * a.kv_heads * a.head_blocks;
   const int64_t step = kWaves * keys_of_piece;
   if (most <= 8 * step) {
@@ -309,11 +309,11 @@ void shape_of(PagedArgs& a, int keys_of_piece) {
     a.splits = 1;
     return;
   }
-  int64_t splits = max(int64_t(units > 256 || most * units < 512 * 1024 ? 512 : 1024) / units, int64_t(1));
-  if (units > 256) splits = max(splits, min(ceil_div(most, 4608), int64_t(4096) / units));
-  const int64_t stretch = ceil_div(max(ceil_div(most, splits), 2 * step), step) * step;
+  int64_t splits = larger(int64_t(units > 256 || most * units < 512 * 1024 ? 512 : 1024) / units, int64_t(1));
+  if (units > 256) splits = larger(splits, smaller(ceil_div(most, 4608), int64_t(4096) / units));
+  const int64_t stretch = ceil_div(larger(ceil_div(most, splits), 2 * step), step) * step;
   const int64_t fits = int64_t(kTable - 4) * a.page / step * step;
-  a.stretch = static_cast<int>(min(min(stretch, fits), ceil_div(most, step) * step));
+  a.stretch = static_cast<int>(smaller(smaller(stretch, fits), ceil_div(most, step) * step));
   a.splits = static_cast<int>(ceil_div(most, a.stretch));
 }
 
@@ -342,8 +342,8 @@ int check_sizes(const char* fn, int dtype, int64_t batch, int heads, int kv_head
   a.n_pages = static_cast<int>(n_pages);
   a.page = page;
   a.frame = static_cast<int>(frame);
-  a.window = static_cast<int>(min(window, most));
-  a.sinks = static_cast<int>(min(sinks, most));
+  a.window = static_cast<int>(smaller(window, most));
+  a.sinks = static_cast<int>(smaller(sinks, most));
   while ((int64_t(1) << a.shift) < page) ++a.shift;
   a.magic = static_cast<unsigned>(((uint64_t(1) << (31 + a.shift)) + page - 1) / page);
   return BSGA_OK;

@@ -27,8 +27,8 @@ struct Seen {
       return;
     }
     const int f = p / frame;
-    hi = static_cast<int>(min(int64_t(f + 1) * frame, int64_t(n_k)));
-    lo = f < window ? 0 : static_cast<int>(min(int64_t(f + 1 - window) * frame, int64_t(hi)));
+    hi = static_cast<int>(smaller(int64_t(f + 1) * frame, int64_t(n_k)));
+    lo = f < window ? 0 : static_cast<int>(smaller(int64_t(f + 1 - window) * frame, int64_t(hi)));
   }
 };
 

@@ -47,8 +47,8 @@ struct Queries {
 __host__ __device__ inline Queries queries_of(const Seen& s, int j) {
   const int f = j / s.frame;
   Queries r;
-  r.first = static_cast<int>(max(int64_t(f) * s.frame - s.q_start, int64_t(0)));
-  r.last = j < s.sinks ? s.n_q : static_cast<int>(max(min((int64_t(f) + s.window) * s.frame - s.q_start, int64_t(s.n_q)), int64_t(0)));
+  r.first = static_cast<int>(larger(int64_t(f) * s.frame - s.q_start, int64_t(0)));
+  r.last = j < s.sinks ? s.n_q : static_cast<int>(larger(smaller((int64_t(f) + s.window) * s.frame - s.q_start, int64_t(s.n_q)), int64_t(0)));
   return r;
 }
 
@@ -724,9 +724,9 @@ __device__ __forceinline__ void key_rows(const BwdArgs& a, int64_t block, int64_
 
 // Queries [first, end) that see at most 256 keys, all from key 0 on: the first ones of a sequence.
 __host__ __device__ inline void early_queries(const Seen& s, int& first, int& end) {
-  const int64_t positions = min(int64_t(kEarlyKeys / s.frame), int64_t(s.window)) * s.frame;
-  first = static_cast<int>(min(max(-int64_t(s.q_start), int64_t(0)), int64_t(s.n_q)));
-  end = static_cast<int>(min(max(positions - s.q_start, int64_t(first)), int64_t(s.n_q)));
+  const int64_t positions = smaller(int64_t(kEarlyKeys / s.frame), int64_t(s.window)) * s.frame;
+  first = static_cast<int>(smaller(larger(-int64_t(s.q_start), int64_t(0)), int64_t(s.n_q)));
+  end = static_cast<int>(smaller(larger(positions - s.q_start, int64_t(first)), int64_t(s.n_q)));
 }
 
 // D of one of these queries by a wave, as sum_j P_j <dO, V_j>: the rounding of O to bf16 in the sum of dO O is seen in dQ where few keys share the
@@ -827,34 +827,34 @@ void shape_of(BwdArgs& a, bool bf16) {
   // tiles of the longest way of each kind, and of all
   int64_t q_most = 0, q_all = 0, k_most = 0, k_all = 0;
   for (int rt = 0; rt < a.row_tiles; ++rt) {
-    const int64_t c = tiles_of(s, rt * kOwnRows, min((rt + 1) * kOwnRows, s.n_q)).count;
-    q_most = max(q_most, c);
+    const int64_t c = tiles_of(s, rt * kOwnRows, smaller((rt + 1) * kOwnRows, s.n_q)).count;
+    q_most = larger(q_most, c);
     q_all += c;
   }
   for (int kt = a.sink_tiles; kt < a.key_tiles; ++kt) {
-    const Queries from = queries_of(s, kt * kOwnRows), to = queries_of(s, min((kt + 1) * kOwnRows, s.n_k) - 1);
+    const Queries from = queries_of(s, kt * kOwnRows), to = queries_of(s, smaller((kt + 1) * kOwnRows, s.n_k) - 1);
     if (to.last <= from.first) continue;
     const int64_t c = (ceil_div(to.last, kTile) - from.first / kTile) * a.group;
-    k_most = max(k_most, c);
+    k_most = larger(k_most, c);
     k_all += c;
   }
   const int64_t sink_most = a.sink_tiles > 0 ? ceil_div(s.n_q, kTile) * a.group : 0;
   const double k_tile = bf16 ? 0.85 : 9.5, q_tile = bf16 ? 0.63 : 7.0;
   const double share = (static_cast<double>(k_all + a.sink_tiles * sink_most) * a.kv_heads * k_tile + static_cast<double>(q_all) * a.heads * q_tile) / 256;
-  const double q_rows = static_cast<double>(a.heads) * s.n_q, sink_rows = static_cast<double>(a.kv_heads) * min(a.sink_tiles * kOwnRows, s.n_k),
+  const double q_rows = static_cast<double>(a.heads) * s.n_q, sink_rows = static_cast<double>(a.kv_heads) * smaller(a.sink_tiles * kOwnRows, s.n_k),
                k_rows = static_cast<double>(a.kv_heads) * s.n_k - sink_rows;
   auto sum_us = [](int64_t splits, double rows, int bytes) { return splits > 1 ? 3.0 + rows * static_cast<double>(splits) * bytes * 2 / 4e6 : 0.0; };
-  const int64_t longest = max(max(q_most, k_most), sink_most);
+  const int64_t longest = larger(larger(q_most, k_most), sink_most);
   double least = -1.0;
   // ways of 1, 2, 3, 4, 6, 8, 12, ... tiles
   for (int64_t kp = 1;; kp += kp > 1 && (kp & (kp - 1)) == 0 ? kp / 2 : kp > 2 ? kp / 3 : 1) {
-    const int64_t splits = max(ceil_div(k_most, kp), int64_t(1)), sink_splits = max(ceil_div(sink_most, kp), int64_t(1));
+    const int64_t splits = larger(ceil_div(k_most, kp), int64_t(1)), sink_splits = larger(ceil_div(sink_most, kp), int64_t(1));
     for (int64_t qp = 1; splits <= 64 && sink_splits <= 256; qp += qp > 1 && (qp & (qp - 1)) == 0 ? qp / 2 : qp > 2 ? qp / 3 : 1) {
-      const int64_t q_splits = max(ceil_div(q_most, qp), int64_t(1));
+      const int64_t q_splits = larger(ceil_div(q_most, qp), int64_t(1));
       if (q_splits <= 64) {
-        const double k_way = max(ceil_div(k_most, splits), ceil_div(sink_most, sink_splits)) * k_tile, q_way = ceil_div(q_most, q_splits) * q_tile;
+        const double k_way = larger(ceil_div(k_most, splits), ceil_div(sink_most, sink_splits)) * k_tile, q_way = ceil_div(q_most, q_splits) * q_tile;
         const int64_t groups = a.kv_heads * (a.sink_tiles * sink_splits + (a.key_tiles - a.sink_tiles) * splits) + int64_t(a.heads) * a.row_tiles * q_splits;
-        const double us = max(max(share, 1.4 * k_way), 1.4 * q_way) + 0.1 * k_way + 0.5 * q_way + 1.5 * static_cast<double>(ceil_div(groups, kPlaces)) + sum_us(splits, k_rows, 512) +
+        const double us = larger(larger(share, 1.4 * k_way), 1.4 * q_way) + 0.1 * k_way + 0.5 * q_way + 1.5 * static_cast<double>(ceil_div(groups, kPlaces)) + sum_us(splits, k_rows, 512) +
                           sum_us(sink_splits, sink_rows, 512) + sum_us(q_splits, q_rows, 256);
         if (least < 0.0 || us < least) {
           least = us;
@@ -872,7 +872,7 @@ void shape_of(BwdArgs& a, bool bf16) {
 size_t stats_bytes(const BwdArgs& a) { return static_cast<size_t>(a.heads) * a.stat_rows * 8; }
 size_t part_q_bytes(const BwdArgs& a) { return a.q_splits > 1 ? static_cast<size_t>(a.q_splits) * a.heads * a.seen.n_q * 256 : 0; }
 size_t part_kv_bytes(const BwdArgs& a, bool sink) {
-  const int64_t sink_rows = min(int64_t(a.sink_tiles) * kOwnRows, int64_t(a.seen.n_k));
+  const int64_t sink_rows = smaller(int64_t(a.sink_tiles) * kOwnRows, int64_t(a.seen.n_k));
   const int splits = sink ? a.sink_splits : a.splits;
   return splits > 1 ? static_cast<size_t>(splits) * a.kv_heads * (sink ? sink_rows : a.seen.n_k - sink_rows) * 512 : 0;
 }
@@ -899,7 +899,7 @@ int launch(const BwdArgs& a, hipStream_t s) {
                        a.q_splits, 0, a.seen.n_q, a.dq, nullptr);
     if (int rc = check_hip(hipGetLastError(), what)) return rc;
   }
-  const int64_t sink_rows = min(int64_t(a.sink_tiles) * kOwnRows, int64_t(a.seen.n_k));
+  const int64_t sink_rows = smaller(int64_t(a.sink_tiles) * kOwnRows, int64_t(a.seen.n_k));
   for (int x = 0; x < 2; ++x) {
     const int splits = x == 0 ? a.sink_splits : a.splits;
     const int64_t rows = x == 0 ? sink_rows : a.seen.n_k - sink_rows;
