@@ -394,8 +394,8 @@ int common(const char* fn, const void* const (&x)[3], const int64_t (&strides)[6
   for (int x = 0; axes > 0 && x < half; x += 8) {
     const double coarse = pow(base, -double(x) / half) * 0.15915494309189533577;  // 1 / (2 pi)
     for (int y = 0; y < 8; ++y) {
-      const double turn = coarse * fine[y];
-      a.turn[x + y] = static_cast<unsigned long long>((turn < 1.0 ? turn : turn - floor(turn)) * 0x1p64);
+      const double turn = coarse * fine[y], part = turn - floor(turn);
+      a.turn[x + y] = static_cast<unsigned long long>((part < 1.0 ? part : 0.0) * 0x1p64);  // (a base next to 0: infinite, and no number less itself)
     }
   }
   return BSGA_OK;
@@ -494,8 +494,9 @@ int bsga_qk_norm_rope_bwd(const void* dq, const void* dk, const void* dv, const 
     if (n_tokens > 0 && (!x[t] != !dy[t] || !x[t] != !dx[t]))
       return fail(BSGA_ERR_INVALID_ARG, "%s: q and k come with the gradients of both sides, dv with dv_in", fn);
     if (!aligned16(dy[t]) || !aligned16(dx[t])) return fail(BSGA_ERR_INVALID_ARG, "%s: gradients must be 16-byte aligned", fn);
+    if (!x[t]) continue;
     const int64_t st = out_strides[2 * t], sh = out_strides[2 * t + 1];
-    if (x[t] && (!whole_stride(st, size) || !whole_stride(sh, size)))
+    if (!whole_stride(st, size) || !whole_stride(sh, size))
       return fail(BSGA_ERR_INVALID_ARG, "%s: the gradients' strides must be multiples of 16 bytes and not negative", fn);
     a.dy[t] = static_cast<const unsigned char*>(dy[t]);
     a.dx[t] = static_cast<unsigned char*>(dx[t]);
