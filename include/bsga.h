@@ -44,6 +44,7 @@ extern "C" {
 
 #define BSGA_BF16 0
 #define BSGA_FP32 1
+#define BSGA_E4M3 2 /* of caches only */
 
 #define BSGA_NORM_NONE 0
 #define BSGA_NORM_RMS 1
@@ -391,6 +392,69 @@ int bsga_paged_attn(const void* q, int64_t q_batch, int64_t q_head, const void* 
                     int heads, int kv_heads, int head_dim, const int32_t* page_table, int64_t table_width, const int32_t* lengths,
                     int64_t n_pages, int page, float softmax_scale, int64_t frame, int64_t window, int64_t sinks, void* out, float* lse,
                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Caches in 8 bits.  A row of 64 numbers is held as 64 e4m3 numbers (OCP: up to 448, no infinities) in a cache [n_pages, kv_heads, page, 64] and one exponent
+ * byte in a tensor of scales [n_pages, kv_heads, page]: a number c of the row stands for c * 2^(byte - 127).  The byte is
+ * 127 + s, where s is the least integer in [-64, 88] with max |x| <= 448 * 2^s over the row's finite numbers x, and x / 2^s is rounded to
+ * the nearest e4m3 number (to even; at most 2^-4 of x off, or 2^(s - 10) if that is more).  Finite numbers above 448 * 2^88 become that, infinities and NaN become NaN.
+ * Other bytes may be read (what they stand for may overflow in sums, or vanish).
+ * What a row stands for is exact in bf16.
+ *
+ * bsga_qk_norm_rope_e4m3: bsga_qk_norm_rope into the pages of such a cache.  q, k, v and the rest as there; a row is quantised from the 32 bits
+ * in which it was normed and turned (v: as it is).
+ *   q          NULL together with q_out; k and v each NULL together with its cache and its scales
+ *   slots      [n_tokens], distinct; tokens whose slot lies outside the cache are not written
+ *   q_out      [heads, n_tokens, 64]
+ *   k_rows, v_rows  nullable [kv_heads, n_tokens, 64], dtype of the tensors: the rows as the cache holds them (also of tokens that are not written), for an attention
+ *              over the new tokens that sees what later ones will see
+ */
+int bsga_qk_norm_rope_e4m3(const void* q, const void* k, const void* v, int64_t q_token, int64_t q_head, int64_t k_token, int64_t k_head,
+                           int64_t v_token, int64_t v_head, int dtype, int64_t n_tokens, int heads, int kv_heads, int head_dim, int norm, double eps,
+                           const void* q_weight, const void* q_bias, const void* k_weight, const void* k_bias, const int32_t* positions, int axes,
+                           double base, const int32_t* slots, int64_t n_pages, int page, void* q_out, void* k_rows, void* v_rows, void* k_cache,
+                           void* v_cache, uint8_t* k_scale, uint8_t* v_scale, void* stream);
+
+/*
+ * Tokens [first, first + n_tokens) of one sequence out of the pages of a cache, head by head, e.g. for bsga_window_attn.
+ *   cache_dtype  BSGA_E4M3 (with k_scale and v_scale), or dtype: rows are moved as they are
+ *   pages      [table_width] int32, the sequence's row of a page table; tokens whose page lies outside [0, n_pages) are zeros
+ *   k_out, v_out  [kv_heads, n_tokens, 64] of type dtype, heads k_head and v_head elements apart (multiples of 16 bytes), must not overlap the caches
+ */
+int bsga_cache_load(const void* k_cache, const void* v_cache, const uint8_t* k_scale, const uint8_t* v_scale, int cache_dtype, int64_t n_pages, int page,
+                    int kv_heads, int head_dim, const int32_t* pages, int64_t table_width, int64_t first, int64_t n_tokens, int dtype, void* k_out,
+                    void* v_out, int64_t k_head, int64_t v_head, void* stream);
+
+/*
+ * bsga_paged_attn over a cache in 8 bits: q and out are of type dtype, the rest as there.  Keys and values are what their numbers and scales stand for: in
+ * bf16 calls keys exactly, values' scales multiply the weights before these are rounded.
+ */
+size_t bsga_paged_attn_e4m3_workspace_bytes(int dtype, int64_t batch, int heads, int kv_heads, int64_t table_width, int64_t n_pages, int page,
+                                            int64_t frame, int64_t window, int64_t sinks);
+int bsga_paged_attn_e4m3(const void* q, int64_t q_batch, int64_t q_head, const void* k_cache, const void* v_cache, const uint8_t* k_scale,
+                         const uint8_t* v_scale, int dtype, int64_t batch, int heads, int kv_heads, int head_dim, const int32_t* page_table,
+                         int64_t table_width, const int32_t* lengths, int64_t n_pages, int page, float softmax_scale, int64_t frame, int64_t window,
+                         int64_t sinks, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of one new token for each sequence where sequences begin with tokens that they share: the keys of such a prefix are read once for all of its
+ * sequences.  Sequence b sees the prefix_lengths[g] tokens of its prefix g and then lengths[b] tokens of its own; its query stands at the last of them, and its window
+ * goes by positions from the prefix's first token on.  The same result as bsga_paged_attn over the two in one table, up to the order of sums.
+ *   cache_dtype  BSGA_E4M3 (with k_scale and v_scale), or dtype; prefixes and own tokens lie in the same caches
+ *   page_table, lengths  as for bsga_paged_attn, of the own tokens: own token j of sequence b lies in row j % page of page page_table[b][j / page]
+ *   prefix_table  [prefixes, prefix_width] int32, likewise;  prefix_lengths [prefixes] int32, clamped into [0, prefix_width * page]
+ *   starts     [prefixes + 1] int32, not decreasing: sequences starts[g] .. starts[g + 1] - 1 have prefix g, those in front of starts[0] and from starts[prefixes] on none;
+ *              clamped into [0, batch].  Where it decreases, results are undefined (but nothing outside the tensors is read or written).
+ *   workspace  bsga_prefix_attn_workspace_bytes(...) bytes, 16-byte aligned; overwritten
+ * Table entries and lengths that do not fit are clamped as there.  A key that a query does not see has no part in its result.  The same bits every time.
+ */
+size_t bsga_prefix_attn_workspace_bytes(int dtype, int cache_dtype, int64_t batch, int heads, int kv_heads, int64_t table_width, int64_t prefixes,
+                                        int64_t prefix_width, int64_t n_pages, int page, int64_t frame, int64_t window, int64_t sinks);
+int bsga_prefix_attn(const void* q, int64_t q_batch, int64_t q_head, const void* k_cache, const void* v_cache, const uint8_t* k_scale, const uint8_t* v_scale,
+                     int dtype, int cache_dtype, int64_t batch, int heads, int kv_heads, int head_dim, const int32_t* page_table, int64_t table_width,
+                     const int32_t* lengths, const int32_t* prefix_table, int64_t prefix_width, const int32_t* prefix_lengths, const int32_t* starts,
+                     int64_t prefixes, int64_t n_pages, int page, float softmax_scale, int64_t frame, int64_t window, int64_t sinks, void* out, float* lse,
+                     void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Measurement aid, not part of the method: the rate the matrix pipes sustain on the MFMA instruction

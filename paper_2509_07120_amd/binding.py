@@ -26,6 +26,7 @@ BSGA_ERR_WORKSPACE = 3
 BSGA_ERR_HIP = 4
 BSGA_BF16 = 0
 BSGA_FP32 = 1
+BSGA_E4M3 = 2
 
 EXPORTED_SYMBOLS = (
     "bsga_version",
@@ -48,9 +49,15 @@ EXPORTED_SYMBOLS = (
     "bsga_linear",
     "bsga_layer_norm",
     "bsga_probe_mfma",
+    "bsga_cache_load",
     "bsga_paged_attn",
+    "bsga_paged_attn_e4m3",
+    "bsga_paged_attn_e4m3_workspace_bytes",
     "bsga_paged_attn_workspace_bytes",
+    "bsga_prefix_attn",
+    "bsga_prefix_attn_workspace_bytes",
     "bsga_qk_norm_rope",
+    "bsga_qk_norm_rope_e4m3",
     "bsga_qk_norm_rope_bwd",
     "bsga_qk_norm_rope_bwd_workspace_bytes",
     "bsga_window_attn",
@@ -154,6 +161,24 @@ def _load() -> ctypes.CDLL:
                                     c_int64, c_int, c_float, c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
     lib.bsga_paged_attn_workspace_bytes.restype = c_size_t
     lib.bsga_paged_attn_workspace_bytes.argtypes = [c_int, c_int64, c_int, c_int, c_int64, c_int64, c_int] + [c_int64] * 3
+    lib.bsga_paged_attn_e4m3.restype = c_int
+    lib.bsga_paged_attn_e4m3.argtypes = [c_void_p, c_int64, c_int64] + [c_void_p] * 4 + [c_int, c_int64, c_int, c_int, c_int, c_void_p, c_int64, c_void_p,
+                                                                                        c_int64, c_int, c_float, c_int64, c_int64, c_int64, c_void_p,
+                                                                                        c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.bsga_paged_attn_e4m3_workspace_bytes.restype = c_size_t
+    lib.bsga_paged_attn_e4m3_workspace_bytes.argtypes = lib.bsga_paged_attn_workspace_bytes.argtypes
+    lib.bsga_qk_norm_rope_e4m3.restype = c_int
+    lib.bsga_qk_norm_rope_e4m3.argtypes = [c_void_p] * 3 + strides + [c_int, c_int64, c_int, c_int, c_int] + norm + [c_void_p] * 3 + [
+        c_int, c_double, c_void_p, c_int64, c_int] + [c_void_p] * 8
+    lib.bsga_cache_load.restype = c_int
+    lib.bsga_cache_load.argtypes = [c_void_p] * 4 + [c_int, c_int64, c_int, c_int, c_int, c_void_p, c_int64, c_int64, c_int64, c_int, c_void_p, c_void_p,
+                                                     c_int64, c_int64, c_void_p]
+    lib.bsga_prefix_attn.restype = c_int
+    lib.bsga_prefix_attn.argtypes = [c_void_p, c_int64, c_int64] + [c_void_p] * 4 + [
+        c_int, c_int, c_int64, c_int, c_int, c_int, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_int64, c_int, c_float,
+        c_int64, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.bsga_prefix_attn_workspace_bytes.restype = c_size_t
+    lib.bsga_prefix_attn_workspace_bytes.argtypes = [c_int, c_int, c_int64, c_int, c_int, c_int64, c_int64, c_int64, c_int64, c_int] + [c_int64] * 3
     return lib
 
 
@@ -906,4 +931,202 @@ def bsga_paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     _check(lib.bsga_paged_attn(_ptr(q), strides[0], strides[1], _ptr(k_cache), _ptr(v_cache), code, B, H, K, d, _ptr(page_table), width,
                                _ptr(lengths), pages, page, 1.0 / math.sqrt(d) if softmax_scale is None else float(softmax_scale), *seen,
                                _ptr(out), _ptr(lse), _ptr(workspace), nbytes, _stream(q)))
+    return (out, lse) if return_lse else out
+
+
+def _pages_of(name: str, t: torch.Tensor, dtype, at: int, shape) -> None:
+    """Whether t is a cache of this shape on this device."""
+    if not t.is_cuda or t.dtype != dtype or t.get_device() != at or not t.is_contiguous():
+        _wrong(t, name, dtype, at, "the tensors")
+    if len(shape) != 4 or t.shape != shape:
+        raise ValueError(f"{name} must be [pages, kv_heads, page, 64]")
+
+
+def _scales_of(k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor], at: int, shape) -> None:
+    """Whether these are the scales of caches of this shape."""
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        if t is None:
+            raise ValueError(f"a cache in 8 bits needs {name}")
+        if not t.is_cuda or t.dtype != torch.uint8 or t.get_device() != at or not t.is_contiguous():
+            _wrong(t, name, torch.uint8, at, "the tensors")
+        if t.shape != shape[:3]:
+            raise ValueError(f"{name} must be [pages, kv_heads, page]")
+
+
+def _cache_of(k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor], dtype, at: int, d: int) -> int:
+    """Checks caches of the tensors' type, or in 8 bits with their scales; their type's code."""
+    shape, coded = k_cache.shape, k_cache.dtype == torch.float8_e4m3fn
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        _pages_of(name, t, torch.float8_e4m3fn if coded else dtype, at, shape)
+    if shape[3] != d:
+        raise ValueError("k_cache must be [pages, kv_heads, page, 64]")
+    if coded:
+        _scales_of(k_scale, v_scale, at, shape)
+        return BSGA_E4M3
+    if k_scale is not None or v_scale is not None:
+        raise ValueError("scales go with caches of torch.float8_e4m3fn")
+    return _dtype_code(k_cache)
+
+
+def bsga_qk_norm_rope_e4m3(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                           k_scale: torch.Tensor, v_scale: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                           q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, q_bias: Optional[torch.Tensor] = None,
+                           k_bias: Optional[torch.Tensor] = None, norm: Optional[str] = "rms", eps: float = 1e-6, base: float = 10000.0,
+                           return_rows: bool = False):
+    """bsga_qk_norm_rope with slots, into caches in 8 bits: k_cache, v_cache [pages, Hkv, page, 64] of torch.float8_e4m3fn, k_scale, v_scale [pages, Hkv, page]
+    uint8; a row stands for its numbers times 2^(scale - 127).  q [N, H, 64] or None, k and v [N, Hkv, 64], slots int32 [N], the rest as there.
+    Returns (q [H, N, 64] or None, k, v): with return_rows the rows [Hkv, N, 64] as the caches hold them, of the tensors' type, else None."""
+    dtype, at, N = k.dtype, k.get_device(), k.shape[0]
+    code = _dtype_code(k)
+    kt, kh, K, d = _rows(k, "k", dtype, at, N)
+    qt, qh, H, qd = (0, 0, K, d) if q is None else _rows(q, "q", dtype, at, N)
+    vt, vh, _, vd = _rows(v, "v", dtype, at, N, K)
+    if qd != d or vd != d:
+        raise ValueError("q, k and v must have the same head dimension")
+    kind = _norm_code(norm)
+    qw, kw = _norm_weight(q_weight, "q_weight", dtype, at, d), _norm_weight(k_weight, "k_weight", dtype, at, d)
+    qb, kb = _norm_weight(q_bias, "q_bias", dtype, at, d), _norm_weight(k_bias, "k_bias", dtype, at, d)
+    where, axes = _norm_positions(positions, at, N)
+    if not slots.is_cuda or slots.dtype != torch.int32 or slots.get_device() != at or not slots.is_contiguous():
+        _wrong(slots, "slots", torch.int32, at, "the tensors")
+    if slots.numel() != N:
+        raise ValueError("slots must have one entry per token")
+    shape = k_cache.shape
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        _pages_of(name, t, torch.float8_e4m3fn, at, shape)
+    if shape[1] != K or shape[3] != d:
+        raise ValueError("k_cache must be [pages, kv_heads, page, 64]")
+    _scales_of(k_scale, v_scale, at, shape)
+    q_out = None if q is None else q.new_empty((H, N, d))
+    k_rows, v_rows = (k.new_empty((2, K, N, d)) if return_rows else (None, None))
+    _check(lib.bsga_qk_norm_rope_e4m3(_ptr(q), k.data_ptr(), v.data_ptr(), qt, qh, kt, kh, vt, vh, code, N, H, K, d, kind, eps, qw, qb, kw, kb, where, axes, base,
+                                      slots.data_ptr(), shape[0], shape[2], _ptr(q_out), _ptr(k_rows), _ptr(v_rows), k_cache.data_ptr(),
+                                      v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _stream(k)))
+    return q_out, k_rows, v_rows
+
+
+def bsga_cache_load(k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.Tensor, n_tokens: int, first: int = 0,
+                    k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None,
+                    out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Tokens [first, first + n_tokens) of one sequence out of the caches [pages, Hkv, page, 64]: (k, v) [Hkv, n_tokens, 64].  pages (int32 [width]) is the
+    sequence's row of a page table; tokens whose page does not exist are zeros.  Caches of torch.float8_e4m3fn come with their scales and are read as
+    `dtype` (bfloat16 unless said otherwise), others as they are.  out: where to, each head's tokens one after the other (heads may be further apart)."""
+    coded = k_cache.dtype == torch.float8_e4m3fn
+    if out is not None:
+        dtype = out[0].dtype if dtype is None else dtype
+    if dtype is None:
+        dtype = torch.bfloat16 if coded else k_cache.dtype
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"unsupported dtype {dtype}: bsga takes bfloat16 or float32")
+    at, d = k_cache.get_device(), 64
+    if not coded and k_cache.dtype != dtype:
+        raise TypeError(f"a cache that is not in 8 bits is read as it is, got {k_cache.dtype} and {dtype}")
+    code = _cache_of(k_cache, v_cache, k_scale, v_scale, dtype, at, d)
+    if not pages.is_cuda or pages.dtype != torch.int32 or pages.get_device() != at or not pages.is_contiguous():
+        _wrong(pages, "pages", torch.int32, at, "the caches")
+    if pages.dim() != 1:
+        raise ValueError("pages must be one sequence's row of a page table")
+    n_pages, K, page, _ = k_cache.shape
+    if out is None:
+        k, v = k_cache.new_empty((2, K, max(n_tokens, 0), d), dtype=dtype)
+    else:
+        k, v = out
+        for name, t in (("out[0]", k), ("out[1]", v)):
+            if t.dtype != dtype:
+                raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+            if not t.is_cuda or t.get_device() != at:
+                raise ValueError(f"{name} must be on the same device as the caches")
+            if t.shape != (K, n_tokens, d) or (n_tokens > 0 and (t.stride(2) != 1 or (n_tokens > 1 and t.stride(1) != d))):
+                raise ValueError(f"{name} must be {(K, n_tokens, d)}, each head's tokens one after the other")
+    _check(lib.bsga_cache_load(_ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), code, n_pages, page, K, d, _ptr(pages), pages.shape[0], first,
+                               n_tokens, BSGA_BF16 if dtype == torch.bfloat16 else BSGA_FP32, _ptr(k), _ptr(v), k.stride(0), v.stride(0), _stream(k_cache)))
+    return k, v
+
+
+def _queries(q: torch.Tensor) -> Tuple[int, int]:
+    """Strides of the sequences and heads of q [batch, heads, 64], whose rows are contiguous."""
+    if not q.is_cuda:
+        raise ValueError("q must be a device tensor")
+    strides = q.stride()
+    if len(strides) != 3 or (strides[2] != 1 and q.shape[2] > 1):
+        raise ValueError("q must be [batch, heads, 64] with contiguous rows")
+    return strides[0], strides[1]
+
+
+def _whole(name: str, t: torch.Tensor, at: int, shape) -> None:
+    """Whether t is an int32 tensor of this shape (None: any number)."""
+    if not t.is_cuda or t.dtype != torch.int32 or t.get_device() != at or not t.is_contiguous():
+        _wrong(t, name, torch.int32, at, "q")
+    if len(t.shape) != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{name} must be {['any' if n is None else n for n in shape]}, got {tuple(t.shape)}")
+
+
+def bsga_paged_attn_e4m3(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                         page_table: torch.Tensor, lengths: torch.Tensor, window: Optional[int] = None, sinks: int = 0, frame: int = 1,
+                         softmax_scale: Optional[float] = None, return_lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """bsga_paged_attn over caches in 8 bits, as bsga_qk_norm_rope_e4m3 writes them: k_cache, v_cache [pages, Hkv, page, 64] of torch.float8_e4m3fn, k_scale,
+    v_scale [pages, Hkv, page] uint8.  q and the result are bfloat16 or float32."""
+    code = _dtype_code(q)
+    strides = _queries(q)
+    B, H, d = q.shape
+    at = q.get_device()
+    if _cache_of(k_cache, v_cache, k_scale, v_scale, torch.float8_e4m3fn, at, d) != BSGA_E4M3:
+        raise TypeError("the caches must be torch.float8_e4m3fn")
+    _whole("page_table", page_table, at, (B, None))
+    _whole("lengths", lengths, at, (B,))
+    if window is not None and window < 1:
+        raise ValueError(f"window must be at least one frame, or None, got {window}")
+    pages, K, page, _ = k_cache.shape
+    width = page_table.shape[1]
+    seen = (frame, 0 if window is None else window, sinks)
+    out = q.new_empty((B, H, d))
+    lse = q.new_empty((B, H), dtype=torch.float32) if return_lse else None
+    if workspace is None:
+        nbytes = lib.bsga_paged_attn_e4m3_workspace_bytes(code, B, H, K, width, pages, page, *seen)
+        if nbytes > 0:
+            workspace = q.new_empty(nbytes, dtype=torch.uint8)
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    _check(lib.bsga_paged_attn_e4m3(_ptr(q), *strides, _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), code, B, H, K, d, _ptr(page_table), width,
+                                    _ptr(lengths), pages, page, 1.0 / math.sqrt(d) if softmax_scale is None else float(softmax_scale), *seen,
+                                    _ptr(out), _ptr(lse), _ptr(workspace), nbytes, _stream(q)))
+    return (out, lse) if return_lse else out
+
+
+def bsga_prefix_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+                     prefix_table: torch.Tensor, prefix_lengths: torch.Tensor, starts: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                     v_scale: Optional[torch.Tensor] = None, window: Optional[int] = None, sinks: int = 0, frame: int = 1,
+                     softmax_scale: Optional[float] = None, return_lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """bsga_paged_attn (or bsga_paged_attn_e4m3, with scales) where sequences begin with tokens that they share, which are read once for all: sequences
+    starts[g] to starts[g + 1] - 1 (int32 [G + 1], not decreasing) see the prefix_lengths[g] (int32 [G]) tokens in the pages prefix_table[g] (int32 [G, prefix
+    width]) and then the lengths[b] tokens of their own in the pages page_table[b]; sequences outside have none.  The query stands at the last of its tokens, and window,
+    sinks and frame go by positions from the prefix's first token on.  Returns O [B, H, 64] (and lse [B, H] float32); a sequence without any token yields zeros and -inf."""
+    code = _dtype_code(q)
+    strides = _queries(q)
+    B, H, d = q.shape
+    at = q.get_device()
+    kind = _cache_of(k_cache, v_cache, k_scale, v_scale, q.dtype, at, d)
+    _whole("page_table", page_table, at, (B, None))
+    _whole("lengths", lengths, at, (B,))
+    _whole("prefix_table", prefix_table, at, (None, None))
+    G, prefix_width = prefix_table.shape
+    _whole("prefix_lengths", prefix_lengths, at, (G,))
+    _whole("starts", starts, at, (G + 1,))
+    if window is not None and window < 1:
+        raise ValueError(f"window must be at least one frame, or None, got {window}")
+    pages, K, page, _ = k_cache.shape
+    width = page_table.shape[1]
+    seen = (frame, 0 if window is None else window, sinks)
+    out = q.new_empty((B, H, d))
+    lse = q.new_empty((B, H), dtype=torch.float32) if return_lse else None
+    if workspace is None:
+        nbytes = lib.bsga_prefix_attn_workspace_bytes(code, kind, B, H, K, width, G, prefix_width, pages, page, *seen)
+        if nbytes > 0:
+            workspace = q.new_empty(nbytes, dtype=torch.uint8)
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    _check(lib.bsga_prefix_attn(_ptr(q), *strides, _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), code, kind, B, H, K, d, _ptr(page_table), width,
+                                _ptr(lengths), _ptr(prefix_table), prefix_width, _ptr(prefix_lengths), _ptr(starts), G, pages, page,
+                                1.0 / math.sqrt(d) if softmax_scale is None else float(softmax_scale), *seen, _ptr(out), _ptr(lse), _ptr(workspace),
+                                nbytes, _stream(q)))
     return (out, lse) if return_lse else out

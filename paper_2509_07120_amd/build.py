@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libbsga.so")
 SOURCES = ["bsga_api.hip", "pool.hip", "select.hip", "gather.hip", "attn_fp32.hip", "attn_bf16.hip", "attn_few.hip", "linear.hip", "probe.hip",
-           "norm_rope.hip", "window.hip", "window_bwd.hip", "paged.hip"]
+           "norm_rope.hip", "window.hip", "window_bwd.hip", "paged.hip", "cache_load.hip", "prefix.hip"]
 
 
 def hipcc_path() -> str:

@@ -9,8 +9,12 @@
 // the lane), and the sums over a row are two quad permutations.  A lane keeps its token over the heads that its workgroup takes: the angles are
 // computed once for them.  Angles are exact: base^(-2j/W) / 2 pi is a 64-bit fraction of a turn, and the product with the position
 // modulo 2^64 is the turn's fraction, whatever the position's size; fp32 would be off by 0.1 at position 10^6.
+//
+// Into a cache in 8 bits (e4m3.h) the row goes from the 32 bits in which it was normed and turned, in one rounding: the largest magnitude is one more
+// pair of quad permutations, and neighbouring lanes swap halves so that each writes 16 bytes.
 #include "bf16_tile.h"
 #include "bsga_internal.h"
+#include "e4m3.h"
 
 #include <math.h>
 
@@ -31,6 +35,7 @@ struct NormRopeArgs {
   int heads[3], group_heads, axes, norm, page;
   float eps;
   unsigned long long turn[32];
+  unsigned char *code[2], *scale[2];  // of k and v, in a cache in 8 bits: y holds the rows as they are read back then, where it is wanted
   // the gradient
   const unsigned char* dy[3];  // [heads, n, 64]
   unsigned char* dx[3];
@@ -150,7 +155,38 @@ __device__ __forceinline__ int kind_of(const NormRopeArgs& a, int y, int& h0, in
   return kind;
 }
 
-template <typename T>
+__device__ __forceinline__ unsigned other_of_pair(unsigned x) {  // lanes 1 0 3 2
+  return static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), 0xb1, 0xf, 0xf, true));
+}
+
+// A row's lanes to 8 bits: the exponent, and the numbers x in code[0], y in code[1].
+__device__ __forceinline__ int to_e4m3(const float (&x)[8], const float (&y)[8], u32x2 (&code)[2]) {
+  float most = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float u = fabsf(x[e]), v = fabsf(y[e]);
+    most = fmaxf(most, fmaxf(u <= 0x1.fffffep127f ? u : 0.f, v <= 0x1.fffffep127f ? v : 0.f));
+  }
+  most = fmaxf(most, __uint_as_float(other_of_pair(__float_as_uint(most))));
+  most = fmaxf(most, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(most), 0x4e, 0xf, 0xf, true)));
+  const int byte = scale_byte(most);
+  const float f = inverse_scale(byte);
+  float u[8], v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    u[e] = x[e] * f;
+    v[e] = y[e] * f;
+    if (byte == kMostScale) {  // the only one whose numbers may be larger
+      u[e] = fabsf(x[e]) <= 0x1.fffffep127f ? fminf(fmaxf(u[e], -448.f), 448.f) : NAN;
+      v[e] = fabsf(y[e]) <= 0x1.fffffep127f ? fminf(fmaxf(v[e], -448.f), 448.f) : NAN;
+    }
+  }
+  code[0] = u32x2{pack_e4m3(u[0], u[1], u[2], u[3]), pack_e4m3(u[4], u[5], u[6], u[7])};
+  code[1] = u32x2{pack_e4m3(v[0], v[1], v[2], v[3]), pack_e4m3(v[4], v[5], v[6], v[7])};
+  return byte;
+}
+
+template <typename T, bool CODED>
 __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
   int h0, h1, group;
   const int kind = kind_of(a, blockIdx.y, h0, h1, group);
@@ -194,7 +230,6 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
 #pragma unroll
     for (int u = 0; u < kHeadsInFlight; ++u) {
       if (h + u >= h1) break;
-      unsigned char* p = dst + (to + (h + u) * step) * kRow;
       float x[8], y[8];
       widen<T>(lo[u], x);
       widen<T>(hi[u], y);
@@ -211,7 +246,36 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
           }
         }
       }
-      if (write) {
+      if (CODED && kind > 0) {
+        u32x2 code[2];
+        const int byte = to_e4m3(x, y, code);
+        // lanes 2j and 2j + 1 hold neighbouring eights of both halves: the first takes those of the first half, the other those of the second
+        const bool odd = c & 1;
+        const u32x2 mine = odd ? code[1] : code[0], gone = odd ? code[0] : code[1];
+        const u32x2 got = {other_of_pair(gone[0]), other_of_pair(gone[1])};
+        if (write) {
+          const int64_t row = to + (h + u) * step;
+          *reinterpret_cast<u32x4*>(a.code[kind - 1] + row * 64 + (odd ? l.second - 8 : l.first)) =
+              odd ? u32x4{got[0], got[1], mine[0], mine[1]} : u32x4{mine[0], mine[1], got[0], got[1]};
+          if (c == 0) a.scale[kind - 1][row] = static_cast<unsigned char>(byte);
+        }
+        if (live && dst != nullptr) {
+          unsigned char* p = dst + ((h + u) * a.n + at) * kRow;
+          const float f = scale_of(byte);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            unsigned char* to_half = p + (half == 0 ? l.first : l.second) * sizeof(T);
+            if constexpr (sizeof(T) == 2) {
+              const u32x2 v0 = unpack_bf16(code[half][0], f), v1 = unpack_bf16(code[half][1], f);
+              *reinterpret_cast<u32x4*>(to_half) = u32x4{v0[0], v0[1], v1[0], v1[1]};
+            } else {
+              reinterpret_cast<f32x4*>(to_half)[0] = unpack_f32(code[half][0]) * f;
+              reinterpret_cast<f32x4*>(to_half)[1] = unpack_f32(code[half][1]) * f;
+            }
+          }
+        }
+      } else if (write) {
+        unsigned char* p = dst + (to + (h + u) * step) * kRow;
         store<T>(p + l.first * sizeof(T), x);
         store<T>(p + l.second * sizeof(T), y);
       }
@@ -412,6 +476,34 @@ int heads_of_a_group(const NormRopeArgs& a, int64_t tiles) {
 
 int groups_of(const NormRopeArgs& a, int kind) { return static_cast<int>(ceil_div(a.heads[kind], a.group_heads)); }
 
+int pages_of(const char* fn, const int32_t* slots, int64_t n_pages, int page, NormRopeArgs& a) {
+  if (!slots) return BSGA_OK;
+  if (page < 1 || page > 65536) return fail(BSGA_ERR_INVALID_ARG, "%s: page must be in [1, 65536] tokens, got %d", fn, page);
+  if (n_pages < 1 || n_pages > ((int64_t(1) << 31) - 1) / page)
+    return fail(BSGA_ERR_INVALID_ARG, "%s: the cache must hold 1 to 2^31 - 1 tokens, got %lld pages of %d", fn, static_cast<long long>(n_pages), page);
+  a.slots = slots;
+  a.page = page;
+  a.n_slots = n_pages * page;
+  return BSGA_OK;
+}
+
+int launch(const char* fn, NormRopeArgs& a, int dtype, bool coded, hipStream_t s) {
+  if (a.n == 0) return BSGA_OK;
+  const int64_t tiles = ceil_div(a.n, kRowsPerGroup);
+  a.group_heads = heads_of_a_group(a, tiles);
+  const int64_t groups = int64_t(groups_of(a, 0)) + groups_of(a, 1) + groups_of(a, 2);
+  if (groups > 65535) return fail(BSGA_ERR_UNSUPPORTED, "%s: too many heads", fn);
+  const dim3 grid(static_cast<unsigned>(tiles), static_cast<unsigned>(groups));
+  if (dtype == BSGA_BF16) {
+    if (coded) hipLaunchKernelGGL((norm_rope_kernel<__bf16, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((norm_rope_kernel<__bf16, false>), grid, dim3(256), 0, s, a);
+  } else {
+    if (coded) hipLaunchKernelGGL((norm_rope_kernel<float, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((norm_rope_kernel<float, false>), grid, dim3(256), 0, s, a);
+  }
+  return check_hip(hipGetLastError(), fn);
+}
+
 }  // namespace
 }  // namespace bsga
 
@@ -437,24 +529,40 @@ int bsga_qk_norm_rope(const void* q, const void* k, const void* v, int64_t q_tok
     if (!aligned16(y[t])) return fail(BSGA_ERR_INVALID_ARG, "%s: outputs must be 16-byte aligned", fn);
     a.y[t] = static_cast<unsigned char*>(y[t]);
   }
-  if (slots) {
-    if (page < 1 || page > 65536) return fail(BSGA_ERR_INVALID_ARG, "%s: page must be in [1, 65536] tokens, got %d", fn, page);
-    if (n_pages < 1 || n_pages > ((int64_t(1) << 31) - 1) / page)
-      return fail(BSGA_ERR_INVALID_ARG, "%s: the cache must hold 1 to 2^31 - 1 tokens, got %lld pages of %d", fn, static_cast<long long>(n_pages), page);
-    a.slots = slots;
-    a.page = page;
-    a.n_slots = n_pages * page;
+  if (int rc = pages_of(fn, slots, n_pages, page, a)) return rc;
+  return launch(fn, a, dtype, false, static_cast<hipStream_t>(stream));
+}
+
+int bsga_qk_norm_rope_e4m3(const void* q, const void* k, const void* v, int64_t q_token, int64_t q_head, int64_t k_token, int64_t k_head,
+                           int64_t v_token, int64_t v_head, int dtype, int64_t n_tokens, int heads, int kv_heads, int head_dim, int norm, double eps,
+                           const void* q_weight, const void* q_bias, const void* k_weight, const void* k_bias, const int32_t* positions, int axes,
+                           double base, const int32_t* slots, int64_t n_pages, int page, void* q_out, void* k_rows, void* v_rows, void* k_cache,
+                           void* v_cache, uint8_t* k_scale, uint8_t* v_scale, void* stream) {
+  const char* fn = "bsga_qk_norm_rope_e4m3";
+  clear_error();
+  NormRopeArgs a = {};
+  const void* const x[3] = {q, k, v};
+  void* const y[3] = {q_out, k_rows, v_rows};
+  void* const code[2] = {k_cache, v_cache};
+  uint8_t* const scale[2] = {k_scale, v_scale};
+  if (int rc = common(fn, x, {q_token, q_head, k_token, k_head, v_token, v_head}, dtype, n_tokens, heads, kv_heads, head_dim, norm, eps,
+                      {q_weight, k_weight}, {q_bias, k_bias}, positions, axes, base, a))
+    return rc;
+  for (int t = 0; t < 3; ++t) {
+    if (!aligned16(y[t])) return fail(BSGA_ERR_INVALID_ARG, "%s: outputs must be 16-byte aligned", fn);
+    a.y[t] = static_cast<unsigned char*>(y[t]);
+    if (n_tokens == 0) continue;  // (tensors without elements have no address)
+    if (t == 0 ? !q != !q_out : !x[t] && y[t]) return fail(BSGA_ERR_INVALID_ARG, "%s: outputs go with their inputs", fn);
+    if (t == 0) continue;
+    if (!x[t] != !code[t - 1] || !x[t] != !scale[t - 1])
+      return fail(BSGA_ERR_INVALID_ARG, "%s: k and v must each come with its cache and its scales", fn);
+    if (!aligned16(code[t - 1])) return fail(BSGA_ERR_INVALID_ARG, "%s: caches must be 16-byte aligned", fn);
+    a.code[t - 1] = static_cast<unsigned char*>(code[t - 1]);
+    a.scale[t - 1] = scale[t - 1];
   }
-  if (n_tokens == 0) return BSGA_OK;
-  const int64_t tiles = ceil_div(n_tokens, kRowsPerGroup);
-  a.group_heads = heads_of_a_group(a, tiles);
-  const int64_t groups = int64_t(groups_of(a, 0)) + groups_of(a, 1) + groups_of(a, 2);
-  if (groups > 65535) return fail(BSGA_ERR_UNSUPPORTED, "%s: too many heads", fn);
-  const dim3 grid(static_cast<unsigned>(tiles), static_cast<unsigned>(groups));
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  if (dtype == BSGA_BF16) hipLaunchKernelGGL(norm_rope_kernel<__bf16>, grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(norm_rope_kernel<float>, grid, dim3(256), 0, s, a);
-  return check_hip(hipGetLastError(), "bsga_qk_norm_rope launch");
+  if (n_tokens > 0 && (k || v) && !slots) return fail(BSGA_ERR_INVALID_ARG, "%s: slots must be non-null", fn);
+  if (int rc = pages_of(fn, slots, n_pages, page, a)) return rc;
+  return launch(fn, a, dtype, true, static_cast<hipStream_t>(stream));
 }
 
 // The workgroups over which a launch's tokens are spread, and the heads of each; needs n, heads.

@@ -1,0 +1,494 @@
+// What the kernels of attention over pages share: operands of 16x16 products for every type of queries and caches, where the keys of a sequence lie, and the
+// loop in which a wave goes over its pieces of them.
+//
+// Query i of a workgroup is column i of S^T = K Q^T and O^T = V^T P^T, in which the weights are operands as they lie in the results.  A piece of keys and
+// values goes from memory straight into the wave's own LDS, two pieces ahead; no wave waits for another.
+#pragma once
+
+#include "e4m3.h"
+#include "window.h"
+
+namespace bsga {
+namespace {
+
+constexpr int kTable = 2048;   // page numbers of a stretch
+constexpr int kHeads = 16;     // queries of a workgroup
+constexpr int kWaves = 4;
+
+// T: type of the queries and results, C: of the cache.
+template <typename T, typename C>
+struct Ops16;
+
+template <>
+struct Ops16<__bf16, __bf16> {
+  typedef bf16x8 A;
+  typedef __bf16 Cache;
+  static constexpr int kRow = 128;   // bytes of a key
+  static constexpr bool kScaled = false;
+  static constexpr int kKeys = 32;   // of a piece
+  static constexpr int kBlocks = 2;  // of 16 keys
+  static constexpr int kSteps = 2;   // products over the 64 numbers of a row
+  static __device__ __forceinline__ f32x4 product(A a, A b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ int swizzle_k(int r) { return swz_k(r); }
+  static __device__ __forceinline__ int swizzle_v(int r) { return swz_v(r); }
+  static __device__ __forceinline__ f32x4 value(const unsigned char* tile, const unsigned*, int r, int d) {  // numbers d .. d + 3 of a value, d a multiple of 4
+    const u32x2 x = *LDS_PTR(u32x2, tile + r * kRow + (((d >> 3) ^ swizzle_v(r)) << 4) + (d & 4) * 2);
+    return f32x4{__uint_as_float(x[0] << 16), __uint_as_float(x[0] & 0xffff0000u), __uint_as_float(x[1] << 16), __uint_as_float(x[1] & 0xffff0000u)};
+  }
+  static __device__ __forceinline__ void row(const unsigned char* p, int q, A (&a)[kSteps]) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) a[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p + (4 * c + q) * 16));
+  }
+  static __device__ __forceinline__ void rows(const unsigned char* tile, const unsigned*, int r, int q, A (&a)[kSteps]) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) a[c] = *LDS_PTR(bf16x8, tile + r * 128 + (((4 * c + q) ^ swz_k(r)) << 4));
+  }
+  // o += V^T P^T: the weights' products in w[block][r], of keys 16 block + 4 q + r
+  static __device__ __forceinline__ void update(const unsigned char* tile, const unsigned*, int lane, const f32x4 (&w)[kBlocks], f32x4 (&o)[4]) {
+    const int m = (lane & 15) >> 2, j = lane & 3, q = lane >> 4;
+    const bf16x8 b = __builtin_bit_cast(
+        bf16x8, u32x4{pack_bf16(w[0][0], w[0][1]), pack_bf16(w[0][2], w[0][3]), pack_bf16(w[1][0], w[1][1]), pack_bf16(w[1][2], w[1][3])});
+#pragma unroll
+    for (int db = 0; db < 4; ++db) {
+      u32x2 x[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = 16 * e + 4 * q + m;
+        const unsigned char* p = tile + r * 128 + (((2 * db + (j >> 1)) ^ swz_v(r)) << 4) + (j & 1) * 8;
+        x[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(p)));
+      }
+      o[db] = product(__builtin_bit_cast(bf16x8, u32x4{x[0][0], x[0][1], x[1][0], x[1][1]}), b, o[db]);
+    }
+  }
+};
+
+template <>
+struct Ops16<float, float> {
+  typedef float A;
+  typedef float Cache;
+  static constexpr int kRow = 256;
+  static constexpr bool kScaled = false;
+  static constexpr int kKeys = 16;
+  static constexpr int kBlocks = 1;
+  static constexpr int kSteps = 16;
+  static __device__ __forceinline__ f32x4 product(A a, A b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ int swizzle_k(int r) { return r & 15; }
+  static __device__ __forceinline__ int swizzle_v(int r) { return r & 15; }
+  static __device__ __forceinline__ f32x4 value(const unsigned char* tile, const unsigned*, int r, int d) {
+    return *LDS_PTR(f32x4, tile + r * kRow + (((d >> 2) ^ swizzle_v(r)) << 4));
+  }
+  static __device__ __forceinline__ void row(const unsigned char* p, int q, A (&a)[kSteps]) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(p + (4 * c + q) * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[4 * c + e] = x[e];
+    }
+  }
+  static __device__ __forceinline__ void rows(const unsigned char* tile, const unsigned*, int r, int q, A (&a)[kSteps]) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const f32x4 x = *LDS_PTR(f32x4, tile + r * 256 + (((4 * c + q) ^ swizzle_k(r)) << 4));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[4 * c + e] = x[e];
+    }
+  }
+  static __device__ __forceinline__ void update(const unsigned char* tile, const unsigned*, int lane, const f32x4 (&w)[kBlocks], f32x4 (&o)[4]) {
+    const int q = lane >> 4;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 4 * q + e, d = 16 * db + (lane & 15);
+        o[db] = product(*LDS_PTR(float, tile + r * 256 + (((d >> 2) ^ swizzle_v(r)) << 4) + (d & 3) * 4), w[0][e], o[db]);
+      }
+  }
+};
+
+// Rows of 64 bytes.  A lane takes 16 numbers of a key at once, so that its products go over the numbers 16 q .. 16 q + 15 in two steps, or in sixteen; queries
+// are laid out for that.  Keys are multiplied by their scale, which is exact; a value's scale goes to its weight, which is in 32 bits there.  Rows are four to
+// the 64 banks: the swizzles keep apart the rows r, r + 4, r + 8, r + 12 that are read whole, and r, r + 4, r + 16, r + 20 that are read transposed.
+struct Ops16E4m3 {
+  typedef E4m3 Cache;
+  static constexpr int kRow = 64;
+  static constexpr bool kScaled = true;
+  static constexpr int kKeys = 64;
+  static constexpr int kBlocks = 4;
+  static __device__ __forceinline__ int swizzle_k(int r) { return (r >> 2) & 3; }
+  static __device__ __forceinline__ int swizzle_v(int r) { return ((r >> 2) & 1) | ((r >> 3) & 2); }
+  static __device__ __forceinline__ f32x4 value(const unsigned char* tile, const unsigned* scales, int r, int d) {
+    return unpack_f32(*LDS_PTR(unsigned, tile + r * kRow + (((d >> 4) ^ swizzle_v(r)) << 4) + (d & 12))) * scale_of(*LDS_PTR(unsigned, scales + r));
+  }
+  static __device__ __forceinline__ u32x4 codes(const unsigned char* tile, int r, int q) { return *LDS_PTR(u32x4, tile + r * kRow + ((q ^ swizzle_k(r)) << 4)); }
+  // number 16 db + (lane & 15) of the keys 32 h + 4 q .. + 3 and 32 h + 16 + 4 q .. + 3
+  static __device__ __forceinline__ u32x2 column(const unsigned char* tile, int lane, int h, int db) {
+    const int m = (lane & 15) >> 1, q = lane >> 4;
+    const int r = 32 * h + 4 * q + (m & 3) + 4 * (m & 4);
+    const unsigned char* p = tile + r * kRow + ((db ^ swizzle_v(r)) << 4) + (lane & 1) * 8;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((s32x2 __attribute__((address_space(3)))*)(p)));
+  }
+  // the weights of keys 16 block + 4 q + r times their values' scales
+  static __device__ __forceinline__ f32x4 scaled(const unsigned* scales, int lane, int block, const f32x4& w) {
+    const u32x4 b = *LDS_PTR(u32x4, scales + 16 * block + 4 * (lane >> 4));
+    f32x4 y;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) y[r] = w[r] * scale_of(b[r]);
+    return y;
+  }
+};
+
+template <>
+struct Ops16<__bf16, E4m3> : Ops16E4m3 {
+  typedef bf16x8 A;
+  static constexpr int kSteps = 2;
+  static __device__ __forceinline__ f32x4 product(A a, A b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ void row(const unsigned char* p, int q, A (&a)[kSteps]) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) a[e] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p + q * 32 + e * 16));
+  }
+  static __device__ __forceinline__ void rows(const unsigned char* tile, const unsigned* scales, int r, int q, A (&a)[kSteps]) {
+    const u32x4 x = codes(tile, r, q);
+    const float f = scale_of(*LDS_PTR(unsigned, scales + r));
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const u32x2 y0 = unpack_bf16(x[2 * e], f), y1 = unpack_bf16(x[2 * e + 1], f);
+      a[e] = __builtin_bit_cast(bf16x8, u32x4{y0[0], y0[1], y1[0], y1[1]});
+    }
+  }
+  static __device__ __forceinline__ void update(const unsigned char* tile, const unsigned* scales, int lane, const f32x4 (&w)[kBlocks], f32x4 (&o)[4]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4 w0 = scaled(scales, lane, 2 * h, w[2 * h]), w1 = scaled(scales, lane, 2 * h + 1, w[2 * h + 1]);
+      const bf16x8 b = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(w0[0], w0[1]), pack_bf16(w0[2], w0[3]), pack_bf16(w1[0], w1[1]), pack_bf16(w1[2], w1[3])});
+#pragma unroll
+      for (int db = 0; db < 4; ++db) {
+        const u32x2 x = column(tile, lane, h, db);
+        const u32x2 y0 = unpack_bf16(x[0], 1.f), y1 = unpack_bf16(x[1], 1.f);
+        o[db] = product(__builtin_bit_cast(bf16x8, u32x4{y0[0], y0[1], y1[0], y1[1]}), b, o[db]);
+      }
+    }
+  }
+};
+
+template <>
+struct Ops16<float, E4m3> : Ops16E4m3 {
+  typedef float A;
+  static constexpr int kSteps = 16;
+  static __device__ __forceinline__ f32x4 product(A a, A b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ void row(const unsigned char* p, int q, A (&a)[kSteps]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(p + q * 64 + e * 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[4 * e + i] = x[i];
+    }
+  }
+  static __device__ __forceinline__ void rows(const unsigned char* tile, const unsigned* scales, int r, int q, A (&a)[kSteps]) {
+    const u32x4 x = codes(tile, r, q);
+    const float f = scale_of(*LDS_PTR(unsigned, scales + r));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f32x4 y = unpack_f32(x[e]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[4 * e + i] = y[i] * f;
+    }
+  }
+  static __device__ __forceinline__ void update(const unsigned char* tile, const unsigned* scales, int lane, const f32x4 (&w)[kBlocks], f32x4 (&o)[4]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4 w0 = scaled(scales, lane, 2 * h, w[2 * h]), w1 = scaled(scales, lane, 2 * h + 1, w[2 * h + 1]);
+#pragma unroll
+      for (int db = 0; db < 4; ++db) {
+        const u32x2 x = column(tile, lane, h, db);
+        const f32x4 y0 = unpack_f32(x[0]), y1 = unpack_f32(x[1]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[db] = product(y0[e], w0[e], o[db]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[db] = product(y1[e], w1[e], o[db]);
+      }
+    }
+  }
+};
+
+// Whether one of the 16 bytes' numbers is not finite.
+template <typename C>
+__device__ __forceinline__ bool any_bad(const u32x4& x) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (std::is_same<C, float>::value) bad = bad || (x[i] & 0x7f800000u) == 0x7f800000u;
+    else if constexpr (std::is_same<C, __bf16>::value) bad = bad || (x[i] & 0x7f80u) == 0x7f80u || (x[i] & 0x7f800000u) == 0x7f800000u;
+    else
+#pragma unroll
+      for (int e = 0; e < 32; e += 8) bad = bad || ((x[i] >> e) & 0x7fu) == 0x7fu;
+  }
+  return bad;
+}
+
+// The pages of a cache.
+struct Pages {
+  const unsigned char *k, *v;          // [n_pages, kv_heads, page, 64]
+  const unsigned char *k_scale, *v_scale;  // [n_pages, kv_heads, page] exponent bytes, of a cache in 8 bits
+  int kv_heads, n_pages, page;
+  unsigned magic;                      // j / page = umulhi(2 j, magic) >> shift, for j < 2^31
+  int shift;
+  __device__ __forceinline__ int of(int j) const { return static_cast<int>(__umulhi(static_cast<unsigned>(j) << 1, magic) >> shift); }
+};
+
+// 16 bytes per lane from memory straight into LDS, as dma16, from a 64-bit address for each lane.
+__device__ __forceinline__ void dma16_at(const unsigned char* p, unsigned lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"  // one wait state between a scalar write of M0 and an LDS-DMA instruction that reads it
+      "global_load_lds_dwordx4 %1, off"
+      :
+      : "s"(lds), "v"(p)
+      : "memory", "m0");
+}
+
+// A byte per lane, as 32 bits at lds + 4 * lane.
+__device__ __forceinline__ void dma_byte_at(const unsigned char* p, unsigned lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_ubyte %1, off"
+      :
+      : "s"(lds), "v"(p)
+      : "memory", "m0");
+}
+
+__device__ __forceinline__ float across(float x, bool maximum) {  // over the four lanes of a column
+#pragma unroll
+  for (int o = 16; o < 64; o <<= 1) {
+    const float y = __shfl_xor(x, o);
+    x = maximum ? fmaxf(x, y) : x + y;
+  }
+  return x;
+}
+
+// The keys that a workgroup goes over: those that a sequence sees, numbered through (x < s is key x, the others lo + x - s), from x0 to x1.  Their page
+// numbers lie in LDS, those of the first tokens before those of the window.
+struct Stretch {
+  int s, lo, x0, x1, a0, a_pages, b0;
+  __device__ __forceinline__ int key(int x) const { return x < s ? x : lo + x - s; }
+  // from x0 to x1, x0 < x1; all threads of the workgroup; a barrier has to follow
+  __device__ __forceinline__ void fill(const Pages& a, const int32_t* pages, int* table) {
+    a0 = a.of(x0), a_pages = x0 < min(x1, s) ? a.of(min(x1, s) - 1) - a0 + 1 : 0;
+    b0 = a.of(lo + max(x0, s) - s);
+    const int b_pages = max(x0, s) < x1 ? a.of(lo + x1 - 1 - s) - b0 + 1 : 0;
+    for (int i = threadIdx.x; i < min(a_pages + b_pages, kTable); i += 64 * kWaves)
+      table[i] = min(max(pages[i < a_pages ? a0 + i : b0 + i - a_pages], 0), a.n_pages - 1);  // a bad entry cannot read out of bounds
+  }
+  // the cache row, of head hk, of the x-th key
+  __device__ __forceinline__ int64_t row(const Pages& a, const int* table, int hk, int x) const {
+    const int j = key(x);
+    const int page = a.of(j);
+    const int at = table[min(x < s ? page - a0 : a_pages + page - b0, kTable - 1)];
+    return (int64_t(at) * a.kv_heads + hk) * a.page + (j - page * a.page);
+  }
+};
+
+template <typename P>
+constexpr int kPiece = P::kKeys * P::kRow;
+template <typename P>
+constexpr int kBuf = 2 * kPiece<P> + (P::kScaled ? 2 * P::kKeys * 4 : 0);  // keys, values, the exponents of both
+template <typename P>
+constexpr int kWaveLds = 2 * kBuf<P>;
+
+// Values that are not finite must not reach columns that do not see them, where a weight of zero would still make NaN of them: such keys are added here for
+// the columns that see them, and are zeros for the matrix product.  Only pieces of which some columns see a part come here.
+template <typename P, typename SeenI>
+__device__ __forceinline__ void leave_bad_out(unsigned char* tile, unsigned* scales, int lane, int left, SeenI seen, const f32x4 (&w)[P::kBlocks], f32x4 (&o)[4]) {
+  constexpr int kChunks = P::kRow / 16, kRowsOfLoad = 64 / kChunks;
+  unsigned long long bad[4], any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const u32x4 x = *LDS_PTR(u32x4, tile + i * 1024 + lane * 16);
+    bad[i] = __ballot(any_bad<typename P::Cache>(x));
+    any |= bad[i];
+  }
+  if (any == 0) return;
+  const int c = lane & 15, q = lane >> 4;
+#pragma unroll
+  for (int blk = 0; blk < P::kBlocks; ++blk)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      for (int qq = 0; qq < 4; ++qq) {
+        const int i = 16 * blk + 4 * qq + r, load = i / kRowsOfLoad;
+        const unsigned long long of = load == 0 ? bad[0] : load == 1 ? bad[1] : load == 2 ? bad[2] : bad[3];
+        const float weight = __shfl(w[blk][r], c + 16 * qq);
+        if (((of >> (i % kRowsOfLoad * kChunks)) & ((1ull << kChunks) - 1)) == 0 || i >= left || !seen(i)) continue;
+#pragma unroll
+        for (int db = 0; db < 4; ++db) o[db] += P::value(tile, scales, i, 16 * db + 4 * q) * weight;
+      }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if ((bad[i] >> (lane / kChunks * kChunks)) & ((1ull << kChunks) - 1)) *reinterpret_cast<u32x4*>(tile + i * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
+}
+
+// One wave over its pieces: what its columns have of maxima, sums (those of a column's four lanes are still to be added) and weighted values.  seen(key, x) tells
+// whether the lane's column sees the key, where MASKED.
+template <typename P, bool MASKED, typename Seen1>
+__device__ __forceinline__ void go_over(const Pages& a, const Stretch& st, const int* table, int hk, int wave, int lane, unsigned char* mine, float scale_log2,
+                                        const typename P::A (&qf)[P::kSteps], Seen1 seen, f32x4 (&o)[4], float& m, float& l) {
+  constexpr int kChunks = P::kRow / 16, kRowsOfLoad = 64 / kChunks, kLoads = P::kKeys / kRowsOfLoad;
+  static_assert(kLoads == 4, "eight loads of a piece");
+  const int c = lane & 15, q = lane >> 4;
+  const unsigned lds = __builtin_amdgcn_readfirstlane(lds_address(mine));
+  const int pieces = (st.x1 - st.x0 + P::kKeys - 1) / P::kKeys;
+  const int r_in = lane / kChunks, pos = lane % kChunks;
+  auto issue = [&](int p, int buf) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = i * kRowsOfLoad + r_in;
+      const int64_t row = st.row(a, table, hk, min(st.x0 + p * P::kKeys + r, st.x1 - 1));  // rows past the end are the last one again, with no weight
+      dma16_at(a.k + row * P::kRow + ((pos ^ P::swizzle_k(r)) << 4), lds + buf * kBuf<P> + i * 1024);
+      dma16_at(a.v + row * P::kRow + ((pos ^ P::swizzle_v(r)) << 4), lds + buf * kBuf<P> + kPiece<P> + i * 1024);
+    }
+    if constexpr (P::kScaled) {
+      static_assert(P::kKeys == 64, "a lane to a key");
+      const int64_t row = st.row(a, table, hk, min(st.x0 + p * P::kKeys + lane, st.x1 - 1));
+      dma_byte_at(a.k_scale + row, lds + buf * kBuf<P> + 2 * kPiece<P>);
+      dma_byte_at(a.v_scale + row, lds + buf * kBuf<P> + 2 * kPiece<P> + 256);
+    }
+  };
+  if (wave < pieces) issue(wave, 0);
+  if (wave + kWaves < pieces) issue(wave + kWaves, 1);
+
+  m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int db = 0; db < 4; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  int buf = 0;
+  for (int p = wave; p < pieces; p += kWaves, buf ^= 1) {
+    if (p + kWaves >= pieces) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    else if constexpr (P::kScaled) asm volatile("s_waitcnt vmcnt(10)" ::: "memory");  // the next piece's loads may be on their way
+    else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+    unsigned char* const kt = mine + buf * kBuf<P>;
+    unsigned* const scales = reinterpret_cast<unsigned*>(kt + 2 * kPiece<P>);
+    const int left = st.x1 - st.x0 - p * P::kKeys;
+    if (left < P::kKeys) {  // the repeated values have weights of zero, which is not nothing if the last one is infinite
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = i * kRowsOfLoad + r_in;
+        if (r >= left) *reinterpret_cast<u32x4*>(kt + kPiece<P> + r * P::kRow + pos * 16) = u32x4{0u, 0u, 0u, 0u};
+      }
+      if constexpr (P::kScaled)
+        if (lane >= left) scales[64 + lane] = 0u;
+    }
+    f32x4 w[P::kBlocks];
+#pragma unroll
+    for (int blk = 0; blk < P::kBlocks; ++blk) {
+      typename P::A ka[P::kSteps];
+      P::rows(kt, scales, 16 * blk + c, q, ka);
+      w[blk] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < P::kSteps; ++e) w[blk] = P::product(ka[e], qf[e], w[blk]);
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int blk = 0; blk < P::kBlocks; ++blk)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = 16 * blk + 4 * q + r;
+        if (i >= left || (MASKED && !seen(st.key(st.x0 + p * P::kKeys + i)))) w[blk][r] = -INFINITY;
+        top = fmaxf(top, w[blk][r]);
+      }
+    top = across(top, true) * scale_log2;
+    if (__any(top > m)) {
+      const float to = fmaxf(m, top);
+      const float keep = to == -INFINITY ? 1.f : exp2f(m - to);
+      m = to;
+      l *= keep;
+#pragma unroll
+      for (int db = 0; db < 4; ++db) o[db] *= keep;
+    }
+    const float from = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int blk = 0; blk < P::kBlocks; ++blk)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        w[blk][r] = __builtin_amdgcn_exp2f(fmaf(w[blk][r], scale_log2, -from));
+        l += w[blk][r];
+      }
+    if constexpr (MASKED) leave_bad_out<P>(kt + kPiece<P>, scales + 64, lane, left, [&](int i) { return seen(st.key(st.x0 + p * P::kKeys + i)); }, w, o);
+    P::update(kt + kPiece<P>, scales + 64, lane, w, o);
+    if (p + 2 * kWaves < pieces) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the operands are in registers: the buffer is free
+      issue(p + 2 * kWaves, buf);
+    }
+  }
+}
+
+// The waves' sums together, each through its own LDS (none of its loads are on their way any more): thread t of the workgroup has numbers 4 (t % 16) .. + 3 of column
+// t / 16, not divided by the sum yet.
+template <typename P>
+__device__ __forceinline__ void join_waves(unsigned char* smem, float (&sums)[kWaves][2][kHeads], int wave, int lane, const f32x4 (&o)[4], float m, float l,
+                                           f32x4& y, float& top, float& sum) {
+  static_assert(kWaveLds<P> >= kHeads * 64 * 4, "sixteen columns in 32 bits");
+  const int c = lane & 15, q = lane >> 4;
+  unsigned char* const mine = smem + wave * kWaveLds<P>;
+  l = across(l, false);
+#pragma unroll
+  for (int db = 0; db < 4; ++db) *reinterpret_cast<f32x4*>(mine + (c * 64 + 16 * db + 4 * q) * 4) = o[db];
+  if (q == 0) {
+    sums[wave][0][c] = m;
+    sums[wave][1][c] = l;
+  }
+  __syncthreads();
+  const int head = threadIdx.x >> 4, d = (threadIdx.x & 15) * 4;
+  top = -INFINITY;
+  bool nan = false;
+#pragma unroll
+  for (int x = 0; x < kWaves; ++x) {
+    top = fmaxf(top, sums[x][0][head]);
+    nan = nan || sums[x][1][head] != sums[x][1][head];
+  }
+  sum = 0.f;
+  y = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int x = 0; x < kWaves; ++x) {
+    const float weight = sums[x][0][head] == -INFINITY ? 0.f : exp2f(sums[x][0][head] - top);
+    sum += sums[x][1][head] * weight;
+    y += *reinterpret_cast<const f32x4*>(smem + x * kWaveLds<P> + (head * 64 + d) * 4) * weight;
+  }
+  if (nan) sum = NAN;
+}
+
+// Keys of a workgroup, and workgroups of a sequence's (or prefix's) keys, `units` of which there are, with at most `most` keys that are seen.  The chip holds
+// 512, and 300 with 64 KB on their way each draw what the memory gives; stretches cost a second
+// kernel, and each wave should have a few pieces.  Measured, us, for at least 512 / 1024 / 2048 / 4096 workgroups: one sequence of 10,992 bf16 keys and 16
+// key heads 14.6 / 15.2 / 15.3 / 15.2; two of 412,200 and 312,300 508 / 482 / 487 / 495; 96 of up to 4,100 keys and 4 key heads 60 (no
+// stretches) / 70 / 64 / 67.  The host knows the most that a sequence can see, not its length: one long sequence among short ones must not be left to one
+// workgroup (4,608 keys take one about 30 us), and the workgroups that find nothing to do have to stay few.
+// Up to 8 pieces for each wave are one workgroup's whatever the launch: 1,024 bf16 keys 9.9 us a call and 27.2 alone, in stretches of 256 with
+// their second kernel 13.8 and 26.7; 512 fp32 keys 13.0 and 30.3, 14.2 and 29.7.
+inline void cut(int64_t most, int64_t units, int keys_of_piece, int page, int& stretch_out, int& splits_out) {
+  most = larger(most, int64_t(1));
+  const int64_t step = kWaves * keys_of_piece;
+  if (most <= 8 * step) {
+    stretch_out = static_cast<int>(ceil_div(most, step) * step);
+    splits_out = 1;
+    return;
+  }
+  int64_t splits = larger(int64_t(units > 256 || most * units < 512 * 1024 ? 512 : 1024) / units, int64_t(1));
+  if (units > 256) splits = larger(splits, smaller(ceil_div(most, 4608), int64_t(4096) / units));
+  const int64_t stretch = ceil_div(larger(ceil_div(most, splits), 2 * step), step) * step;
+  const int64_t fits = int64_t(kTable - 4) * page / step * step;
+  stretch_out = static_cast<int>(smaller(smaller(stretch, fits), ceil_div(most, step) * step));
+  splits_out = static_cast<int>(ceil_div(most, stretch_out));
+}
+
+inline int check_pages(const char* fn, int kv_heads, int64_t n_pages, int page, Pages& a) {
+  if (page < 1 || page > 65536) return fail(BSGA_ERR_INVALID_ARG, "%s: page must be in [1, 65536] tokens, got %d", fn, page);
+  if (n_pages < 0 || n_pages > (int64_t(1) << 30)) return fail(BSGA_ERR_INVALID_ARG, "%s: n_pages must be in [0, 2^30], got %lld", fn, (long long)n_pages);
+  a.kv_heads = kv_heads;
+  a.n_pages = static_cast<int>(n_pages);
+  a.page = page;
+  a.shift = 0;
+  while ((int64_t(1) << a.shift) < page) ++a.shift;
+  a.magic = static_cast<unsigned>(((uint64_t(1) << (31 + a.shift)) + page - 1) / page);
+  return BSGA_OK;
+}
+
+}  // namespace
+}  // namespace bsga
