@@ -396,8 +396,8 @@ int bsga_paged_attn(const void* q, int64_t q_batch, int64_t q_head, const void* 
 /*
  * Caches in 8 bits.  A row of 64 numbers is held as 64 e4m3 numbers (OCP: up to 448, no infinities) in a cache [n_pages, kv_heads, page, 64] and one exponent
  * byte in a tensor of scales [n_pages, kv_heads, page]: a number c of the row stands for c * 2^(byte - 127).  The byte is
- * 127 + s, where s is the least integer in [-64, 88] with max |x| <= 448 * 2^s over the row's finite numbers x, and x / 2^s is rounded to
- * the nearest e4m3 number (to even; at most 2^-4 of x off, or 2^(s - 10) if that is more).  Finite numbers above 448 * 2^88 become that, infinities and NaN become NaN.
+ * 127 + s, where s is the least integer in [-64, 80] with max |x| <= 448 * 2^s over the row's finite numbers x, and x / 2^s is rounded to
+ * the nearest e4m3 number (to even; at most 2^-4 of x off, or 2^(s - 10) if that is more).  Finite numbers above 448 * 2^80 become that, infinities and NaN become NaN.
  * Other bytes may be read (what they stand for may overflow in sums, or vanish).
  * What a row stands for is exact in bf16.
  *

@@ -2,8 +2,8 @@
 // the row; a number c stands for c * 2^(b - 127).  The exponent is the least that keeps the row's largest finite number at or below 448, so that every
 // rounding is at most half a step, 2^-4 of the number, down to 2^-15 of the largest.  A power of two and no factor of 32 bits: what a number
 // stands for has four significant bits and is exact in bf16, and one byte of 65 is the scale, where a factor would take four of 68 and round again.
-// Exponents stay in [-64, 88]: the weights of an attention, at most 1, times scales from there on are no subnormal numbers, and 2^30 keys of 448 * 2^88 add up to less than
-// there is in 32 bits.  So numbers above 448 * 2^88 = 1.4e29 become that, and those below 2^-74 become zero.
+// Exponents stay in [-64, 80]: the weights of an attention times scales from there on are no subnormal numbers, and 2^30 keys of 448 * 2^80 with weights up to 2^8 add up
+// to less than there is in 32 bits.  So numbers above 448 * 2^80 = 5.4e26 become that, and those below 2^-74 become zero.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -14,7 +14,7 @@ namespace bsga {
 namespace {
 
 struct E4m3 {};                     // as a type of a cache
-constexpr int kLeastScale = 127 - 64, kMostScale = 127 + 88;
+constexpr int kLeastScale = 127 - 64, kMostScale = 127 + 80;
 
 // The exponent byte of a row whose largest finite magnitude is `most`: 448 = 1.75 * 2^8.
 __device__ __forceinline__ int scale_byte(float most) {

@@ -212,7 +212,7 @@ struct Ops16<float, E4m3> : Ops16E4m3 {
 
 // Whether one of the 16 bytes' numbers is not finite.
 template <typename C>
-__device__ __forceinline__ bool any_bad(const u32x4& x) {
+__device__ __forceinline__ bool any_bad(u32x4 x) {
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -243,6 +243,27 @@ __device__ __forceinline__ void dma16_at(const unsigned char* p, unsigned lds) {
       "global_load_lds_dwordx4 %1, off"
       :
       : "s"(lds), "v"(p)
+      : "memory", "m0");
+}
+
+// The same from an address that all lanes share and a 32-bit offset for each.
+__device__ __forceinline__ void dma16_from(const unsigned char* base, unsigned offset, unsigned lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2"
+      :
+      : "s"(lds), "v"(offset), "s"(base)
+      : "memory", "m0");
+}
+
+__device__ __forceinline__ void dma_byte_from(const unsigned char* base, unsigned offset, unsigned lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_ubyte %1, %2"
+      :
+      : "s"(lds), "v"(offset), "s"(base)
       : "memory", "m0");
 }
 
@@ -288,6 +309,101 @@ struct Stretch {
   }
 };
 
+// Pieces of keys and values on their way into a wave's LDS: kKeys keys, then as many values, then the exponents of both.  A piece that lies in one page has one address for
+// all lanes, and its lanes' offsets are known beforehand: no vector instructions; others look their rows up lane by lane.
+template <typename P>
+struct PieceLoad {
+  static constexpr int kChunks = P::kRow / 16, kRowsOfLoad = 64 / kChunks, kLoads = P::kKeys / kRowsOfLoad, kBytes = P::kKeys * P::kRow;
+  static constexpr int kInFlight = 2 * kLoads + (P::kScaled ? 2 : 0);  // loads of a piece
+  static_assert(kLoads == 4, "eight loads of keys and values");
+  unsigned k[kLoads], v[kLoads];
+  int lane, r_in, pos;
+
+  __device__ __forceinline__ explicit PieceLoad(int lane) : lane(lane), r_in(lane / kChunks), pos(lane % kChunks) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = i * kRowsOfLoad + r_in;
+      k[i] = r * P::kRow + ((pos ^ P::swizzle_k(r)) << 4);
+      v[i] = r * P::kRow + ((pos ^ P::swizzle_v(r)) << 4);
+    }
+  }
+  // the keys from the x-th on
+  __device__ __forceinline__ void issue(const Pages& a, const Stretch& st, const int* table, int hk, int x, unsigned lds) const {
+    x = scalar(x);
+    const int j = st.key(x), page = a.of(j), inside = j - page * a.page;
+    if (x + P::kKeys <= st.x1 && (x >= st.s || x + P::kKeys <= st.s) && inside + P::kKeys <= a.page) {
+      const int at = scalar(table[min(x < st.s ? page - st.a0 : st.a_pages + page - st.b0, kTable - 1)]);
+      const int64_t row = (int64_t(at) * a.kv_heads + hk) * a.page + inside;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        dma16_from(a.k + row * P::kRow, k[i], lds + i * 1024);
+        dma16_from(a.v + row * P::kRow, v[i], lds + kBytes + i * 1024);
+      }
+      if constexpr (P::kScaled) {
+        dma_byte_from(a.k_scale + row, lane, lds + 2 * kBytes);
+        dma_byte_from(a.v_scale + row, lane, lds + 2 * kBytes + 256);
+      }
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = i * kRowsOfLoad + r_in;
+      const int64_t row = st.row(a, table, hk, min(x + r, st.x1 - 1));  // rows past the end are the last one again, with no weight
+      dma16_at(a.k + row * P::kRow + ((pos ^ P::swizzle_k(r)) << 4), lds + i * 1024);
+      dma16_at(a.v + row * P::kRow + ((pos ^ P::swizzle_v(r)) << 4), lds + kBytes + i * 1024);
+    }
+    if constexpr (P::kScaled) {
+      static_assert(P::kKeys == 64, "a lane to a key");
+      const int64_t row = st.row(a, table, hk, min(x + lane, st.x1 - 1));
+      dma_byte_at(a.k_scale + row, lds + 2 * kBytes);
+      dma_byte_at(a.v_scale + row, lds + 2 * kBytes + 256);
+    }
+  }
+  // The keys of a piece in LDS whose values (or their exponents) are not finite.
+  __device__ __forceinline__ unsigned long long bad_keys(const unsigned char* piece) const {
+    unsigned long long in[kLoads], any = 0;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      in[i] = __ballot(any_bad<typename P::Cache>(*LDS_PTR(u32x4, piece + kBytes + i * 1024 + lane * 16)));
+      any |= in[i];
+    }
+    bool bad = false;
+    if (any != 0) {
+      const int i = lane / kRowsOfLoad;
+      const unsigned long long of = i == 0 ? in[0] : i == 1 ? in[1] : i == 2 ? in[2] : in[3];
+      bad = lane < P::kKeys && ((of >> (lane % kRowsOfLoad * kChunks)) & ((1ull << kChunks) - 1)) != 0;
+    }
+    if constexpr (P::kScaled) bad = bad || LDS_PTR(unsigned, piece + 2 * kBytes)[64 + lane] == 255u;
+    return __ballot(bad);
+  }
+  __device__ __forceinline__ void clear_keys(unsigned char* piece, unsigned long long keys) const {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = i * kRowsOfLoad + r_in;
+      if ((keys >> r) & 1) *reinterpret_cast<u32x4*>(piece + kBytes + r * P::kRow + pos * 16) = u32x4{0u, 0u, 0u, 0u};
+    }
+    if constexpr (P::kScaled)
+      if ((keys >> lane) & 1) reinterpret_cast<unsigned*>(piece + 2 * kBytes)[64 + lane] = 0u;
+  }
+  // until the piece that was asked for first is there, of two (or one, the last)
+  static __device__ __forceinline__ void wait(bool last) {
+    static_assert(kInFlight == 8 || kInFlight == 10, "counts below");
+    if (last) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    else if constexpr (kInFlight == 10) asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+  }
+  // values (and their exponents) that only fill the last piece: their weights are zero, which is not nothing if the one that is repeated is infinite
+  __device__ __forceinline__ void clear_from(unsigned char* piece, int left) const {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = i * kRowsOfLoad + r_in;
+      if (r >= left) *reinterpret_cast<u32x4*>(piece + kBytes + r * P::kRow + pos * 16) = u32x4{0u, 0u, 0u, 0u};
+    }
+    if constexpr (P::kScaled)
+      if (lane >= left) reinterpret_cast<unsigned*>(piece + 2 * kBytes)[64 + lane] = 0u;
+  }
+};
+
 template <typename P>
 constexpr int kPiece = P::kKeys * P::kRow;
 template <typename P>
@@ -295,35 +411,27 @@ constexpr int kBuf = 2 * kPiece<P> + (P::kScaled ? 2 * P::kKeys * 4 : 0);  // ke
 template <typename P>
 constexpr int kWaveLds = 2 * kBuf<P>;
 
-// Values that are not finite must not reach columns that do not see them, where a weight of zero would still make NaN of them: such keys are added here for
+// Values that are not finite must not reach columns that do not see them, where a weight of zero would still make NaN of them: such keys are added here, for
 // the columns that see them, and are zeros for the matrix product.  Only pieces of which some columns see a part come here.
 template <typename P, typename SeenI>
-__device__ __forceinline__ void leave_bad_out(unsigned char* tile, unsigned* scales, int lane, int left, SeenI seen, const f32x4 (&w)[P::kBlocks], f32x4 (&o)[4]) {
-  constexpr int kChunks = P::kRow / 16, kRowsOfLoad = 64 / kChunks;
-  unsigned long long bad[4], any = 0;
+__device__ __forceinline__ void leave_bad_out(const PieceLoad<P>& load, unsigned char* piece, SeenI seen, const f32x4 (&w)[P::kBlocks], f32x4 (&o)[4]) {
+  unsigned long long bad = load.bad_keys(piece);
+  if (bad == 0) return;
+  const int c = load.lane & 15, q = load.lane >> 4;
+  const unsigned* const scales = reinterpret_cast<const unsigned*>(piece + 2 * PieceLoad<P>::kBytes);
+  for (unsigned long long left = bad; left != 0; left &= left - 1) {
+    const int i = __builtin_ctzll(left);
+    float weight = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const u32x4 x = *LDS_PTR(u32x4, tile + i * 1024 + lane * 16);
-    bad[i] = __ballot(any_bad<typename P::Cache>(x));
-    any |= bad[i];
+    for (int blk = 0; blk < P::kBlocks; ++blk)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) weight = blk == i >> 4 && r == (i & 3) ? w[blk][r] : weight;
+    weight = __shfl(weight, c + 16 * ((i >> 2) & 3));
+    if (!seen(i)) continue;
+#pragma unroll
+    for (int db = 0; db < 4; ++db) o[db] += P::value(piece + PieceLoad<P>::kBytes, scales + 64, i, 16 * db + 4 * q) * weight;
   }
-  if (any == 0) return;
-  const int c = lane & 15, q = lane >> 4;
-#pragma unroll
-  for (int blk = 0; blk < P::kBlocks; ++blk)
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      for (int qq = 0; qq < 4; ++qq) {
-        const int i = 16 * blk + 4 * qq + r, load = i / kRowsOfLoad;
-        const unsigned long long of = load == 0 ? bad[0] : load == 1 ? bad[1] : load == 2 ? bad[2] : bad[3];
-        const float weight = __shfl(w[blk][r], c + 16 * qq);
-        if (((of >> (i % kRowsOfLoad * kChunks)) & ((1ull << kChunks) - 1)) == 0 || i >= left || !seen(i)) continue;
-#pragma unroll
-        for (int db = 0; db < 4; ++db) o[db] += P::value(tile, scales, i, 16 * db + 4 * q) * weight;
-      }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if ((bad[i] >> (lane / kChunks * kChunks)) & ((1ull << kChunks) - 1)) *reinterpret_cast<u32x4*>(tile + i * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
+  load.clear_keys(piece, bad);
 }
 
 // One wave over its pieces: what its columns have of maxima, sums (those of a column's four lanes are still to be added) and weighted values.  seen(key, x) tells
@@ -331,27 +439,11 @@ __device__ __forceinline__ void leave_bad_out(unsigned char* tile, unsigned* sca
 template <typename P, bool MASKED, typename Seen1>
 __device__ __forceinline__ void go_over(const Pages& a, const Stretch& st, const int* table, int hk, int wave, int lane, unsigned char* mine, float scale_log2,
                                         const typename P::A (&qf)[P::kSteps], Seen1 seen, f32x4 (&o)[4], float& m, float& l) {
-  constexpr int kChunks = P::kRow / 16, kRowsOfLoad = 64 / kChunks, kLoads = P::kKeys / kRowsOfLoad;
-  static_assert(kLoads == 4, "eight loads of a piece");
   const int c = lane & 15, q = lane >> 4;
   const unsigned lds = __builtin_amdgcn_readfirstlane(lds_address(mine));
   const int pieces = (st.x1 - st.x0 + P::kKeys - 1) / P::kKeys;
-  const int r_in = lane / kChunks, pos = lane % kChunks;
-  auto issue = [&](int p, int buf) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int r = i * kRowsOfLoad + r_in;
-      const int64_t row = st.row(a, table, hk, min(st.x0 + p * P::kKeys + r, st.x1 - 1));  // rows past the end are the last one again, with no weight
-      dma16_at(a.k + row * P::kRow + ((pos ^ P::swizzle_k(r)) << 4), lds + buf * kBuf<P> + i * 1024);
-      dma16_at(a.v + row * P::kRow + ((pos ^ P::swizzle_v(r)) << 4), lds + buf * kBuf<P> + kPiece<P> + i * 1024);
-    }
-    if constexpr (P::kScaled) {
-      static_assert(P::kKeys == 64, "a lane to a key");
-      const int64_t row = st.row(a, table, hk, min(st.x0 + p * P::kKeys + lane, st.x1 - 1));
-      dma_byte_at(a.k_scale + row, lds + buf * kBuf<P> + 2 * kPiece<P>);
-      dma_byte_at(a.v_scale + row, lds + buf * kBuf<P> + 2 * kPiece<P> + 256);
-    }
-  };
+  const PieceLoad<P> load(lane);
+  auto issue = [&](int p, int buf) { load.issue(a, st, table, hk, st.x0 + p * P::kKeys, lds + buf * kBuf<P>); };
   if (wave < pieces) issue(wave, 0);
   if (wave + kWaves < pieces) issue(wave + kWaves, 1);
 
@@ -360,21 +452,11 @@ __device__ __forceinline__ void go_over(const Pages& a, const Stretch& st, const
   for (int db = 0; db < 4; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
   int buf = 0;
   for (int p = wave; p < pieces; p += kWaves, buf ^= 1) {
-    if (p + kWaves >= pieces) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    else if constexpr (P::kScaled) asm volatile("s_waitcnt vmcnt(10)" ::: "memory");  // the next piece's loads may be on their way
-    else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+    load.wait(p + kWaves >= pieces);  // the next piece's loads may be on their way
     unsigned char* const kt = mine + buf * kBuf<P>;
     unsigned* const scales = reinterpret_cast<unsigned*>(kt + 2 * kPiece<P>);
     const int left = st.x1 - st.x0 - p * P::kKeys;
-    if (left < P::kKeys) {  // the repeated values have weights of zero, which is not nothing if the last one is infinite
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int r = i * kRowsOfLoad + r_in;
-        if (r >= left) *reinterpret_cast<u32x4*>(kt + kPiece<P> + r * P::kRow + pos * 16) = u32x4{0u, 0u, 0u, 0u};
-      }
-      if constexpr (P::kScaled)
-        if (lane >= left) scales[64 + lane] = 0u;
-    }
+    if (left < P::kKeys) load.clear_from(kt, left);
     f32x4 w[P::kBlocks];
 #pragma unroll
     for (int blk = 0; blk < P::kBlocks; ++blk) {
@@ -410,7 +492,7 @@ __device__ __forceinline__ void go_over(const Pages& a, const Stretch& st, const
         w[blk][r] = __builtin_amdgcn_exp2f(fmaf(w[blk][r], scale_log2, -from));
         l += w[blk][r];
       }
-    if constexpr (MASKED) leave_bad_out<P>(kt + kPiece<P>, scales + 64, lane, left, [&](int i) { return seen(st.key(st.x0 + p * P::kKeys + i)); }, w, o);
+    if constexpr (MASKED) leave_bad_out<P>(load, kt, [&](int i) { return seen(st.key(st.x0 + p * P::kKeys + i)); }, w, o);
     P::update(kt + kPiece<P>, scales + 64, lane, w, o);
     if (p + 2 * kWaves < pieces) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the operands are in registers: the buffer is free

@@ -17,7 +17,7 @@ struct PrefixArgs {
   const int32_t *prefix_table, *prefix_lengths, *starts;   // sequences starts[g] .. starts[g + 1] - 1 have prefix g
   float *part, *part_lse;             // [splits + own_splits][batch, heads, 64] and [..][batch, heads]
   int batch, heads, group, head_blocks, table_width, prefixes, prefix_width, frame, window, sinks;
-  int splits, stretch, own_splits, own_stretch;
+  int splits, stretch, own_splits, own_stretch, queries;  // queries of a tile
   float scale_log2;
 
   __device__ __forceinline__ int start(int g) const { return min(max(starts[g], 0), batch); }
@@ -138,6 +138,304 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefix_kernel(const PrefixArgs
   leave(a, split, row_of(i, b), d, y, top, sum);
 }
 
+// Operands of 32x32x16 products, queries in bf16: S^T = K Q^T has keys as rows, O^T = V^T P^T numbers of the values.
+template <typename C>
+struct Wide;
+
+template <>
+struct Wide<__bf16> {
+  typedef __bf16 Cache;
+  static constexpr int kRow = 128, kKeys = 32;
+  static constexpr bool kScaled = false;
+  static __device__ __forceinline__ int swizzle_k(int r) { return Ops<__bf16>::swizzle(r); }
+  static __device__ __forceinline__ int swizzle_v(int r) { return Ops<__bf16>::swizzle(r); }
+  static __device__ __forceinline__ void query(const unsigned char* p, int g, bf16x8 (&a)[4]) { Ops<__bf16>::row(p, g, a); }
+  static __device__ __forceinline__ void keys(const unsigned char* tile, const unsigned*, int r0, int lane, bf16x8 (&a)[4]) {
+    Ops<__bf16>::rows(tile, r0 + (lane & 31), lane >> 5, a);
+  }
+  static __device__ __forceinline__ void values(const unsigned char* tile, int r0, int db, int lane, bf16x8 (&a)[2]) { Ops<__bf16>::columns(tile, r0, db, lane, a); }
+  static __device__ __forceinline__ float value(const unsigned char* tile, const unsigned*, int r, int d) {
+    return __uint_as_float(static_cast<unsigned>(*LDS_PTR(unsigned short, tile + r * kRow + (((d >> 3) ^ swizzle_v(r)) << 4) + (d & 7) * 2)) << 16);
+  }
+};
+
+// Rows of 64 bytes, four to the 64 banks: a lane half takes 32 numbers of a key, 8 for each of four steps, so the swizzle of keys keeps r, r + 4, r + 8, r + 12 apart;
+// columns are read in two neighbouring chunks of the rows r and r + 8 together.
+template <>
+struct Wide<E4m3> {
+  typedef E4m3 Cache;
+  static constexpr int kRow = 64, kKeys = 64;
+  static constexpr bool kScaled = true;
+  static __device__ __forceinline__ int swizzle_k(int r) { return (r >> 2) & 3; }
+  static __device__ __forceinline__ int swizzle_v(int r) { return (r >> 2) & 2; }
+  static __device__ __forceinline__ void query(const unsigned char* p, int g, bf16x8 (&a)[4]) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) a[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p + (4 * g + c) * 16));
+  }
+  static __device__ __forceinline__ void keys(const unsigned char* tile, const unsigned* scales, int r0, int lane, bf16x8 (&a)[4]) {
+    const int r = r0 + (lane & 31), g = lane >> 5;
+    const float f = scale_of(*LDS_PTR(unsigned, scales + r));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u32x4 x = *LDS_PTR(u32x4, tile + r * kRow + (((2 * g + i) ^ swizzle_k(r)) << 4));
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const u32x2 y0 = unpack_bf16(x[2 * e], f), y1 = unpack_bf16(x[2 * e + 1], f);
+        a[2 * i + e] = __builtin_bit_cast(bf16x8, u32x4{y0[0], y0[1], y1[0], y1[1]});
+      }
+    }
+  }
+  static __device__ __forceinline__ void values(const unsigned char* tile, int r0, int db, int lane, bf16x8 (&a)[2]) {
+    const int m = (lane & 15) >> 1, G = lane >> 4;
+#pragma unroll
+    for (int cp = 0; cp < 2; ++cp) {
+      const int r = r0 + 16 * cp + 4 * (G >> 1) + (m & 3) + 2 * (m & 4);
+      const unsigned char* p = tile + r * kRow + (((2 * db + (G & 1)) ^ swizzle_v(r)) << 4) + (lane & 1) * 8;
+      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((s32x2 __attribute__((address_space(3)))*)(p)));
+      const u32x2 y0 = unpack_bf16(x[0], 1.f), y1 = unpack_bf16(x[1], 1.f);
+      a[cp] = __builtin_bit_cast(bf16x8, u32x4{y0[0], y0[1], y1[0], y1[1]});
+    }
+  }
+  static __device__ __forceinline__ float value(const unsigned char* tile, const unsigned* scales, int r, int d) {
+    const unsigned char x = *LDS_PTR(unsigned char, tile + r * kRow + (((d >> 4) ^ swizzle_v(r)) << 4) + (d & 15));
+    return unpack_f32(x)[0] * scale_of(*LDS_PTR(unsigned, scales + r));
+  }
+};
+
+constexpr float kRaise = 8.0f;  // the running maximum follows when a piece exceeds it by 2^8
+
+// The same for 32 R queries, bf16.  A wave has them all, as columns, and goes over its own pieces of the keys; what it holds of a piece serves R products.
+template <typename C, int R>
+__global__ __launch_bounds__(64 * kWaves, 2) void prefix_wide_kernel(const PrefixArgs a) {
+  typedef Wide<C> P;
+  constexpr int kQueries = 32 * R, kBytes = PieceLoad<P>::kBytes, kBufBytes = 2 * kBytes + (P::kScaled ? 512 : 0);
+  constexpr int kWaveBytes = larger(2 * kBufBytes, kQueries * 64 * 4);
+  __shared__ __align__(16) unsigned char smem[kWaves * kWaveBytes];
+  __shared__ int table[kTable];
+  __shared__ float sums[kWaves][2][kQueries];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, g = lane >> 5;
+  // workgroup w runs on XCD w % 8: the tiles of queries that read the same keys follow each other on one
+  const int pairs = a.pages.kv_heads * a.splits, tiles = gridDim.x / (8 * ((pairs + 7) / 8));
+  const int pair = blockIdx.x / 8 / tiles * 8 + blockIdx.x % 8;
+  if (pair >= pairs) return;
+  const int hk = pair / a.splits, split = pair % a.splits;
+  int tile;
+  const int of = unit_of(a, blockIdx.x / 8 % tiles, kQueries, lane, tile);
+  if (of < 0) return;
+  const int b0 = a.start(of), first = tile * kQueries, queries = min((a.start(of + 1) - b0) * a.group - first, kQueries);
+  auto row_of = [&](int i, int& b) {  // query i of the tile: its sequence, and its row of the result
+    const int x = first + i;
+    b = b0 + x / a.group;
+    return int64_t(b) * a.heads + hk * a.group + x % a.group;
+  };
+  const int length = a.prefix_length(of);
+  int lo[R], b[R];
+  int64_t row[R];
+  Stretch st = {};
+  st.lo = length;
+  int most = 0;
+#pragma unroll
+  for (int e = 0; e < R; ++e) {
+    int s;
+    row[e] = row_of(min(32 * e + n, queries - 1), b[e]);
+    a.seen(length + a.length(b[e]), lo[e], s);
+    lo[e] = min(lo[e], length);
+    st.lo = min(st.lo, lo[e]);
+    most = max(most, lo[e]);
+  }
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    st.lo = min(st.lo, __shfl_xor(st.lo, o));
+    most = max(most, __shfl_xor(most, o));
+  }
+  st.lo = scalar(st.lo);
+  most = scalar(most);
+  st.s = min(a.sinks, st.lo);
+  const int count = st.s + length - st.lo;
+  st.x0 = split * a.stretch, st.x1 = min(st.x0 + a.stretch, count);
+  if (st.x0 >= st.x1) {  // the whole workgroup
+    int to;
+    if (threadIdx.x < queries) {
+      const int64_t at = row_of(threadIdx.x, to);
+      a.part_lse[int64_t(split) * a.batch * a.heads + at] = -INFINITY;
+    }
+    return;
+  }
+  st.fill(a.pages, a.prefix_table + int64_t(of) * a.prefix_width, table);
+  bf16x8 qf[R][4];
+#pragma unroll
+  for (int e = 0; e < R; ++e) P::query(a.q.p + b[e] * a.q.token + (row[e] - int64_t(b[e]) * a.heads) * a.q.head, g, qf[e]);
+  __syncthreads();
+
+  unsigned char* const mine = smem + wave * kWaveBytes;
+  const unsigned lds = scalar(lds_address(mine));
+  const int pieces = (st.x1 - st.x0 + P::kKeys - 1) / P::kKeys;
+  const PieceLoad<P> load(lane);
+  auto issue = [&](int p, int buf) { load.issue(a.pages, st, table, hk, st.x0 + p * P::kKeys, lds + buf * kBufBytes); };
+  if (wave < pieces) issue(wave, 0);
+  if (wave + kWaves < pieces) issue(wave + kWaves, 1);
+
+  f32x16 o[R][2];
+  float m[R], l[R];
+#pragma unroll
+  for (int e = 0; e < R; ++e) {
+    m[e] = -INFINITY, l[e] = 0.f;
+    clear(o[e][0]);
+    clear(o[e][1]);
+  }
+  int buf = 0;
+  for (int p = wave; p < pieces; p += kWaves, buf ^= 1) {
+    load.wait(p + kWaves >= pieces);
+    unsigned char* const kt = mine + buf * kBufBytes;
+    unsigned char* const vt = kt + kBytes;
+    const unsigned* const scales = reinterpret_cast<const unsigned*>(kt + 2 * kBytes);
+    const int x = st.x0 + p * P::kKeys, left = st.x1 - x;
+    if (left < P::kKeys) load.clear_from(kt, left);
+    // key i of the piece is key x + i of the stretch, and no query sees less than keys `most` ..; those in front of it are looked at one by one
+    const bool masked = left < P::kKeys || (x + P::kKeys > st.s && st.key(max(x, st.s)) < most);
+    const unsigned long long bad = masked && most > st.lo ? load.bad_keys(kt) : 0;  // (values that are not finite must not meet weights of zero)
+#pragma unroll
+    for (int h = 0; h < P::kKeys / 32; ++h) {
+      bf16x8 ka[4];
+      P::keys(kt, scales, 32 * h, lane, ka);
+      f32x16 w[R];
+#pragma unroll
+      for (int e = 0; e < R; ++e) {
+        clear(w[e]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w[e] = Ops<__bf16>::product(ka[c], qf[e][c], w[e]);
+      }
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < R; ++e)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int r = 32 * h + 8 * (i >> 2) + 4 * g + (i & 3), j = st.key(x + r);
+            if (r >= left || (j < lo[e] && j >= a.sinks)) w[e][i] = -INFINITY;
+          }
+      }
+      float top[R];
+      bool raise = false;
+#pragma unroll
+      for (int e = 0; e < R; ++e) {
+        top[e] = w[e][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top[e] = fmaxf(top[e], w[e][i]);
+        top[e] = top_of_halves(top[e]) * a.scale_log2;
+        raise = raise || top[e] > m[e] + kRaise;
+      }
+      if (__any(raise)) {
+#pragma unroll
+        for (int e = 0; e < R; ++e) {
+          const float to = fmaxf(m[e], top[e]);
+          const float keep = to == -INFINITY ? 1.f : exp2f(m[e] - to);
+          m[e] = to;
+          l[e] *= keep;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            o[e][0][i] *= keep;
+            o[e][1][i] *= keep;
+          }
+        }
+      }
+      bf16x8 pw[R][2];
+#pragma unroll
+      for (int e = 0; e < R; ++e) {
+        const float from = m[e] == -INFINITY ? 0.f : m[e];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          w[e][i] = __builtin_amdgcn_exp2f(fmaf(w[e][i], a.scale_log2, -from));
+          l[e] += w[e][i];
+        }
+      }
+      unsigned long long alone = P::kKeys == 32 ? bad : (bad >> (32 * h)) & 0xffffffffull;
+      if (alone != 0) {
+        const unsigned long long these = alone << (32 * h);
+        for (; alone != 0; alone &= alone - 1) {
+          const int r = __builtin_ctzll(alone), j = st.key(x + 32 * h + r), in_lane = 4 * (r >> 3) + (r & 3);
+#pragma unroll
+          for (int e = 0; e < R; ++e) {
+            float weight = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) weight = i == in_lane ? w[e][i] : weight;
+            weight = __shfl(weight, n + 32 * ((r >> 2) & 1));
+            if (j < lo[e] && j >= a.sinks) continue;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              o[e][i >> 4][i & 15] += weight * P::value(vt, scales + 64, 32 * h + r, 32 * (i >> 4) + 8 * ((i & 15) >> 2) + 4 * g + (i & 3));
+          }
+        }
+        load.clear_keys(kt, these);
+      }
+      if constexpr (P::kScaled) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const u32x4 by = *LDS_PTR(u32x4, scales + 64 + 32 * h + 8 * i + 4 * g);
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < R; ++e) w[e][4 * i + r] *= scale_of(by[r]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < R; ++e) Ops<__bf16>::round(w[e], pw[e]);
+#pragma unroll
+      for (int db = 0; db < 2; ++db) {
+        bf16x8 va[2];
+        P::values(vt, 32 * h, db, lane, va);
+#pragma unroll
+        for (int e = 0; e < R; ++e)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) o[e][db] = Ops<__bf16>::product(va[c], pw[e][c], o[e][db]);
+      }
+    }
+    if (p + 2 * kWaves < pieces) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the operands are in registers: the buffer is free
+      issue(p + 2 * kWaves, buf);
+    }
+  }
+
+  // the waves together: each leaves its sums in its own LDS (none of its loads are on their way any more)
+#pragma unroll
+  for (int e = 0; e < R; ++e) {
+#pragma unroll
+    for (int db = 0; db < 2; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(mine + ((32 * e + n) * 64 + (((8 * db + 2 * i + g) ^ (n & 15)) * 4)) * 4) =
+            f32x4{o[e][db][4 * i], o[e][db][4 * i + 1], o[e][db][4 * i + 2], o[e][db][4 * i + 3]};
+    l[e] += __shfl_xor(l[e], 32);
+    if (g == 0) {
+      sums[wave][0][32 * e + n] = m[e];
+      sums[wave][1][32 * e + n] = l[e];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < 2 * R; ++e) {
+    const int i = 16 * e + (threadIdx.x >> 4), chunk = threadIdx.x & 15;
+    float top = -INFINITY, sum = 0.f;
+    bool nan = false;
+#pragma unroll
+    for (int x = 0; x < kWaves; ++x) {
+      top = fmaxf(top, sums[x][0][i]);
+      nan = nan || sums[x][1][i] != sums[x][1][i];
+    }
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < kWaves; ++x) {
+      const float weight = sums[x][0][i] == -INFINITY ? 0.f : exp2f(sums[x][0][i] - top);
+      sum += sums[x][1][i] * weight;
+      y += *reinterpret_cast<const f32x4*>(smem + x * kWaveBytes + (i * 64 + ((chunk ^ (i & 15)) * 4)) * 4) * weight;
+    }
+    if (nan) sum = NAN;
+    int to;
+    if (i < queries) leave(a, split, row_of(i, to), chunk * 4, y, top, sum);
+  }
+}
+
 // The own keys of a sequence.
 template <typename T, typename C>
 __global__ __launch_bounds__(64 * kWaves, 2) void own_kernel(const PrefixArgs a) {
@@ -191,14 +489,17 @@ int64_t tiles_of(const PrefixArgs& a, int tile) {
   return smaller(queries / tile + smaller(int64_t(a.prefixes), int64_t(a.batch)), queries);
 }
 
-void shape_of(PrefixArgs& a, int keys) {
+void shape_of(PrefixArgs& a, int dtype, int cache_dtype) {
+  const int keys = keys_of_piece(dtype, cache_dtype);
+  const int64_t of_a_prefix = ceil_div(int64_t(a.batch) * a.group, larger(smaller(int64_t(a.prefixes), int64_t(a.batch)), int64_t(1)));  // about
+  a.queries = dtype != BSGA_BF16 || of_a_prefix <= 16 ? kHeads : of_a_prefix <= 32 ? 32 : 64;
   int64_t most = int64_t(a.prefix_width) * a.pages.page, own = int64_t(a.table_width) * a.pages.page;
   if (a.window > 0) {
     const int64_t seen = int64_t(a.window) * a.frame + a.sinks;
     most = smaller(most, seen);
     own = smaller(own, seen);
   }
-  const int64_t units = larger(ceil_div(int64_t(a.batch) * a.group, kHeads), int64_t(1)) * a.pages.kv_heads;
+  const int64_t units = larger(ceil_div(int64_t(a.batch) * a.group, a.queries), int64_t(1)) * a.pages.kv_heads;
   cut(most, units, keys, a.pages.page, a.stretch, a.splits);
   cut(own, int64_t(a.batch) * a.pages.kv_heads * a.head_blocks, keys, a.pages.page, a.own_stretch, a.own_splits);
 }
@@ -238,11 +539,25 @@ int check_sizes(const char* fn, int dtype, int cache_dtype, int64_t batch, int h
   return BSGA_OK;
 }
 
+template <typename C, int R>
+void launch_wide(const PrefixArgs& a, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(8 * ceil_div(int64_t(a.pages.kv_heads) * a.splits, 8) * tiles_of(a, 32 * R)));
+  hipLaunchKernelGGL((prefix_wide_kernel<C, R>), grid, dim3(64 * kWaves), 0, s, a);
+}
+
 template <typename T, typename C>
 int launch(const PrefixArgs& a, unsigned char* out, float* lse, hipStream_t s) {
   if (a.prefixes > 0) {
-    const dim3 grid(static_cast<unsigned>(a.splits), static_cast<unsigned>(a.pages.kv_heads), static_cast<unsigned>(tiles_of(a, kHeads)));
-    hipLaunchKernelGGL((prefix_kernel<T, C>), grid, dim3(64 * kWaves), 0, s, a);
+    bool narrow = true;
+    if constexpr (std::is_same<T, __bf16>::value) {
+      narrow = a.queries == kHeads;
+      if (a.queries == 64) launch_wide<C, 2>(a, s);
+      if (a.queries == 32) launch_wide<C, 1>(a, s);
+    }
+    if (narrow) {
+      const dim3 grid(static_cast<unsigned>(a.splits), static_cast<unsigned>(a.pages.kv_heads), static_cast<unsigned>(tiles_of(a, kHeads)));
+      hipLaunchKernelGGL((prefix_kernel<T, C>), grid, dim3(64 * kWaves), 0, s, a);
+    }
   }
   const dim3 grid(static_cast<unsigned>(a.own_splits), static_cast<unsigned>(a.pages.kv_heads * a.head_blocks), static_cast<unsigned>(a.batch));
   hipLaunchKernelGGL((own_kernel<T, C>), grid, dim3(64 * kWaves), 0, s, a);
@@ -262,7 +577,7 @@ size_t bsga_prefix_attn_workspace_bytes(int dtype, int cache_dtype, int64_t batc
   PrefixArgs a = {};
   if (check_sizes("", dtype, cache_dtype, batch, heads, kv_heads, table_width, prefixes, prefix_width, n_pages, page, frame, window, sinks, a) || batch == 0)
     return 0;
-  shape_of(a, keys_of_piece(dtype, cache_dtype));
+  shape_of(a, dtype, cache_dtype);
   return part_bytes(a);
 }
 
@@ -298,7 +613,7 @@ int bsga_prefix_attn(const void* q, int64_t q_batch, int64_t q_head, const void*
   a.prefix_lengths = prefix_lengths;
   a.starts = starts;
   a.scale_log2 = softmax_scale * kLog2e;
-  shape_of(a, keys_of_piece(dtype, cache_dtype));
+  shape_of(a, dtype, cache_dtype);
   const size_t need = part_bytes(a);
   if (!workspace || workspace_bytes < need)
     return fail(BSGA_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace ? workspace_bytes : 0, need);

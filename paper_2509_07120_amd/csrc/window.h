@@ -184,6 +184,13 @@ __device__ __forceinline__ void clear(f32x16& x) {
   for (int i = 0; i < 16; ++i) x[i] = 0.f;
 }
 
+// The larger of what lanes n and n + 32 have, in both, without the way through LDS.
+__device__ __forceinline__ float top_of_halves(float x) {
+  const unsigned u = __float_as_uint(x);
+  const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+}
+
 // Of a lane's numbers of one product, of tile rows `at` + 8 (i / 4) + i % 4, those outside [first, last) become `hidden`: three instructions for each.
 __device__ __forceinline__ void keep(f32x16& x, int at, int first, int last, float hidden) {
   const int from = first - at;

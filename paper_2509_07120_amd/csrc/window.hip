@@ -71,13 +71,6 @@ __device__ void exact_row(const WindowArgs& a, const unsigned char* q, const uns
   if (lse != nullptr && lane == 0) *lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// The larger of what lanes n and n + 32 have, in both, without the way through LDS.
-__device__ __forceinline__ float top_of_halves(float x) {
-  const unsigned u = __float_as_uint(x);
-  const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-}
-
 template <int N>
 using Int = std::integral_constant<int, N>;
 
