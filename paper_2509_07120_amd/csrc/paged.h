@@ -29,8 +29,8 @@ struct Ops16<__bf16, __bf16> {
   static constexpr int kBlocks = 2;  // of 16 keys
   static constexpr int kSteps = 2;   // products over the 64 numbers of a row
   static __device__ __forceinline__ f32x4 product(A a, A b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-  static __device__ __forceinline__ int swizzle_k(int r) { return swz_k(r); }
-  static __device__ __forceinline__ int swizzle_v(int r) { return swz_v(r); }
+  static __host__ __device__ constexpr int swizzle_k(int r) { return swz_k(r); }
+  static __host__ __device__ constexpr int swizzle_v(int r) { return swz_v(r); }
   static __device__ __forceinline__ f32x4 value(const unsigned char* tile, const unsigned*, int r, int d) {  // numbers d .. d + 3 of a value, d a multiple of 4
     const u32x2 x = *LDS_PTR(u32x2, tile + r * kRow + (((d >> 3) ^ swizzle_v(r)) << 4) + (d & 4) * 2);
     return f32x4{__uint_as_float(x[0] << 16), __uint_as_float(x[0] & 0xffff0000u), __uint_as_float(x[1] << 16), __uint_as_float(x[1] & 0xffff0000u)};
@@ -72,8 +72,8 @@ struct Ops16<float, float> {
   static constexpr int kBlocks = 1;
   static constexpr int kSteps = 16;
   static __device__ __forceinline__ f32x4 product(A a, A b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
-  static __device__ __forceinline__ int swizzle_k(int r) { return r & 15; }
-  static __device__ __forceinline__ int swizzle_v(int r) { return r & 15; }
+  static __host__ __device__ constexpr int swizzle_k(int r) { return r & 15; }
+  static __host__ __device__ constexpr int swizzle_v(int r) { return r & 15; }
   static __device__ __forceinline__ f32x4 value(const unsigned char* tile, const unsigned*, int r, int d) {
     return *LDS_PTR(f32x4, tile + r * kRow + (((d >> 2) ^ swizzle_v(r)) << 4));
   }
@@ -114,8 +114,8 @@ struct Ops16E4m3 {
   static constexpr bool kScaled = true;
   static constexpr int kKeys = 64;
   static constexpr int kBlocks = 4;
-  static __device__ __forceinline__ int swizzle_k(int r) { return (r >> 2) & 3; }
-  static __device__ __forceinline__ int swizzle_v(int r) { return ((r >> 2) & 1) | ((r >> 3) & 2); }
+  static __host__ __device__ constexpr int swizzle_k(int r) { return (r >> 2) & 3; }
+  static __host__ __device__ constexpr int swizzle_v(int r) { return ((r >> 2) & 1) | ((r >> 3) & 2); }
   static __device__ __forceinline__ f32x4 value(const unsigned char* tile, const unsigned* scales, int r, int d) {
     return unpack_f32(*LDS_PTR(unsigned, tile + r * kRow + (((d >> 4) ^ swizzle_v(r)) << 4) + (d & 12))) * scale_of(*LDS_PTR(unsigned, scales + r));
   }
@@ -316,16 +316,24 @@ struct PieceLoad {
   static constexpr int kChunks = P::kRow / 16, kRowsOfLoad = 64 / kChunks, kLoads = P::kKeys / kRowsOfLoad, kBytes = P::kKeys * P::kRow;
   static constexpr int kInFlight = 2 * kLoads + (P::kScaled ? 2 : 0);  // loads of a piece
   static_assert(kLoads == 4, "eight loads of keys and values");
-  unsigned k[kLoads], v[kLoads];
+  // loads whose lanes have the same places in them, 1024 bytes further: their swizzles are those of rows kRowsOfLoad * (1, 2 or 4) apart
+  static constexpr int patterns(int (*swizzle)(int)) {
+    for (int n = 1; n < kLoads; n *= 2) {
+      bool same = true;
+      for (int r = 0; r + n * kRowsOfLoad < P::kKeys; ++r) same = same && swizzle(r) == swizzle(r + n * kRowsOfLoad);
+      if (same) return n;
+    }
+    return kLoads;
+  }
+  static constexpr int kPlacesK = patterns(P::swizzle_k), kPlacesV = patterns(P::swizzle_v);
+  unsigned k[kPlacesK], v[kPlacesV];
   int lane, r_in, pos;
 
   __device__ __forceinline__ explicit PieceLoad(int lane) : lane(lane), r_in(lane / kChunks), pos(lane % kChunks) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int r = i * kRowsOfLoad + r_in;
-      k[i] = r * P::kRow + ((pos ^ P::swizzle_k(r)) << 4);
-      v[i] = r * P::kRow + ((pos ^ P::swizzle_v(r)) << 4);
-    }
+    for (int i = 0; i < kPlacesK; ++i) k[i] = r_in * P::kRow + ((pos ^ P::swizzle_k(i * kRowsOfLoad + r_in)) << 4);
+#pragma unroll
+    for (int i = 0; i < kPlacesV; ++i) v[i] = r_in * P::kRow + ((pos ^ P::swizzle_v(i * kRowsOfLoad + r_in)) << 4);
   }
   // the keys from the x-th on
   __device__ __forceinline__ void issue(const Pages& a, const Stretch& st, const int* table, int hk, int x, unsigned lds) const {
@@ -336,8 +344,8 @@ struct PieceLoad {
       const int64_t row = (int64_t(at) * a.kv_heads + hk) * a.page + inside;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        dma16_from(a.k + row * P::kRow, k[i], lds + i * 1024);
-        dma16_from(a.v + row * P::kRow, v[i], lds + kBytes + i * 1024);
+        dma16_from(a.k + row * P::kRow + i * 1024, k[i % kPlacesK], lds + i * 1024);
+        dma16_from(a.v + row * P::kRow + i * 1024, v[i % kPlacesV], lds + kBytes + i * 1024);
       }
       if constexpr (P::kScaled) {
         dma_byte_from(a.k_scale + row, lane, lds + 2 * kBytes);

@@ -147,15 +147,15 @@ struct Wide<__bf16> {
   typedef __bf16 Cache;
   static constexpr int kRow = 128, kKeys = 32;
   static constexpr bool kScaled = false;
-  static __device__ __forceinline__ int swizzle_k(int r) { return Ops<__bf16>::swizzle(r); }
-  static __device__ __forceinline__ int swizzle_v(int r) { return Ops<__bf16>::swizzle(r); }
+  static __host__ __device__ constexpr int swizzle_k(int r) { return Ops<__bf16>::swizzle(r); }
+  static __host__ __device__ constexpr int swizzle_v(int r) { return Ops<__bf16>::swizzle(r); }
   static __device__ __forceinline__ void query(const unsigned char* p, int g, bf16x8 (&a)[4]) { Ops<__bf16>::row(p, g, a); }
   static __device__ __forceinline__ void keys(const unsigned char* tile, const unsigned*, int r0, int lane, bf16x8 (&a)[4]) {
     Ops<__bf16>::rows(tile, r0 + (lane & 31), lane >> 5, a);
   }
   static __device__ __forceinline__ void values(const unsigned char* tile, int r0, int db, int lane, bf16x8 (&a)[2]) { Ops<__bf16>::columns(tile, r0, db, lane, a); }
-  static __device__ __forceinline__ float value(const unsigned char* tile, const unsigned*, int r, int d) {
-    return __uint_as_float(static_cast<unsigned>(*LDS_PTR(unsigned short, tile + r * kRow + (((d >> 3) ^ swizzle_v(r)) << 4) + (d & 7) * 2)) << 16);
+  static __device__ __forceinline__ float number(const unsigned char* p, const unsigned char*, int64_t row, int d) {
+    return Ops<__bf16>::number(p + row * kRow, d);
   }
 };
 
@@ -166,8 +166,8 @@ struct Wide<E4m3> {
   typedef E4m3 Cache;
   static constexpr int kRow = 64, kKeys = 64;
   static constexpr bool kScaled = true;
-  static __device__ __forceinline__ int swizzle_k(int r) { return (r >> 2) & 3; }
-  static __device__ __forceinline__ int swizzle_v(int r) { return (r >> 2) & 2; }
+  static __host__ __device__ constexpr int swizzle_k(int r) { return (r >> 2) & 3; }
+  static __host__ __device__ constexpr int swizzle_v(int r) { return (r >> 2) & 2; }
   static __device__ __forceinline__ void query(const unsigned char* p, int g, bf16x8 (&a)[4]) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) a[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p + (4 * g + c) * 16));
@@ -196,11 +196,45 @@ struct Wide<E4m3> {
       a[cp] = __builtin_bit_cast(bf16x8, u32x4{y0[0], y0[1], y1[0], y1[1]});
     }
   }
-  static __device__ __forceinline__ float value(const unsigned char* tile, const unsigned* scales, int r, int d) {
-    const unsigned char x = *LDS_PTR(unsigned char, tile + r * kRow + (((d >> 4) ^ swizzle_v(r)) << 4) + (d & 15));
-    return unpack_f32(x)[0] * scale_of(*LDS_PTR(unsigned, scales + r));
+  static __device__ __forceinline__ float number(const unsigned char* p, const unsigned char* scale, int64_t row, int d) {
+    return unpack_f32(p[row * kRow + d])[0] * scale_of(scale[row]);
   }
 };
+
+// One query by a wave, over the keys of a stretch that it sees and no others: where values that are not finite have met weights of zero in the
+// products.  For results that are right, not for speed.
+template <typename C>
+__device__ void one_query(const PrefixArgs& a, const Stretch& st, const int* table, int hk, int split, int64_t row, const unsigned char* q, int lo, int lane) {
+  typedef Wide<C> P;
+  float m = -INFINITY, l = 0.f, o = 0.f;
+  for (int x0 = st.x0; x0 < st.x1; x0 += 64) {
+    const int x = min(x0 + lane, st.x1 - 1), j = st.key(x);
+    const bool sees = x0 + lane < st.x1 && (j >= lo || j < a.sinks);
+    const int64_t at = st.row(a.pages, table, hk, x);
+    float s = -INFINITY;
+    if (sees) {
+      s = 0.f;
+      for (int d = 0; d < 64; ++d) s += Ops<__bf16>::number(q, d) * P::number(a.pages.k, a.pages.k_scale, at, d);
+      s *= a.scale_log2;
+    }
+    float top = s;
+    for (int e = 32; e > 0; e >>= 1) top = fmaxf(top, __shfl_xor(top, e));
+    const float to = fmaxf(m, top), keep = m == -INFINITY ? 0.f : exp2f(m - to);
+    const float w = sees ? exp2f(s - (to == -INFINITY ? 0.f : to)) : 0.f;  // (NaN stays)
+    float sum = w;
+    for (int e = 32; e > 0; e >>= 1) sum += __shfl_xor(sum, e);
+    l = l * keep + sum;
+    o *= keep;
+    m = to;
+    for (unsigned long long left = __ballot(sees); left != 0; left &= left - 1) {
+      const int e = __builtin_ctzll(left);
+      o += __shfl(w, e) * P::number(a.pages.v, a.pages.v_scale, __shfl(at, e), lane);
+    }
+  }
+  const int64_t rows = int64_t(a.batch) * a.heads;
+  a.part[(split * rows + row) * 64 + lane] = l == 0.f ? 0.f : o / l;
+  if (lane == 0) a.part_lse[split * rows + row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
 
 constexpr float kRaise = 8.0f;  // the running maximum follows when a piece exceeds it by 2^8
 
@@ -286,6 +320,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefix_wide_kernel(const Prefi
     clear(o[e][1]);
   }
   int buf = 0;
+  bool bad = false;  // whether a value that is not finite has met weights of zero
   for (int p = wave; p < pieces; p += kWaves, buf ^= 1) {
     load.wait(p + kWaves >= pieces);
     unsigned char* const kt = mine + buf * kBufBytes;
@@ -295,8 +330,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefix_wide_kernel(const Prefi
     if (left < P::kKeys) load.clear_from(kt, left);
     // key i of the piece is key x + i of the stretch, and no query sees less than keys `most` ..; those in front of it are looked at one by one
     const bool masked = left < P::kKeys || (x + P::kKeys > st.s && st.key(max(x, st.s)) < most);
-    const unsigned long long bad = masked && most > st.lo ? load.bad_keys(kt) : 0;  // (values that are not finite must not meet weights of zero)
-#pragma unroll
+    if (masked && most > st.lo && load.bad_keys(kt) != 0) bad = true;
+#pragma unroll 1
     for (int h = 0; h < P::kKeys / 32; ++h) {
       bf16x8 ka[4];
       P::keys(kt, scales, 32 * h, lane, ka);
@@ -350,25 +385,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefix_wide_kernel(const Prefi
           l[e] += w[e][i];
         }
       }
-      unsigned long long alone = P::kKeys == 32 ? bad : (bad >> (32 * h)) & 0xffffffffull;
-      if (alone != 0) {
-        const unsigned long long these = alone << (32 * h);
-        for (; alone != 0; alone &= alone - 1) {
-          const int r = __builtin_ctzll(alone), j = st.key(x + 32 * h + r), in_lane = 4 * (r >> 3) + (r & 3);
-#pragma unroll
-          for (int e = 0; e < R; ++e) {
-            float weight = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) weight = i == in_lane ? w[e][i] : weight;
-            weight = __shfl(weight, n + 32 * ((r >> 2) & 1));
-            if (j < lo[e] && j >= a.sinks) continue;
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              o[e][i >> 4][i & 15] += weight * P::value(vt, scales + 64, 32 * h + r, 32 * (i >> 4) + 8 * ((i & 15) >> 2) + 4 * g + (i & 3));
-          }
-        }
-        load.clear_keys(kt, these);
-      }
       if constexpr (P::kScaled) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -412,7 +428,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefix_wide_kernel(const Prefi
       sums[wave][1][32 * e + n] = l[e];
     }
   }
-  __syncthreads();
+  if (__syncthreads_or(bad)) {
+    for (int i = wave; i < queries; i += kWaves) {
+      int to, low, s;
+      const int64_t row = row_of(i, to);
+      a.seen(length + a.length(to), low, s);
+      one_query<C>(a, st, table, hk, split, row, a.q.p + to * a.q.token + (row - int64_t(to) * a.heads) * a.q.head, low, lane);
+    }
+    return;
+  }
 #pragma unroll
   for (int e = 0; e < 2 * R; ++e) {
     const int i = 16 * e + (threadIdx.x >> 4), chunk = threadIdx.x & 15;
