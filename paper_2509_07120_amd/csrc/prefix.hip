@@ -17,12 +17,19 @@ struct PrefixArgs {
   const int32_t *prefix_table, *prefix_lengths, *starts;   // sequences starts[g] .. starts[g + 1] - 1 have prefix g
   float *part, *part_lse;             // [splits + own_splits][batch, heads, 64] and [..][batch, heads]
   int batch, heads, group, head_blocks, table_width, prefixes, prefix_width, frame, window, sinks;
-  int splits, stretch, own_splits, own_stretch, queries;  // queries of a tile
+  int splits, stretch, own_splits, own_stretch;
+  int queries, tiles, blocks;  // queries of a tile, tiles of all prefixes, workgroups for prefixes (own keys have those behind them)
   float scale_log2;
 
   __device__ __forceinline__ int start(int g) const { return min(max(starts[g], 0), batch); }
   __device__ __forceinline__ int prefix_length(int g) const { return min(max(prefix_lengths[g], 0), prefix_width * pages.page); }
   __device__ __forceinline__ int length(int b) const { return min(max(lengths[b], 0), table_width * pages.page); }
+  // Workgroup `block` of those for prefixes: the tiles of queries that read the same keys follow each other on one XCD (workgroup w runs on XCD w % 8).
+  __device__ __forceinline__ bool place(int block, int& hk, int& split, int& unit) const {
+    const int pair = block / 8 / tiles * 8 + block % 8;
+    hk = pair / splits, split = pair % splits, unit = block / 8 % tiles;
+    return pair < pages.kv_heads * splits;
+  }
   // of a query with n tokens up to itself: the first key of its window, and the first tokens in front of that it sees
   __device__ __forceinline__ void seen(int n, int& lo, int& s) const {
     lo = s = 0;
@@ -32,6 +39,13 @@ struct PrefixArgs {
       s = min(sinks, lo);
     }
   }
+};
+
+// LDS of a workgroup; pieces: a wave's share follows the other's.
+struct Shared {
+  unsigned char* pieces;
+  int* table;               // [kTable]
+  float* sums;              // [kWaves][2][queries]
 };
 
 // The prefix of sequence b, or -1: whole waves.
@@ -74,17 +88,17 @@ __device__ __forceinline__ void leave(const PrefixArgs& a, int part, int64_t row
 
 // The keys of a prefix, for 16 of the queries of its sequences at one key head.
 template <typename T, typename C>
-__global__ __launch_bounds__(64 * kWaves, 2) void prefix_kernel(const PrefixArgs a) {
+__device__ __forceinline__ void over_prefix(const PrefixArgs& a, const Shared& lds, int block) {
   typedef Ops16<T, C> P;
-  __shared__ __align__(16) unsigned char smem[kWaves * kWaveLds<P>];
-  __shared__ int table[kTable];
-  __shared__ float sums[kWaves][2][kHeads];
+  unsigned char* const smem = lds.pieces;
+  int* const table = lds.table;
+  float (&sums)[kWaves][2][kHeads] = *reinterpret_cast<float (*)[kWaves][2][kHeads]>(lds.sums);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4;
-  const int split = blockIdx.x, hk = blockIdx.y;
-  int tile;
-  const int g = unit_of(a, blockIdx.z, kHeads, lane, tile);
+  int hk, split, unit, tile;
+  if (!a.place(block, hk, split, unit)) return;
+  const int g = unit_of(a, unit, kHeads, lane, tile);
   if (g < 0) return;
   const int b0 = a.start(g), first = tile * kHeads, queries = min((a.start(g + 1) - b0) * a.group - first, kHeads);
   auto row_of = [&](int i, int& b) {  // query i of the tile: its sequence, and its row of the result
@@ -238,25 +252,24 @@ __device__ void one_query(const PrefixArgs& a, const Stretch& st, const int* tab
 
 constexpr float kRaise = 8.0f;  // the running maximum follows when a piece exceeds it by 2^8
 
+template <typename C, int R>
+constexpr int kWideLds = larger(2 * (2 * PieceLoad<Wide<C>>::kBytes + (Wide<C>::kScaled ? 512 : 0)), 32 * R * 64 * 4);
+
 // The same for 32 R queries, bf16.  A wave has them all, as columns, and goes over its own pieces of the keys; what it holds of a piece serves R products.
 template <typename C, int R>
-__global__ __launch_bounds__(64 * kWaves, 2) void prefix_wide_kernel(const PrefixArgs a) {
+__device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shared& shared, int block) {
   typedef Wide<C> P;
   constexpr int kQueries = 32 * R, kBytes = PieceLoad<P>::kBytes, kBufBytes = 2 * kBytes + (P::kScaled ? 512 : 0);
-  constexpr int kWaveBytes = larger(2 * kBufBytes, kQueries * 64 * 4);
-  __shared__ __align__(16) unsigned char smem[kWaves * kWaveBytes];
-  __shared__ int table[kTable];
-  __shared__ float sums[kWaves][2][kQueries];
+  constexpr int kWaveBytes = kWideLds<C, R>;
+  unsigned char* const smem = shared.pieces;
+  int* const table = shared.table;
+  float (&sums)[kWaves][2][kQueries] = *reinterpret_cast<float (*)[kWaves][2][kQueries]>(shared.sums);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, g = lane >> 5;
-  // workgroup w runs on XCD w % 8: the tiles of queries that read the same keys follow each other on one
-  const int pairs = a.pages.kv_heads * a.splits, tiles = gridDim.x / (8 * ((pairs + 7) / 8));
-  const int pair = blockIdx.x / 8 / tiles * 8 + blockIdx.x % 8;
-  if (pair >= pairs) return;
-  const int hk = pair / a.splits, split = pair % a.splits;
-  int tile;
-  const int of = unit_of(a, blockIdx.x / 8 % tiles, kQueries, lane, tile);
+  int hk, split, unit, tile;
+  if (!a.place(block, hk, split, unit)) return;
+  const int of = unit_of(a, unit, kQueries, lane, tile);
   if (of < 0) return;
   const int b0 = a.start(of), first = tile * kQueries, queries = min((a.start(of + 1) - b0) * a.group - first, kQueries);
   auto row_of = [&](int i, int& b) {  // query i of the tile: its sequence, and its row of the result
@@ -462,16 +475,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefix_wide_kernel(const Prefi
 
 // The own keys of a sequence.
 template <typename T, typename C>
-__global__ __launch_bounds__(64 * kWaves, 2) void own_kernel(const PrefixArgs a) {
+__device__ __forceinline__ void over_own(const PrefixArgs& a, const Shared& lds, int block) {
   typedef Ops16<T, C> P;
-  __shared__ __align__(16) unsigned char smem[kWaves * kWaveLds<P>];
-  __shared__ int table[kTable];
-  __shared__ float sums[kWaves][2][kHeads];
+  unsigned char* const smem = lds.pieces;
+  int* const table = lds.table;
+  float (&sums)[kWaves][2][kHeads] = *reinterpret_cast<float (*)[kWaves][2][kHeads]>(lds.sums);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4;
-  const int b = blockIdx.z, split = blockIdx.x;
-  const int hk = blockIdx.y / a.head_blocks, hb = blockIdx.y - hk * a.head_blocks;
+  const int split = block % a.own_splits, of = block / a.own_splits;
+  const int hb = of % a.head_blocks, hk = of / a.head_blocks % a.pages.kv_heads, b = of / a.head_blocks / a.pages.kv_heads;
   const int heads = min(kHeads, a.group - hb * kHeads), h0 = hk * a.group + hb * kHeads;
   const int64_t rows = int64_t(a.batch) * a.heads, row0 = int64_t(b) * a.heads + h0;
   const int g = prefix_of(a, b, lane);
@@ -503,6 +516,25 @@ __global__ __launch_bounds__(64 * kWaves, 2) void own_kernel(const PrefixArgs a)
   leave(a, a.splits + split, row0 + head, (threadIdx.x & 15) * 4, y, top, sum);
 }
 
+template <typename T, typename C, int Q>
+constexpr int lds_of_wave() {
+  if constexpr (Q == kHeads) return kWaveLds<Ops16<T, C>>;
+  else return larger(kWaveLds<Ops16<T, C>>, kWideLds<C, Q / 32>);
+}
+
+// Q: queries of a tile.
+template <typename T, typename C, int Q>
+__global__ __launch_bounds__(64 * kWaves, 2) void prefix_kernel(const PrefixArgs a) {
+  __shared__ __align__(16) unsigned char pieces[kWaves * lds_of_wave<T, C, Q>()];
+  __shared__ int table[kTable];
+  __shared__ float sums[kWaves * 2 * Q];
+  const Shared shared = {pieces, table, sums};
+  const int block = blockIdx.x;
+  if (block >= a.blocks) over_own<T, C>(a, shared, block - a.blocks);
+  else if constexpr (Q == kHeads) over_prefix<T, C>(a, shared, block);
+  else over_prefix_wide<C, Q / 32>(a, shared, block);
+}
+
 int keys_of_piece(int dtype, int cache_dtype) {
   return cache_dtype == BSGA_E4M3 ? Ops16E4m3::kKeys : dtype == BSGA_BF16 ? Ops16<__bf16, __bf16>::kKeys : Ops16<float, float>::kKeys;
 }
@@ -513,7 +545,8 @@ int64_t tiles_of(const PrefixArgs& a, int tile) {
   return smaller(queries / tile + smaller(int64_t(a.prefixes), int64_t(a.batch)), queries);
 }
 
-void shape_of(PrefixArgs& a, int dtype, int cache_dtype) {
+// Returns the workgroups of the launch.
+int64_t shape_of(PrefixArgs& a, int dtype, int cache_dtype) {
   const int keys = keys_of_piece(dtype, cache_dtype);
   const int64_t of_a_prefix = ceil_div(int64_t(a.batch) * a.group, larger(smaller(int64_t(a.prefixes), int64_t(a.batch)), int64_t(1)));  // about
   a.queries = dtype != BSGA_BF16 || of_a_prefix <= 16 ? kHeads : of_a_prefix <= 32 ? 32 : 64;
@@ -526,6 +559,10 @@ void shape_of(PrefixArgs& a, int dtype, int cache_dtype) {
   const int64_t units = larger(ceil_div(int64_t(a.batch) * a.group, a.queries), int64_t(1)) * a.pages.kv_heads;
   cut(most, units, keys, a.pages.page, a.stretch, a.splits);
   cut(own, int64_t(a.batch) * a.pages.kv_heads * a.head_blocks, keys, a.pages.page, a.own_stretch, a.own_splits);
+  a.tiles = a.prefixes > 0 ? static_cast<int>(tiles_of(a, a.queries)) : 0;
+  const int64_t blocks = 8 * ceil_div(int64_t(a.pages.kv_heads) * a.splits, 8) * a.tiles;
+  a.blocks = static_cast<int>(smaller(blocks, int64_t(INT32_MAX)));
+  return blocks + int64_t(a.own_splits) * a.pages.kv_heads * a.head_blocks * a.batch;
 }
 
 size_t part_bytes(const PrefixArgs& a) { return (static_cast<size_t>(a.splits) + a.own_splits) * a.batch * a.heads * 65 * sizeof(float); }
@@ -563,28 +600,16 @@ int check_sizes(const char* fn, int dtype, int cache_dtype, int64_t batch, int h
   return BSGA_OK;
 }
 
-template <typename C, int R>
-void launch_wide(const PrefixArgs& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(8 * ceil_div(int64_t(a.pages.kv_heads) * a.splits, 8) * tiles_of(a, 32 * R)));
-  hipLaunchKernelGGL((prefix_wide_kernel<C, R>), grid, dim3(64 * kWaves), 0, s, a);
-}
-
 template <typename T, typename C>
-int launch(const PrefixArgs& a, unsigned char* out, float* lse, hipStream_t s) {
-  if (a.prefixes > 0) {
-    bool narrow = true;
-    if constexpr (std::is_same<T, __bf16>::value) {
-      narrow = a.queries == kHeads;
-      if (a.queries == 64) launch_wide<C, 2>(a, s);
-      if (a.queries == 32) launch_wide<C, 1>(a, s);
-    }
-    if (narrow) {
-      const dim3 grid(static_cast<unsigned>(a.splits), static_cast<unsigned>(a.pages.kv_heads), static_cast<unsigned>(tiles_of(a, kHeads)));
-      hipLaunchKernelGGL((prefix_kernel<T, C>), grid, dim3(64 * kWaves), 0, s, a);
-    }
+int launch(const PrefixArgs& a, int64_t blocks, unsigned char* out, float* lse, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(blocks));
+  if constexpr (std::is_same<T, __bf16>::value) {
+    if (a.queries == 64) hipLaunchKernelGGL((prefix_kernel<T, C, 64>), grid, dim3(64 * kWaves), 0, s, a);
+    else if (a.queries == 32) hipLaunchKernelGGL((prefix_kernel<T, C, 32>), grid, dim3(64 * kWaves), 0, s, a);
+    else hipLaunchKernelGGL((prefix_kernel<T, C, kHeads>), grid, dim3(64 * kWaves), 0, s, a);
+  } else {
+    hipLaunchKernelGGL((prefix_kernel<T, C, kHeads>), grid, dim3(64 * kWaves), 0, s, a);
   }
-  const dim3 grid(static_cast<unsigned>(a.own_splits), static_cast<unsigned>(a.pages.kv_heads * a.head_blocks), static_cast<unsigned>(a.batch));
-  hipLaunchKernelGGL((own_kernel<T, C>), grid, dim3(64 * kWaves), 0, s, a);
   if (int rc = check_hip(hipGetLastError(), "bsga_prefix_attn")) return rc;
   return launch_join<T>(a.part, a.part_lse, int64_t(a.batch) * a.heads, a.splits + a.own_splits, out, lse, s);
 }
@@ -637,7 +662,8 @@ int bsga_prefix_attn(const void* q, int64_t q_batch, int64_t q_head, const void*
   a.prefix_lengths = prefix_lengths;
   a.starts = starts;
   a.scale_log2 = softmax_scale * kLog2e;
-  shape_of(a, dtype, cache_dtype);
+  const int64_t blocks = shape_of(a, dtype, cache_dtype);
+  if (blocks > INT32_MAX) return fail(BSGA_ERR_UNSUPPORTED, "%s: too many keys of too many queries for one launch", fn);
   const size_t need = part_bytes(a);
   if (!workspace || workspace_bytes < need)
     return fail(BSGA_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace ? workspace_bytes : 0, need);
@@ -646,8 +672,8 @@ int bsga_prefix_attn(const void* q, int64_t q_batch, int64_t q_head, const void*
   a.part_lse = a.part + (int64_t(a.splits) + a.own_splits) * batch * heads * 64;
   unsigned char* const to = static_cast<unsigned char*>(out);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (dtype == BSGA_BF16) return cache_dtype == BSGA_E4M3 ? launch<__bf16, E4m3>(a, to, lse, s) : launch<__bf16, __bf16>(a, to, lse, s);
-  return cache_dtype == BSGA_E4M3 ? launch<float, E4m3>(a, to, lse, s) : launch<float, float>(a, to, lse, s);
+  if (dtype == BSGA_BF16) return cache_dtype == BSGA_E4M3 ? launch<__bf16, E4m3>(a, blocks, to, lse, s) : launch<__bf16, __bf16>(a, blocks, to, lse, s);
+  return cache_dtype == BSGA_E4M3 ? launch<float, E4m3>(a, blocks, to, lse, s) : launch<float, float>(a, blocks, to, lse, s);
 }
 
 }  // extern "C"
