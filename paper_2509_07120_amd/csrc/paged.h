@@ -442,6 +442,13 @@ __device__ __forceinline__ void leave_bad_out(const PieceLoad<P>& load, unsigned
   load.clear_keys(piece, bad);
 }
 
+// Queries are waited for here, and not at their first use in the loop, where that would be waiting for the pieces on their way as well, each time.
+template <typename A, int N>
+__device__ __forceinline__ void have(A (&q)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(q[i]));
+}
+
 // One wave over its pieces: what its columns have of maxima, sums (those of a column's four lanes are still to be added) and weighted values.  seen(key, x) tells
 // whether the lane's column sees the key, where MASKED.
 template <typename P, bool MASKED, typename Seen1>

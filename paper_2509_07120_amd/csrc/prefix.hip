@@ -19,7 +19,7 @@ struct PrefixArgs {
   int batch, heads, group, head_blocks, table_width, prefixes, prefix_width, frame, window, sinks;
   int splits, stretch, own_splits, own_stretch;
   int queries, tiles, blocks;  // queries of a tile, tiles of all prefixes, workgroups for prefixes (own keys have those behind them)
-  float scale_log2;
+  float scale_log2, ln2_scale;        // c = scale log2(e), 1 / c
 
   __device__ __forceinline__ int start(int g) const { return min(max(starts[g], 0), batch); }
   __device__ __forceinline__ int prefix_length(int g) const { return min(max(prefix_lengths[g], 0), prefix_width * pages.page); }
@@ -164,7 +164,7 @@ struct Wide<__bf16> {
   static __host__ __device__ constexpr int swizzle_k(int r) { return Ops<__bf16>::swizzle(r); }
   static __host__ __device__ constexpr int swizzle_v(int r) { return Ops<__bf16>::swizzle(r); }
   static __device__ __forceinline__ void query(const unsigned char* p, int g, bf16x8 (&a)[4]) { Ops<__bf16>::row(p, g, a); }
-  static __device__ __forceinline__ void keys(const unsigned char* tile, const unsigned*, int r0, int lane, bf16x8 (&a)[4]) {
+  static __device__ __forceinline__ void keys(const unsigned char* tile, float, int r0, int lane, bf16x8 (&a)[4]) {
     Ops<__bf16>::rows(tile, r0 + (lane & 31), lane >> 5, a);
   }
   static __device__ __forceinline__ void values(const unsigned char* tile, int r0, int db, int lane, bf16x8 (&a)[2]) { Ops<__bf16>::columns(tile, r0, db, lane, a); }
@@ -186,9 +186,8 @@ struct Wide<E4m3> {
 #pragma unroll
     for (int c = 0; c < 4; ++c) a[c] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p + (4 * g + c) * 16));
   }
-  static __device__ __forceinline__ void keys(const unsigned char* tile, const unsigned* scales, int r0, int lane, bf16x8 (&a)[4]) {
+  static __device__ __forceinline__ void keys(const unsigned char* tile, float f, int r0, int lane, bf16x8 (&a)[4]) {  // f: scale of key r0 + lane % 32
     const int r = r0 + (lane & 31), g = lane >> 5;
-    const float f = scale_of(*LDS_PTR(unsigned, scales + r));
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const u32x4 x = *LDS_PTR(u32x4, tile + r * kRow + (((2 * g + i) ^ swizzle_k(r)) << 4));
@@ -249,8 +248,6 @@ __device__ void one_query(const PrefixArgs& a, const Stretch& st, const int* tab
   a.part[(split * rows + row) * 64 + lane] = l == 0.f ? 0.f : o / l;
   if (lane == 0) a.part_lse[split * rows + row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
-
-constexpr float kRaise = 8.0f;  // the running maximum follows when a piece exceeds it by 2^8
 
 template <typename C, int R>
 constexpr int kWideLds = larger(2 * (2 * PieceLoad<Wide<C>>::kBytes + (Wide<C>::kScaled ? 512 : 0)), 32 * R * 64 * 4);
@@ -314,6 +311,8 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
   bf16x8 qf[R][4];
 #pragma unroll
   for (int e = 0; e < R; ++e) P::query(a.q.p + b[e] * a.q.token + (row[e] - int64_t(b[e]) * a.heads) * a.q.head, g, qf[e]);
+#pragma unroll
+  for (int e = 0; e < R; ++e) have(qf[e]);
   __syncthreads();
 
   unsigned char* const mine = smem + wave * kWaveBytes;
@@ -324,62 +323,105 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
   if (wave < pieces) issue(wave, 0);
   if (wave + kWaves < pieces) issue(wave + kWaves, 1);
 
+  // Weights are 2^(c x - m).  The reference m is the largest logit of a column's first keys, and stays until the sum of its weights passes 2^24: then the
+  // half piece is done again with an m that follows the largest logit and the sum.  That saves a maximum over every piece, a tenth of the vector instructions.
+  // In 8 bits a value's scale 2^s is part of its weight, which costs nothing: products begin with s / c in place of zero, and the sum takes 2^-s of the weight.
   f32x16 o[R][2];
-  float m[R], l[R];
+  float m[R], minus[R], l[R];  // minus: what is added to logits, -m or, as long as nothing was seen, 0
 #pragma unroll
   for (int e = 0; e < R; ++e) {
-    m[e] = -INFINITY, l[e] = 0.f;
+    m[e] = -INFINITY, minus[e] = 0.f, l[e] = 0.f;
     clear(o[e][0]);
     clear(o[e][1]);
   }
   int buf = 0;
-  bool bad = false;  // whether a value that is not finite has met weights of zero
+  bool bad = false, first_half = true;  // bad: whether a value that is not finite has met weights of zero
   for (int p = wave; p < pieces; p += kWaves, buf ^= 1) {
     load.wait(p + kWaves >= pieces);
     unsigned char* const kt = mine + buf * kBufBytes;
     unsigned char* const vt = kt + kBytes;
-    const unsigned* const scales = reinterpret_cast<const unsigned*>(kt + 2 * kBytes);
+    float* const extra = reinterpret_cast<float*>(kt + 2 * kBytes);
     const int x = st.x0 + p * P::kKeys, left = st.x1 - x;
     if (left < P::kKeys) load.clear_from(kt, left);
     // key i of the piece is key x + i of the stretch, and no query sees less than keys `most` ..; those in front of it are looked at one by one
     const bool masked = left < P::kKeys || (x + P::kKeys > st.s && st.key(max(x, st.s)) < most);
     if (masked && most > st.lo && load.bad_keys(kt) != 0) bad = true;
+    float k_scale = 1.f;
+    if constexpr (P::kScaled) {  // a lane to a key: the exponents make room for what they stand for
+      const unsigned kb = reinterpret_cast<unsigned*>(extra)[lane], vb = reinterpret_cast<unsigned*>(extra)[64 + lane];
+      k_scale = scale_of(kb);
+      extra[lane] = (static_cast<float>(vb) - 127.f) * a.ln2_scale;
+      extra[64 + lane] = inverse_scale(vb);
+    }
 #pragma unroll 1
     for (int h = 0; h < P::kKeys / 32; ++h) {
-      bf16x8 ka[4];
-      P::keys(kt, scales, 32 * h, lane, ka);
       f32x16 w[R];
+      auto products = [&]() {
+        bf16x8 ka[4];
+        P::keys(kt, P::kScaled ? __shfl(k_scale, 32 * h + n) : 1.f, 32 * h, lane, ka);
+        f32x16 from;
+        clear(from);
+        if constexpr (P::kScaled)
 #pragma unroll
-      for (int e = 0; e < R; ++e) {
-        clear(w[e]);
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 y = *LDS_PTR(f32x4, extra + 32 * h + 8 * i + 4 * g);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) w[e] = Ops<__bf16>::product(ka[c], qf[e][c], w[e]);
-      }
-      if (masked) {
+            for (int r = 0; r < 4; ++r) from[4 * i + r] = y[r];
+          }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int e = 0; e < R; ++e) w[e] = Ops<__bf16>::product(ka[c], qf[e][c], c == 0 ? from : w[e]);
+        if (masked) {
+          asm volatile("");  // (a branch: most pieces are not)
+#pragma unroll
+          for (int e = 0; e < R; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int r = 32 * h + 8 * (i >> 2) + 4 * g + (i & 3), j = st.key(x + r);
+              w[e][i] = (r >= left) | ((j < lo[e]) & (j >= a.sinks)) ? -INFINITY : w[e][i];
+            }
+        }
+      };
+      float sum[R];
+      auto weights = [&]() {
 #pragma unroll
         for (int e = 0; e < R; ++e)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int r = 32 * h + 8 * (i >> 2) + 4 * g + (i & 3), j = st.key(x + r);
-            if (r >= left || (j < lo[e] && j >= a.sinks)) w[e][i] = -INFINITY;
-          }
-      }
-      float top[R];
-      bool raise = false;
+          for (int i = 0; i < 16; ++i) w[e][i] = __builtin_amdgcn_exp2f(fmaf(w[e][i], a.scale_log2, minus[e]));
 #pragma unroll
-      for (int e = 0; e < R; ++e) {
-        top[e] = w[e][0];
+        for (int e = 0; e < R; ++e) sum[e] = l[e];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top[e] = fmaxf(top[e], w[e][i]);
-        top[e] = top_of_halves(top[e]) * a.scale_log2;
-        raise = raise || top[e] > m[e] + kRaise;
+        for (int i = 0; i < 4; ++i) {
+          f32x4 y = {1.f, 1.f, 1.f, 1.f};
+          if constexpr (P::kScaled) y = *LDS_PTR(f32x4, extra + 64 + 32 * h + 8 * i + 4 * g);
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < R; ++e) sum[e] = P::kScaled ? fmaf(w[e][4 * i + r], y[r], sum[e]) : sum[e] + w[e][4 * i + r];
+        }
+      };
+      products();
+      bool again = first_half;
+      if (!first_half) {
+        weights();
+#pragma unroll
+        for (int e = 0; e < R; ++e) again = again || !(sum[e] <= 0x1p24f) || m[e] == -INFINITY;
       }
-      if (__any(raise)) {
+      if (__any(again)) {
+        if (!first_half) products();
+        first_half = false;
 #pragma unroll
         for (int e = 0; e < R; ++e) {
-          const float to = fmaxf(m[e], top[e]);
+          float top = w[e][0];
+#pragma unroll
+          for (int i = 1; i < 16; ++i) top = fmaxf(top, w[e][i]);
+          float to = fmaxf(m[e], top_of_halves(top) * a.scale_log2);
+          const float grown = top_of_halves(l[e]);
+          if (grown > 0x1p16f) to = fmaxf(to, m[e] + log2f(grown));
           const float keep = to == -INFINITY ? 1.f : exp2f(m[e] - to);
           m[e] = to;
+          minus[e] = to == -INFINITY ? 0.f : -to;
           l[e] *= keep;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
@@ -387,29 +429,14 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
             o[e][1][i] *= keep;
           }
         }
+        weights();
       }
       bf16x8 pw[R][2];
 #pragma unroll
       for (int e = 0; e < R; ++e) {
-        const float from = m[e] == -INFINITY ? 0.f : m[e];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          w[e][i] = __builtin_amdgcn_exp2f(fmaf(w[e][i], a.scale_log2, -from));
-          l[e] += w[e][i];
-        }
+        l[e] = sum[e];
+        Ops<__bf16>::round(w[e], pw[e]);
       }
-      if constexpr (P::kScaled) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const u32x4 by = *LDS_PTR(u32x4, scales + 64 + 32 * h + 8 * i + 4 * g);
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int e = 0; e < R; ++e) w[e][4 * i + r] *= scale_of(by[r]);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < R; ++e) Ops<__bf16>::round(w[e], pw[e]);
 #pragma unroll
       for (int db = 0; db < 2; ++db) {
         bf16x8 va[2];
@@ -558,6 +585,11 @@ int64_t shape_of(PrefixArgs& a, int dtype, int cache_dtype) {
   }
   const int64_t units = larger(ceil_div(int64_t(a.batch) * a.group, a.queries), int64_t(1)) * a.pages.kv_heads;
   cut(most, units, keys, a.pages.page, a.stretch, a.splits);
+  if (a.queries > kHeads && a.splits > 1) {
+    const int64_t step = int64_t(kWaves) * keys, want = larger(int64_t(512) / units, int64_t(1));
+    a.stretch = static_cast<int>(smaller(int64_t(a.stretch) * 64, smaller(ceil_div(larger(ceil_div(most, want), 2 * step), step) * step, int64_t(kTable - 4) * a.pages.page / step * step)));
+    a.splits = static_cast<int>(ceil_div(most, a.stretch));
+  }
   cut(own, int64_t(a.batch) * a.pages.kv_heads * a.head_blocks, keys, a.pages.page, a.own_stretch, a.own_splits);
   a.tiles = a.prefixes > 0 ? static_cast<int>(tiles_of(a, a.queries)) : 0;
   const int64_t blocks = 8 * ceil_div(int64_t(a.pages.kv_heads) * a.splits, 8) * a.tiles;
@@ -662,6 +694,7 @@ int bsga_prefix_attn(const void* q, int64_t q_batch, int64_t q_head, const void*
   a.prefix_lengths = prefix_lengths;
   a.starts = starts;
   a.scale_log2 = softmax_scale * kLog2e;
+  a.ln2_scale = 1.f / a.scale_log2;
   const int64_t blocks = shape_of(a, dtype, cache_dtype);
   if (blocks > INT32_MAX) return fail(BSGA_ERR_UNSUPPORTED, "%s: too many keys of too many queries for one launch", fn);
   const size_t need = part_bytes(a);
