@@ -335,7 +335,8 @@ struct PieceLoad {
 #pragma unroll
     for (int i = 0; i < kPlacesV; ++i) v[i] = r_in * P::kRow + ((pos ^ P::swizzle_v(i * kRowsOfLoad + r_in)) << 4);
   }
-  // the keys from the x-th on
+  // the keys from the x-th on; FRESH: places are not kept in registers for the lanes' own ways
+  template <bool FRESH = false>
   __device__ __forceinline__ void issue(const Pages& a, const Stretch& st, const int* table, int hk, int x, unsigned lds) const {
     x = scalar(x);
     const int j = st.key(x), page = a.of(j), inside = j - page * a.page;
@@ -353,16 +354,17 @@ struct PieceLoad {
       }
       return;
     }
+    const int l = FRESH ? fresh_lane() : lane, in = l / kChunks, chunk = l % kChunks;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int r = i * kRowsOfLoad + r_in;
+      const int r = i * kRowsOfLoad + in;
       const int64_t row = st.row(a, table, hk, min(x + r, st.x1 - 1));  // rows past the end are the last one again, with no weight
-      dma16_at(a.k + row * P::kRow + ((pos ^ P::swizzle_k(r)) << 4), lds + i * 1024);
-      dma16_at(a.v + row * P::kRow + ((pos ^ P::swizzle_v(r)) << 4), lds + kBytes + i * 1024);
+      dma16_at(a.k + row * P::kRow + ((chunk ^ P::swizzle_k(r)) << 4), lds + i * 1024);
+      dma16_at(a.v + row * P::kRow + ((chunk ^ P::swizzle_v(r)) << 4), lds + kBytes + i * 1024);
     }
     if constexpr (P::kScaled) {
       static_assert(P::kKeys == 64, "a lane to a key");
-      const int64_t row = st.row(a, table, hk, min(x + lane, st.x1 - 1));
+      const int64_t row = st.row(a, table, hk, min(x + l, st.x1 - 1));
       dma_byte_at(a.k_scale + row, lds + 2 * kBytes);
       dma_byte_at(a.v_scale + row, lds + 2 * kBytes + 256);
     }

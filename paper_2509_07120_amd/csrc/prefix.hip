@@ -167,7 +167,9 @@ struct Wide<__bf16> {
   static __device__ __forceinline__ void keys(const unsigned char* tile, float, int r0, int lane, bf16x8 (&a)[4]) {
     Ops<__bf16>::rows(tile, r0 + (lane & 31), lane >> 5, a);
   }
-  static __device__ __forceinline__ void values(const unsigned char* tile, int r0, int db, int lane, bf16x8 (&a)[2]) { Ops<__bf16>::columns(tile, r0, db, lane, a); }
+  typedef bf16x8 Raw;  // a value operand as it is read
+  static __device__ __forceinline__ void values(const unsigned char* tile, int r0, int db, int lane, Raw (&a)[2]) { Ops<__bf16>::columns(tile, r0, db, lane, a); }
+  static __device__ __forceinline__ bf16x8 operand(Raw x) { return x; }
   static __device__ __forceinline__ float number(const unsigned char* p, const unsigned char*, int64_t row, int d) {
     return Ops<__bf16>::number(p + row * kRow, d);
   }
@@ -198,15 +200,18 @@ struct Wide<E4m3> {
       }
     }
   }
-  static __device__ __forceinline__ void values(const unsigned char* tile, int r0, int db, int lane, bf16x8 (&a)[2]) {
+  typedef u32x2 Raw;
+  static __device__ __forceinline__ bf16x8 operand(Raw x) {
+    const u32x2 y0 = unpack_bf16(x[0], 1.f), y1 = unpack_bf16(x[1], 1.f);
+    return __builtin_bit_cast(bf16x8, u32x4{y0[0], y0[1], y1[0], y1[1]});
+  }
+  static __device__ __forceinline__ void values(const unsigned char* tile, int r0, int db, int lane, Raw (&a)[2]) {
     const int m = (lane & 15) >> 1, G = lane >> 4;
 #pragma unroll
     for (int cp = 0; cp < 2; ++cp) {
       const int r = r0 + 16 * cp + 4 * (G >> 1) + (m & 3) + 2 * (m & 4);
       const unsigned char* p = tile + r * kRow + (((2 * db + (G & 1)) ^ swizzle_v(r)) << 4) + (lane & 1) * 8;
-      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((s32x2 __attribute__((address_space(3)))*)(p)));
-      const u32x2 y0 = unpack_bf16(x[0], 1.f), y1 = unpack_bf16(x[1], 1.f);
-      a[cp] = __builtin_bit_cast(bf16x8, u32x4{y0[0], y0[1], y1[0], y1[1]});
+      a[cp] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((s32x2 __attribute__((address_space(3)))*)(p)));
     }
   }
   static __device__ __forceinline__ float number(const unsigned char* p, const unsigned char* scale, int64_t row, int d) {
@@ -319,7 +324,7 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
   const unsigned lds = scalar(lds_address(mine));
   const int pieces = (st.x1 - st.x0 + P::kKeys - 1) / P::kKeys;
   const PieceLoad<P> load(lane);
-  auto issue = [&](int p, int buf) { load.issue(a.pages, st, table, hk, st.x0 + p * P::kKeys, lds + buf * kBufBytes); };
+  auto issue = [&](int p, int buf) { load.template issue<true>(a.pages, st, table, hk, st.x0 + p * P::kKeys, lds + buf * kBufBytes); };
   if (wave < pieces) issue(wave, 0);
   if (wave + kWaves < pieces) issue(wave + kWaves, 1);
 
@@ -335,7 +340,7 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
     clear(o[e][1]);
   }
   int buf = 0;
-  bool bad = false, first_half = true;  // bad: whether a value that is not finite has met weights of zero
+  int bad = 0, first_half = 1;  // bad: whether a value that is not finite has met weights of zero
   for (int p = wave; p < pieces; p += kWaves, buf ^= 1) {
     load.wait(p + kWaves >= pieces);
     unsigned char* const kt = mine + buf * kBufBytes;
@@ -344,8 +349,8 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
     const int x = st.x0 + p * P::kKeys, left = st.x1 - x;
     if (left < P::kKeys) load.clear_from(kt, left);
     // key i of the piece is key x + i of the stretch, and no query sees less than keys `most` ..; those in front of it are looked at one by one
-    const bool masked = left < P::kKeys || (x + P::kKeys > st.s && st.key(max(x, st.s)) < most);
-    if (masked && most > st.lo && load.bad_keys(kt) != 0) bad = true;
+    const bool masked = (left < P::kKeys) | ((x + P::kKeys > st.s) & (st.key(max(x, st.s)) < most));
+    if (masked & (most > st.lo)) bad |= load.bad_keys(kt) != 0;
     float k_scale = 1.f;
     if constexpr (P::kScaled) {  // a lane to a key: the exponents make room for what they stand for
       const unsigned kb = reinterpret_cast<unsigned*>(extra)[lane], vb = reinterpret_cast<unsigned*>(extra)[64 + lane];
@@ -373,12 +378,13 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
 #pragma unroll
           for (int e = 0; e < R; ++e) w[e] = Ops<__bf16>::product(ka[c], qf[e][c], c == 0 ? from : w[e]);
         if (masked) {
-          asm volatile("");  // (a branch: most pieces are not)
+          int r0 = 32 * h + 4 * g;
+          asm volatile("" : "+v"(r0));  // (most pieces are not: nothing of this is computed beforehand)
 #pragma unroll
           for (int e = 0; e < R; ++e)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const int r = 32 * h + 8 * (i >> 2) + 4 * g + (i & 3), j = st.key(x + r);
+              const int r = r0 + 8 * (i >> 2) + (i & 3), j = st.key(x + r);
               w[e][i] = (r >= left) | ((j < lo[e]) & (j >= a.sinks)) ? -INFINITY : w[e][i];
             }
         }
@@ -402,15 +408,18 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
         }
       };
       products();
-      bool again = first_half;
+      typename P::Raw raw[2][2];
+#pragma unroll
+      for (int db = 0; db < 2; ++db) P::values(vt, 32 * h, db, lane, raw[db]);
+      int again = first_half;
       if (!first_half) {
         weights();
 #pragma unroll
-        for (int e = 0; e < R; ++e) again = again || !(sum[e] <= 0x1p24f) || m[e] == -INFINITY;
+        for (int e = 0; e < R; ++e) again |= !(sum[e] <= 0x1p24f) | (m[e] == -INFINITY);
       }
       if (__any(again)) {
         if (!first_half) products();
-        first_half = false;
+        first_half = 0;
 #pragma unroll
         for (int e = 0; e < R; ++e) {
           float top = w[e][0];
@@ -439,12 +448,12 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
       }
 #pragma unroll
       for (int db = 0; db < 2; ++db) {
-        bf16x8 va[2];
-        P::values(vt, 32 * h, db, lane, va);
 #pragma unroll
-        for (int e = 0; e < R; ++e)
+        for (int c = 0; c < 2; ++c) {
+          const bf16x8 v = P::operand(raw[db][c]);
 #pragma unroll
-          for (int c = 0; c < 2; ++c) o[e][db] = Ops<__bf16>::product(va[c], pw[e][c], o[e][db]);
+          for (int e = 0; e < R; ++e) o[e][db] = Ops<__bf16>::product(v, pw[e][c], o[e][db]);
+        }
       }
     }
     if (p + 2 * kWaves < pieces) {
