@@ -561,7 +561,8 @@ __device__ __forceinline__ void join_waves(unsigned char* smem, float (&sums)[kW
 // workgroup (4,608 keys take one about 30 us), and the workgroups that find nothing to do have to stay few.
 // Up to 8 pieces for each wave are one workgroup's whatever the launch: 1,024 bf16 keys 9.9 us a call and 27.2 alone, in stretches of 256 with
 // their second kernel 13.8 and 26.7; 512 fp32 keys 13.0 and 30.3, 14.2 and 29.7.
-inline void cut(int64_t most, int64_t units, int keys_of_piece, int page, int& stretch_out, int& splits_out) {
+// places: so many workgroups, if that is not 0.
+inline void cut(int64_t most, int64_t units, int keys_of_piece, int page, int& stretch_out, int& splits_out, int64_t places = 0) {
   most = larger(most, int64_t(1));
   const int64_t step = kWaves * keys_of_piece;
   if (most <= 8 * step) {
@@ -571,6 +572,7 @@ inline void cut(int64_t most, int64_t units, int keys_of_piece, int page, int& s
   }
   int64_t splits = larger(int64_t(units > 256 || most * units < 512 * 1024 ? 512 : 1024) / units, int64_t(1));
   if (units > 256) splits = larger(splits, smaller(ceil_div(most, 4608), int64_t(4096) / units));
+  if (places > 0) splits = larger(places / units, int64_t(1));
   const int64_t stretch = ceil_div(larger(ceil_div(most, splits), 2 * step), step) * step;
   const int64_t fits = int64_t(kTable - 4) * page / step * step;
   stretch_out = static_cast<int>(smaller(smaller(stretch, fits), ceil_div(most, step) * step));

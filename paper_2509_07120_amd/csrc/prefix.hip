@@ -523,14 +523,19 @@ __device__ __forceinline__ void over_own(const PrefixArgs& a, const Shared& lds,
   const int hb = of % a.head_blocks, hk = of / a.head_blocks % a.pages.kv_heads, b = of / a.head_blocks / a.pages.kv_heads;
   const int heads = min(kHeads, a.group - hb * kHeads), h0 = hk * a.group + hb * kHeads;
   const int64_t rows = int64_t(a.batch) * a.heads, row0 = int64_t(b) * a.heads + h0;
-  const int g = prefix_of(a, b, lane);
-  if (g < 0 && split == 0 && threadIdx.x < heads)  // nobody else writes the prefix's parts of this sequence
-    for (int x = 0; x < a.splits; ++x) a.part_lse[x * rows + row0 + threadIdx.x] = -INFINITY;
-  const int behind = g < 0 ? 0 : a.prefix_length(g), length = a.length(b);
+  const int length = a.length(b);
   Stretch st = {};
-  a.seen(behind + length, st.lo, st.s);
-  st.s = max(st.s - behind, 0);
-  st.lo = min(max(st.lo - behind, 0), length);
+  if (a.window > 0 || split == 0) {  // (where it is in the sequence matters to a window only)
+    const int g = prefix_of(a, b, lane);
+    if (g < 0 && split == 0 && threadIdx.x < heads)  // nobody else writes the prefix's parts of this sequence
+      for (int x = 0; x < a.splits; ++x) a.part_lse[x * rows + row0 + threadIdx.x] = -INFINITY;
+    if (a.window > 0) {
+      const int behind = g < 0 ? 0 : a.prefix_length(g);
+      a.seen(behind + length, st.lo, st.s);
+      st.s = max(st.s - behind, 0);
+      st.lo = min(max(st.lo - behind, 0), length);
+    }
+  }
   const int count = st.s + length - st.lo;
   st.x0 = split * a.own_stretch, st.x1 = min(st.x0 + a.own_stretch, count);
   if (st.x0 >= st.x1) {  // the whole workgroup
@@ -581,6 +586,10 @@ int64_t tiles_of(const PrefixArgs& a, int tile) {
   return smaller(queries / tile + smaller(int64_t(a.prefixes), int64_t(a.batch)), queries);
 }
 
+// Tiles of 32 and 64 queries take so long over a piece that a workgroup more than the chip holds is a round more, and what they leave for the join counts.  If one tile
+// reads a key head's keys, one workgroup to a CU does, beside those of the own keys; otherwise all places are taken.  256 / 384 / 512 / 1024 workgroups, us:
+// 64 sequences of 16 heads on 100 frames, 2,000 own tokens at most, 167 / 169 / 176 / 196, in 8 bits with one own token 108 / 118 / 118 / 134; 8 of 16 heads to 2
+// 28 / 34 / 37 / 45; but with more tiles, 64 of 16 heads to 4, 104 / 79 / 70 / 81, 128 of them in 8 bits 189 / 137 / 115 / 120.
 // Returns the workgroups of the launch.
 int64_t shape_of(PrefixArgs& a, int dtype, int cache_dtype) {
   const int keys = keys_of_piece(dtype, cache_dtype);
@@ -593,12 +602,7 @@ int64_t shape_of(PrefixArgs& a, int dtype, int cache_dtype) {
     own = smaller(own, seen);
   }
   const int64_t units = larger(ceil_div(int64_t(a.batch) * a.group, a.queries), int64_t(1)) * a.pages.kv_heads;
-  cut(most, units, keys, a.pages.page, a.stretch, a.splits);
-  if (a.queries > kHeads && a.splits > 1) {
-    const int64_t step = int64_t(kWaves) * keys, want = larger(int64_t(512) / units, int64_t(1));
-    a.stretch = static_cast<int>(smaller(int64_t(a.stretch) * 64, smaller(ceil_div(larger(ceil_div(most, want), 2 * step), step) * step, int64_t(kTable - 4) * a.pages.page / step * step)));
-    a.splits = static_cast<int>(ceil_div(most, a.stretch));
-  }
+  cut(most, units, keys, a.pages.page, a.stretch, a.splits, a.queries == kHeads ? 0 : units == a.pages.kv_heads ? 256 : 512);
   cut(own, int64_t(a.batch) * a.pages.kv_heads * a.head_blocks, keys, a.pages.page, a.own_stretch, a.own_splits);
   a.tiles = a.prefixes > 0 ? static_cast<int>(tiles_of(a, a.queries)) : 0;
   const int64_t blocks = 8 * ceil_div(int64_t(a.pages.kv_heads) * a.splits, 8) * a.tiles;
