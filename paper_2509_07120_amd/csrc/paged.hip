@@ -61,7 +61,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(const PagedArgs a
 
   f32x4 o[4];
   float m, l;
-  go_over<P, false>(a.pages, st, table, hk, wave, lane, smem + wave * kWaveLds<P>, a.scale_log2, qf, [](int) { return true; }, o, m, l);
+  go_over<P, false, P::kScaled>(a.pages, st, table, hk, wave, lane, smem + wave * kWaveLds<P>, a.scale_log2, qf, [](int) { return true; }, o, m, l);
   f32x4 y;
   float top, sum;
   join_waves<P>(smem, sums, wave, lane, o, m, l, y, top, sum);

@@ -141,9 +141,9 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, const Shared& l
   float m, l;
   unsigned char* const mine = smem + wave * kWaveLds<P>;
   if (most > st.lo)
-    go_over<P, true>(a.pages, st, table, hk, wave, lane, mine, a.scale_log2, qf, [&](int j) { return j >= lo || j < a.sinks; }, o, m, l);
+    go_over<P, true, true>(a.pages, st, table, hk, wave, lane, mine, a.scale_log2, qf, [&](int j) { return j >= lo || j < a.sinks; }, o, m, l);
   else
-    go_over<P, false>(a.pages, st, table, hk, wave, lane, mine, a.scale_log2, qf, [](int) { return true; }, o, m, l);
+    go_over<P, false, true>(a.pages, st, table, hk, wave, lane, mine, a.scale_log2, qf, [](int) { return true; }, o, m, l);
   f32x4 y;
   float top, sum;
   join_waves<P>(smem, sums, wave, lane, o, m, l, y, top, sum);
@@ -548,7 +548,7 @@ __device__ __forceinline__ void over_own(const PrefixArgs& a, const Shared& lds,
   __syncthreads();
   f32x4 o[4];
   float m, l;
-  go_over<P, false>(a.pages, st, table, hk, wave, lane, smem + wave * kWaveLds<P>, a.scale_log2, qf, [](int) { return true; }, o, m, l);
+  go_over<P, false, true>(a.pages, st, table, hk, wave, lane, smem + wave * kWaveLds<P>, a.scale_log2, qf, [](int) { return true; }, o, m, l);
   f32x4 y;
   float top, sum;
   join_waves<P>(smem, sums, wave, lane, o, m, l, y, top, sum);
