@@ -328,6 +328,12 @@ struct Stretch {
     for (int i = threadIdx.x; i < min(a_pages + b_pages, kTable); i += 64 * kWaves)
       table[i] = min(max(pages[i < a_pages ? a0 + i : b0 + i - a_pages], 0), a.n_pages - 1);  // a bad entry cannot read out of bounds
   }
+  // The same without a window, where nothing of it goes by the sequence's length, which then is on its way at the same time; x0 is set, s and lo are 0.
+  __device__ __forceinline__ void fill_ahead(const Pages& a, const int32_t* pages, int width, int stretch, int* table) {
+    b0 = a.of(x0);
+    for (int i = threadIdx.x; i < min(min(width - b0, (stretch + a.page - 2) / a.page + 1), kTable); i += 64 * kWaves)
+      table[i] = min(max(pages[b0 + i], 0), a.n_pages - 1);
+  }
   // the cache row, of head hk, of the x-th key
   __device__ __forceinline__ int64_t row(const Pages& a, const int* table, int hk, int x) const {
     const int j = key(x);

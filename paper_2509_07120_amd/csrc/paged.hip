@@ -41,20 +41,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(const PagedArgs a
   const int h0 = hk * a.group + hb * kHeads;                  // the first of them
   const int64_t rows = int64_t(a.batch) * a.heads, row0 = int64_t(b) * a.heads + h0;
 
-  const int length = min(max(a.lengths[b], 0), a.table_width * a.pages.page);
   Stretch st = {};
+  st.x0 = split * a.stretch;
+  const int32_t* const pages = a.page_table + int64_t(b) * a.table_width;
+  if (a.window == 0) st.fill_ahead(a.pages, pages, a.table_width, a.stretch, table);
+  const int length = min(max(a.lengths[b], 0), a.table_width * a.pages.page);
   if (a.window > 0 && length > 0) {
     const int f = (length - 1) / a.frame;
     st.lo = f < a.window ? 0 : (f + 1 - a.window) * a.frame;
     st.s = min(a.sinks, st.lo);
   }
   const int count = st.s + length - st.lo;
-  st.x0 = split * a.stretch, st.x1 = min(st.x0 + a.stretch, count);
+  st.x1 = min(st.x0 + a.stretch, count);
   if (st.x0 >= st.x1 && a.splits > 1) {  // the whole workgroup: the sequence has no keys here
     if (threadIdx.x < heads) a.part_lse[split * rows + row0 + threadIdx.x] = -INFINITY;
     return;
   }
-  st.fill(a.pages, a.page_table + int64_t(b) * a.table_width, table);
+  if (a.window > 0) st.fill(a.pages, pages, table);
   typename P::A qf[P::kSteps];
   P::row(a.q.p + b * a.q.token + (h0 + min(c, heads - 1)) * a.q.head, q, qf);
   __syncthreads();

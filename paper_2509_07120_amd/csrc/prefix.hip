@@ -106,13 +106,15 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, const Shared& l
     b = b0 + x / a.group;
     return int64_t(b) * a.heads + hk * a.group + x % a.group;
   };
+  Stretch st = {};
+  st.x0 = split * a.stretch;
+  if (a.window == 0) st.fill_ahead(a.pages, a.prefix_table + int64_t(g) * a.prefix_width, a.prefix_width, a.stretch, table);
   const int length = a.prefix_length(g);
   int b;
   const int64_t row = row_of(min(c, queries - 1), b);
   int lo, s;
   a.seen(length + a.length(b), lo, s);
   lo = min(lo, length);
-  Stretch st = {};
   st.lo = lo;
   int most = lo;
 #pragma unroll
@@ -124,7 +126,7 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, const Shared& l
   most = __builtin_amdgcn_readfirstlane(most);
   st.s = min(a.sinks, st.lo);
   const int count = st.s + length - st.lo;
-  st.x0 = split * a.stretch, st.x1 = min(st.x0 + a.stretch, count);
+  st.x1 = min(st.x0 + a.stretch, count);
   if (st.x0 >= st.x1) {  // the whole workgroup
     int of;
     if (threadIdx.x < queries) {
@@ -133,9 +135,10 @@ __device__ __forceinline__ void over_prefix(const PrefixArgs& a, const Shared& l
     }
     return;
   }
-  st.fill(a.pages, a.prefix_table + int64_t(g) * a.prefix_width, table);
+  if (a.window > 0) st.fill(a.pages, a.prefix_table + int64_t(g) * a.prefix_width, table);
   typename P::A qf[P::kSteps];
   P::row(a.q.p + b * a.q.token + (row - int64_t(b) * a.heads) * a.q.head, q, qf);
+  have(qf);
   __syncthreads();
   f32x4 o[4];
   float m, l;
@@ -279,10 +282,12 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
     b = b0 + x / a.group;
     return int64_t(b) * a.heads + hk * a.group + x % a.group;
   };
+  Stretch st = {};
+  st.x0 = split * a.stretch;
+  if (a.window == 0) st.fill_ahead(a.pages, a.prefix_table + int64_t(of) * a.prefix_width, a.prefix_width, a.stretch, table);
   const int length = a.prefix_length(of);
   int lo[R], b[R];
   int64_t row[R];
-  Stretch st = {};
   st.lo = length;
   int most = 0;
 #pragma unroll
@@ -303,7 +308,7 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
   most = scalar(most);
   st.s = min(a.sinks, st.lo);
   const int count = st.s + length - st.lo;
-  st.x0 = split * a.stretch, st.x1 = min(st.x0 + a.stretch, count);
+  st.x1 = min(st.x0 + a.stretch, count);
   if (st.x0 >= st.x1) {  // the whole workgroup
     int to;
     if (threadIdx.x < queries) {
@@ -312,7 +317,7 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
     }
     return;
   }
-  st.fill(a.pages, a.prefix_table + int64_t(of) * a.prefix_width, table);
+  if (a.window > 0) st.fill(a.pages, a.prefix_table + int64_t(of) * a.prefix_width, table);
   bf16x8 qf[R][4];
 #pragma unroll
   for (int e = 0; e < R; ++e) P::query(a.q.p + b[e] * a.q.token + (row[e] - int64_t(b[e]) * a.heads) * a.q.head, g, qf[e]);
@@ -523,8 +528,11 @@ __device__ __forceinline__ void over_own(const PrefixArgs& a, const Shared& lds,
   const int hb = of % a.head_blocks, hk = of / a.head_blocks % a.pages.kv_heads, b = of / a.head_blocks / a.pages.kv_heads;
   const int heads = min(kHeads, a.group - hb * kHeads), h0 = hk * a.group + hb * kHeads;
   const int64_t rows = int64_t(a.batch) * a.heads, row0 = int64_t(b) * a.heads + h0;
-  const int length = a.length(b);
   Stretch st = {};
+  st.x0 = split * a.own_stretch;
+  const int32_t* const own_pages = a.page_table + int64_t(b) * a.table_width;
+  if (a.window == 0) st.fill_ahead(a.pages, own_pages, a.table_width, a.own_stretch, table);
+  const int length = a.length(b);
   if (a.window > 0 || split == 0) {  // (where it is in the sequence matters to a window only)
     const int g = prefix_of(a, b, lane);
     if (g < 0 && split == 0 && threadIdx.x < heads)  // nobody else writes the prefix's parts of this sequence
@@ -537,14 +545,15 @@ __device__ __forceinline__ void over_own(const PrefixArgs& a, const Shared& lds,
     }
   }
   const int count = st.s + length - st.lo;
-  st.x0 = split * a.own_stretch, st.x1 = min(st.x0 + a.own_stretch, count);
+  st.x1 = min(st.x0 + a.own_stretch, count);
   if (st.x0 >= st.x1) {  // the whole workgroup
     if (threadIdx.x < heads) a.part_lse[(a.splits + split) * rows + row0 + threadIdx.x] = -INFINITY;
     return;
   }
-  st.fill(a.pages, a.page_table + int64_t(b) * a.table_width, table);
+  if (a.window > 0) st.fill(a.pages, own_pages, table);
   typename P::A qf[P::kSteps];
   P::row(a.q.p + b * a.q.token + (h0 + min(c, heads - 1)) * a.q.head, q, qf);
+  have(qf);
   __syncthreads();
   f32x4 o[4];
   float m, l;
