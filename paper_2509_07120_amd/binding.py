@@ -934,38 +934,43 @@ def bsga_paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     return (out, lse) if return_lse else out
 
 
-def _pages_of(name: str, t: torch.Tensor, dtype, at: int, shape) -> None:
-    """Whether t is a cache of this shape on this device."""
+# (steps of a few sequences are bound by the host: one condition for what is right, and the words for what is not in a function of their own)
+def _wrong_cache(name: str, t: torch.Tensor, dtype, at: int) -> None:
     if not t.is_cuda or t.dtype != dtype or t.get_device() != at or not t.is_contiguous():
         _wrong(t, name, dtype, at, "the tensors")
-    if len(shape) != 4 or t.shape != shape:
-        raise ValueError(f"{name} must be [pages, kv_heads, page, 64]")
+    raise ValueError(f"{name} must be [pages, kv_heads, page, 64]")
 
 
-def _scales_of(k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor], at: int, shape) -> None:
-    """Whether these are the scales of caches of this shape."""
-    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-        if t is None:
-            raise ValueError(f"a cache in 8 bits needs {name}")
-        if not t.is_cuda or t.dtype != torch.uint8 or t.get_device() != at or not t.is_contiguous():
-            _wrong(t, name, torch.uint8, at, "the tensors")
-        if t.shape != shape[:3]:
-            raise ValueError(f"{name} must be [pages, kv_heads, page]")
+def _wrong_scale(name: str, t: Optional[torch.Tensor], at: int) -> None:
+    if t is None:
+        raise ValueError(f"a cache in 8 bits needs {name}")
+    if not t.is_cuda or t.dtype != torch.uint8 or t.get_device() != at or not t.is_contiguous():
+        _wrong(t, name, torch.uint8, at, "the tensors")
+    raise ValueError(f"{name} must be [pages, kv_heads, page]")
 
 
-def _cache_of(k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor], dtype, at: int, d: int) -> int:
-    """Checks caches of the tensors' type, or in 8 bits with their scales; their type's code."""
-    shape, coded = k_cache.shape, k_cache.dtype == torch.float8_e4m3fn
-    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        _pages_of(name, t, torch.float8_e4m3fn if coded else dtype, at, shape)
-    if shape[3] != d:
-        raise ValueError("k_cache must be [pages, kv_heads, page, 64]")
+def _cache_of(k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor], dtype, at: int, d: int,
+              heads: Optional[int] = None):
+    """Checks caches of this type, or in 8 bits with their scales, on device `at`: their type's code, pages, heads and page."""
+    shape = k_cache.shape
+    coded = k_cache.dtype is torch.float8_e4m3fn
+    kind = torch.float8_e4m3fn if coded else dtype
+    if len(shape) != 4 or k_cache.dtype is not kind or k_cache.get_device() != at or at < 0 or not k_cache.is_contiguous() or shape[3] != d or (
+            heads is not None and shape[1] != heads):
+        _wrong_cache("k_cache", k_cache, kind, at)
+    if v_cache.dtype is not kind or v_cache.get_device() != at or not v_cache.is_contiguous() or v_cache.shape != shape:
+        _wrong_cache("v_cache", v_cache, kind, at)
+    pages, heads, page, _ = shape
     if coded:
-        _scales_of(k_scale, v_scale, at, shape)
-        return BSGA_E4M3
+        want = shape[:3]
+        if k_scale is None or k_scale.dtype is not torch.uint8 or k_scale.get_device() != at or not k_scale.is_contiguous() or k_scale.shape != want:
+            _wrong_scale("k_scale", k_scale, at)
+        if v_scale is None or v_scale.dtype is not torch.uint8 or v_scale.get_device() != at or not v_scale.is_contiguous() or v_scale.shape != want:
+            _wrong_scale("v_scale", v_scale, at)
+        return BSGA_E4M3, pages, heads, page
     if k_scale is not None or v_scale is not None:
         raise ValueError("scales go with caches of torch.float8_e4m3fn")
-    return _dtype_code(k_cache)
+    return _dtype_code(k_cache), pages, heads, page
 
 
 def bsga_qk_norm_rope_e4m3(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -991,16 +996,13 @@ def bsga_qk_norm_rope_e4m3(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.
         _wrong(slots, "slots", torch.int32, at, "the tensors")
     if slots.numel() != N:
         raise ValueError("slots must have one entry per token")
-    shape = k_cache.shape
-    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        _pages_of(name, t, torch.float8_e4m3fn, at, shape)
-    if shape[1] != K or shape[3] != d:
-        raise ValueError("k_cache must be [pages, kv_heads, page, 64]")
-    _scales_of(k_scale, v_scale, at, shape)
+    _, pages, _, page = _cache_of(k_cache, v_cache, k_scale, v_scale, torch.float8_e4m3fn, at, d, K)
     q_out = None if q is None else q.new_empty((H, N, d))
-    k_rows, v_rows = (k.new_empty((2, K, N, d)) if return_rows else (None, None))
+    k_rows = v_rows = None
+    if return_rows:
+        k_rows, v_rows = k.new_empty((K, N, d)), k.new_empty((K, N, d))
     _check(lib.bsga_qk_norm_rope_e4m3(_ptr(q), k.data_ptr(), v.data_ptr(), qt, qh, kt, kh, vt, vh, code, N, H, K, d, kind, eps, qw, qb, kw, kb, where, axes, base,
-                                      slots.data_ptr(), shape[0], shape[2], _ptr(q_out), _ptr(k_rows), _ptr(v_rows), k_cache.data_ptr(),
+                                      slots.data_ptr(), pages, page, _ptr(q_out), _ptr(k_rows), _ptr(v_rows), k_cache.data_ptr(),
                                       v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _stream(k)))
     return q_out, k_rows, v_rows
 
@@ -1021,14 +1023,14 @@ def bsga_cache_load(k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.T
     at, d = k_cache.get_device(), 64
     if not coded and k_cache.dtype != dtype:
         raise TypeError(f"a cache that is not in 8 bits is read as it is, got {k_cache.dtype} and {dtype}")
-    code = _cache_of(k_cache, v_cache, k_scale, v_scale, dtype, at, d)
+    code, n_pages, K, page = _cache_of(k_cache, v_cache, k_scale, v_scale, dtype, at, d)
     if not pages.is_cuda or pages.dtype != torch.int32 or pages.get_device() != at or not pages.is_contiguous():
         _wrong(pages, "pages", torch.int32, at, "the caches")
     if pages.dim() != 1:
         raise ValueError("pages must be one sequence's row of a page table")
-    n_pages, K, page, _ = k_cache.shape
     if out is None:
-        k, v = k_cache.new_empty((2, K, max(n_tokens, 0), d), dtype=dtype)
+        shape = (K, max(n_tokens, 0), d)
+        k, v = k_cache.new_empty(shape, dtype=dtype), k_cache.new_empty(shape, dtype=dtype)
     else:
         k, v = out
         for name, t in (("out[0]", k), ("out[1]", v)):
@@ -1053,12 +1055,23 @@ def _queries(q: torch.Tensor) -> Tuple[int, int]:
     return strides[0], strides[1]
 
 
-def _whole(name: str, t: torch.Tensor, at: int, shape) -> None:
-    """Whether t is an int32 tensor of this shape (None: any number)."""
-    if not t.is_cuda or t.dtype != torch.int32 or t.get_device() != at or not t.is_contiguous():
-        _wrong(t, name, torch.int32, at, "q")
-    if len(t.shape) != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        raise ValueError(f"{name} must be {['any' if n is None else n for n in shape]}, got {tuple(t.shape)}")
+def _numbers(name: str, t: torch.Tensor, at: int, n: int) -> int:
+    """The address of an int32 tensor [n]."""
+    if t.dtype is not torch.int32 or t.get_device() != at or not t.is_contiguous() or t.dim() != 1 or t.shape[0] != n:
+        if not t.is_cuda or t.dtype != torch.int32 or t.get_device() != at or not t.is_contiguous():
+            _wrong(t, name, torch.int32, at, "q")
+        raise ValueError(f"{name} must be [{n}], got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _table(name: str, t: torch.Tensor, at: int, rows: Optional[int]) -> Tuple[int, int, int]:
+    """The address, rows and width of an int32 tensor [rows, width]."""
+    shape = t.shape
+    if t.dtype is not torch.int32 or t.get_device() != at or not t.is_contiguous() or len(shape) != 2 or (rows is not None and shape[0] != rows):
+        if not t.is_cuda or t.dtype != torch.int32 or t.get_device() != at or not t.is_contiguous():
+            _wrong(t, name, torch.int32, at, "q")
+        raise ValueError(f"{name} must be [{'any' if rows is None else rows}, width], got {tuple(shape)}")
+    return t.data_ptr(), shape[0], shape[1]
 
 
 def bsga_paged_attn_e4m3(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
@@ -1070,14 +1083,11 @@ def bsga_paged_attn_e4m3(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
     strides = _queries(q)
     B, H, d = q.shape
     at = q.get_device()
-    if _cache_of(k_cache, v_cache, k_scale, v_scale, torch.float8_e4m3fn, at, d) != BSGA_E4M3:
-        raise TypeError("the caches must be torch.float8_e4m3fn")
-    _whole("page_table", page_table, at, (B, None))
-    _whole("lengths", lengths, at, (B,))
+    _, pages, K, page = _cache_of(k_cache, v_cache, k_scale, v_scale, torch.float8_e4m3fn, at, d)
+    table, _, width = _table("page_table", page_table, at, B)
+    many = _numbers("lengths", lengths, at, B)
     if window is not None and window < 1:
         raise ValueError(f"window must be at least one frame, or None, got {window}")
-    pages, K, page, _ = k_cache.shape
-    width = page_table.shape[1]
     seen = (frame, 0 if window is None else window, sinks)
     out = q.new_empty((B, H, d))
     lse = q.new_empty((B, H), dtype=torch.float32) if return_lse else None
@@ -1087,9 +1097,9 @@ def bsga_paged_attn_e4m3(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
             workspace = q.new_empty(nbytes, dtype=torch.uint8)
     else:
         nbytes = workspace.numel() * workspace.element_size()
-    _check(lib.bsga_paged_attn_e4m3(_ptr(q), *strides, _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), code, B, H, K, d, _ptr(page_table), width,
-                                    _ptr(lengths), pages, page, 1.0 / math.sqrt(d) if softmax_scale is None else float(softmax_scale), *seen,
-                                    _ptr(out), _ptr(lse), _ptr(workspace), nbytes, _stream(q)))
+    _check(lib.bsga_paged_attn_e4m3(q.data_ptr(), *strides, k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), code, B, H, K, d, table,
+                                    width, many, pages, page, 1.0 / math.sqrt(d) if softmax_scale is None else float(softmax_scale), *seen, out.data_ptr(),
+                                    _ptr(lse), _ptr(workspace), nbytes, _stream(q)))
     return (out, lse) if return_lse else out
 
 
@@ -1105,17 +1115,13 @@ def bsga_prefix_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     strides = _queries(q)
     B, H, d = q.shape
     at = q.get_device()
-    kind = _cache_of(k_cache, v_cache, k_scale, v_scale, q.dtype, at, d)
-    _whole("page_table", page_table, at, (B, None))
-    _whole("lengths", lengths, at, (B,))
-    _whole("prefix_table", prefix_table, at, (None, None))
-    G, prefix_width = prefix_table.shape
-    _whole("prefix_lengths", prefix_lengths, at, (G,))
-    _whole("starts", starts, at, (G + 1,))
+    kind, pages, K, page = _cache_of(k_cache, v_cache, k_scale, v_scale, q.dtype, at, d)
+    table, _, width = _table("page_table", page_table, at, B)
+    many = _numbers("lengths", lengths, at, B)
+    prefix, G, prefix_width = _table("prefix_table", prefix_table, at, None)
+    long, begin = _numbers("prefix_lengths", prefix_lengths, at, G), _numbers("starts", starts, at, G + 1)
     if window is not None and window < 1:
         raise ValueError(f"window must be at least one frame, or None, got {window}")
-    pages, K, page, _ = k_cache.shape
-    width = page_table.shape[1]
     seen = (frame, 0 if window is None else window, sinks)
     out = q.new_empty((B, H, d))
     lse = q.new_empty((B, H), dtype=torch.float32) if return_lse else None
@@ -1125,8 +1131,7 @@ def bsga_prefix_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
             workspace = q.new_empty(nbytes, dtype=torch.uint8)
     else:
         nbytes = workspace.numel() * workspace.element_size()
-    _check(lib.bsga_prefix_attn(_ptr(q), *strides, _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), code, kind, B, H, K, d, _ptr(page_table), width,
-                                _ptr(lengths), _ptr(prefix_table), prefix_width, _ptr(prefix_lengths), _ptr(starts), G, pages, page,
-                                1.0 / math.sqrt(d) if softmax_scale is None else float(softmax_scale), *seen, _ptr(out), _ptr(lse), _ptr(workspace),
-                                nbytes, _stream(q)))
+    _check(lib.bsga_prefix_attn(q.data_ptr(), *strides, k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), code, kind, B, H, K, d, table, width,
+                                many, prefix, prefix_width, long, begin, G, pages, page, 1.0 / math.sqrt(d) if softmax_scale is None else float(softmax_scale),
+                                *seen, out.data_ptr(), _ptr(lse), _ptr(workspace), nbytes, _stream(q)))
     return (out, lse) if return_lse else out
