@@ -1,13 +1,13 @@
-"""Attention over a growing sequence of frames: a layer that is trained on whole sequences, takes a prompt at once and then one token after the
+"""Attention over a growing sequence of frames: a layer that is trained on whole sequences, takes a prompt at once or in parts and then one token after the
 other, with the bsga kernels: norms of queries and keys with the position rotation, attention with a sliding window of frames and
-first tokens that stay visible, attention of single tokens over a paged cache.
+first tokens that stay visible, attention of single tokens over a paged cache, which may be in 8 bits and shared by sequences that begin alike.
 
 Integration shape only, as GlobalAttentionBlock: random weights.
 """
 from __future__ import annotations
 
 from contextlib import contextmanager
-from typing import List, Optional, Sequence
+from typing import List, Optional, Sequence, Tuple
 
 import torch
 import torch.nn.functional as F
@@ -66,23 +66,63 @@ class PagedCache:
     """Keys and values of several sequences in pages [pages, kv_heads, page, 64], and which page holds which tokens.  The bookkeeping is
     the host's; grow() and trim() bring the device's table and lengths up to date on the current stream.  Places of the table without a page, of
     freed ones too, hold -1, which bsga_paged_attn takes for page 0: check_seen() tells whether a window reaches them.
+    dtype torch.float8_e4m3fn: keys and values are held in 8 bits, each row with a scale of its own (k_scale, v_scale; see bsga_qk_norm_rope_e4m3).
+    share() lets several sequences begin with the tokens of one.
     width: pages of the longest sequence, by default all.  The attention is dealt out by it, so a table much wider than its sequences is slow: 16
     sequences of 12,000 tokens on 4 key heads, page 64, take 38 us with a width of 188 and 225 with 3,008."""
 
     def __init__(self, sequences: int, pages: int, kv_heads: int, page: int = 64, width: Optional[int] = None, dtype=torch.bfloat16,
                  device="cuda"):
         self.page, self.width = page, pages if width is None else width
-        self.k = torch.zeros((pages, kv_heads, page, 64), dtype=dtype, device=device)
+        self.k = torch.zeros((pages, kv_heads, page, 64), dtype=torch.uint8 if dtype is torch.float8_e4m3fn else dtype, device=device)
         self.v = torch.zeros_like(self.k)
+        self.scales = {}
+        if dtype is torch.float8_e4m3fn:
+            self.k, self.v = self.k.view(dtype), self.v.view(dtype)
+            self.scales = {t: torch.full((pages, kv_heads, page), 127, dtype=torch.uint8, device=device) for t in ("k_scale", "v_scale")}
         self.page_table = torch.full((sequences, self.width), -1, dtype=torch.int32, device=device)
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
         self._free = list(range(pages - 1, -1, -1))
         self._pages: List[List[int]] = [[] for _ in range(sequences)]
         self._length = [0] * sequences
         self._freed = [(0, 0)] * sequences  # (all of a sequence's freed pages lie in [first, end))
+        # shared first tokens: (first sequence, end, pages, tokens), in the sequences' order, and what bsga_prefix_attn takes of them
+        self._shared: List[Tuple[int, int, List[int], int]] = []
+        self._behind = [0] * sequences  # tokens in front of a sequence's own
+        self.prefixes: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None
+        self.behind: Optional[torch.Tensor] = None
 
     def _send(self, values, like: torch.Tensor) -> torch.Tensor:
         return torch.tensor(values, dtype=torch.int32).to(like.device)
+
+    def share(self, b: int, sequences: Sequence[int]) -> None:
+        """The tokens of sequence b become the first ones of `sequences`: neighbours, in order, without tokens (apart from b, which may be one of them and has none
+        of its own any more) and without shared ones.  They are held and read once, and stay until the cache goes.  Their positions begin behind them."""
+        sequences = list(sequences)
+        n, first, end = self._length[b], sequences[0] if sequences else 0, sequences[-1] + 1 if sequences else 0
+        if not sequences or sequences != list(range(first, end)) or first < 0 or end > len(self._length):
+            raise ValueError(f"sequences that share tokens must be neighbours, in order, got {sequences}")
+        if n == 0 or self._behind[b] > 0 or any(page < 0 for page in self._pages[b]):
+            raise ValueError(f"sequence {b} has no tokens of its own to share, begins with shared ones, or some have been freed")
+        if any(self._behind[i] > 0 or (i != b and self._length[i] > 0) for i in sequences):
+            raise ValueError("sequences that are to share tokens must have none yet")
+        self._shared = sorted(self._shared + [(first, end, self._pages[b], n)], key=lambda x: x[:2])
+        self._pages[b], self._length[b] = [], 0
+        for i in sequences:
+            self._behind[i] = n
+        of = {begin: (pages, tokens) for begin, _, pages, tokens in self._shared}
+        starts = self._starts()
+        rows = [of.get(x, ([], 0)) for x in starts[:-1]]  # (between those that share, sequences with nothing in front of them)
+        width = max(len(pages) for pages, _ in rows)
+        self.prefixes = (self._send([pages + [-1] * (width - len(pages)) for pages, _ in rows], self.lengths),
+                         self._send([tokens for _, tokens in rows], self.lengths), self._send(starts, self.lengths))
+        self.behind = self._send(self._behind, self.lengths)
+        self.page_table[b] = -1
+        self.lengths.copy_(torch.tensor(self._length, dtype=torch.int32))
+
+    def _own(self, b: int, lo: int, sinks: int) -> Tuple[int, int]:
+        """The first own token of a window that begins at position lo, and the own tokens among the first `sinks`."""
+        return max(0, lo - self._behind[b]), max(0, min(sinks, lo) - self._behind[b])
 
     def grow(self, counts: Sequence[int]) -> torch.Tensor:
         """Room for counts[b] more tokens of each sequence; returns their slots (int32, those of sequence 0 first), for
@@ -128,7 +168,7 @@ class PagedCache:
             raise
 
     def trim(self, window: Optional[int], sinks: int = 0, frame: int = 1) -> int:
-        """Frees the pages that no later query sees (window = None: none); returns how many."""
+        """Frees the pages that no later query sees (window = None: none); returns how many.  Those of shared tokens stay."""
         if (window is not None and window < 1) or sinks < 0 or frame < 1:
             raise ValueError(f"window must be at least one frame, or None, sinks >= 0 and frame >= 1, got {window}, {sinks} and {frame}")
         if window is None:
@@ -137,8 +177,8 @@ class PagedCache:
         for b, n in enumerate(self._length):
             if n == 0:
                 continue
-            lo = max(0, ((n - 1) // frame + 1 - window) * frame)
-            gone = [i for i in range(-(-min(sinks, lo) // self.page), lo // self.page) if self._pages[b][i] >= 0]
+            lo, kept = self._own(b, max(0, ((self._behind[b] + n - 1) // frame + 1 - window) * frame), sinks)
+            gone = [i for i in range(-(-kept // self.page), lo // self.page) if self._pages[b][i] >= 0]
             if not gone:
                 continue
             for i in gone:
@@ -156,10 +196,41 @@ class PagedCache:
         for b, (first, end) in enumerate(self._freed):
             if first == end:
                 continue
-            lo = 0 if window is None else max(0, (self._length[b] // frame + 1 - window) * frame)
-            kept, near = -(-min(sinks, lo) // self.page), lo // self.page  # pages [0, kept) and from `near` on are seen
+            lo, kept = self._own(b, 0 if window is None else max(0, ((self._behind[b] + self._length[b]) // frame + 1 - window) * frame), sinks)
+            kept, near = -(-kept // self.page), lo // self.page  # pages [0, kept) and from `near` on are seen
             if any(self._pages[b][i] < 0 for part in (range(first, min(kept, end)), range(max(first, near), end)) for i in part):
                 raise ValueError(f"sequence {b} of the cache: tokens that a window of {window} with {sinks} first tokens sees have been freed")
+
+    def load(self, b: int, window: Optional[int] = None, sinks: int = 0, frame: int = 1, n_tokens: int = 0, dtype=torch.bfloat16):
+        """Keys and values [kv_heads, n, 64] of the n tokens of sequence b, shared ones first, head by head, for bsga_window_attn: those that its last
+        n_tokens tokens see.  What none of them sees is not read; tiles of it that the attention reads beside seen tokens hold zeros."""
+        total = self._behind[b] + self._length[b]
+        lo = 0 if window is None else max(0, ((total - n_tokens) // frame + 1 - window) * frame)
+        lo = min(lo, total)
+        first = min(sinks, lo)
+        shape = (self.k.shape[1], total, 64)
+        out = [torch.empty(shape, dtype=dtype if self.scales else self.k.dtype, device=self.k.device) for _ in range(2)]
+        if first < lo:
+            for x in out:
+                x[:, first:min(first + 64, lo)] = 0
+                x[:, max(first, lo - 64):lo] = 0
+        behind = self._behind[b]
+        for begin, end in ((0, first), (lo, total)):
+            for row, start, stop in ((None, 0, behind), (self.page_table[b], behind, total)):
+                x, y = max(begin, start), min(end, stop)
+                if x >= y:
+                    continue
+                if row is None:
+                    row = self.prefixes[0][sum(s <= b for s in self._starts()[:-1]) - 1]
+                B.bsga_cache_load(self.k, self.v, row, y - x, x - start, **self.scales, out=tuple(t[:, x:y] for t in out))
+        return out
+
+    def _starts(self) -> List[int]:
+        starts, at = [], 0
+        for begin, stop, _, _ in self._shared:
+            starts += ([at] if at < begin else []) + [begin]
+            at = stop
+        return starts + [at]
 
 
 def _takes(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor) -> bool:
@@ -185,9 +256,10 @@ class StreamAttention(torch.nn.Module):
     sequence), window of `window` frames of `frame` tokens and the first `sinks` tokens (see bsga_window_attn).
 
     forward(x) takes a whole sequence, with gradients; prefill(x, cache, b) the same for sequence b of an empty cache, and fills it;
-    step(x, cache) one more token for every sequence of the cache.  With frame > 1 that is another function than forward() and prefill(), whose tokens
-    see their whole frame: a token that comes alone sees its own frame up to itself, since the others are not there yet.  There is no way yet to
-    take a whole new frame on a cache."""
+    extend(x, cache, b) more tokens of a sequence that may have some: a new frame, or a prompt in parts; step(x, cache) one more token for every sequence of
+    the cache.  With frame > 1 a step is another function than the others, whose tokens
+    see their whole frame: a token that comes alone sees its own frame up to itself, since the others are not there yet (nor are those of a frame's later parts for its
+    earlier ones).  On a cache in 8 bits all tokens, those of a prompt too, see keys and values as the cache holds them."""
 
     def __init__(self, heads: int = 16, kv_heads: Optional[int] = None, window: Optional[int] = None, sinks: int = 0, frame: int = 1,
                  norm: str = "rms", base: float = 10000.0, dtype=torch.bfloat16, device="cuda", seed: int = 0, eps: float = 1e-6):
@@ -229,7 +301,7 @@ class StreamAttention(torch.nn.Module):
 
     @torch.no_grad()
     def prefill(self, x: torch.Tensor, cache: PagedCache, b: int, positions: Optional[torch.Tensor] = None) -> torch.Tensor:
-        if cache._length[b] != 0:
+        if cache._length[b] != 0 or cache._behind[b] != 0:
             raise ValueError(f"sequence {b} of the cache is not empty")
         N = x.shape[0]
         counts = [0] * len(cache._length)
@@ -237,21 +309,53 @@ class StreamAttention(torch.nn.Module):
         with cache.growing(counts) as slots:
             q, k, v = self._split(self._linear(x, self.w_qkv, self.b_qkv))
             positions = self._places(N, x.device) if positions is None else positions
-            q, k, v = B.bsga_qk_norm_rope(q, k, positions, self.q_weight, self.k_weight, self.q_bias, self.k_bias, v=v, norm=self.norm, eps=self.eps,
-                                          base=self.base)
-            # (what the attention reads in one piece goes into the pages as well; it is normed and turned already)
-            B.bsga_qk_norm_rope(k.transpose(0, 1), k.transpose(0, 1), v=v.transpose(0, 1), norm=None, k_cache=cache.k, v_cache=cache.v, slots=slots)
-            o = B.bsga_window_attn(q, k, v, **self.seen)
-            return self._linear(B.bsga_merge_heads(o) if N > 0 else o.view(0, self.heads * 64), self.w_out, self.b_out)
+            if cache.scales:
+                q, k, v = B.bsga_qk_norm_rope_e4m3(q, k, v, cache.k, cache.v, **cache.scales, slots=slots, positions=positions, **self._norms(), return_rows=True)
+            else:
+                q, k, v = B.bsga_qk_norm_rope(q, k, positions, v=v, **self._norms())
+                # (what the attention reads in one piece goes into the pages as well; it is normed and turned already)
+                B.bsga_qk_norm_rope(k.transpose(0, 1), k.transpose(0, 1), v=v.transpose(0, 1), norm=None, k_cache=cache.k, v_cache=cache.v, slots=slots)
+            return self._out(B.bsga_window_attn(q, k, v, **self.seen))
+
+    def _norms(self):
+        return dict(q_weight=self.q_weight, k_weight=self.k_weight, q_bias=self.q_bias, k_bias=self.k_bias, norm=self.norm, eps=self.eps, base=self.base)
+
+    def _out(self, o: torch.Tensor) -> torch.Tensor:
+        return self._linear(B.bsga_merge_heads(o) if o.shape[1] > 0 else o.view(0, self.heads * 64), self.w_out, self.b_out)
+
+    def _store(self, q, k, v, positions, cache: PagedCache, slots: torch.Tensor) -> torch.Tensor:
+        """Queries normed and turned [heads, N, 64], keys and values on their way into the cache."""
+        if cache.scales:
+            return B.bsga_qk_norm_rope_e4m3(q, k, v, cache.k, cache.v, **cache.scales, slots=slots, positions=positions, **self._norms())[0]
+        return B.bsga_qk_norm_rope(q, k, positions, v=v, **self._norms(), k_cache=cache.k, v_cache=cache.v, slots=slots)[0]
+
+    @torch.no_grad()
+    def extend(self, x: torch.Tensor, cache: PagedCache, b: int, positions: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x [N, heads * 64], the next N tokens of sequence b of the cache, which see those that are there and each other as in forward()."""
+        cache.check_seen(**self.seen)
+        N, n = x.shape[0], cache._behind[b] + cache._length[b]
+        counts = [0] * len(cache._length)
+        counts[b] = N
+        with cache.growing(counts) as slots:
+            q, k, v = self._split(self._linear(x, self.w_qkv, self.b_qkv))
+            positions = self._places(N, x.device) + n if positions is None else positions
+            q = self._store(q, k, v, positions, cache, slots)
+            k, v = cache.load(b, **self.seen, n_tokens=N, dtype=x.dtype)
+            return self._out(B.bsga_window_attn(q, k, v, **self.seen))
 
     @torch.no_grad()
     def step(self, x: torch.Tensor, cache: PagedCache, positions: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x [sequences, heads * 64], one token for each sequence."""
         cache.check_seen(**self.seen)
-        positions = cache.lengths.clone() if positions is None else positions
+        if positions is None:
+            positions = cache.lengths.clone() if cache.behind is None else cache.lengths + cache.behind
         with cache.growing([1] * x.shape[0]) as slots:
             q, k, v = self._split(self._linear(x, self.w_qkv, self.b_qkv))
-            q, _, _ = B.bsga_qk_norm_rope(q, k, positions, self.q_weight, self.k_weight, self.q_bias, self.k_bias, v=v, norm=self.norm, eps=self.eps,
-                                          base=self.base, k_cache=cache.k, v_cache=cache.v, slots=slots)
-            o = B.bsga_paged_attn(q.transpose(0, 1), cache.k, cache.v, cache.page_table, cache.lengths, **self.seen)
+            q = self._store(q, k, v, positions, cache, slots).transpose(0, 1)
+            if cache.prefixes is not None:
+                o = B.bsga_prefix_attn(q, cache.k, cache.v, cache.page_table, cache.lengths, *cache.prefixes, **cache.scales, **self.seen)
+            elif cache.scales:
+                o = B.bsga_paged_attn_e4m3(q, cache.k, cache.v, **cache.scales, page_table=cache.page_table, lengths=cache.lengths, **self.seen)
+            else:
+                o = B.bsga_paged_attn(q, cache.k, cache.v, cache.page_table, cache.lengths, **self.seen)
             return self._linear(o.view(x.shape[0], -1), self.w_out, self.b_out)
