@@ -445,6 +445,7 @@ int bsga_paged_attn_e4m3(const void* q, int64_t q_batch, int64_t q_head, const v
  *   prefix_table  [prefixes, prefix_width] int32, likewise;  prefix_lengths [prefixes] int32, clamped into [0, prefix_width * page]
  *   starts     [prefixes + 1] int32, not decreasing: sequences starts[g] .. starts[g + 1] - 1 have prefix g, those in front of starts[0] and from starts[prefixes] on none;
  *              clamped into [0, batch].  Where it decreases, results are undefined (but nothing outside the tensors is read or written).
+ *   softmax_scale  at least 2^-100
  *   workspace  bsga_prefix_attn_workspace_bytes(...) bytes, 16-byte aligned; overwritten
  * Table entries and lengths that do not fit are clamped as there.  A key that a query does not see has no part in its result.  The same bits every time.
  */

@@ -610,7 +610,8 @@ int64_t shape_of(PrefixArgs& a, int dtype, int cache_dtype) {
     most = smaller(most, seen);
     own = smaller(own, seen);
   }
-  const int64_t units = larger(ceil_div(int64_t(a.batch) * a.group, a.queries), int64_t(1)) * a.pages.kv_heads;
+  const int64_t tiles = larger(ceil_div(int64_t(a.batch) * a.group, a.queries), smaller(int64_t(a.prefixes), int64_t(a.batch)));  // about
+  const int64_t units = larger(tiles, int64_t(1)) * a.pages.kv_heads;
   cut(most, units, keys, a.pages.page, a.stretch, a.splits, a.queries == kHeads ? 0 : units == a.pages.kv_heads ? 256 : 512);
   cut(own, int64_t(a.batch) * a.pages.kv_heads * a.head_blocks, keys, a.pages.page, a.own_stretch, a.own_splits);
   a.tiles = a.prefixes > 0 ? static_cast<int>(tiles_of(a, a.queries)) : 0;
@@ -695,7 +696,9 @@ int bsga_prefix_attn(const void* q, int64_t q_batch, int64_t q_head, const void*
   if (head_dim != 64) return fail(BSGA_ERR_UNSUPPORTED, "%s: head_dim must be 64, got %d", fn, head_dim);
   if (int rc = check_sizes(fn, dtype, cache_dtype, batch, heads, kv_heads, table_width, prefixes, prefix_width, n_pages, page, frame, window, sinks, a))
     return rc;
-  if (!(softmax_scale > 0.0f) || !isfinite(softmax_scale)) return fail(BSGA_ERR_INVALID_ARG, "%s: softmax_scale must be finite and > 0", fn);
+  // (a value's exponent is divided by it, see over_prefix_wide)
+  if (!(softmax_scale >= 0x1p-100f) || !isfinite(softmax_scale))
+    return fail(BSGA_ERR_INVALID_ARG, "%s: softmax_scale must be finite and at least 2^-100", fn);
   if (batch == 0) return BSGA_OK;
   if (int rc = check_view(fn, "q", q, q_batch, q_head, dtype == BSGA_BF16 ? 2 : 4, a.q)) return rc;
   const bool any = a.table_width > 0 || a.prefixes > 0;

@@ -105,6 +105,9 @@ def test_prefixes(B):  # noqa: F811
     for name in ("pt", "pl", "starts"):
         assert _prefix(B, **{name: None}) == 1 and "non-null" in _err(B)
     assert _prefix(B, b=65535, h=65535, kh=1) == 2 and "too many" in _err(B)
+    assert _prefix(B, b=65535, width=1 << 20, page=1, pages=1 << 30, h=16, kh=16) == 2 and "one launch" in _err(B)
+    for scale in (2.0 ** -101, 1e-45, float("inf")):
+        assert _prefix(B, scale=scale) == 1 and "softmax_scale" in _err(B)
 
 
 def test_workspaces(B):  # noqa: F811

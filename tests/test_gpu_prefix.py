@@ -99,6 +99,60 @@ def test_logits_of_any_size(B, cache, dtype, gain):
     check_all(o, lse, args[0], whole)
 
 
+@pytest.mark.parametrize("cache,dtype", [("bf16", "bf16"), ("e4m3", "bf16"), ("fp32", "fp32")])
+@pytest.mark.parametrize("scale", [2.0 ** -100, 2.0 ** -20, 3.0])
+@pytest.mark.parametrize("sequences", [4, 30, 100])
+def test_scales_of_logits(B, cache, dtype, scale, sequences):
+    args, scales, whole = draw([500], [0, sequences], [i % 7 for i in range(sequences)], 2, 2, 32, cache, dtype)
+    o, lse = B.bsga_prefix_attn(*args, **scales, return_lse=True, softmax_scale=scale)
+    for b, (k, v) in enumerate(whole):
+        check(o[b][:, None], lse[b][:, None], args[0][b][:, None], k, v, torch.ones((1, k.shape[1]), dtype=torch.bool, device="cuda"), scale)
+
+
+@pytest.mark.parametrize("sequences", [4, 30, 100])
+@pytest.mark.parametrize("byte", [63, 207])
+def test_values_of_any_size(B, byte, sequences):
+    """Rows whose values have the smallest and the largest scale that is written, beside others: what each stands for."""
+    args, scales, whole = draw([700], [0, sequences], [i % 5 for i in range(sequences)], 2, 2, 16, "e4m3", "bf16")
+    vs = scales["v_scale"]
+    vs.masked_fill_(vs != 255, byte)
+    some = torch.rand(vs.shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)) < 0.2
+    mixed = torch.where(some & (vs != 255), byte + (8 if byte < 127 else -8), vs).to(torch.uint8)
+    scales["v_scale"] = mixed
+    o = B.bsga_prefix_attn(*args, **scales)
+    kc, vc, table, n, pt = args[1], args[2], args[3], args[4].tolist(), args[5]
+    for b in range(sequences):
+        rows = [torch.cat([values(c[t].view(torch.uint8), s[t]).transpose(0, 1).reshape(2, -1, 64)[:, :m] for t, m in
+                           ((pt[0, :44].long(), 700), (table[b, :-(-n[b] // 16)].long(), n[b]))], 1) for c, s in ((kc, scales["k_scale"]), (vc, mixed))]
+        f = 2.0 ** (127 - byte)
+        check((o[b].double() * f).float().bfloat16()[:, None], None, args[0][b][:, None], rows[0], rows[1] * f,
+              torch.ones((1, rows[0].shape[1]), dtype=torch.bool, device="cuda"))
+
+
+def test_sums_that_grow(B):
+    """Logits that rise along the prefix, far beyond the first ones, and many keys of nearly one logit: the reference follows."""
+    for cache in ("bf16", "e4m3"):
+        for sequences in (4, 30, 100):
+            args, scales, whole = draw([9000], [0, sequences], [1] * sequences, 1, 1, 64, cache, "bf16")
+            pages = args[5][0, :-(-9000 // 64)].long()
+            up = torch.arange(pages.numel(), device="cuda")
+            if cache == "e4m3":  # a power of two every few pages, and values of small scales
+                scales["k_scale"][pages] = (112 + up // 14).clamp(max=130).to(torch.uint8)[:, None, None].expand_as(scales["k_scale"][pages])
+                scales["v_scale"][pages] = 90
+                k, v = (values(c[pages].view(torch.uint8), s[pages]).transpose(0, 1).reshape(1, -1, 64)[:, :9000] for c, s in
+                        ((args[1], scales["k_scale"]), (args[2], scales["v_scale"])))
+                f = 2.0 ** 37
+            else:
+                args[1][pages] *= (0.05 * up)[:, None, None, None].to(args[1].dtype)
+                k, v = (c[pages].transpose(0, 1).reshape(1, -1, 64)[:, :9000] for c in (args[1], args[2]))
+                f = 1.0
+            args[4].zero_()
+            o, lse = B.bsga_prefix_attn(*args, **scales, return_lse=True)
+            for b in range(sequences):
+                check((o[b].double() * f).float().bfloat16()[:, None], lse[b][:, None], args[0][b][:, None], k, v * f,
+                      torch.ones((1, 9000), dtype=torch.bool, device="cuda"))
+
+
 @pytest.mark.parametrize("queries_of_a_head", [3, 60, 300])
 @pytest.mark.parametrize("cache,dtype", [("bf16", "bf16"), ("e4m3", "bf16"), ("fp32", "fp32")])
 def test_the_rows_it_sees_decide(B, cache, dtype, queries_of_a_head):
