@@ -47,7 +47,7 @@ struct Ops16<__bf16, __bf16> {
   struct Raw {
     bf16x8 a[4];
   };
-  static __device__ __forceinline__ void fetch(const unsigned char* tile, int lane, Raw& raw) {
+  static __device__ __forceinline__ void fetch(const unsigned char* tile, const unsigned*, int lane, Raw& raw) {
     const int m = (lane & 15) >> 2, j = lane & 3, q = lane >> 4;
 #pragma unroll
     for (int db = 0; db < 4; ++db) {
@@ -62,7 +62,7 @@ struct Ops16<__bf16, __bf16> {
     }
   }
   // o += V^T P^T: the weights' products in w[block][r], of keys 16 block + 4 q + r
-  static __device__ __forceinline__ void update(const Raw& raw, const unsigned*, int, const f32x4 (&w)[kBlocks], f32x4 (&o)[4]) {
+  static __device__ __forceinline__ void update(const Raw& raw, const f32x4 (&w)[kBlocks], f32x4 (&o)[4]) {
     const bf16x8 b = __builtin_bit_cast(
         bf16x8, u32x4{pack_bf16(w[0][0], w[0][1]), pack_bf16(w[0][2], w[0][3]), pack_bf16(w[1][0], w[1][1]), pack_bf16(w[1][2], w[1][3])});
 #pragma unroll
@@ -104,7 +104,7 @@ struct Ops16<float, float> {
   struct Raw {
     float a[4][4];
   };
-  static __device__ __forceinline__ void fetch(const unsigned char* tile, int lane, Raw& raw) {
+  static __device__ __forceinline__ void fetch(const unsigned char* tile, const unsigned*, int lane, Raw& raw) {
     const int q = lane >> 4;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
@@ -114,7 +114,7 @@ struct Ops16<float, float> {
         raw.a[db][e] = *LDS_PTR(float, tile + r * 256 + (((d >> 2) ^ swizzle_v(r)) << 4) + (d & 3) * 4);
       }
   }
-  static __device__ __forceinline__ void update(const Raw& raw, const unsigned*, int, const f32x4 (&w)[kBlocks], f32x4 (&o)[4]) {
+  static __device__ __forceinline__ void update(const Raw& raw, const f32x4 (&w)[kBlocks], f32x4 (&o)[4]) {
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -146,19 +146,21 @@ struct Ops16E4m3 {
   }
   struct Raw {
     u32x2 a[2][4];
+    u32x4 scale[4];  // of the keys 16 block + 4 q + r
   };
-  static __device__ __forceinline__ void fetch(const unsigned char* tile, int lane, Raw& raw) {
+  static __device__ __forceinline__ void fetch(const unsigned char* tile, const unsigned* scales, int lane, Raw& raw) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int db = 0; db < 4; ++db) raw.a[h][db] = column(tile, lane, h, db);
+#pragma unroll
+    for (int blk = 0; blk < 4; ++blk) raw.scale[blk] = *LDS_PTR(u32x4, scales + 16 * blk + 4 * (lane >> 4));
   }
-  // the weights of keys 16 block + 4 q + r times their values' scales
-  static __device__ __forceinline__ f32x4 scaled(const unsigned* scales, int lane, int block, const f32x4& w) {
-    const u32x4 b = *LDS_PTR(u32x4, scales + 16 * block + 4 * (lane >> 4));
+  // weights times their values' scales
+  static __device__ __forceinline__ f32x4 scaled(const u32x4& scale, const f32x4& w) {
     f32x4 y;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) y[r] = w[r] * scale_of(b[r]);
+    for (int r = 0; r < 4; ++r) y[r] = w[r] * scale_of(scale[r]);
     return y;
   }
 };
@@ -181,10 +183,10 @@ struct Ops16<__bf16, E4m3> : Ops16E4m3 {
       a[e] = __builtin_bit_cast(bf16x8, u32x4{y0[0], y0[1], y1[0], y1[1]});
     }
   }
-  static __device__ __forceinline__ void update(const Raw& raw, const unsigned* scales, int lane, const f32x4 (&w)[kBlocks], f32x4 (&o)[4]) {
+  static __device__ __forceinline__ void update(const Raw& raw, const f32x4 (&w)[kBlocks], f32x4 (&o)[4]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const f32x4 w0 = scaled(scales, lane, 2 * h, w[2 * h]), w1 = scaled(scales, lane, 2 * h + 1, w[2 * h + 1]);
+      const f32x4 w0 = scaled(raw.scale[2 * h], w[2 * h]), w1 = scaled(raw.scale[2 * h + 1], w[2 * h + 1]);
       const bf16x8 b = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(w0[0], w0[1]), pack_bf16(w0[2], w0[3]), pack_bf16(w1[0], w1[1]), pack_bf16(w1[2], w1[3])});
 #pragma unroll
       for (int db = 0; db < 4; ++db) {
@@ -219,10 +221,10 @@ struct Ops16<float, E4m3> : Ops16E4m3 {
       for (int i = 0; i < 4; ++i) a[4 * e + i] = y[i] * f;
     }
   }
-  static __device__ __forceinline__ void update(const Raw& raw, const unsigned* scales, int lane, const f32x4 (&w)[kBlocks], f32x4 (&o)[4]) {
+  static __device__ __forceinline__ void update(const Raw& raw, const f32x4 (&w)[kBlocks], f32x4 (&o)[4]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const f32x4 w0 = scaled(scales, lane, 2 * h, w[2 * h]), w1 = scaled(scales, lane, 2 * h + 1, w[2 * h + 1]);
+      const f32x4 w0 = scaled(raw.scale[2 * h], w[2 * h]), w1 = scaled(raw.scale[2 * h + 1], w[2 * h + 1]);
 #pragma unroll
       for (int db = 0; db < 4; ++db) {
         const u32x2 x = raw.a[h][db];
@@ -518,7 +520,12 @@ __device__ __forceinline__ void go_over(const Pages& a, const Stretch& st, const
       for (int e = 0; e < P::kSteps; ++e) w[blk] = P::product(ka[e], qf[e], w[blk]);
     }
     typename P::Raw raw;
-    if constexpr (!MASKED) P::fetch(kt + kPiece<P>, lane, raw);
+    constexpr bool kEarly = STEADY && !MASKED;
+    if constexpr (!MASKED) P::fetch(kt + kPiece<P>, scales + 64, lane, raw);
+    if constexpr (kEarly) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // all of the piece is in registers: the buffer is free
+      if (p + 2 * kWaves < pieces) issue(p + 2 * kWaves, buf);
+    }
     if (MASKED || left < P::kKeys) {
 #pragma unroll
       for (int blk = 0; blk < P::kBlocks; ++blk)
@@ -584,10 +591,10 @@ __device__ __forceinline__ void go_over(const Pages& a, const Stretch& st, const
     }
     if constexpr (MASKED) {
       leave_bad_out<P>(load, kt, [&](int i) { return seen(st.key(st.x0 + p * P::kKeys + i)); }, w, o);
-      P::fetch(kt + kPiece<P>, lane, raw);
+      P::fetch(kt + kPiece<P>, scales + 64, lane, raw);
     }
-    P::update(raw, scales + 64, lane, w, o);
-    if (p + 2 * kWaves < pieces) {
+    P::update(raw, w, o);
+    if (!kEarly && p + 2 * kWaves < pieces) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the operands are in registers: the buffer is free
       issue(p + 2 * kWaves, buf);
     }
