@@ -6,7 +6,7 @@ Usage (from the repository root, after the rocprofv3 runs listed in each summary
     python -m paper_2509_07120_amd.profile_summary traffic <dir FETCH_SIZE run> <dir WRITE_SIZE run> <dir TCC run>
     python -m paper_2509_07120_amd.profile_summary pipes   <dir of counter run A> <dir of counter run B> ...
     python -m paper_2509_07120_amd.profile_summary topk    <dir TCC run at rho 0.9> <dir pipe-counter run at rho 0.9>
-    python -m paper_2509_07120_amd.profile_summary case    <name in perf/cases.py or perf/operators.py> <dir of --kernel-trace --stats run> <dir of counter run>
+    python -m paper_2509_07120_amd.profile_summary case    <name in perf/cases.py, perf/operators.py or perf/more_operators.py> <dir of --kernel-trace --stats run> <dir of counter run>
 
 Each sub-command reads the `*_kernel_stats.csv`, `*_kernel_trace.csv` or `*_counter_collection.csv`
 files rocprofv3 wrote with `--output-format csv`, prints what it found, and rewrites the matching
@@ -333,7 +333,8 @@ def cmd_case(name: str, d_stats: str, d_pipes: str) -> None:
     def label(n):  # kernels over __bf16 keep their mangled names, or get a wrong one
         hit = re.search(r"_ZN4bsga12_GLOBAL__N_1\d+(\w+?_kernel)I(\w*?)E(?:E?v|$)", n)
         if hit:
-            return f"{hit.group(1)}<{', '.join('bf16' if a == 'DF16b' else a[2:-1] for a in re.findall(r'DF16b|L.[0-9]+E', hit.group(2) + 'E'))}>"
+            types = {"DF16b": "bf16", "NS0_4E4m3E": "e4m3", "f": "float", "h": "e4m3"}
+            return f"{hit.group(1)}<{', '.join(types.get(a) or a[2:-1] for a in re.findall(r'DF16b|NS0_4E4m3E|L.[0-9]+E|[fh]', hit.group(2) + 'E'))}>"
         hit = re.search(r"bsga::.*?(\w+_kernel(?:<[^>]*>)?)\(", n)
         return hit.group(1).replace("<bool _Accum, bool, E>", "<bf16>") if hit else None
 
@@ -348,8 +349,10 @@ def cmd_case(name: str, d_stats: str, d_pipes: str) -> None:
     times = kernels((r["Kernel_Name"], (int(r["End_Timestamp"]) - int(r["Start_Timestamp"])) / 1e3) for r in trace)
     pipes = kernels((x["name"], x) for x in dispatches(d_pipes))
     counters = "SQ_VALU_MFMA_BUSY_CYCLES SQ_BUSY_CU_CYCLES SQ_LDS_IDX_ACTIVE SQ_WAVE_CYCLES SQ_WAIT_ANY SQ_WAIT_INST_ANY SQ_ACTIVE_INST_VALU SQ_LDS_BANK_CONFLICT"
-    listed = os.path.join(os.path.dirname(PROFILES), "perf", "operators.py")
-    module = "perf.operators as C; C.own = True" if f'"{name}"' in open(listed).read() else "perf.cases as C"
+    module = "perf.cases as C"
+    for of in ("operators", "more_operators"):
+        if f'"{name}"' in open(os.path.join(ROOT, "perf", of + ".py")).read():
+            module = f"perf.{of} as C; C.own = True"
     run = (f"python3 -c \"import sys; sys.path.insert(0, '<repo>'); import {module}; c = [x for x in C.listed() if x['name'] == '{name}'][0]; "
            f"s = C.prepare(c, 1); [C.run(s) for _ in range({passes})]; C.torch.cuda.synchronize()\"")
     path = os.path.join(PROFILES, f"{name}_kernels.md")
