@@ -447,6 +447,7 @@ int bsga_paged_attn_e4m3(const void* q, int64_t q_batch, int64_t q_head, const v
  *              clamped into [0, batch].  Where it decreases, results are undefined (but nothing outside the tensors is read or written).
  *   softmax_scale  at least 2^-100
  *   workspace  bsga_prefix_attn_workspace_bytes(...) bytes, 16-byte aligned; overwritten
+ * One launch: BSGA_ERR_UNSUPPORTED where it would take 2^24 workgroups or more (tens of thousands of sequences with several key heads and long tables).
  * Table entries and lengths that do not fit are clamped as there.  A key that a query does not see has no part in its result.  The same bits every time.
  */
 size_t bsga_prefix_attn_workspace_bytes(int dtype, int cache_dtype, int64_t batch, int heads, int kv_heads, int64_t table_width, int64_t prefixes,
