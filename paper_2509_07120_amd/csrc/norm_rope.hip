@@ -10,8 +10,10 @@
 // computed once for them.  Angles are exact: base^(-2j/W) / 2 pi is a 64-bit fraction of a turn, and the product with the position
 // modulo 2^64 is the turn's fraction, whatever the position's size; fp32 would be off by 0.1 at position 10^6.
 //
-// Into a cache in 8 bits (e4m3.h) the row goes from the 32 bits in which it was normed and turned, in one rounding: the largest magnitude is one more
-// pair of quad permutations, and neighbouring lanes swap halves so that each writes 16 bytes.
+// Into a cache in 8 bits (e4m3.h) the row goes from the 32 bits in which it was normed and turned, in one rounding: the largest magnitude is one more pair of
+// quad permutations, and neighbouring lanes swap halves so that each writes 16 bytes.  100 frames, with the rows returned as they are read back (1.97 GB): 395
+// us, 5.0 TB/s. Keys normed and turned in 64 bits, so that no number at a border between two codes goes to the other side than the definition's: 449 us; 32
+// bits stay, a code is half a step and 2^-22 from the number at most either way.
 #include "bf16_tile.h"
 #include "bsga_internal.h"
 #include "e4m3.h"
