@@ -419,7 +419,8 @@ int bsga_qk_norm_rope_e4m3(const void* q, const void* k, const void* v, int64_t 
  * Tokens [first, first + n_tokens) of one sequence out of the pages of a cache, head by head, e.g. for bsga_window_attn.
  *   cache_dtype  BSGA_E4M3 (with k_scale and v_scale), or dtype: rows are moved as they are
  *   pages      [table_width] int32, the sequence's row of a page table; tokens whose page lies outside [0, n_pages) are zeros
- *   k_out, v_out  [kv_heads, n_tokens, 64] of type dtype, heads k_head and v_head elements apart (multiples of 16 bytes), must not overlap the caches
+ *   k_out, v_out  [kv_heads, n_tokens, 64] of type dtype, heads k_head and v_head elements apart (multiples of 16 bytes, a head's rows at
+ *              least), must not overlap the caches
  */
 int bsga_cache_load(const void* k_cache, const void* v_cache, const uint8_t* k_scale, const uint8_t* v_scale, int cache_dtype, int64_t n_pages, int page,
                     int kv_heads, int head_dim, const int32_t* pages, int64_t table_width, int64_t first, int64_t n_tokens, int dtype, void* k_out,

@@ -1003,7 +1003,7 @@ def bsga_qk_norm_rope_e4m3(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.
         k_rows, v_rows = k.new_empty((K, N, d)), k.new_empty((K, N, d))
     _check(lib.bsga_qk_norm_rope_e4m3(_ptr(q), k.data_ptr(), v.data_ptr(), qt, qh, kt, kh, vt, vh, code, N, H, K, d, kind, eps, qw, qb, kw, kb, where, axes, base,
                                       slots.data_ptr(), pages, page, _ptr(q_out), _ptr(k_rows), _ptr(v_rows), k_cache.data_ptr(),
-                                      v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _stream(k)))
+                                      v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _stream_here(k)))
     return q_out, k_rows, v_rows
 
 
@@ -1041,8 +1041,26 @@ def bsga_cache_load(k_cache: torch.Tensor, v_cache: torch.Tensor, pages: torch.T
             if t.shape != (K, n_tokens, d) or (n_tokens > 0 and (t.stride(2) != 1 or (n_tokens > 1 and t.stride(1) != d))):
                 raise ValueError(f"{name} must be {(K, n_tokens, d)}, each head's tokens one after the other")
     _check(lib.bsga_cache_load(_ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), code, n_pages, page, K, d, _ptr(pages), pages.shape[0], first,
-                               n_tokens, BSGA_BF16 if dtype == torch.bfloat16 else BSGA_FP32, _ptr(k), _ptr(v), k.stride(0), v.stride(0), _stream(k_cache)))
+                               n_tokens, BSGA_BF16 if dtype == torch.bfloat16 else BSGA_FP32, _ptr(k), _ptr(v), k.stride(0), v.stride(0), _stream_here(k_cache)))
     return k, v
+
+
+# Kernels go to the current device's default stream where its handle is 0: tensors of another device would be read from there.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _stream_here(t: torch.Tensor) -> int:
+    """The current stream of t's device, which must be the current one."""
+    if t.get_device() != _current_device():
+        raise ValueError(f"the tensors must be on the current device, got {t.device} (use torch.cuda.device)")
+    return _stream(t)
+
+
+def _scratch(workspace: torch.Tensor, at: int) -> int:
+    """Bytes of a caller's workspace on device `at`."""
+    if not workspace.is_cuda or workspace.get_device() != at or not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous and on the tensors' device")
+    return workspace.numel() * workspace.element_size()
 
 
 def _queries(q: torch.Tensor) -> Tuple[int, int]:
@@ -1096,10 +1114,10 @@ def bsga_paged_attn_e4m3(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
         if nbytes > 0:
             workspace = q.new_empty(nbytes, dtype=torch.uint8)
     else:
-        nbytes = workspace.numel() * workspace.element_size()
+        nbytes = _scratch(workspace, at)
     _check(lib.bsga_paged_attn_e4m3(q.data_ptr(), *strides, k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), code, B, H, K, d, table,
                                     width, many, pages, page, 1.0 / math.sqrt(d) if softmax_scale is None else float(softmax_scale), *seen, out.data_ptr(),
-                                    _ptr(lse), _ptr(workspace), nbytes, _stream(q)))
+                                    _ptr(lse), _ptr(workspace), nbytes, _stream_here(q)))
     return (out, lse) if return_lse else out
 
 
@@ -1130,8 +1148,8 @@ def bsga_prefix_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
         if nbytes > 0:
             workspace = q.new_empty(nbytes, dtype=torch.uint8)
     else:
-        nbytes = workspace.numel() * workspace.element_size()
+        nbytes = _scratch(workspace, at)
     _check(lib.bsga_prefix_attn(q.data_ptr(), *strides, k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), code, kind, B, H, K, d, table, width,
                                 many, prefix, prefix_width, long, begin, G, pages, page, 1.0 / math.sqrt(d) if softmax_scale is None else float(softmax_scale),
-                                *seen, out.data_ptr(), _ptr(lse), _ptr(workspace), nbytes, _stream(q)))
+                                *seen, out.data_ptr(), _ptr(lse), _ptr(workspace), nbytes, _stream_here(q)))
     return (out, lse) if return_lse else out

@@ -105,6 +105,7 @@ extern "C" int bsga_cache_load(const void* k_cache, const void* v_cache, const u
   for (int t = 0; t < 2; ++t) {
     if (!aligned16(cache[t]) || !aligned16(out[t])) return fail(BSGA_ERR_INVALID_ARG, "%s: caches and outputs must be 16-byte aligned", fn);
     if (!whole_stride(head[t], size)) return fail(BSGA_ERR_INVALID_ARG, "%s: strides of the heads must be multiples of 16 bytes and not negative", fn);
+    if (kv_heads > 1 && head[t] < n_tokens * 64) return fail(BSGA_ERR_INVALID_ARG, "%s: the outputs' heads must not overlap", fn);
     a.cache[t] = static_cast<const unsigned char*>(cache[t]);
     a.scale[t] = scale[t];
     a.out[t] = static_cast<unsigned char*>(out[t]);

@@ -48,6 +48,7 @@ def test_reading_back(B):  # noqa: F811
     assert call(ks=None) == 1 and call(vs=None) == 1 and "scale" in _err(B)
     assert call(k=A + 8) == 1 and call(vo=A + 8) == 1 and "aligned" in _err(B)
     assert call(kst=60) == 1 and call(vst=-64) == 1 and "strides" in _err(B)
+    assert call(kst=6336) == 1 and call(vst=0) == 1 and "overlap" in _err(B)
     assert call(n=0) == 0 and call(first=160, n=0) == 0
 
 
@@ -182,3 +183,31 @@ def test_tensors(B):  # noqa: F811
                             (dict(st=t((3,), torch.int64), **scales), TypeError, "starts"), (dict(window=0, **scales), ValueError, "window")):
         with pytest.raises(error, match=text):
             prefix(**kw)
+
+
+def test_another_device_and_workspaces(B, monkeypatch):  # noqa: F811
+    t = _OnDevice
+    c, s, i, x = t((20, 2, 16, 64), E4M3), t((20, 2, 16), torch.uint8), lambda *shape: t(shape, torch.int32), t((3, 2, 64))  # noqa: E731
+
+    def store():
+        B.bsga_qk_norm_rope_e4m3(x, x, x, c, c, s, s, i(3))
+
+    def load():
+        B.bsga_cache_load(c, c, i(5), 10, 0, s, s)
+
+    def paged(**kw):
+        B.bsga_paged_attn_e4m3(t((3, 4, 64)), c, c, s, s, i(3, 10), i(3), **kw)
+
+    def prefix(**kw):
+        B.bsga_prefix_attn(t((3, 4, 64)), c, c, i(3, 10), i(3), i(2, 5), i(2), i(3), s, s, **kw)
+
+    for call in (paged, prefix):
+        scattered = t((1 << 10, 1 << 10), torch.uint8).t()
+        scattered.index_ = 0
+        for workspace in (torch.empty(1 << 20, dtype=torch.uint8), t((1 << 20,), torch.uint8, index=1), scattered):
+            with pytest.raises(ValueError, match="workspace must"):
+                call(workspace=workspace)
+    monkeypatch.setattr(B.binding, "_current_device", lambda: 1)
+    for call in (store, load, paged, prefix):
+        with pytest.raises(ValueError, match="current device"):
+            call()
