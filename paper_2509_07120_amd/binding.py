@@ -10,6 +10,7 @@ exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from typing import Optional, Tuple
@@ -1063,6 +1064,17 @@ def _scratch(workspace: torch.Tensor, at: int) -> int:
     return workspace.numel() * workspace.element_size()
 
 
+# (what a step's sizes ask for is the same from step to step)
+@functools.lru_cache(maxsize=1024)
+def _paged_bytes(*sizes: int) -> int:
+    return lib.bsga_paged_attn_e4m3_workspace_bytes(*sizes)
+
+
+@functools.lru_cache(maxsize=1024)
+def _prefix_bytes(*sizes: int) -> int:
+    return lib.bsga_prefix_attn_workspace_bytes(*sizes)
+
+
 def _queries(q: torch.Tensor) -> Tuple[int, int]:
     """Strides of the sequences and heads of q [batch, heads, 64], whose rows are contiguous."""
     if not q.is_cuda:
@@ -1110,7 +1122,7 @@ def bsga_paged_attn_e4m3(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.
     out = q.new_empty((B, H, d))
     lse = q.new_empty((B, H), dtype=torch.float32) if return_lse else None
     if workspace is None:
-        nbytes = lib.bsga_paged_attn_e4m3_workspace_bytes(code, B, H, K, width, pages, page, *seen)
+        nbytes = _paged_bytes(code, B, H, K, width, pages, page, *seen)
         if nbytes > 0:
             workspace = q.new_empty(nbytes, dtype=torch.uint8)
     else:
@@ -1144,7 +1156,7 @@ def bsga_prefix_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     out = q.new_empty((B, H, d))
     lse = q.new_empty((B, H), dtype=torch.float32) if return_lse else None
     if workspace is None:
-        nbytes = lib.bsga_prefix_attn_workspace_bytes(code, kind, B, H, K, width, G, prefix_width, pages, page, *seen)
+        nbytes = _prefix_bytes(code, kind, B, H, K, width, G, prefix_width, pages, page, *seen)
         if nbytes > 0:
             workspace = q.new_empty(nbytes, dtype=torch.uint8)
     else:
