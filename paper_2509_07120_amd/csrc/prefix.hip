@@ -609,9 +609,9 @@ int64_t tiles_of(const PrefixArgs& a, int tile) {
 }
 
 // Tiles of 32 and 64 queries take so long over a piece that a workgroup more than the chip holds is a round more, and what they leave for the join counts.  If one tile
-// reads a key head's keys, one workgroup to a CU does, beside those of the own keys; otherwise all places are taken.  256 / 384 / 512 / 1024 workgroups, us:
-// 64 sequences of 16 heads on 100 frames, 2,000 own tokens at most, 167 / 169 / 176 / 196, in 8 bits with one own token 108 / 118 / 118 / 134; 8 of 16 heads to 2
-// 28 / 34 / 37 / 45; but with more tiles, 64 of 16 heads to 4, 104 / 79 / 70 / 81, 128 of them in 8 bits 189 / 137 / 115 / 120.
+// reads a key head's keys, one workgroup to a CU does, beside those of the own keys; otherwise all places are taken, unless that leaves less than 2,048 keys to each.
+// 256 / 384 / 512 / 1024 workgroups, us: 64 sequences of 16 heads on 100 frames, 2,000 own tokens at most, 152 / 157 / 158 / 163, 8 of 16 heads to 2 24 / 27 / 27 / 33; with more
+// tiles, 64 of 16 heads to 4, 84 / 81 / 70 / 82, 128 of them in 8 bits 144 / 136 / 116 / 121; 128 of 8 heads on 20, 40 and 60 frames 35 / 39 / 41, 52 / 55 / 57, 66 / 65 / 67.
 // Returns the workgroups of the launch.
 int64_t shape_of(PrefixArgs& a, int dtype, int cache_dtype) {
   const int keys = keys_of_piece(dtype, cache_dtype);
@@ -625,7 +625,8 @@ int64_t shape_of(PrefixArgs& a, int dtype, int cache_dtype) {
   }
   const int64_t tiles = larger(ceil_div(int64_t(a.batch) * a.group, a.queries), smaller(int64_t(a.prefixes), int64_t(a.batch)));  // about
   const int64_t units = larger(tiles, int64_t(1)) * a.pages.kv_heads;
-  cut(most, units, keys, a.pages.page, a.stretch, a.splits, a.queries == kHeads ? 0 : units == a.pages.kv_heads ? 256 : 512);
+  const int64_t places = units == a.pages.kv_heads || most * units < 512 * 2048 ? 256 : 512;
+  cut(most, units, keys, a.pages.page, a.stretch, a.splits, a.queries == kHeads ? 0 : places);
   cut(own, int64_t(a.batch) * a.pages.kv_heads * a.head_blocks, keys, a.pages.page, a.own_stretch, a.own_splits);
   a.tiles = a.prefixes > 0 ? static_cast<int>(tiles_of(a, a.queries)) : 0;
   const int64_t blocks = 8 * ceil_div(int64_t(a.pages.kv_heads) * a.splits, 8) * a.tiles;
