@@ -25,6 +25,7 @@ struct PagedArgs {
   float* lse;                         // [batch, heads] or null
   float *part, *part_lse;             // with stretches: [splits][batch, heads, 64] and [splits][batch, heads]
   int batch, heads, group, head_blocks, table_width, frame, window, sinks, splits, stretch;
+  int dealt;                          // whether the grid is one row, see attend()
   float scale_log2;
 };
 
@@ -37,8 +38,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_kernel(const PagedArgs a
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, q = lane >> 4;
-  const int b = blockIdx.z, split = blockIdx.x;
-  const int hk = blockIdx.y / a.head_blocks, hb = blockIdx.y - hk * a.head_blocks;
+  int b = blockIdx.z, split = blockIdx.x, of = blockIdx.y;
+  if (a.dealt) {
+    const int heads_of = a.pages.kv_heads * a.head_blocks, turn = blockIdx.x >> 3, eight = turn / heads_of, pair = eight * 8 + ((blockIdx.x - eight) & 7);
+    of = turn % heads_of, split = pair / a.batch, b = pair % a.batch;
+    if (split >= a.splits) return;
+  }
+  const int hk = of / a.head_blocks, hb = of - hk * a.head_blocks;
   const int heads = min(kHeads, a.group - hb * kHeads);       // query heads of this workgroup,
   const int h0 = hk * a.group + hb * kHeads;                  // the first of them
   const int64_t rows = int64_t(a.batch) * a.heads, row0 = int64_t(b) * a.heads + h0;
@@ -154,7 +160,13 @@ int attend(const char* fn, bool coded, const void* q, int64_t q_batch, int64_t q
   a.part = static_cast<float*>(workspace);
   a.part_lse = a.part + int64_t(a.splits) * rows * 64;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const dim3 grid(static_cast<unsigned>(a.splits), static_cast<unsigned>(kv_heads * a.head_blocks), static_cast<unsigned>(batch));
+  // Workgroup w runs on XCD w % 8.  From four sequences on, first stretches, which more of them have, come first, and each sequence's and each number's stretches are
+  // dealt out to all XCDs; a stretch's heads, which read the same pages, follow each other on one.  Against a row of stretches for each head and sequence, us in bf16
+  // and 8 bits: 16 sequences of 12,000 tokens on 4 key heads in a table for 192,512 154 -> 71, 125 -> 50; 16 of 1,000 to 100,000 116 -> 103, 72 -> 54; 4 of 100,000 and
+  // 8 of 100,000 on 8 80 -> 80, 155 -> 160, 47 -> 46, 95 -> 90.  Two of 412,200 and 312,300 478 -> 485, 251 -> 256: fewer than four are as they were.
+  const int64_t of = int64_t(kv_heads) * a.head_blocks, pairs = batch * a.splits, blocks = 8 * ceil_div(pairs, 8) * of;
+  a.dealt = batch >= 4 && pairs >= 64 && blocks < (int64_t(1) << 32) / (64 * kWaves);  // (a grid has up to 2^32 - 1 threads)
+  const dim3 grid = a.dealt ? dim3(static_cast<unsigned>(blocks)) : dim3(static_cast<unsigned>(a.splits), static_cast<unsigned>(of), static_cast<unsigned>(batch));
   if (dtype == BSGA_BF16) {
     if (coded) hipLaunchKernelGGL((paged_kernel<__bf16, E4m3>), grid, dim3(64 * kWaves), 0, s, a);
     else hipLaunchKernelGGL((paged_kernel<__bf16, __bf16>), grid, dim3(64 * kWaves), 0, s, a);

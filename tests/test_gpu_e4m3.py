@@ -231,6 +231,27 @@ def test_attention(B, lengths, H, K, page, window, sinks, frame, dtype):
     assert torch.equal(B.bsga_paged_attn_e4m3(q.contiguous(), kc, vc, ks, vs, table, n, **what), o)
 
 
+@pytest.mark.parametrize("coded", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lengths,H,K,width,window", [([3000, 2000, 1000, 1], 4, 4, 2000, None), ([40] * 9 + [0, 1500] + [7] * 10, 6, 2, 500, None),
+                                                      ([900, 30, 2600, 0, 1], 40, 2, 1000, None), ([5000] + [1] * 15, 2, 1, 320, 3000)])
+def test_tables_wider_than_their_sequences(B, lengths, H, K, width, window, dtype, coded):
+    """Many stretches that no sequence has, or the longest alone."""
+    kc, vc, ks, vs, table, seqs = cached(lengths, K, 16)
+    table = torch.cat([table, torch.full((len(lengths), width), -1, dtype=torch.int32, device="cuda")], 1)[:, :width].contiguous()
+    q, n = queries(len(lengths), H, TYPES[dtype]), torch.tensor(lengths, dtype=torch.int32).cuda()
+    if coded:
+        o, lse = B.bsga_paged_attn_e4m3(q, kc, vc, ks, vs, table, n, window=window, return_lse=True)
+    else:
+        kc, vc = (values(c, s).to(TYPES[dtype]) for c, s in ((kc, ks), (vc, vs)))
+        o, lse = B.bsga_paged_attn(q, kc, vc, table, n, window=window, return_lse=True)
+    for b, (k, v) in enumerate(seqs):
+        if lengths[b] == 0:
+            assert bool((o[b] == 0).all()) and bool((lse[b] == -math.inf).all())
+        else:
+            check(o[b][:, None], lse[b][:, None], q[b][:, None], k, v, visible(lengths[b], window, 0, 1)[None])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("gain", [2.0 ** -20, 4.0, 16.0])
 def test_logits_of_any_size(B, dtype, gain):
