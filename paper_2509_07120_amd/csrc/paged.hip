@@ -162,8 +162,9 @@ int attend(const char* fn, bool coded, const void* q, int64_t q_batch, int64_t q
   hipStream_t s = static_cast<hipStream_t>(stream);
   // Workgroup w runs on XCD w % 8.  From four sequences on, first stretches, which more of them have, come first, and each sequence's and each number's stretches are
   // dealt out to all XCDs; a stretch's heads, which read the same pages, follow each other on one.  Against a row of stretches for each head and sequence, us in bf16
-  // and 8 bits: 16 sequences of 12,000 tokens on 4 key heads in a table for 192,512 154 -> 71, 125 -> 50; 16 of 1,000 to 100,000 116 -> 103, 72 -> 54; 4 of 100,000 and
-  // 8 of 100,000 on 8 80 -> 80, 155 -> 160, 47 -> 46, 95 -> 90.  Two of 412,200 and 312,300 478 -> 485, 251 -> 256: fewer than four are as they were.
+  // and 8 bits: 16 sequences of 12,000 tokens on 4 key heads in a table for 192,512 160 -> 74, 124 -> 51; 16 of 1,000 to 100,000 177 -> 163, 100 -> 88; on 8 key heads, 12
+  // of 60,000 in a table for 128,000 301 -> 248, 160 -> 133; 4 of 20,000 to 100,000 46 -> 47, 32 -> 32.  Two of 412,200 and 312,300 478 -> 485, 251 -> 256: fewer than
+  // four are as they were.
   const int64_t of = int64_t(kv_heads) * a.head_blocks, pairs = batch * a.splits, blocks = 8 * ceil_div(pairs, 8) * of;
   a.dealt = batch >= 4 && pairs >= 64 && blocks < (int64_t(1) << 32) / (64 * kWaves);  // (a grid has up to 2^32 - 1 threads)
   const dim3 grid = a.dealt ? dim3(static_cast<unsigned>(blocks)) : dim3(static_cast<unsigned>(a.splits), static_cast<unsigned>(of), static_cast<unsigned>(batch));
