@@ -401,8 +401,8 @@ int bsga_paged_attn(const void* q, int64_t q_batch, int64_t q_head, const void* 
  * Other bytes may be read (what they stand for may overflow in sums, or vanish).
  * What a row stands for is exact in bf16.
  *
- * bsga_qk_norm_rope_e4m3: bsga_qk_norm_rope into the pages of such a cache.  q, k, v and the rest as there; a row is quantised from the 32 bits
- * in which it was normed and turned (v: as it is).
+ * bsga_qk_norm_rope_e4m3: bsga_qk_norm_rope into the pages of such a cache.  q, k, v and the rest as there; a key is rounded
+ * once, to what it is after norm and turn in exact arithmetic (up to 2^-40: 64 bits decide where 32 leave a rounding open), a value as it is.
  *   q          NULL together with q_out; k and v each NULL together with its cache and its scales
  *   slots      [n_tokens], distinct; tokens whose slot lies outside the cache are not written
  *   q_out      [heads, n_tokens, 64]

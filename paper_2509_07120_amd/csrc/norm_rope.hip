@@ -11,9 +11,9 @@
 // modulo 2^64 is the turn's fraction, whatever the position's size; fp32 would be off by 0.1 at position 10^6.
 //
 // Into a cache in 8 bits (e4m3.h) the row goes from the 32 bits in which it was normed and turned, in one rounding: the largest magnitude is one more pair of
-// quad permutations, and neighbouring lanes swap halves so that each writes 16 bytes.  100 frames, with the rows returned as they are read back (1.97 GB): 395
-// us, 5.0 TB/s. Keys normed and turned in 64 bits, so that no number at a border between two codes goes to the other side than the definition's: 449 us; 32
-// bits stay, a code is half a step and 2^-22 from the number at most either way.
+// quad permutations, and neighbouring lanes swap halves so that each writes 16 bytes.  A key of which the 32 bits' own error leaves a rounding open (rounded from the
+// least and the largest that it may be, it differs) is done again in 64 bits at the end, by a wave with a lane to a number.  100 frames, with the rows returned as they
+// are read back (1.97 GB): 427 us, 4.6 TB/s; by 32 bits alone, where one key number in 200,000 went to the other side of a border, 396, all keys in 64 bits 449.
 #include "bf16_tile.h"
 #include "bsga_internal.h"
 #include "e4m3.h"
@@ -36,6 +36,7 @@ struct NormRopeArgs {
   int64_t n, n_slots;
   int heads[3], group_heads, axes, norm, page;
   float eps;
+  double eps64;
   unsigned long long turn[32];
   unsigned char *code[2], *scale[2];  // of k and v, in a cache in 8 bits: y holds the rows as they are read back then, where it is wanted
   // the gradient
@@ -117,14 +118,25 @@ __device__ __forceinline__ void weights(const unsigned char* p, const Lane& l, f
   widen<T>(raw, hi);
 }
 
-// (a, b) become the row before the weight; the factor that the row was multiplied with is returned.
-__device__ __forceinline__ float normalise(int norm, float eps, float (&a)[8], float (&b)[8]) {
+__device__ __forceinline__ float tree_sum(const float (&x)[8]) { return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7])); }
+
+// (a, b) become the row before the weight; the factor that the row was multiplied with is returned.  shift: the mean that was taken off, in units of the result.
+// TREE: sums by halves, which are less off.
+template <bool TREE = false>
+__device__ __forceinline__ float normalise(int norm, float eps, float (&a)[8], float (&b)[8], float* shift = nullptr) {
   if (norm == BSGA_NORM_NONE) return 1.f;
+  float mean = 0.f;
   if (norm == BSGA_NORM_LAYER) {
     float s = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) s += a[e] * 0x1p-6f + b[e] * 0x1p-6f;  // (the mean of values that fit fits, their sum may not)
-    const float mean = row_sum(s);
+    if constexpr (TREE) {
+      float t[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = a[e] * 0x1p-6f + b[e] * 0x1p-6f;
+      s = tree_sum(t);
+    }
+    mean = row_sum(s);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       a[e] -= mean;
@@ -134,12 +146,19 @@ __device__ __forceinline__ float normalise(int norm, float eps, float (&a)[8], f
   float s = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) s += a[e] * a[e] + b[e] * b[e];
+  if constexpr (TREE) {
+    float t[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] = a[e] * a[e] + b[e] * b[e];
+    s = tree_sum(t);
+  }
   const float r = 1.f / sqrtf(row_sum(s) * 0x1p-6f + eps);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     a[e] *= r;
     b[e] *= r;
   }
+  if (shift != nullptr) *shift = fabsf(mean) * r;
   return r;
 }
 
@@ -161,8 +180,15 @@ __device__ __forceinline__ unsigned other_of_pair(unsigned x) {  // lanes 1 0 3 
   return static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), 0xb1, 0xf, 0xf, true));
 }
 
-// A row's lanes to 8 bits: the exponent, and the numbers x in code[0], y in code[1].
-__device__ __forceinline__ int to_e4m3(const float (&x)[8], const float (&y)[8], u32x2 (&code)[2]) {
+// How far a key that was normed and turned in 32 bits may be off, relative to its pair's length, in units of 2^-24.  Before the turn 5.5: half of 2 + 3 + 2 for the sum of
+// 64 squares, one each for the root and its inverse, a half each for two products.  The angle 3.1, half a turn in 24 bits; sine and cosine 1.4, an ulp each; the turn 1.3.
+// A mean is off by 1 + 1 + 3 + 2 + 0.5 units of the magnitudes that it is of, in units of the result the mean's own and at most one more.
+constexpr float kOff = 12 * 0x1p-24f, kOffMean = 7.5f * 0x1p-24f, kOffBias = 5.5f * 0x1p-24f;
+
+// A row's lanes to 8 bits: the exponent, and the numbers x in code[0], y in code[1].  doubt: whether the exponent or a number may be another if the row's numbers
+// are off by kOff of their pair and `terms`: the least and the largest that a number may be are rounded, and differ.
+template <bool DOUBT>
+__device__ __forceinline__ int to_e4m3(const float (&x)[8], const float (&y)[8], float terms, u32x2 (&code)[2], bool& doubt) {
   float most = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -183,13 +209,94 @@ __device__ __forceinline__ int to_e4m3(const float (&x)[8], const float (&y)[8],
       v[e] = fabsf(y[e]) <= 0x1.fffffep127f ? fminf(fmaxf(v[e], -448.f), 448.f) : NAN;
     }
   }
-  code[0] = u32x2{pack_e4m3(u[0], u[1], u[2], u[3]), pack_e4m3(u[4], u[5], u[6], u[7])};
-  code[1] = u32x2{pack_e4m3(v[0], v[1], v[2], v[3]), pack_e4m3(v[4], v[5], v[6], v[7])};
+  auto pack = [&](const float* t) { return u32x2{pack_e4m3(t[0], t[1], t[2], t[3]), pack_e4m3(t[4], t[5], t[6], t[7])}; };
+  if constexpr (DOUBT) {
+    const float off = terms * f;
+    float w[8], z[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float of_pair = fmaf(fabsf(u[e]) + fabsf(v[e]), kOff, off);
+      w[e] = fminf(u[e] + of_pair, 448.f);  // (NaN becomes 448, and the other one does not)
+      z[e] = fminf(v[e] + of_pair, 448.f);
+      u[e] = fmaxf(u[e] - of_pair, -448.f);
+      v[e] = fmaxf(v[e] - of_pair, -448.f);
+    }
+    const u32x2 a = pack(w), b = pack(z);
+    code[0] = pack(u);
+    code[1] = pack(v);
+    const float top = most * f;
+    doubt = ((a[0] ^ code[0][0]) | (a[1] ^ code[0][1]) | (b[0] ^ code[1][0]) | (b[1] ^ code[1][1])) != 0u;
+    doubt = doubt | (fabsf(top - 448.f) <= fmaf(1024.f, kOff, off)) | (fabsf(top - 224.f) <= fmaf(1024.f, kOff, off));
+  } else {
+    code[0] = pack(u);
+    code[1] = pack(v);
+  }
   return byte;
 }
 
+// To 32 bits for a rounding that follows: what is not a number of 32 bits becomes the neighbour with an odd last bit, which no later rounding takes for a tie.
+__device__ __forceinline__ float to_odd(double x) {
+  const float f = static_cast<float>(x);
+  const double back = static_cast<double>(f);
+  unsigned u = __float_as_uint(f);
+  if (back != x && fabsf(f) <= 0x1.fffffep127f) u = (fabs(back) > fabs(x) ? u - 1u : u) | 1u;
+  return __uint_as_float(u);
+}
+
+template <typename F>
+__device__ __forceinline__ double over_wave(double x, F f) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = f(x, __shfl_xor(x, o));
+  return x;
+}
+
+// Keys by a wave in 64 bits, one after the other, a lane to a number: of heads h0 .. h1 - 1 of the 16 tokens from `first` on, those whose lanes have the head's bit of `open`.
+template <typename T>
+__device__ __forceinline__ void keys_in_64_bits(const NormRopeArgs& a, int64_t first, int h0, int h1, unsigned open, int lane) {
+  if (__ballot(open != 0) == 0) return;
+  const auto add = [](double x, double y) { return x + y; };
+  const auto larger_of = [](double x, double y) { return fmax(x, y); };
+  const auto number = [&](const unsigned char* p) { return static_cast<float>(reinterpret_cast<const T*>(p)[lane]); };
+  const float weight = a.weight[1] != nullptr ? number(a.weight[1]) : 1.f, bias = a.bias[1] != nullptr ? number(a.bias[1]) : 0.f;
+  const int half = a.axes == 2 ? 16 : 32;
+  const unsigned long long of_position = a.turn[lane & (half - 1)];
+  for (int h = h0; h < h1; ++h)
+    for (unsigned long long rows = __ballot((open >> (h - h0)) & 1); rows != 0;) {
+      const int r = __builtin_ctzll(rows) >> 2;
+      rows &= ~(15ull << (4 * r));
+      const int64_t i = first + r;
+      const float of_row = number(a.x[1] + i * a.x_token[1] + h * a.x_head[1]);
+      const int slot = a.slots[i];
+      const long long at = a.axes > 0 ? a.positions[i * a.axes + (a.axes == 2 ? lane >> 5 : 0)] : 0;
+      double x = of_row;
+      if (a.norm == BSGA_NORM_LAYER) x -= over_wave(x, add) * 0x1p-6;
+      if (a.norm != BSGA_NORM_NONE) x /= sqrt(over_wave(x * x, add) * 0x1p-6 + a.eps64);
+      x = x * static_cast<double>(weight) + static_cast<double>(bias);
+      if (a.axes > 0) {
+        double sine, cosine;
+        sincospi(static_cast<double>(static_cast<long long>(static_cast<unsigned long long>(at) * of_position)) * 0x1p-63, &sine, &cosine);
+        const double other = __shfl_xor(x, half);
+        x = x * cosine + ((lane & half) != 0 ? other : -other) * sine;
+      }
+      const bool finite = fabs(x) < 0x1.ffffffp127;  // as 32 bits have it
+      const double most = over_wave(finite ? fabs(x) : 0.0, larger_of);
+      float up = static_cast<float>(most);
+      if (static_cast<double>(up) < most) up = __uint_as_float(__float_as_uint(up) + 1u);
+      const int byte = scale_byte(up);
+      const double t = x * static_cast<double>(inverse_scale(byte));
+      const unsigned code = pack_e4m3(finite ? to_odd(fmin(fmax(t, -448.0), 448.0)) : NAN, 0.f, 0.f, 0.f) & 0xffu;
+      if (slot >= 0 && slot < a.n_slots) {
+        const unsigned page = static_cast<unsigned>(slot) / static_cast<unsigned>(a.page);
+        const int64_t row = (int64_t(page) * a.heads[1] + h) * a.page + (static_cast<unsigned>(slot) - page * a.page);
+        a.code[0][row * 64 + lane] = static_cast<unsigned char>(code);
+        if (lane == 0) a.scale[0][row] = static_cast<unsigned char>(byte);
+      }
+      if (a.y[1] != nullptr) reinterpret_cast<T*>(a.y[1])[(int64_t(h) * a.n + i) * 64 + lane] = static_cast<T>(unpack_f32(code)[0] * scale_of(byte));
+    }
+}
+
 template <typename T, bool CODED>
-__global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
+__global__ __launch_bounds__(256, CODED && sizeof(T) == 2 ? 3 : 1) void norm_rope_kernel(const NormRopeArgs a) {
   int h0, h1, group;
   const int kind = kind_of(a, blockIdx.y, h0, h1, group);
   const int c = threadIdx.x & 3;
@@ -227,16 +334,29 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
     weights<T>(a.weight[kind], l, 1.f, wa, wb);
     weights<T>(a.bias[kind], l, 0.f, ba, bb);
   }
+  // Keys that are rounded to 8 bits from 32: those whose rounding the 32 bits leave open are left for the end
+  const bool exact = a.norm == BSGA_NORM_NONE && a.axes == 0 && a.weight[1] == nullptr && a.bias[1] == nullptr;
+  float most_weight = 0.f, most_bias = 0.f;
+  const float of_mean = a.norm == BSGA_NORM_LAYER ? kOffMean : 0.f;
+  unsigned open = 0;
+  if (CODED && kind == 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      most_weight = fmaxf(most_weight, fmaxf(fabsf(wa[e]), fabsf(wb[e])));
+      most_bias = fmaxf(most_bias, fmaxf(fabsf(ba[e]), fabsf(bb[e])));
+    }
+  }
   for (int h = h0; h < h1; h += kHeadsInFlight) {
     if (h > h0) fetch(h);
 #pragma unroll
     for (int u = 0; u < kHeadsInFlight; ++u) {
       if (h + u >= h1) break;
-      float x[8], y[8];
+      float x[8], y[8], shift = 0.f;
       widen<T>(lo[u], x);
       widen<T>(hi[u], y);
       if (kind < 2) {
-        normalise(a.norm, a.eps, x, y);
+        if (CODED && kind == 1) normalise<true>(a.norm, a.eps, x, y, &shift);
+        else normalise(a.norm, a.eps, x, y);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           x[e] = fmaf(x[e], wa[e], ba[e]);
@@ -250,18 +370,23 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
       }
       if (CODED && kind > 0) {
         u32x2 code[2];
-        const int byte = to_e4m3(x, y, code);
+        bool doubt = false;
+        int byte;
+        if (kind == 1 && !exact) byte = to_e4m3<true>(x, y, fmaf(shift * kOffMean + of_mean, most_weight, most_bias * kOffBias), code, doubt);
+        else byte = to_e4m3<false>(x, y, 0.f, code, doubt);
+        const bool left = ((__ballot(doubt) >> (threadIdx.x & 60)) & 15) != 0;  // any of the row's lanes
+        open |= static_cast<unsigned>(left) << (h + u - h0);
         // lanes 2j and 2j + 1 hold neighbouring eights of both halves: the first takes those of the first half, the other those of the second
         const bool odd = c & 1;
         const u32x2 mine = odd ? code[1] : code[0], gone = odd ? code[0] : code[1];
         const u32x2 got = {other_of_pair(gone[0]), other_of_pair(gone[1])};
-        if (write) {
+        if (write && !left) {
           const int64_t row = to + (h + u) * step;
           *reinterpret_cast<u32x4*>(a.code[kind - 1] + row * 64 + (odd ? l.second - 8 : l.first)) =
               odd ? u32x4{got[0], got[1], mine[0], mine[1]} : u32x4{mine[0], mine[1], got[0], got[1]};
           if (c == 0) a.scale[kind - 1][row] = static_cast<unsigned char>(byte);
         }
-        if (live && dst != nullptr) {
+        if (live && !left && dst != nullptr) {
           unsigned char* p = dst + ((h + u) * a.n + at) * kRow;
           const float f = scale_of(byte);
 #pragma unroll
@@ -283,6 +408,8 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
       }
     }
   }
+  if (CODED && kind == 1)
+    keys_in_64_bits<T>(a, int64_t(blockIdx.x) * kRowsPerGroup + (threadIdx.x >> 6) * 16, h0, h1, live ? open : 0u, threadIdx.x & 63);
 }
 
 template <typename T>
@@ -451,6 +578,7 @@ int common(const char* fn, const void* const (&x)[3], const int64_t (&strides)[6
   a.n = n_tokens;
   a.norm = norm;
   a.eps = static_cast<float>(eps);
+  a.eps64 = eps;
   a.positions = positions;
   a.axes = axes;
   // base^(-(8 x + y) / half) / 2 pi as a product of two powers (calls on few rows are bound by the host: 12 powers in place of 32)

@@ -157,6 +157,37 @@ def test_normed_and_turned(B, dtype, N, H, K, norm, axes, base):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("norm,axes,base,mean", [("rms", 1, 1e4, 0.0), ("layer", 2, 100.0, 0.0), ("layer", 1, 5e5, 30.0), ("rms", 0, 1e4, 0.0), (None, 2, 100.0, 0.0)])
+def test_keys_are_the_nearest_numbers(B, dtype, norm, axes, base, mean):
+    """No key goes to the other side of a border between two numbers: two million of them, bit for bit what the definition in float64 makes (which is itself off
+    by 2^-40 at positions up to 4096, so that one number in 2^37 may differ)."""
+    g = torch.Generator(device="cuda").manual_seed(int(base) + axes)
+    N, K, page = 8192, 4, 64
+    k = (torch.randn((N, K, 64), generator=g, device="cuda") * torch.exp2(torch.randint(-3, 4, (N, K, 1), generator=g, device="cuda")) + mean).to(TYPES[dtype])
+    w = (1 + 0.2 * torch.randn(64, generator=g, device="cuda")).to(TYPES[dtype]) if norm else None
+    bias = (0.3 * torch.randn(64, generator=g, device="cuda")).to(TYPES[dtype]) if norm == "layer" else None
+    positions = torch.randint(0, 4097, (N, axes), generator=g, device="cuda").int() if axes else None
+    slots = torch.randperm(N, generator=g, device="cuda").int()
+    kc, vc, ks, vs = empty_cache(N // page, K, page)
+    rows = B.bsga_qk_norm_rope_e4m3(None, k, k, kc, vc, ks, vs, slots, positions, k_weight=w, k_bias=bias, norm=norm, base=base, return_rows=True)[1]
+    x = k.double()
+    if norm:
+        x = x - x.mean(-1, keepdim=True) if norm == "layer" else x
+        x = x / torch.sqrt(x.square().mean(-1, keepdim=True) + 1e-6) * w.double()
+        x = x if bias is None else x + bias.double()
+    if axes:
+        half = 32 // axes
+        angle = positions.double()[:, None, :, None] * base ** (-torch.arange(half, dtype=torch.float64, device="cuda") / half)
+        a, b = x.view(N, K, axes, 2, half).unbind(3)
+        x = torch.stack([a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()], 3).view(N, K, 64)
+    want, s = quantised(x)
+    page_of, row_of = slots.long() // page, slots.long() % page
+    assert torch.equal(ks[page_of, :, row_of].int(), (s + 127).int())
+    assert torch.equal(values(kc, ks)[page_of, :, row_of], want)
+    assert torch.equal(rows.transpose(0, 1).double(), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("n,K,page,first,count", [(1, 1, 16, 0, 1), (100, 3, 16, 7, 60), (1400, 2, 1374, 1370, 30), (500, 16, 64, 0, 500), (70, 4, 1, 3, 64), (200, 1, 24, 200, 0)])
 def test_tokens_read_back(B, n, K, page, first, count, dtype):
     t = TYPES[dtype]
