@@ -243,10 +243,29 @@ __device__ __forceinline__ float to_odd(double x) {
   return __uint_as_float(u);
 }
 
+template <int DPP>
+__device__ __forceinline__ double of_other(double x) {
+  const unsigned long long u = __builtin_bit_cast(unsigned long long, x);
+  const int low = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), DPP, 0xf, 0xf, true);
+  const int high = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), DPP, 0xf, 0xf, true);
+  return __builtin_bit_cast(double, static_cast<unsigned long long>(static_cast<unsigned>(high)) << 32 | static_cast<unsigned>(low));
+}
+
+// f over all lanes: pairs, quads, eights (lanes mirrored within them), sixteens, then across rows of sixteen.
 template <typename F>
 __device__ __forceinline__ double over_wave(double x, F f) {
+  x = f(x, of_other<0xb1>(x));
+  x = f(x, of_other<0x4e>(x));
+  x = f(x, of_other<0x141>(x));
+  x = f(x, of_other<0x140>(x));
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = f(x, __shfl_xor(x, o));
+  for (int step = 0; step < 2; ++step) {
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, x);
+    const unsigned low = static_cast<unsigned>(u), high = static_cast<unsigned>(u >> 32);
+    const auto a = step == 0 ? __builtin_amdgcn_permlane16_swap(low, low, false, false) : __builtin_amdgcn_permlane32_swap(low, low, false, false);
+    const auto b = step == 0 ? __builtin_amdgcn_permlane16_swap(high, high, false, false) : __builtin_amdgcn_permlane32_swap(high, high, false, false);
+    x = f(__builtin_bit_cast(double, static_cast<unsigned long long>(b[0]) << 32 | a[0]), __builtin_bit_cast(double, static_cast<unsigned long long>(b[1]) << 32 | a[1]));
+  }
   return x;
 }
 
