@@ -13,7 +13,7 @@
 // Into a cache in 8 bits (e4m3.h) the row goes from the 32 bits in which it was normed and turned, in one rounding: the largest magnitude is one more pair of
 // quad permutations, and neighbouring lanes swap halves so that each writes 16 bytes.  A key of which the 32 bits' own error leaves a rounding open (rounded from the
 // least and the largest that it may be, it differs) is done again in 64 bits at the end, by a wave with a lane to a number.  100 frames, with the rows returned as they
-// are read back (1.97 GB): 427 us, 4.6 TB/s; by 32 bits alone, where one key number in 200,000 went to the other side of a border, 396, all keys in 64 bits 449.
+// are read back (1.97 GB): 424 us, 4.6 TB/s; by 32 bits alone, where one key number in 200,000 went to the other side of a border, 396, all keys in 64 bits 449.
 #include "bf16_tile.h"
 #include "bsga_internal.h"
 #include "e4m3.h"

@@ -8,8 +8,8 @@
 // S^T = K Q^T and O^T = V^T P^T, in which the weights are operands as they lie in the results.
 // The waves' sums are joined through LDS; stretches of one sequence by a second kernel.
 // Two sequences of 412,200 and 312,300 keys of 16 heads, 2.97 GB: 480 us, 6.2 TB/s; 96 of 1 to 12,000, window of 4096, 16 query heads to 4 key heads: 66 us, 5.0 TB/s.
-// In 8 bits, where pieces are 64 keys of 65 bytes (8 KB on their way for each wave are enough for the same reason: half the bytes, and two numbers' products to one of
-// them), 1.51 GB 250 us, 6.0 TB/s, and 39.5 us, 4.2 TB/s: there the longest sequences, one to a CU, wait for the chain of a piece's operations.
+// In 8 bits, where pieces are 64 keys of 65 bytes (8 KB on their way for each wave are enough: half the bytes, and two numbers' products to one of them), 1.51 GB 250 us,
+// 6.0 TB/s, and 39 us, 4.3 TB/s: 36 in the kernel, 27 of them by bytes, the rest from the lengths over the pages to the first piece, and the longest sequences' end.
 #include "paged.h"
 
 #include <math.h>
