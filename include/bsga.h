@@ -450,6 +450,7 @@ int bsga_paged_attn_e4m3(const void* q, int64_t q_batch, int64_t q_head, const v
  *   workspace  bsga_prefix_attn_workspace_bytes(...) bytes, 16-byte aligned; overwritten
  * One launch: BSGA_ERR_UNSUPPORTED where it would take 2^24 workgroups or more (tens of thousands of sequences with several key heads and long tables).
  * Table entries and lengths that do not fit are clamped as there.  A key that a query does not see has no part in its result.  The same bits every time.
+ * In 8 bits, prefixes of more than 16 queries to a key head whose value scales go beyond 2^16 (values of 2.9e7), or below 2^-64, are slow, one query after the other: 20 ms for a stretch of some thousand tokens.
  */
 size_t bsga_prefix_attn_workspace_bytes(int dtype, int cache_dtype, int64_t batch, int heads, int kv_heads, int64_t table_width, int64_t prefixes,
                                         int64_t prefix_width, int64_t n_pages, int page, int64_t frame, int64_t window, int64_t sinks);

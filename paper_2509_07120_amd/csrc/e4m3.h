@@ -2,8 +2,9 @@
 // the row; a number c stands for c * 2^(b - 127).  The exponent is the least that keeps the row's largest finite number at or below 448, so that every
 // rounding is at most half a step, 2^-4 of the number, down to 2^-15 of the largest.  A power of two and no factor of 32 bits: what a number
 // stands for has four significant bits and is exact in bf16, and one byte of 65 is the scale, where a factor would take four of 68 and round again.
-// Exponents stay in [-64, 80]: the weights of an attention times scales from there on are no subnormal numbers, and 2^30 keys of 448 * 2^80 with weights up to 2^8 add up
-// to less than there is in 32 bits.  So numbers above 448 * 2^80 = 5.4e26 become that, and those below 2^-74 become zero.
+// Exponents stay in [-64, 80]: a scale times a weight of 2^-62 or more, which is all that counts, is no subnormal number, and keys of 448 * 2^80 whose weights add up to
+// 2^26 (four lanes of 2^24 each, where a reference of the weights follows) add up to less than there is in 32 bits.  So numbers above 448 * 2^80 = 5.4e26 become that,
+// and those below 2^-74 become zero.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -438,7 +438,7 @@ struct PieceLoad {
     else if constexpr (kInFlight == 10) asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
   }
-  // values (and their exponents) that only fill the last piece: their weights are zero, which is not nothing if the one that is repeated is infinite
+  // values that only fill the last piece become zeros (of scale 1): their weights are zero, which is not nothing if the one that is repeated is infinite
   __device__ __forceinline__ void clear_from(unsigned char* piece, int left) const {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -446,7 +446,7 @@ struct PieceLoad {
       if (r >= left) *reinterpret_cast<u32x4*>(piece + kBytes + r * P::kRow + pos * 16) = u32x4{0u, 0u, 0u, 0u};
     }
     if constexpr (P::kScaled)
-      if (lane >= left) reinterpret_cast<unsigned*>(piece + 2 * kBytes)[64 + lane] = 0u;
+      if (lane >= left) reinterpret_cast<unsigned*>(piece + 2 * kBytes)[64 + lane] = 127u;
   }
 };
 

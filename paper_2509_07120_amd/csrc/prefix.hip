@@ -236,8 +236,11 @@ struct Wide<E4m3> {
   }
 };
 
+// Value scales that may be part of a weight, see over_prefix_wide.
+constexpr unsigned kMostInWeight = 127 + 16;
+
 // One query by a wave, over the keys of a stretch that it sees and no others: where values that are not finite have met weights of zero in the
-// products.  For results that are right, not for speed.
+// products, and where values' scales are too far apart.  For results that are right, not for speed.
 template <typename C>
 __device__ void one_query(const PrefixArgs& a, const Stretch& st, const int* table, int hk, int split, int64_t row, const unsigned char* q, int lo, int lane) {
   typedef Wide<C> P;
@@ -349,6 +352,9 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
   // Weights are 2^(c x - m).  The reference m is the largest logit of a column's first keys, and stays until the sum of its weights passes 2^24: then the
   // half piece is done again with an m that follows the largest logit and the sum.  That saves a maximum over every piece, a tenth of the vector instructions.
   // In 8 bits a value's scale 2^s is part of its weight, which costs nothing: products begin with s / c in place of zero, and the sum takes 2^-s of the weight.
+  // A weight below 2^-126 is zero, in the sum as well, so this holds for s of -64 to 16 only: with L the logarithm of the sum, m is L + 17 at most, and a key is
+  // lost if its logit is below L + 17 - 126 + 64 = L - 45: 2^30 of them are 2^-15 of the sum, less than a rounding to bf16.  And m is L - 70 at least (64 for the scales of
+  // the first keys), so that a wave whose m lies 126 below another's has 2^-39 of the sum.  Stretches with values above 448 * 2^16 (or foreign bytes) go by one_query.
   f32x16 o[R][2];
   float m[R], minus[R], l[R];  // minus: what is added to logits, -m or, as long as nothing was seen, 0
 #pragma unroll
@@ -359,6 +365,7 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
   }
   int buf = 0;
   int bad = 0, first_half = 1;  // bad: whether a value that is not finite has met weights of zero
+  unsigned apart = 0;           // the farthest value scale from the least that fits into weights
   for (int p = wave; p < pieces; p += kWaves, buf ^= 1) {
     load.wait(p + kWaves >= pieces);
     unsigned char* const kt = mine + buf * kBufBytes;
@@ -372,6 +379,7 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
     float k_scale = 1.f;
     if constexpr (P::kScaled) {  // a lane to a key: the exponents make room for what they stand for
       const unsigned kb = reinterpret_cast<unsigned*>(extra)[lane], vb = reinterpret_cast<unsigned*>(extra)[64 + lane];
+      apart = max(apart, vb - kLeastScale);
       k_scale = scale_of(kb);
       extra[lane] = (static_cast<float>(vb) - 127.f) * a.ln2_scale;
       extra[64 + lane] = inverse_scale(vb);
@@ -495,7 +503,7 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
       sums[wave][1][32 * e + n] = l[e];
     }
   }
-  if (__syncthreads_or(bad)) {
+  if (__syncthreads_or(bad | (apart > kMostInWeight - kLeastScale))) {
     for (int i = wave; i < queries; i += kWaves) {
       int to, low, s;
       const int64_t row = row_of(i, to);
