@@ -370,19 +370,19 @@ __device__ __forceinline__ void over_prefix_wide(const PrefixArgs& a, const Shar
     load.wait(p + kWaves >= pieces);
     unsigned char* const kt = mine + buf * kBufBytes;
     unsigned char* const vt = kt + kBytes;
-    float* const extra = reinterpret_cast<float*>(kt + 2 * kBytes);
+    unsigned* const extra = reinterpret_cast<unsigned*>(kt + 2 * kBytes);
     const int x = st.x0 + p * P::kKeys, left = st.x1 - x;
     if (left < P::kKeys) load.clear_from(kt, left);
     // key i of the piece is key x + i of the stretch, and no query sees less than keys `most` ..; those in front of it are looked at one by one
     const bool masked = (left < P::kKeys) | ((x + P::kKeys > st.s) & (st.key(max(x, st.s)) < most));
     if (masked & (most > st.lo)) bad |= load.bad_keys(kt) != 0;
     float k_scale = 1.f;
-    if constexpr (P::kScaled) {  // a lane to a key: the exponents make room for what they stand for
-      const unsigned kb = reinterpret_cast<unsigned*>(extra)[lane], vb = reinterpret_cast<unsigned*>(extra)[64 + lane];
+    if constexpr (P::kScaled) {  // a lane to a key: the exponents make room for what they stand for (as bits: stores of another type could pass the loads)
+      const unsigned kb = extra[lane], vb = extra[64 + lane];
       apart = max(apart, vb - kLeastScale);
       k_scale = scale_of(kb);
-      extra[lane] = (static_cast<float>(vb) - 127.f) * a.ln2_scale;
-      extra[64 + lane] = inverse_scale(vb);
+      extra[lane] = __float_as_uint((static_cast<float>(vb) - 127.f) * a.ln2_scale);
+      extra[64 + lane] = __float_as_uint(inverse_scale(vb));
     }
 #pragma unroll 1
     for (int h = 0; h < P::kKeys / 32; ++h) {
