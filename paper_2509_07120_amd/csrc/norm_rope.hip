@@ -12,7 +12,7 @@
 //
 // Into a cache in 8 bits (e4m3.h) the row goes from the 32 bits in which it was normed and turned, in one rounding: the largest magnitude is one more pair of
 // quad permutations, and neighbouring lanes swap halves so that each writes 16 bytes.  A key of which the 32 bits' own error leaves a rounding open (rounded from the
-// least and the largest that it may be, it differs) is done again in 64 bits at the end, by a wave with a lane to a number.  100 frames, with the rows returned as they
+// least and the largest that it may be, it differs), or whose squares 32 bits do not hold, is done again in 64 bits at the end, by a wave with a lane to a number.  100 frames, with the rows returned as they
 // are read back (1.97 GB): 424 us, 4.6 TB/s; by 32 bits alone, where one key number in 200,000 went to the other side of a border, 396, all keys in 64 bits 449.
 #include "bf16_tile.h"
 #include "bsga_internal.h"
@@ -120,7 +120,8 @@ __device__ __forceinline__ void weights(const unsigned char* p, const Lane& l, f
 
 __device__ __forceinline__ float tree_sum(const float (&x)[8]) { return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7])); }
 
-// (a, b) become the row before the weight; the factor that the row was multiplied with is returned.  shift: the mean that was taken off, in units of the result.
+// (a, b) become the row before the weight; the factor that the row was multiplied with is returned.  shift: the mean that was taken off, in units of the result,
+// and infinite, which leaves every rounding open, where the sum of the squares is, or so small that squares lose bits below 2^-126.
 // TREE: sums by halves, which are less off.
 template <bool TREE = false>
 __device__ __forceinline__ float normalise(int norm, float eps, float (&a)[8], float (&b)[8], float* shift = nullptr) {
@@ -152,13 +153,13 @@ __device__ __forceinline__ float normalise(int norm, float eps, float (&a)[8], f
     for (int e = 0; e < 8; ++e) t[e] = a[e] * a[e] + b[e] * b[e];
     s = tree_sum(t);
   }
-  const float r = 1.f / sqrtf(row_sum(s) * 0x1p-6f + eps);
+  const float square = row_sum(s) * 0x1p-6f + eps, r = 1.f / sqrtf(square);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     a[e] *= r;
     b[e] *= r;
   }
-  if (shift != nullptr) *shift = fabsf(mean) * r;
+  if (shift != nullptr) *shift = square >= 0x1p-100f && square <= 0x1.fffffep127f ? fabsf(mean) * r : INFINITY;
   return r;
 }
 
