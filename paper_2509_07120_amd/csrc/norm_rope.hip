@@ -12,8 +12,8 @@
 //
 // Into a cache in 8 bits (e4m3.h) the row goes from the 32 bits in which it was normed and turned, in one rounding: the largest magnitude is one more pair of
 // quad permutations, and neighbouring lanes swap halves so that each writes 16 bytes.  A key of which the 32 bits' own error leaves a rounding open (rounded from the
-// least and the largest that it may be, it differs), or whose squares 32 bits do not hold, is done again in 64 bits at the end, by a wave with a lane to a number.  100 frames, with the rows returned as they
-// are read back (1.97 GB): 424 us, 4.6 TB/s; by 32 bits alone, where one key number in 200,000 went to the other side of a border, 396, all keys in 64 bits 449.
+// least and the largest that it may be, it differs), or whose squares 32 bits do not hold, is done again in 64 bits at the end, by a wave with a lane to a number.  100 frames,
+// with the rows returned as they are read back (1.97 GB): 431 us, 4.6 TB/s; by 32 bits alone, where one key number in 200,000 went to the other side of a border, 396, all keys in 64 bits 449.
 #include "bf16_tile.h"
 #include "bsga_internal.h"
 #include "e4m3.h"
@@ -118,10 +118,12 @@ __device__ __forceinline__ void weights(const unsigned char* p, const Lane& l, f
   widen<T>(raw, hi);
 }
 
+constexpr float kMostShift = 0x1p16f;  // see kOff
+
 __device__ __forceinline__ float tree_sum(const float (&x)[8]) { return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7])); }
 
 // (a, b) become the row before the weight; the factor that the row was multiplied with is returned.  shift: the mean that was taken off, in units of the result,
-// and infinite, which leaves every rounding open, where the sum of the squares is, or so small that squares lose bits below 2^-126.
+// and infinite, which leaves every rounding open, where it is large, where the sum of the squares is infinite, or so small that squares lose bits below 2^-126.
 // TREE: sums by halves, which are less off.
 template <bool TREE = false>
 __device__ __forceinline__ float normalise(int norm, float eps, float (&a)[8], float (&b)[8], float* shift = nullptr) {
@@ -159,7 +161,10 @@ __device__ __forceinline__ float normalise(int norm, float eps, float (&a)[8], f
     a[e] *= r;
     b[e] *= r;
   }
-  if (shift != nullptr) *shift = square >= 0x1p-100f && square <= 0x1.fffffep127f ? fabsf(mean) * r : INFINITY;
+  if (shift != nullptr) {
+    const float by = fabsf(mean) * r;
+    *shift = square >= 0x1p-100f && square <= 0x1.fffffep127f && by <= kMostShift ? by : INFINITY;
+  }
   return r;
 }
 
@@ -181,10 +186,14 @@ __device__ __forceinline__ unsigned other_of_pair(unsigned x) {  // lanes 1 0 3 
   return static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), 0xb1, 0xf, 0xf, true));
 }
 
-// How far a key that was normed and turned in 32 bits may be off, relative to its pair's length, in units of 2^-24.  Before the turn 5.5: half of 2 + 3 + 2 for the sum of
-// 64 squares, one each for the root and its inverse, a half each for two products.  The angle 3.1, half a turn in 24 bits; sine and cosine 1.4, an ulp each; the turn 1.3.
-// A mean is off by 1 + 1 + 3 + 2 + 0.5 units of the magnitudes that it is of, in units of the result the mean's own and at most one more.
-constexpr float kOff = 12 * 0x1p-24f, kOffMean = 7.5f * 0x1p-24f, kOffBias = 5.5f * 0x1p-24f;
+// How far a key that was normed and turned in 32 bits may be off, relative to its pair's length, in units of 2^-24, a whole one for each rounding.  Before the turn 9: for the
+// mean of the squares 2 + 3 + 2 and 1 for eps, half of which is the root's, one each for the root, its inverse, the product with that, the difference from a mean, and the
+// product with the weight.  The angle 1.6, half a turn in 24 bits; sine and cosine 1.4, an ulp each; the turn 2, the sums by which it is looked for 1; a tenth for products of
+// errors.  A bias is 8 of its own (what its number has before it is added), in both numbers of a pair, so times sqrt(2).  A mean is off by 1 + 3 + 2 units of the magnitudes that
+// it is of, in units of the result the mean's own and at most one more, in both numbers too; what that does to the squares is less than an eighth of it as long as the
+// mean is at most 2^16 of those units.  Weights up to 2^40: what a number loses below 2^-126 before them is nothing behind them.
+constexpr float kOff = 15.1f * 0x1p-24f, kOffMean = 10 * 0x1p-24f, kOffBias = 12 * 0x1p-24f;
+constexpr float kMostWeight = 0x1p40f;
 
 // A row's lanes to 8 bits: the exponent, and the numbers x in code[0], y in code[1].  doubt: whether the exponent or a number may be another if the row's numbers
 // are off by kOff of their pair and `terms`: the least and the largest that a number may be are rounded, and differ.
@@ -365,6 +374,7 @@ __global__ __launch_bounds__(256, CODED && sizeof(T) == 2 ? 3 : 1) void norm_rop
       most_weight = fmaxf(most_weight, fmaxf(fabsf(wa[e]), fabsf(wb[e])));
       most_bias = fmaxf(most_bias, fmaxf(fabsf(ba[e]), fabsf(bb[e])));
     }
+    if (most_weight > kMostWeight) most_bias = INFINITY;  // (no row is sure)
   }
   for (int h = h0; h < h1; h += kHeadsInFlight) {
     if (h > h0) fetch(h);

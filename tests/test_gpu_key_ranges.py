@@ -63,3 +63,21 @@ def test_a_mean_far_above_what_is_left(B, mean, spread, dtype):  # noqa: F811
     at, row = slots.long() // page, slots.long() % page
     assert torch.equal(ks[at, :, row].int(), (s + 127).int())
     assert torch.equal(values(kc, ks)[at, :, row], want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("weight,size", [(1e30, 1.0), (1e35, 1e-35), (1e-30, 1.0), (3e12, 1e-36)])
+def test_weights_of_any_size(B, weight, size, dtype):  # noqa: F811
+    """What a number loses below 2^-126 before the weight comes back behind it: an eps of 10^12 keeps rows of small numbers small until then."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    N, K, page = 200, 2, 40
+    k = (size * torch.randn((N, K, 64), generator=g, device="cuda").double()).to(TYPES[dtype])
+    w = (weight * (1 + 0.2 * torch.randn(64, generator=g, device="cuda").double())).to(k.dtype)
+    positions = torch.randint(0, 4097, (N, 1), generator=g, device="cuda").int()
+    slots = torch.randperm(N, generator=g, device="cuda").int()
+    kc, vc, ks, vs = empty_cache(N // page, K, page)
+    B.bsga_qk_norm_rope_e4m3(None, k, k, kc, vc, ks, vs, slots, positions, k_weight=w, norm="rms", eps=1e12)
+    want, s = quantised(_want(k, w, None, positions, "rms", 1e12))
+    at, row = slots.long() // page, slots.long() % page
+    assert torch.equal(ks[at, :, row].int(), (s + 127).int())
+    assert torch.equal(values(kc, ks)[at, :, row], want)
