@@ -384,6 +384,7 @@ int bsga_window_attn_bwd(const void* dout, const void* q, const void* k, const v
  *   lengths     [batch] int32 device array, clamped into [0, table_width * page]; 0: zeros, lse = -inf
  *   out         [batch, heads, 64];  lse nullable [batch, heads] float32
  *   workspace   bsga_paged_attn_workspace_bytes(...) bytes, 16-byte aligned; overwritten: long sequences are shared out between workgroups
+ * BSGA_ERR_UNSUPPORTED where a launch would take 2^24 workgroups or more (batch * heads of 2^24 and more rows in more than eight stretches, or of 2^28).
  * Cache rows that the query does not see are not read.  bf16 and fp32, arithmetic as bsga_window_attn; the same bits every time.
  */
 size_t bsga_paged_attn_workspace_bytes(int dtype, int64_t batch, int heads, int kv_heads, int64_t table_width, int64_t n_pages, int page,
@@ -421,6 +422,7 @@ int bsga_qk_norm_rope_e4m3(const void* q, const void* k, const void* v, int64_t 
  *   pages      [table_width] int32, the sequence's row of a page table; tokens whose page lies outside [0, n_pages) are zeros
  *   k_out, v_out  [kv_heads, n_tokens, 64] of type dtype, heads k_head and v_head elements apart (multiples of 16 bytes, a head's rows at
  *              least), must not overlap the caches
+ *   n_tokens   up to 2^30 - 64
  */
 int bsga_cache_load(const void* k_cache, const void* v_cache, const uint8_t* k_scale, const uint8_t* v_scale, int cache_dtype, int64_t n_pages, int page,
                     int kv_heads, int head_dim, const int32_t* pages, int64_t table_width, int64_t first, int64_t n_tokens, int dtype, void* k_out,

@@ -92,6 +92,8 @@ extern "C" int bsga_cache_load(const void* k_cache, const void* v_cache, const u
   if (first < 0 || n_tokens < 0 || first > most || n_tokens > table_width * page - first)
     return fail(BSGA_ERR_INVALID_ARG, "%s: tokens %lld to %lld + %lld do not lie in the sequence's pages", fn, (long long)first, (long long)first, (long long)n_tokens);
   if (n_tokens == 0) return BSGA_OK;
+  if (ceil_div(n_tokens, kTokens) >= (int64_t(1) << 32) / 256)  // (a grid has up to 2^32 - 1 threads)
+    return fail(BSGA_ERR_UNSUPPORTED, "%s: too many tokens for one launch, got %lld", fn, (long long)n_tokens);
   const int size = dtype == BSGA_BF16 ? 2 : 4;
   if (!pages || !k_out || !v_out || (n_pages > 0 && (!k_cache || !v_cache)))
     return fail(BSGA_ERR_INVALID_ARG, "%s: k_cache, v_cache, pages, k_out and v_out must be non-null", fn);

@@ -152,11 +152,13 @@ int attend(const char* fn, bool coded, const void* q, int64_t q_batch, int64_t q
   a.lse = lse;
   a.scale_log2 = softmax_scale * kLog2e;
   shape_of(a, keys_of_piece(dtype, coded));
+  const int64_t rows = batch * heads;
+  if (a.splits > 1 && workgroups_of_join(rows, a.splits) >= (int64_t(1) << 32) / 256)  // (a grid has up to 2^32 - 1 threads)
+    return fail(BSGA_ERR_UNSUPPORTED, "%s: too many keys of too many queries for one launch", fn);
   const size_t need = part_bytes(a);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(BSGA_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", fn, workspace ? workspace_bytes : 0, need);
   if (!aligned16(workspace)) return fail(BSGA_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", fn);
-  const int64_t rows = batch * heads;
   a.part = static_cast<float*>(workspace);
   a.part_lse = a.part + int64_t(a.splits) * rows * 64;
   hipStream_t s = static_cast<hipStream_t>(stream);

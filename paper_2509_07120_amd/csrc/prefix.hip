@@ -743,8 +743,7 @@ int bsga_prefix_attn(const void* q, int64_t q_batch, int64_t q_head, const void*
   a.scale_log2 = softmax_scale * kLog2e;
   a.ln2_scale = 1.f / a.scale_log2;
   const int64_t blocks = shape_of(a, dtype, cache_dtype);
-  const int64_t join = a.splits + a.own_splits > 8 ? batch * heads : 0;
-  if (larger(blocks, join) >= (int64_t(1) << 32) / (64 * kWaves))  // (a grid has up to 2^32 - 1 threads)
+  if (larger(blocks, workgroups_of_join(batch * heads, a.splits + a.own_splits)) >= (int64_t(1) << 32) / (64 * kWaves))  // (a grid has up to 2^32 - 1 threads)
     return fail(BSGA_ERR_UNSUPPORTED, "%s: too many keys of too many queries for one launch", fn);
   const size_t need = part_bytes(a);
   if (!workspace || workspace_bytes < need)

@@ -355,12 +355,13 @@ __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ par
   if (lse != nullptr && d == 0) lse[row] = top == -INFINITY ? -INFINITY : top + log2f(sum) * kLn2;
 }
 
+inline int64_t workgroups_of_join(int64_t rows, int splits) { return splits > 8 ? rows : ceil_div(rows, 16); }
+
 template <typename T>
 int launch_join(const float* part, const float* part_lse, int64_t rows, int splits, unsigned char* out, float* lse, hipStream_t s) {
-  if (splits > 8)
-    hipLaunchKernelGGL((join_kernel<T, true>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, s, part, part_lse, rows, splits, out, lse);
-  else
-    hipLaunchKernelGGL((join_kernel<T, false>), dim3(static_cast<unsigned>(ceil_div(rows, 16))), dim3(256), 0, s, part, part_lse, rows, splits, out, lse);
+  const dim3 grid(static_cast<unsigned>(workgroups_of_join(rows, splits)));
+  if (splits > 8) hipLaunchKernelGGL((join_kernel<T, true>), grid, dim3(256), 0, s, part, part_lse, rows, splits, out, lse);
+  else hipLaunchKernelGGL((join_kernel<T, false>), grid, dim3(256), 0, s, part, part_lse, rows, splits, out, lse);
   return check_hip(hipGetLastError(), "attention launch");
 }
 
