@@ -298,7 +298,8 @@ int bsga_layer_norm(const void* x, const void* weight, const void* bias, double 
  * Norms of queries and keys for each head and the rotation by position, in one pass, on the way from a projection's output to
  * the attention's layout.  A row x is the 64 numbers of one head of one token:
  *   norm       BSGA_NORM_NONE; BSGA_NORM_RMS: n = x / sqrt(mean x^2 + eps) * weight;
- *              BSGA_NORM_LAYER: n = (x - mean) / sqrt(variance + eps) * weight + bias; statistics in fp32
+ *              BSGA_NORM_LAYER: n = (x - mean) / sqrt(variance + eps) * weight + bias; statistics in fp32 (rows with numbers
+ *              above 2^60, whose squares may add up to more than there is, become zeros, or the bias)
  *   axes       0 (positions NULL): no rotation.  1 or 2: the row is one segment of 64 or two of 32; in a segment of width W the numbers
  *              j and j + W/2 turn by positions[token, segment] * base^(-2j/W).  Positions are any int32; angles do not lose precision
  *              with their size.
@@ -403,7 +404,8 @@ int bsga_paged_attn(const void* q, int64_t q_batch, int64_t q_head, const void* 
  * What a row stands for is exact in bf16.
  *
  * bsga_qk_norm_rope_e4m3: bsga_qk_norm_rope into the pages of such a cache.  q, k, v and the rest as there; a key is rounded
- * once, to what it is after norm and turn in exact arithmetic (up to 2^-40: 64 bits decide where 32 leave a rounding open), a value as it is.
+ * once, to what it is after norm and turn in exact arithmetic (64 bits decide where 32 leave a rounding open; they are off by 2^-40 of a pair, and by 2^-51 w where
+ * it is turned by an angle w), a value as it is.
  *   q          NULL together with q_out; k and v each NULL together with its cache and its scales
  *   slots      [n_tokens], distinct; tokens whose slot lies outside the cache are not written
  *   q_out      [heads, n_tokens, 64]
@@ -452,6 +454,7 @@ int bsga_paged_attn_e4m3(const void* q, int64_t q_batch, int64_t q_head, const v
  *   workspace  bsga_prefix_attn_workspace_bytes(...) bytes, 16-byte aligned; overwritten
  * One launch: BSGA_ERR_UNSUPPORTED where it would take 2^24 workgroups or more (tens of thousands of sequences with several key heads and long tables).
  * Table entries and lengths that do not fit are clamped as there.  A key that a query does not see has no part in its result.  The same bits every time.
+ * Values of bf16 and fp32 caches are below 2^100: sums of larger ones may become infinite.
  * In 8 bits, prefixes of more than 16 queries to a key head whose value scales go beyond 2^16 (values of 2.9e7), or below 2^-64, are slow, one query after the other: 20 ms for a stretch of some thousand tokens.
  */
 size_t bsga_prefix_attn_workspace_bytes(int dtype, int cache_dtype, int64_t batch, int heads, int kv_heads, int64_t table_width, int64_t prefixes,

@@ -7,8 +7,8 @@
 //
 // HBM-bound: 100 frames of 48 heads (1.69 GB) 338 us, 5.0 TB/s, where a copy of 1 GiB reaches 5.1.  A row is read once and written once.  Four lanes hold a row, lane c eight of its pairs (so that the rotation stays in
 // the lane), and the sums over a row are two quad permutations.  A lane keeps its token over the heads that its workgroup takes: the angles are
-// computed once for them.  Angles are exact: base^(-2j/W) / 2 pi is a 64-bit fraction of a turn, and the product with the position
-// modulo 2^64 is the turn's fraction, whatever the position's size; fp32 would be off by 0.1 at position 10^6.
+// computed once for them.  base^(-2j/W) / 2 pi, of 64-bit arithmetic, is a 64-bit fraction of a turn, and the product with the position modulo 2^64 is the turn's fraction: an angle w is
+// off by 2^-51 w, whatever its size; fp32 would be off by 0.1 at position 10^6.
 //
 // Into a cache in 8 bits (e4m3.h) the row goes from the 32 bits in which it was normed and turned, in one rounding: the largest magnitude is one more pair of
 // quad permutations, and neighbouring lanes swap halves so that each writes 16 bytes.  A key of which the 32 bits' own error leaves a rounding open (rounded from the

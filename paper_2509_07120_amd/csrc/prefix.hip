@@ -7,8 +7,8 @@
 // A key and value are read once for a tile of queries of one key head, and by the tiles of a prefix one after the other from the same L2: 64 queries do 64 flop
 // to the byte in bf16 and 126 in 8 bits, so few queries are bound by HBM and many by what the vector pipe does for a weight (an exponential, its share of a
 // rounding, of a sum and of the conversions of the key and value) beside the two products, of which a wave does one piece's at a time. 64 sequences of 16 heads
-// on 137,400 tokens, up to 2,000 of their own, bf16 (0.83 GB): 152 us, 5.5 TB/s; 128 of 16 heads to 4 on as many, up to 500 of their own, in 8 bits: 106 us,
-// 680 TFLOP/s (exponentials alone 34 us); 60 on five prefixes of up to 82,440 with a window in frames: 57 us; 8 on 5,496: 13.9, of which the host's call is
+// on 137,400 tokens, up to 2,000 of their own, bf16 (0.83 GB): 152 us, 5.5 TB/s; 128 of 16 heads to 4 on as many, up to 500 of their own, in 8 bits: 107 us,
+// 670 TFLOP/s (exponentials alone 34 us); 60 on five prefixes of up to 82,440 with a window in frames: 57 us; 8 on 5,496: 13.5, of which the host's call is
 // most.
 #include "paged.h"
 
